@@ -388,6 +388,148 @@ mf_status mf_dual_gemm_bf16(int M, int N, int K, const void* A0, int lda0, const
                             float* C0, int ldc0, const float* bias0, float* C1, int ldc1,
                             const float* bias1, unsigned terms, void* stream);
 
+/* ---- Attention operators on packed token rows --------------------------------------------
+ * Like mf_dual_gemm_bf16 these take no handle: every buffer, workspace included, is the
+ * caller's, a call enqueues kernels on `stream` of the current device and returns, allocates
+ * nothing and keeps nothing for the next call.  Each carries a forward tangent beside the
+ * primal values when the tangent pointers (names ending in d) are given, which is how the
+ * sweep's forward-over-reverse products run through them, and each has its backward pass.
+ *
+ * Rows are tokens.  A batch is packed: sequence b owns rows seq_start[b] .. seq_start[b+1]-1,
+ * seq_start [n_seq+1] int32 on the device, ascending from 0, n_seq >= 1; empty sequences are
+ * fine.  Rows at or behind seq_start[n_seq] belong to no sequence: nothing of theirs is
+ * computed, and their rows of every output stay as they were.  With seq_start = NULL the
+ * n_rows rows are n_seq sequences of equal length (n_rows a multiple of n_seq).  The contents
+ * of seq_start are read on the device and cannot be refused: values out of order give
+ * undefined results, but no access outside the n_rows rows.
+ *
+ * Row buffers are row-major with a leading dimension in elements: a multiple of 8, and at
+ * least the columns used; their first element lies on a 16-byte boundary.  So q, k and v may
+ * be column ranges of one buffer.  head_dim is a multiple of 8, at most 128. */
+enum { MF_ROPE_HALF = 0, MF_ROPE_INTERLEAVED = 1 };
+enum { MF_ROPE_SCALE_NONE = 0, MF_ROPE_SCALE_LINEAR = 1, MF_ROPE_SCALE_BASE = 2,
+       MF_ROPE_SCALE_BANDS = 3 };
+
+/* Rotary positions.  The first `dims` elements of a head (even; 0 = the whole head) are
+ * dims/2 pairs, (j, j + dims/2) with MF_ROPE_HALF and (2j, 2j+1) with MF_ROPE_INTERLEAVED;
+ * at position p pair j turns by p w_j, w_j = base^(-2j/dims) (base 0 = 10000), and is
+ * multiplied by mscale (0 = 1); the other elements stay.  Scaling for contexts longer than
+ * those trained on, by factor > 0:
+ *   LINEAR  w_j / factor;
+ *   BASE    base * factor^(dims/(dims-2)) in place of base (dims > 2): the slowest pair turns
+ *           factor times slower, the fastest as before;
+ *   BANDS   pairs with more than high_turns turns over orig_len positions keep w_j, those with
+ *           fewer than low_turns get w_j / factor, and between the two (0 <= low < high) the
+ *           weight of w_j rises linearly with the turns.
+ * Angles are reduced modulo a turn in 64-bit fixed point, so that far positions cost no
+ * accuracy (about 1e-7 in cos and sin, as at position 0). */
+typedef struct {
+  int layout, dims;
+  float base;
+  int scaling;
+  float factor;
+  int orig_len;
+  float low_turns, high_turns, mscale;
+} mf_rope_desc;
+
+/* RMS norm of every query and key head (when gains are given), then the rotation.  A row holds
+ * n_heads query heads, n_kv_heads key heads and n_copy_heads heads that are only converted
+ * (the values), head_dim elements each.  For a head x with gain g:
+ *   r = (mean x^2 + eps)^(-1/2),  y = R(p) (g x r)              (no gains: y = R(p) x)
+ *   tangent: y' = R(p) (g' x r + g (x' r + x r')),  r' = -r^3 mean(x x')
+ *  n_rows   rows of every buffer; with 0 only gradients of gains are written (zeros).
+ *  x_prec, y_prec  element types, MF_PREC_FP32 or MF_PREC_BF16: fp32 to fp32, fp32 to bf16 or
+ *           bf16 to bf16.  Arithmetic is float32, results are rounded once.
+ *  x, xd    rows and their tangent (nullable: no tangent), leading dimension ldx.
+ *  y, yd    outputs, ldy.  y may be x (and yd xd) where types and leading dimensions agree.
+ *  gq, gk   [head_dim] float32 gains of query and key heads (both or neither); gqd, gkd their
+ *           tangents (nullable: zero).
+ *  pos      [n_rows] int32 positions, any sign (nullable: the row's place in its sequence).
+ *  seq_start, n_seq  as above; with pos given, both may be 0: every row is taken.
+ * The backward pass takes the forward's x, xd (with gains only), gains, positions and
+ *  dy, dyd  gradients of y and y' (type y_prec, lddy), and writes
+ *  dx, dxd  gradients of x and their tangents (type y_prec, lddx; dx may be dy);
+ *  dgq, dgk, dgqd, dgkd  gradients of the gains [head_dim] float32, summed over rows and heads
+ *           in a fixed order (nullable only without gains, the tangents without xd):
+ *   dy_ = R(p)^T dy,  dg = sum dy_ x r,  dx = r a - r^3 x mean(x a) with a = g dy_.
+ *  work     mf_qk_rope_work_bytes() bytes on a 16-byte boundary, needed with gains; its
+ *           contents need not be kept.  Calls that overlap in time need one each.
+ * Errors: MF_ERR_INVALID_ARG, MF_ERR_UNSUPPORTED (a type pair not listed), MF_ERR_CUDA. */
+typedef struct {
+  int64_t n_rows;
+  int n_heads, n_kv_heads, n_copy_heads, head_dim;
+  int x_prec, y_prec;
+  float eps;
+  mf_rope_desc rope;
+  const void *x, *xd;
+  int64_t ldx;
+  void *y, *yd;
+  int64_t ldy;
+  const float *gq, *gk, *gqd, *gkd;
+  const int32_t* pos;
+  const int32_t* seq_start;
+  int n_seq;
+  const void *dy, *dyd;
+  int64_t lddy;
+  void *dx, *dxd;
+  int64_t lddx;
+  float *dgq, *dgk, *dgqd, *dgkd;
+  void* work;
+  size_t work_bytes;
+} mf_qk_rope_args;
+
+mf_status mf_qk_rope_fwd(const mf_qk_rope_args* args, void* stream);
+mf_status mf_qk_rope_bwd(const mf_qk_rope_args* args, void* stream);
+mf_status mf_qk_rope_work_bytes(const mf_qk_rope_args* args, size_t* bytes);
+
+/* Causal attention of packed sequences with grouped heads, bf16 operands and float32
+ * accumulation: query head h reads key/value head h / (n_heads / n_kv_heads), and row q of a
+ * sequence attends to that sequence's rows up to and including q:
+ *   S = scale q k^T,  P = softmax(S),  o = P v,  lse = log sum exp(S)
+ *   tangent: S' = scale (q' k^T + q k'^T),  rbar = sum P S',
+ *            o' = (P (*) (S' - rbar)) v + P v'
+ *  n_rows   rows of every buffer; 0 is a call that does nothing.
+ *  scale    > 0; 0 = head_dim^(-1/2).
+ *  q [..][n_heads * head_dim], k, v [..][n_kv_heads * head_dim] bf16 with ldq, ldk, ldv; their
+ *           tangents qd, kd, vd (all or none; head_dim <= 64 with tangents) with the same ld.
+ *  o, od    bf16, ldo.   lse, rbar  [n_heads][n_rows] float32 (rbar with tangents).
+ * The backward pass takes the forward's inputs and outputs, the output gradients
+ *  d_o, d_od  bf16, lddo, and writes (sums over a group's query heads and over rows are taken
+ *  in a fixed order, in float32)
+ *  dq, dk, dv, dqd, dkd, dvd  bf16, lddq, lddk, lddv.
+ *  work     mf_attn_work_bytes() bytes on a 16-byte boundary; its contents need not be kept.
+ *           Calls that overlap in time need one each.
+ * No value outside a row's own keys reaches it, not finite or not: what a masked place or a
+ * row behind the last sequence holds does not matter.  A row that does attend to a key row
+ * with a NaN or an infinity gets NaN or infinity itself.
+ *  status   device int32 (nullable): raised to MF_ERR_TIMEOUT when a bounded wait of a kernel
+ *           ran out; outputs are then undefined.
+ * Errors: MF_ERR_INVALID_ARG, MF_ERR_UNSUPPORTED (tangents of heads wider than 64),
+ * MF_ERR_CUDA. */
+typedef struct {
+  int64_t n_rows;
+  int n_heads, n_kv_heads, head_dim;
+  float scale;
+  const int32_t* seq_start;
+  int n_seq;
+  const void *q, *k, *v, *qd, *kd, *vd;
+  int64_t ldq, ldk, ldv;
+  void *o, *od;
+  int64_t ldo;
+  float *lse, *rbar;
+  const void *d_o, *d_od;
+  int64_t lddo;
+  void *dq, *dk, *dv, *dqd, *dkd, *dvd;
+  int64_t lddq, lddk, lddv;
+  void* work;
+  size_t work_bytes;
+  int32_t* status;
+} mf_attn_args;
+
+mf_status mf_attn_fwd(const mf_attn_args* args, void* stream);
+mf_status mf_attn_bwd(const mf_attn_args* args, void* stream);
+mf_status mf_attn_work_bytes(const mf_attn_args* args, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

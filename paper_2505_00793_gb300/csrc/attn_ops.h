@@ -1,0 +1,61 @@
+// Operators on packed token rows (the entry points mf_qk_rope_* and mf_attn_* of ops_capi.cu,
+// which checks the arguments; kernels in rope_ops.cu and attn_rows.cu).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace mf {
+
+// Sequences of a packed batch: rows 0 .. rows-1; start [n+1] on the device, or null for
+// sequences of len rows each.
+struct SeqRows {
+  const int* start = nullptr;
+  int n = 0, len = 0, rows = 0;
+};
+
+// Blocks of a head-norm launch (four per SM), which bounds its partial sums.
+constexpr int kRopeMaxBlocks = 4 * 152;
+
+struct RopeParams {
+  SeqRows seq;
+  int Hq = 0, Hkv = 0, Hc = 0, D = 0;   // query, key and converted heads of D elements
+  int R = 0;                            // rotated elements
+  bool half = true;                     // pairs (j, j + R/2), else (2j, 2j + 1)
+  float eps = 0.f, mscale = 1.f;
+  const void *x = nullptr, *xd = nullptr;
+  void *y = nullptr, *yd = nullptr;
+  const void *dy = nullptr, *dyd = nullptr;
+  void *dx = nullptr, *dxd = nullptr;
+  int64_t ldx = 0, ldy = 0, lddy = 0, lddx = 0;
+  const float *gq = nullptr, *gk = nullptr, *gqd = nullptr, *gkd = nullptr;
+  float *dgq = nullptr, *dgk = nullptr, *dgqd = nullptr, *dgkd = nullptr;
+  float* part = nullptr;                // [blocks][2 or 4][D] partial gain gradients
+  const int* pos = nullptr;
+  // set by qk_rope: lanes a head takes, parts a row is cut into, vector access
+  int lanes = 1, chunks = 1;
+  bool vec = false;
+  uint64_t phase[64];                   // 2^-64 turns a position, per rotated pair
+};
+cudaError_t qk_rope(RopeParams p, bool bwd, bool x_bf16, bool y_bf16, cudaStream_t s);
+
+struct AttnParams {
+  SeqRows seq;
+  int Hq = 0, Hkv = 0, D = 0;
+  float scale = 1.f;
+  const __nv_bfloat16 *q = nullptr, *k = nullptr, *v = nullptr;
+  const __nv_bfloat16 *qd = nullptr, *kd = nullptr, *vd = nullptr;
+  __nv_bfloat16 *o = nullptr, *od = nullptr;
+  const __nv_bfloat16 *d_o = nullptr, *d_od = nullptr;
+  __nv_bfloat16 *dq = nullptr, *dk = nullptr, *dv = nullptr;
+  __nv_bfloat16 *dqd = nullptr, *dkd = nullptr, *dvd = nullptr;
+  int64_t ldq = 0, ldk = 0, ldv = 0, ldo = 0, lddo = 0, lddq = 0, lddk = 0, lddv = 0;
+  float *lse = nullptr, *rbar = nullptr;     // [Hq][rows]
+  float *Dr = nullptr, *Drd = nullptr;       // backward: D = rowsum(dO O) and its tangent
+  int* status = nullptr;
+};
+cudaError_t attn_rows_fwd(const AttnParams& p, bool dual, cudaStream_t s);
+cudaError_t attn_rows_bwd(const AttnParams& p, bool dual, cudaStream_t s);
+
+}  // namespace mf

@@ -36,7 +36,9 @@ EXPORTS = ["mf_create", "mf_destroy", "mf_set_allocator", "mf_param_count",
            "mf_workspace_bytes", "mf_release_workspace", "mf_inner_rollout", "mf_hvp",
            "mf_meta_grad", "mf_sync", "mf_status_string", "mf_last_error", "mf_stats",
            "mf_set_kernel_timing", "mf_kernel_time", "mf_inject_fault", "mf_dual_gemm_bf16",
-           "mf_hvp_noalloc", "mf_set_option", "mf_replay_gemms", "mf_checkpoint_plan"]
+           "mf_hvp_noalloc", "mf_set_option", "mf_replay_gemms", "mf_checkpoint_plan",
+           "mf_qk_rope_fwd", "mf_qk_rope_bwd", "mf_qk_rope_work_bytes", "mf_attn_fwd",
+           "mf_attn_bwd", "mf_attn_work_bytes"]
 
 
 class mf_model_desc(C.Structure):
@@ -52,6 +54,41 @@ class mf_loop_desc(C.Structure):
                 ("momentum", C.c_float), ("meta_kind", C.c_int), ("hvp_mode", C.c_int),
                 ("ckpt_every", C.c_int), ("optimizer", C.c_int), ("beta1", C.c_float),
                 ("beta2", C.c_float), ("adam_eps", C.c_float), ("ckpt_slots", C.c_int)]
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
+
+
+class mf_rope_desc(C.Structure):
+    _fields_ = [("layout", C.c_int), ("dims", C.c_int), ("base", C.c_float),
+                ("scaling", C.c_int), ("factor", C.c_float), ("orig_len", C.c_int),
+                ("low_turns", C.c_float), ("high_turns", C.c_float), ("mscale", C.c_float)]
+
+
+def _ptrs(names):
+    return [(n, C.c_void_p) for n in names.split()]
+
+
+class mf_qk_rope_args(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("n_heads", C.c_int), ("n_kv_heads", C.c_int),
+                ("n_copy_heads", C.c_int), ("head_dim", C.c_int), ("x_prec", C.c_int),
+                ("y_prec", C.c_int), ("eps", C.c_float), ("rope", mf_rope_desc),
+                *_ptrs("x xd"), ("ldx", C.c_int64), *_ptrs("y yd"), ("ldy", C.c_int64),
+                *_ptrs("gq gk gqd gkd pos seq_start"), ("n_seq", C.c_int),
+                *_ptrs("dy dyd"), ("lddy", C.c_int64), *_ptrs("dx dxd"), ("lddx", C.c_int64),
+                *_ptrs("dgq dgk dgqd dgkd work"), ("work_bytes", C.c_size_t)]
+
+
+class mf_attn_args(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("n_heads", C.c_int), ("n_kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("scale", C.c_float), *_ptrs("seq_start"),
+                ("n_seq", C.c_int), *_ptrs("q k v qd kd vd"), ("ldq", C.c_int64),
+                ("ldk", C.c_int64), ("ldv", C.c_int64), *_ptrs("o od"), ("ldo", C.c_int64),
+                *_ptrs("lse rbar d_o d_od"), ("lddo", C.c_int64),
+                *_ptrs("dq dk dv dqd dkd dvd"), ("lddq", C.c_int64), ("lddk", C.c_int64),
+                ("lddv", C.c_int64), *_ptrs("work"), ("work_bytes", C.c_size_t),
+                *_ptrs("status")]
 
 
 class MixflowError(RuntimeError):
@@ -205,6 +242,222 @@ def mf_dual_gemm_bf16(M, N, K, A0, A1, B0, B1, C0, C1, terms, bias0=None, bias1=
                                  terms, _stream(stream))
     if st != 0:
         raise MixflowError(st, "mf_dual_gemm_bf16")
+
+
+# ---- operators on packed token rows (mixflow.h, "Attention operators") --------------------
+
+def rope_desc(layout="half", dims=0, base=10000.0, scaling="none", factor=1.0, orig_len=0,
+              low_turns=1.0, high_turns=4.0, mscale=1.0) -> mf_rope_desc:
+    """Rotary positions: ``layout`` "half" or "interleaved", the first ``dims`` elements of each
+    head (0 = all), ``scaling`` "none", "linear", "base" or "bands" by ``factor``."""
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout: {layout!r}, expected one of {list(ROPE_LAYOUTS)}")
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling: {scaling!r}, expected one of {list(ROPE_SCALINGS)}")
+    return mf_rope_desc(ROPE_LAYOUTS[layout], dims, base, ROPE_SCALINGS[scaling], factor,
+                        orig_len, low_turns, high_turns, mscale)
+
+
+class _Call:
+    """Argument struct of one operator call, filled tensor by tensor.  The first tensor sets
+    the device; every other must live there, have the stated type, and hold the stated rows and
+    columns with unit stride along its rows."""
+
+    def __init__(self, args, first):
+        if not first.is_cuda:
+            raise ValueError(f"expected CUDA tensors, got one on {first.device}")
+        self.a, self.device = args, first.device
+
+    def _base(self, t, name, dtype):
+        if t.dtype != dtype:
+            raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name}: on {t.device}, expected {self.device}")
+
+    def rows(self, name, t, dtype, rows, cols, ld=None):
+        """A row buffer [rows][>= cols]; ``ld`` names the struct's leading-dimension field, which
+        a tangent shares with its primal."""
+        if t is None:
+            return
+        self._base(t, name, dtype)
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < cols or \
+                (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}, expected "
+                             f"[{rows}][{cols} or more] with unit stride along its rows")
+        # one row has no stride: any leading dimension that holds it will do
+        step = t.stride(0) if rows > 1 else -(-t.shape[1] // 8) * 8
+        have = getattr(self.a, ld)
+        if have and have != step and rows > 1:
+            raise ValueError(f"{name}: row stride {step}, expected {have} as its primal has")
+        if not have:
+            setattr(self.a, ld, step)
+        setattr(self.a, name, t.data_ptr())
+
+    def vec(self, name, t, dtype, shape):
+        if t is None:
+            return
+        self._base(t, name, dtype)
+        if tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected contiguous {shape}")
+        setattr(self.a, name, t.data_ptr())
+
+    def seq(self, seq_start, n_seq):
+        import torch
+        if seq_start is not None:
+            if seq_start.dim() != 1 or seq_start.shape[0] < 2:
+                raise ValueError(f"seq_start: shape {tuple(seq_start.shape)}, expected [n_seq + 1]")
+            n_seq = seq_start.shape[0] - 1
+            self.vec("seq_start", seq_start, torch.int32, (n_seq + 1,))
+        self.a.n_seq = n_seq
+
+    def work(self, work):
+        if work is None:
+            return
+        if work.device != self.device or not work.is_contiguous():
+            raise ValueError(f"work: expected a contiguous tensor on {self.device}")
+        self.a.work, self.a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
+
+    def run(self, fn, stream):
+        import torch
+        if self.device.index != torch.cuda.current_device():
+            with torch.cuda.device(self.device):
+                return self.run(fn, stream)
+        st = getattr(lib(), fn)(C.byref(self.a), _stream(stream))
+        if st != 0:
+            raise MixflowError(st, fn)
+
+
+def _prec(t, name):
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name}: dtype {t.dtype}, expected torch.float32 or torch.bfloat16")
+    return PRECISIONS["bf16" if t.dtype == torch.bfloat16 else "fp32"]
+
+
+def _rope_call(first, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
+               pos, seq_start, n_seq):
+    import torch
+    a = mf_qk_rope_args()
+    c = _Call(a, first)
+    a.n_rows = first.shape[0]
+    a.n_heads, a.n_kv_heads, a.n_copy_heads, a.head_dim = n_heads, n_kv_heads, n_copy_heads, head_dim
+    a.eps, a.rope = eps, rope
+    for name, g in (("gq", gq), ("gk", gk), ("gqd", gqd), ("gkd", gkd)):
+        c.vec(name, g, torch.float32, (head_dim,))
+    c.vec("pos", pos, torch.int32, (a.n_rows,))
+    c.seq(seq_start, n_seq)
+    return c
+
+
+def mf_qk_rope_fwd(x, y, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, xd=None, yd=None,
+                   gq=None, gk=None, gqd=None, gkd=None, eps=1e-6, pos=None, seq_start=None,
+                   n_seq=1, stream=None):
+    """Rows of heads x [N][(n_heads + n_kv_heads + n_copy_heads) head_dim] -> y: RMS norm of the
+    query and key heads (with gains gq, gk), rotary positions, the type of y; xd -> yd the
+    tangent (see mixflow.h)."""
+    c = _rope_call(x, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
+                   pos, seq_start, n_seq)
+    c.a.x_prec, c.a.y_prec = _prec(x, "x"), _prec(y, "y")
+    n, cols = x.shape[0], (n_heads + n_kv_heads + n_copy_heads) * head_dim
+    c.rows("x", x, x.dtype, n, cols, "ldx")
+    c.rows("xd", xd, x.dtype, n, cols, "ldx")
+    c.rows("y", y, y.dtype, n, cols, "ldy")
+    c.rows("yd", yd, y.dtype, n, cols, "ldy")
+    c.run("mf_qk_rope_fwd", stream)
+
+
+def mf_qk_rope_bwd(dy, dx, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, x=None, xd=None,
+                   dyd=None, dxd=None, gq=None, gk=None, gqd=None, gkd=None, dgq=None, dgk=None,
+                   dgqd=None, dgkd=None, eps=1e-6, pos=None, seq_start=None, n_seq=1, work=None,
+                   stream=None):
+    """Backward of mf_qk_rope_fwd: dy (dyd) -> dx (dxd) and, with gains, dgq, dgk (dgqd, dgkd)
+    and x (xd) as the forward had them; work: mf_qk_rope_work_bytes bytes."""
+    import torch
+    c = _rope_call(dy, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
+                   pos, seq_start, n_seq)
+    c.a.y_prec = _prec(dy, "dy")
+    c.a.x_prec = c.a.y_prec if x is None else _prec(x, "x")
+    n, cols = dy.shape[0], (n_heads + n_kv_heads + n_copy_heads) * head_dim
+    qk = (n_heads + n_kv_heads) * head_dim
+    c.rows("dy", dy, dy.dtype, n, cols, "lddy")
+    c.rows("dyd", dyd, dy.dtype, n, cols, "lddy")
+    c.rows("dx", dx, dy.dtype, n, cols, "lddx")
+    c.rows("dxd", dxd, dy.dtype, n, cols, "lddx")
+    c.rows("x", x, None if x is None else x.dtype, n, qk, "ldx")
+    c.rows("xd", xd, None if x is None else x.dtype, n, qk, "ldx")
+    for name, g in (("dgq", dgq), ("dgk", dgk), ("dgqd", dgqd), ("dgkd", dgkd)):
+        c.vec(name, g, torch.float32, (head_dim,))
+    c.work(work)
+    c.run("mf_qk_rope_bwd", stream)
+
+
+def mf_qk_rope_work_bytes(n_rows, n_heads, n_kv_heads, head_dim, dual=False):
+    """Bytes of `work` that mf_qk_rope_bwd takes with gains."""
+    a = mf_qk_rope_args()
+    a.n_rows, a.n_heads, a.n_kv_heads, a.head_dim = n_rows, n_heads, n_kv_heads, head_dim
+    a.dyd = 16 if dual else None
+    return _bytes_of("mf_qk_rope_work_bytes", a)
+
+
+def mf_attn_work_bytes(n_rows, n_heads, dual=False):
+    """Bytes of `work` that mf_attn_bwd takes."""
+    a = mf_attn_args()
+    a.n_rows, a.n_heads = n_rows, n_heads
+    a.qd = 16 if dual else None
+    return _bytes_of("mf_attn_work_bytes", a)
+
+
+def _bytes_of(fn, a):
+    b = C.c_size_t()
+    st = getattr(lib(), fn)(C.byref(a), C.byref(b))
+    if st != 0:
+        raise MixflowError(st, fn)
+    return b.value
+
+
+def _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, rbar, seq_start,
+               n_seq, scale, status):
+    import torch
+    bf, f32 = torch.bfloat16, torch.float32
+    a = mf_attn_args()
+    c = _Call(a, q)
+    n, cq, ck = q.shape[0], n_heads * head_dim, n_kv_heads * head_dim
+    a.n_rows, a.n_heads, a.n_kv_heads, a.head_dim, a.scale = n, n_heads, n_kv_heads, head_dim, scale
+    c.seq(seq_start, n_seq)
+    for name, t, cols, ld in (("q", q, cq, "ldq"), ("k", k, ck, "ldk"), ("v", v, ck, "ldv"),
+                              ("qd", qd, cq, "ldq"), ("kd", kd, ck, "ldk"), ("vd", vd, ck, "ldv"),
+                              ("o", o, cq, "ldo"), ("od", od, cq, "ldo")):
+        c.rows(name, t, bf, n, cols, ld)
+    c.vec("lse", lse, f32, (n_heads, n))
+    c.vec("rbar", rbar, f32, (n_heads, n))
+    c.vec("status", status, torch.int32, (1,))
+    return c
+
+
+def mf_attn_fwd(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd=None, kd=None, vd=None, od=None,
+                rbar=None, seq_start=None, n_seq=1, scale=0.0, status=None, stream=None):
+    """Causal attention of packed bf16 rows q [N][n_heads head_dim], k, v [N][n_kv_heads head_dim]
+    -> o, lse [n_heads][N]; with qd, kd, vd the tangents od, rbar (see mixflow.h)."""
+    _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, rbar, seq_start,
+               n_seq, scale, status).run("mf_attn_fwd", stream)
+
+
+def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd=None,
+                kd=None, vd=None, od=None, rbar=None, dod=None, dqd=None, dkd=None, dvd=None,
+                seq_start=None, n_seq=1, scale=0.0, status=None, stream=None):
+    """Backward of mf_attn_fwd from its inputs and outputs and d_o (dod) -> dq, dk, dv (dqd, dkd,
+    dvd); work: mf_attn_work_bytes bytes."""
+    import torch
+    c = _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, rbar, seq_start,
+                   n_seq, scale, status)
+    n, cq, ck = q.shape[0], n_heads * head_dim, n_kv_heads * head_dim
+    for name, t, cols, ld in (("d_o", d_o, cq, "lddo"), ("d_od", dod, cq, "lddo"),
+                              ("dq", dq, cq, "lddq"), ("dk", dk, ck, "lddk"), ("dv", dv, ck, "lddv"),
+                              ("dqd", dqd, cq, "lddq"), ("dkd", dkd, ck, "lddk"),
+                              ("dvd", dvd, ck, "lddv")):
+        c.rows(name, t, torch.bfloat16, n, cols, ld)
+    c.work(work)
+    c.run("mf_attn_bwd", stream)
 
 
 class MixFlow:
