@@ -55,6 +55,8 @@ struct AttnParams {
   float *Dr = nullptr, *Drd = nullptr;       // backward: D = rowsum(dO O) and its tangent
   int* status = nullptr;
 };
+// tcgen05 forward (attn_tc.cu): heads of up to 128 columns, 64 with tangents.
+cudaError_t attn_tc_fwd(const AttnParams& p, bool dual, cudaStream_t s);
 cudaError_t attn_rows_fwd(const AttnParams& p, bool dual, cudaStream_t s);
 cudaError_t attn_rows_bwd(const AttnParams& p, bool dual, cudaStream_t s);
 

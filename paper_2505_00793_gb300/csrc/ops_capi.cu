@@ -254,7 +254,7 @@ mf_status mf_attn_fwd(const mf_attn_args* args, void* stream) {
   AttnParams p;
   const mf_status st = attn_params(*args, false, &p);
   if (st != MF_OK || args->n_rows == 0) return st;
-  return done(mf::attn_rows_fwd(p, args->qd != nullptr, static_cast<cudaStream_t>(stream)));
+  return done(mf::attn_tc_fwd(p, args->qd != nullptr, static_cast<cudaStream_t>(stream)));
 }
 
 mf_status mf_attn_bwd(const mf_attn_args* args, void* stream) {

@@ -1401,6 +1401,22 @@ bool make_map2(CUtensorMap* m, CUtensorMapDataType dt, int esize, const void* pt
          CUDA_SUCCESS;
 }
 
+// Heads of D bf16 columns side by side in rows of ld elements, as {columns, rows, heads};
+// box 64 columns x box_rows (columns from D on read as zeros).
+bool make_head_map(CUtensorMap* m, const void* ptr, int D, int rows, int64_t ld, int heads,
+                   int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(rows),
+                        static_cast<cuuint64_t>(heads)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(D) * 2};
+  cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box,
+            estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // K-major bf16 operand [rows][K] (leading dimension ld), box 64 x box_rows.
 bool make_map(CUtensorMap* m, const void* ptr, int K, int rows, int ld, int box_rows,
               int batch = 1, int64_t bstride = 0) {
