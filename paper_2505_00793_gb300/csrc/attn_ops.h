@@ -1,5 +1,5 @@
 // Operators on packed token rows (the entry points mf_qk_rope_* and mf_attn_* of ops_capi.cu,
-// which checks the arguments; kernels in rope_ops.cu and attn_rows.cu).
+// which checks the arguments; kernels in rope_ops.cu and attn_tc.cu).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -55,9 +55,8 @@ struct AttnParams {
   float *Dr = nullptr, *Drd = nullptr;       // backward: D = rowsum(dO O) and its tangent
   int* status = nullptr;
 };
-// tcgen05 forward (attn_tc.cu): heads of up to 128 columns, 64 with tangents.
+// Both passes (attn_tc.cu): heads of up to 128 columns, 64 with tangents.
 cudaError_t attn_tc_fwd(const AttnParams& p, bool dual, cudaStream_t s);
-cudaError_t attn_rows_fwd(const AttnParams& p, bool dual, cudaStream_t s);
-cudaError_t attn_rows_bwd(const AttnParams& p, bool dual, cudaStream_t s);
+cudaError_t attn_tc_bwd(const AttnParams& p, bool dual, cudaStream_t s);
 
 }  // namespace mf

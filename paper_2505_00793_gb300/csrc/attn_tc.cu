@@ -28,7 +28,7 @@ namespace mf {
 namespace {
 
 constexpr int TR = 128;                       // rows of a CTA's own tile (MMA M)
-constexpr int ATOM64 = 64 * 128, ATOM128 = 128 * 128;   // bytes of [64 or 128 rows][64] bf16
+constexpr int ATOM128 = 128 * 128;            // bytes of [128 rows][64] bf16
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
 // MN-major operand of 64-column boxes of 128-byte rows, `box` bytes apart.
@@ -583,7 +583,814 @@ cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
                   C::SMEM, s, q, k, v, qd, kd, vd, p);
 }
 
+// ---- backward -------------------------------------------------------------------------------------
+// Two kernels, so that every sum keeps a fixed order: attn_tc_bwd_q_kernel, one CTA per (query
+// head, 128 query rows), walks key tiles for dQ (and computes D = rowsum(dO O) on its way), and
+// attn_tc_bwd_kv_kernel, one CTA per (key/value head, 128 key rows), walks the query tiles of its
+// group's heads for dK and dV.  Both recompute the scores.
+//
+// Key-row kernel, per query tile (scores transposed: key rows are TMEM lanes):
+//   S^T = K Q^T,  S'^T = K' Q^T + K Q'^T,  dP^T = V dO^T,  dP'^T = V' dO^T + V dO'^T
+//   P^T = exp(S^T - lse), P'^T = P^T (S'^T - rbar)       over S^T, S'^T as bf16
+//   dV += P^T dO,  dV' += P'^T dO + P^T dO'
+//   dS^T = P^T (dP^T - D),  dS'^T = P'^T (dP^T - D) + P^T (dP'^T - D')   over dP^T, dP'^T
+//   dK += dS^T Q,  dK' += dS'^T Q + dS^T Q'
+// The products run in the order  dV(i) S(i+1) | dK(i) dP(i+1):  while the row warps turn dP(i)
+// into dS(i), the tensor cores work on dV(i) and S(i+1); while they turn S(i+1) into P(i+1), on
+// dK(i) and dP(i+1).
+// Query-row kernel, per key tile:  dS as above, untransposed, over dP;  dQ += dS K,
+// dQ' += dS' K + dS K',  in the order  S(j+1) | dQ(j) dP(j+1).
+template <bool DUAL, int HDP>
+struct BwdCfg {
+  static constexpr int NA = HDP / 64;
+  static constexpr int BT = HDP == 128 ? 128 : 64;         // streamed rows a tile
+  static constexpr int NT = DUAL ? 2 : 1;
+  static constexpr int EW = 8;                             // row warps: two threads a row
+  static constexpr int THREADS = 64 + 32 * EW;
+  static constexpr int CW = BT / 2;                        // columns of a row thread
+  static constexpr int RES1 = NT * NA * ATOM128;           // K (K') or V (V'); Q (Q') or dO (dO')
+  static constexpr int BATOM = BT * 128;
+  static constexpr int TILE_B = NT * NA * BATOM;           // one streamed operand with its tangent
+  static constexpr int STAGE_B = 2 * TILE_B;
+  static constexpr int STAGES = HDP == 128 ? 2 : DUAL ? 4 : 3;
+  static constexpr int CTAS = DUAL || HDP == 128 ? 1 : 2;
+  static constexpr int NSTAT = DUAL ? 4 : 2;               // lse, D (rbar, D')
+  static constexpr int STAT_F = NSTAT * BT;
+  static constexpr int SMEM_Q = 2 * RES1 + STAGES * STAGE_B + 1024;
+  static constexpr int SMEM_KV = SMEM_Q + STAGES * STAT_F * 4;
+  static_assert(SMEM_KV + 1024 <= 227 * 1024, "a CTA's shared memory");
+  // TMEM: S (S'), dP (dP'), then the accumulators, tangents behind their primal
+  static constexpr uint32_t C_S = 0, C_SD = BT, C_DP = NT * BT, C_DPD = C_DP + BT;
+  static constexpr uint32_t C_A = 2 * NT * BT;             // dV (dV') or dQ (dQ')
+  static constexpr uint32_t C_B = C_A + NT * HDP;          // dK (dK')
+  static constexpr uint32_t COLS_KV = C_B + NT * HDP <= 256 ? 256 : 512;
+  static constexpr uint32_t COLS_Q = C_B <= 256 ? 256 : 512;
+};
+
+__device__ __forceinline__ void row_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// Column sums of a row's dO (*) O over this thread's half of the head, with the tangent.
+template <bool DUAL>
+__device__ __forceinline__ float2 row_dots(const TcParams2& p, int64_t row, int h, int c0, int c1) {
+  float s = 0.f, sd = 0.f;
+  const int64_t oo = row * p.ldo + h * p.D, og = row * p.lddo + h * p.D;
+  auto f8 = [](const __nv_bfloat16* x, float (&v)[8]) {
+    const uint4 w = *reinterpret_cast<const uint4*>(x);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(u[i] << 16);
+      v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  };
+  for (int c = c0; c < c1 && c < p.D; c += 8) {
+    float o[8], g[8], od[8], gd[8];
+    f8(p.o + oo + c, o);
+    f8(p.d_o + og + c, g);
+    if (DUAL) {
+      f8(p.od + oo + c, od);
+      f8(p.d_od + og + c, gd);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s += o[i] * g[i];
+      if (DUAL) sd += o[i] * gd[i] + od[i] * g[i];
+    }
+  }
+  return make_float2(s, sd);
+}
+
+// bf16 pair that is NaN where its row is noted as not finite and attends.
+__device__ __forceinline__ uint32_t nan_pair(uint32_t w, bool o0, bool o1) {
+  return (o0 && (w & 1) ? 0x7fffu : 0u) | (o1 && (w & 2) ? 0x7fff0000u : 0u);
+}
+
+template <bool DUAL, int HDP>
+__global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>::CTAS)
+    attn_tc_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                          const __grid_constant__ CUtensorMap tmKd, const __grid_constant__ CUtensorMap tmVd,
+                          const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmO,
+                          const __grid_constant__ CUtensorMap tmQd, const __grid_constant__ CUtensorMap tmOd,
+                          const __grid_constant__ TcParams2 p) {
+  using C = BwdCfg<DUAL, HDP>;
+  constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t res_full, s_full, dp_full, p_full, ds_full, drain;
+  __shared__ __align__(8) uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
+  __shared__ uint32_t bad[C::STAGES][4];
+  __shared__ SeqTile st_rows;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* sRes = smem;                        // K (K'), V (V')
+  uint8_t* sSt = smem + 2 * C::RES1;           // stage: Q (Q'), dO (dO')
+  float* sStat = reinterpret_cast<float*>(sSt + C::STAGES * C::STAGE_B);
+  // heads fastest; the first rows of a long sequence (the longest walks) come first
+  const int hk = static_cast<int>(blockIdx.x % p.Hkv);
+  const int row0 = static_cast<int>(blockIdx.x / p.Hkv) * TR;
+  const int G = p.Hq / p.Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  pdl_entry();
+  const int nvalid = min(seq_total(p.seq) - row0, TR);
+  if (nvalid <= 0) return;
+  seq_tile_init(p.seq, row0, st_rows);
+  if (threadIdx.x == 0) {
+    mbar_init(&res_full, 1);
+    mbar_init(&s_full, 1);
+    mbar_init(&dp_full, 1);
+    mbar_init(&p_full, C::EW);
+    mbar_init(&ds_full, C::EW);
+    mbar_init(&drain, 1);
+    for (int i = 0; i < C::STAGES; ++i) {
+      mbar_init(&st_full[i], 2);
+      mbar_init(&st_empty[i], 1);
+      mbar_init(&st_clean[i], 1);
+    }
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(&tmem_slot)),
+                 "r"(C::COLS_KV));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  __syncthreads();
+  seq_tile_fill(p.seq, row0, st_rows, C::THREADS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tb = tmem_slot;
+  volatile int* abort = &abort_flag;
+  const int hi0 = tile_hi(st_rows, row0, 0), hi1 = tile_hi(st_rows, row0, nvalid - 1);
+  const int nqt = (hi1 - row0 + BT - 1) / BT;       // query tiles of a head
+  const int ntile = nqt * G;
+  // whether some key row is not attended to by the whole of query tile t
+  auto mixed = [&](int t) { return t * BT < nvalid - 1 || row0 + t * BT + BT > hi0; };
+
+  if (warp == 0) {
+    // ---- loads: TMA by one lane, row statistics by all -------------------------------------------
+    if (elect_one()) {
+      mbar_expect_tx(&res_full, 2 * C::RES1);
+#pragma unroll
+      for (int a = 0; a < NA; ++a) {
+        tma_load_3d(sRes + a * ATOM128, &tmK, &res_full, 64 * a, row0, hk);
+        tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmV, &res_full, 64 * a, row0, hk);
+        if (DUAL) {
+          tma_load_3d(sRes + (NA + a) * ATOM128, &tmKd, &res_full, 64 * a, row0, hk);
+          tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmVd, &res_full, 64 * a, row0, hk);
+        }
+      }
+    }
+    __syncwarp();
+    int issued = 0, t = 0, h = hk * G;
+    for (int i = 0; i < ntile; ++i) {
+      const int st = i % C::STAGES;
+      if (!wwait(&st_empty[st], ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+      const int qr = row0 + t * BT;
+      if (elect_one()) {
+        mbar_expect_tx(&st_full[st], C::STAGE_B);
+        uint8_t* b = sSt + st * C::STAGE_B;
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+          tma_load_3d(b + a * C::BATOM, &tmQ, &st_full[st], 64 * a, qr, h);
+          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmO, &st_full[st], 64 * a, qr, h);
+          if (DUAL) {
+            tma_load_3d(b + (NA + a) * C::BATOM, &tmQd, &st_full[st], 64 * a, qr, h);
+            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmOd, &st_full[st], 64 * a, qr, h);
+          }
+        }
+      }
+      __syncwarp();
+      float* sst = sStat + st * C::STAT_F;
+      const int64_t base = static_cast<int64_t>(h) * p.seq.rows;
+      float v[C::NSTAT][BT / 32];
+#pragma unroll
+      for (int e = 0; e < BT / 32; ++e) {
+        const int row = qr + 32 * e + lane;
+        const bool in = row < p.seq.rows;
+        v[0][e] = in ? p.lse[base + row] * LOG2E : 0.f;
+        v[1][e] = in ? p.Dr[base + row] : 0.f;
+        if (DUAL) {
+          v[2][e] = in ? p.rbar[base + row] : 0.f;
+          v[3][e] = in ? p.Drd[base + row] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < C::NSTAT; ++k)
+#pragma unroll
+        for (int e = 0; e < BT / 32; ++e) sst[k * BT + 32 * e + lane] = v[k][e];
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(&st_full[st]);
+      ++issued;
+      if (++t == nqt) { t = 0; ++h; }
+    }
+    __syncwarp();
+    mbar_wait(&res_full, 0, p.status, FTC_WAIT_NS);
+    drain_loads(st_full, issued, C::STAGES, p.status);
+  } else if (warp == 1) {
+    // ---- products ------------------------------------------------------------------------------------
+    constexpr uint32_t idS = idesc_bf16(TR, BT), idS2 = idesc_bf16(TR, 2 * BT);
+    constexpr uint32_t idA = idesc_bf16(TR, HDP) | (1u << 16), idA2 = idesc_bf16(TR, 2 * HDP) | (1u << 16);
+    const uint64_t dK = sdesc_sw128(smem_u32(sRes)), dV = dK + (C::RES1 >> 4);
+    constexpr uint64_t RD = NA * ATOM128 >> 4;            // a resident operand's tangent
+    const uint64_t kSt = sdesc_sw128(smem_u32(sSt)), mSt = sdesc_mn(smem_u32(sSt), C::BATOM);
+    constexpr uint64_t ST = C::STAGE_B >> 4, DO = C::TILE_B >> 4;
+    // X Y^T into column c (and the tangent's next to it)
+    auto score = [&](uint64_t x, uint64_t y, uint32_t c) {
+#pragma unroll
+      for (int kk = 0; kk < HDP / 16; ++kk)
+        mma_bf16(tb + c, x + (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3),
+                 y + (kk >> 2) * (C::BATOM >> 4) + 2 * (kk & 3), DUAL ? idS2 : idS, kk > 0);
+      if (DUAL) {
+#pragma unroll
+        for (int kk = 0; kk < HDP / 16; ++kk)
+          mma_bf16(tb + c + BT, x + RD + 2 * kk, y + 2 * kk, idS, 1);
+      }
+    };
+    // acc += A^T-rows (TMEM columns a, tangent a + BT) times streamed rows y
+    auto accum = [&](uint32_t c, uint32_t a, uint64_t y, bool first) {
+#pragma unroll
+      for (int kk = 0; kk < BT / 16; ++kk) {
+        // the two threads of a row keep their halves apart
+        const uint32_t ac = a + (kk / (CW / 16)) * CW + (kk % (CW / 16)) * 8;
+        const uint32_t acc = (!first || kk > 0) ? 1u : 0u;
+        mma_ts(tb + c, tb + ac, y + 128 * kk, DUAL ? idA2 : idA, acc);
+        if (DUAL) mma_ts(tb + c + HDP, tb + ac + BT, y + 128 * kk, idA, 1);
+      }
+    };
+    int t = 0;      // query tile of the tile being looked over
+    auto look_over = [&](int i) -> bool {
+      const int st = i % C::STAGES;
+      if (!wwait(&st_full[st], (i / C::STAGES) & 1, p.status, abort)) return false;
+      if (mixed(t)) scrub(sSt + st * C::STAGE_B, BT, 2 * C::NT * NA, bad[st], lane);
+      if (++t == nqt) t = 0;
+      if (lane == 0) mbar_arrive_local(&st_clean[st]);
+      __syncwarp();
+      return true;
+    };
+    bool ok = wwait(&res_full, 0, p.status, abort) && look_over(0);
+    if (ok) {
+      tc_fence_after();
+      if (elect_one()) {
+        score(dK, kSt, C::C_S);
+        mma_commit(&s_full);
+        score(dV, kSt + DO, C::C_DP);
+        mma_commit(&dp_full);
+      }
+      __syncwarp();
+    }
+    for (int i = 0; ok && i < ntile; ++i) {
+      const int st = i % C::STAGES, sn = (i + 1) % C::STAGES;
+      const bool more = i + 1 < ntile;
+      if (more && !look_over(i + 1)) break;
+      if (!wwait(&p_full, i & 1, p.status, abort)) break;
+      tc_fence_after();
+      if (elect_one()) {
+        accum(C::C_A, C::C_S, mSt + st * ST + DO, i == 0);
+        if (more) {
+          score(dK, kSt + sn * ST, C::C_S);
+          mma_commit(&s_full);
+        }
+      }
+      __syncwarp();
+      if (!wwait(&ds_full, i & 1, p.status, abort)) break;
+      tc_fence_after();
+      if (elect_one()) {
+        accum(C::C_B, C::C_DP, mSt + st * ST, i == 0);
+        mma_commit(&st_empty[st]);
+        if (more) {
+          score(dV, kSt + sn * ST + DO, C::C_DP);
+          mma_commit(&dp_full);
+        }
+      }
+      __syncwarp();
+    }
+    if (elect_one()) mma_commit(&drain);
+    __syncwarp();
+    mbar_wait(&drain, 0, p.status, FTC_WAIT_NS);
+  } else {
+    // ---- rows: key row r (TMEM lane r), query columns cb .. cb + CW - 1 ---------------------------------
+    const int q4 = warp & 3;
+    const int r = q4 * 32 + lane;
+    const int half = (warp - 2) >> 2, cb = half * CW;
+    const uint32_t lane_base = tb + (static_cast<uint32_t>(q4 * 32) << 16) + cb;
+    const int hi = tile_hi(st_rows, row0, r);
+    const uint64_t c2p = pair(p.c2, p.c2), neg1 = pair(-1.f, -1.f), sc = pair(p.scale, p.scale);
+    bool ok = true;
+    int t = 0;
+    for (int i = 0; i < ntile; ++i) {
+      const int st = i % C::STAGES;
+      const uint32_t ph = (i / C::STAGES) & 1;
+      const bool mx = mixed(t);
+      // columns a .. b - 1 (of the tile) attend to this key
+      const int a = r - t * BT, b = hi - (row0 + t * BT);
+      if (++t == nqt) t = 0;
+      if (!wwait(&st_full[st], ph, p.status, abort)) { ok = false; break; }   // the statistics
+      uint32_t badw[CW / 32];
+      bool any_bad = false;
+      if (mx) {
+        if (!wwait(&st_clean[st], ph, p.status, abort)) { ok = false; break; }
+#pragma unroll
+        for (int w = 0; w < CW / 32; ++w) { badw[w] = bad[st][cb / 32 + w]; any_bad |= badw[w] != 0; }
+      }
+      const float4* stat = reinterpret_cast<const float4*>(sStat + st * C::STAT_F + cb);
+      if (!wwait(&s_full, i & 1, p.status, abort)) { ok = false; break; }
+      tc_fence_after();
+      auto own = [&](int c) { return cb + c >= a && cb + c < b; };
+      float pr[CW], pd[DUAL ? CW : 1];
+      auto probs = [&](auto masked) {
+        constexpr bool MASK = decltype(masked)::value;
+#pragma unroll
+        for (int c0 = 0; c0 < CW; c0 += 16) {
+          float sv[16], sd[16];
+          uint32_t pk[8], pdk[8];
+          tmem_ld16_nowait(lane_base + C::C_S + c0, sv);
+          if (DUAL) tmem_ld16_nowait(lane_base + C::C_SD + c0, sd);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 l4 = stat[(c0 + e) / 4];
+            const uint64_t lv[2] = {pair(l4.x, l4.y), pair(l4.z, l4.w)};
+            float4 r4 = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (DUAL) r4 = stat[2 * (BT / 4) + (c0 + e) / 4];
+            const uint64_t rv[2] = {pair(r4.x, r4.y), pair(r4.z, r4.w)};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int f = e + 2 * u, c = c0 + f;
+              const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, mul2(lv[u], neg1)));
+              float p0 = ex2(x.x), p1 = ex2(x.y);
+              const bool o0 = !MASK || own(c), o1 = !MASK || own(c + 1);
+              if (!o0) p0 = 0.f;
+              if (!o1) p1 = 0.f;
+              pr[c] = p0;
+              pr[c + 1] = p1;
+              pk[f / 2] = pack_bf16x2(p0, p1);
+              if (DUAL) {
+                float2 y = halves(mul2(pair(p0, p1),
+                                       fma2(pair(sd[f], sd[f + 1]), sc, mul2(rv[u], neg1))));
+                if (!o0) y.x = 0.f;
+                if (!o1) y.y = 0.f;
+                pd[c] = y.x;
+                pd[DUAL ? c + 1 : 0] = y.y;
+                pdk[f / 2] = pack_bf16x2(y.x, y.y);
+              }
+              if (MASK && any_bad) {
+                const uint32_t n = nan_pair(badw[c >> 5] >> (c & 31), o0, o1);
+                pk[f / 2] |= n;
+                if (DUAL) pdk[f / 2] |= n;
+              }
+            }
+          }
+          tmem_st8(lane_base + C::C_S + c0 / 2, pk);
+          if (DUAL) tmem_st8(lane_base + C::C_SD + c0 / 2, pdk);
+        }
+      };
+      if (mx) probs(std::true_type{});
+      else probs(std::false_type{});
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(&p_full);
+      if (!wwait(&dp_full, i & 1, p.status, abort)) { ok = false; break; }
+      tc_fence_after();
+      auto scores = [&](auto masked) {
+        constexpr bool MASK = decltype(masked)::value;
+#pragma unroll
+        for (int c0 = 0; c0 < CW; c0 += 16) {
+          float dp[16], dd[16];
+          uint32_t sk[8], sdk[8];
+          tmem_ld16_nowait(lane_base + C::C_DP + c0, dp);
+          if (DUAL) tmem_ld16_nowait(lane_base + C::C_DPD + c0, dd);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 d4 = stat[BT / 4 + (c0 + e) / 4];
+            const uint64_t dv[2] = {pair(d4.x, d4.y), pair(d4.z, d4.w)};
+            float4 g4 = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (DUAL) g4 = stat[3 * (BT / 4) + (c0 + e) / 4];
+            const uint64_t gv[2] = {pair(g4.x, g4.y), pair(g4.z, g4.w)};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int f = e + 2 * u, c = c0 + f;
+              const uint64_t pp = pair(pr[c], pr[c + 1]);
+              const uint64_t x = fma2(dv[u], neg1, pair(dp[f], dp[f + 1]));
+              float2 s = halves(mul2(pp, x));
+              const bool o0 = !MASK || own(c), o1 = !MASK || own(c + 1);
+              if (!o0) s.x = 0.f;
+              if (!o1) s.y = 0.f;
+              sk[f / 2] = pack_bf16x2(s.x, s.y);
+              if (DUAL) {
+                const uint64_t y = fma2(gv[u], neg1, pair(dd[f], dd[f + 1]));
+                float2 z = halves(fma2(pair(pd[c], pd[DUAL ? c + 1 : 0]), x, mul2(pp, y)));
+                if (!o0) z.x = 0.f;
+                if (!o1) z.y = 0.f;
+                sdk[f / 2] = pack_bf16x2(z.x, z.y);
+              }
+              if (MASK && any_bad) {
+                const uint32_t n = nan_pair(badw[c >> 5] >> (c & 31), o0, o1);
+                sk[f / 2] |= n;
+                if (DUAL) sdk[f / 2] |= n;
+              }
+            }
+          }
+          tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
+          if (DUAL) tmem_st8(lane_base + C::C_DPD + c0 / 2, sdk);
+        }
+      };
+      if (mx) scores(std::true_type{});
+      else scores(std::false_type{});
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(&ds_full);
+    }
+    if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
+      tc_fence_after();
+      const int64_t row = row0 + r;
+      const bool on = r < nvalid;
+      const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16);
+      auto put = [&](uint32_t c, __nv_bfloat16* dst, float f) {
+#pragma unroll 1
+        for (int c0 = half * (HDP / 2); c0 < (half + 1) * (HDP / 2); c0 += 16) {
+          if (c0 >= p.D) break;
+          float v[16];
+          tmem_ld16(acc + c + c0, v);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] *= f;
+          if (on) put16(dst, c0, p.D, v);
+        }
+      };
+      put(C::C_A, p.dv + row * p.lddv + hk * p.D, 1.f);
+      put(C::C_B, p.dk + row * p.lddk + hk * p.D, p.scale);
+      if (DUAL) {
+        put(C::C_A + HDP, p.dvd + row * p.lddv + hk * p.D, 1.f);
+        put(C::C_B + HDP, p.dkd + row * p.lddk + hk * p.D, p.scale);
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
+                 "r"(C::COLS_KV));
+  }
+}
+
+template <bool DUAL, int HDP>
+__global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>::CTAS)
+    attn_tc_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmO,
+                         const __grid_constant__ CUtensorMap tmQd, const __grid_constant__ CUtensorMap tmOd,
+                         const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                         const __grid_constant__ CUtensorMap tmKd, const __grid_constant__ CUtensorMap tmVd,
+                         const __grid_constant__ TcParams2 p) {
+  using C = BwdCfg<DUAL, HDP>;
+  constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t res_full, s_full, s_free, dp_full, ds_full, drain;
+  __shared__ __align__(8) uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
+  __shared__ uint32_t bad[C::STAGES][4];
+  __shared__ float2 sD[2][TR];
+  __shared__ SeqTile st_rows;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* sRes = smem;                        // Q (Q'), dO (dO')
+  uint8_t* sSt = smem + 2 * C::RES1;           // stage: K (K'), V (V')
+  const int h = static_cast<int>(blockIdx.x % p.Hq);
+  const int row0 = (p.tiles - 1 - static_cast<int>(blockIdx.x / p.Hq)) * TR;
+  const int hk = h / (p.Hq / p.Hkv);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  pdl_entry();
+  const int nvalid = min(seq_total(p.seq) - row0, TR);
+  if (nvalid <= 0) return;
+  seq_tile_init(p.seq, row0, st_rows);
+  if (threadIdx.x == 0) {
+    mbar_init(&res_full, 1);
+    mbar_init(&s_full, 1);
+    mbar_init(&s_free, C::EW);
+    mbar_init(&dp_full, 1);
+    mbar_init(&ds_full, C::EW);
+    mbar_init(&drain, 1);
+    for (int i = 0; i < C::STAGES; ++i) {
+      mbar_init(&st_full[i], 1);
+      mbar_init(&st_empty[i], 1);
+      mbar_init(&st_clean[i], 1);
+    }
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(&tmem_slot)),
+                 "r"(C::COLS_Q));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  __syncthreads();
+  seq_tile_fill(p.seq, row0, st_rows, C::THREADS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tb = tmem_slot;
+  volatile int* abort = &abort_flag;
+  const int k0 = tile_lo(st_rows, row0, 0), lo1 = tile_lo(st_rows, row0, nvalid - 1);
+  const int nkt = (row0 + nvalid - k0 + BT - 1) / BT;
+  auto mixed = [&](int j) { return k0 + j * BT + BT - 1 > row0 || k0 + j * BT < lo1; };
+
+  if (warp == 0) {
+    if (elect_one()) {
+      // ---- TMA producer ---------------------------------------------------------------------------
+      mbar_expect_tx(&res_full, 2 * C::RES1);
+#pragma unroll
+      for (int a = 0; a < NA; ++a) {
+        tma_load_3d(sRes + a * ATOM128, &tmQ, &res_full, 64 * a, row0, h);
+        tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmO, &res_full, 64 * a, row0, h);
+        if (DUAL) {
+          tma_load_3d(sRes + (NA + a) * ATOM128, &tmQd, &res_full, 64 * a, row0, h);
+          tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmOd, &res_full, 64 * a, row0, h);
+        }
+      }
+      int issued = 0;
+      for (int j = 0; j < nkt; ++j) {
+        const int st = j % C::STAGES;
+        if (!fwait(&st_empty[st], ((j / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+        mbar_expect_tx(&st_full[st], C::STAGE_B);
+        uint8_t* b = sSt + st * C::STAGE_B;
+        const int kr = k0 + j * BT;
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+          tma_load_3d(b + a * C::BATOM, &tmK, &st_full[st], 64 * a, kr, hk);
+          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmV, &st_full[st], 64 * a, kr, hk);
+          if (DUAL) {
+            tma_load_3d(b + (NA + a) * C::BATOM, &tmKd, &st_full[st], 64 * a, kr, hk);
+            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmVd, &st_full[st], 64 * a, kr, hk);
+          }
+        }
+        ++issued;
+      }
+      mbar_wait(&res_full, 0, p.status, FTC_WAIT_NS);
+      drain_loads(st_full, issued, C::STAGES, p.status);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---- products ------------------------------------------------------------------------------------
+    constexpr uint32_t idS = idesc_bf16(TR, BT), idS2 = idesc_bf16(TR, 2 * BT);
+    constexpr uint32_t idA = idesc_bf16(TR, HDP) | (1u << 16), idA2 = idesc_bf16(TR, 2 * HDP) | (1u << 16);
+    const uint64_t dQ = sdesc_sw128(smem_u32(sRes)), dO = dQ + (C::RES1 >> 4);
+    constexpr uint64_t RD = NA * ATOM128 >> 4;
+    const uint64_t kSt = sdesc_sw128(smem_u32(sSt)), mSt = sdesc_mn(smem_u32(sSt), C::BATOM);
+    constexpr uint64_t ST = C::STAGE_B >> 4, VO = C::TILE_B >> 4;
+    auto score = [&](uint64_t x, uint64_t y, uint32_t c) {
+#pragma unroll
+      for (int kk = 0; kk < HDP / 16; ++kk)
+        mma_bf16(tb + c, x + (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3),
+                 y + (kk >> 2) * (C::BATOM >> 4) + 2 * (kk & 3), DUAL ? idS2 : idS, kk > 0);
+      if (DUAL) {
+#pragma unroll
+        for (int kk = 0; kk < HDP / 16; ++kk)
+          mma_bf16(tb + c + BT, x + RD + 2 * kk, y + 2 * kk, idS, 1);
+      }
+    };
+    auto look_over = [&](int j) -> bool {
+      const int st = j % C::STAGES;
+      if (!wwait(&st_full[st], (j / C::STAGES) & 1, p.status, abort)) return false;
+      // K (K') multiplies dS; V (V') only meets dO, whose product with a masked key is dropped
+      if (mixed(j)) scrub(sSt + st * C::STAGE_B, BT, C::NT * NA, bad[st], lane);
+      if (lane == 0) mbar_arrive_local(&st_clean[st]);
+      __syncwarp();
+      return true;
+    };
+    bool ok = wwait(&res_full, 0, p.status, abort) && look_over(0);
+    if (ok) {
+      tc_fence_after();
+      if (elect_one()) {
+        score(dQ, kSt, C::C_S);
+        mma_commit(&s_full);
+        score(dO, kSt + VO, C::C_DP);
+        mma_commit(&dp_full);
+      }
+      __syncwarp();
+    }
+    for (int j = 0; ok && j < nkt; ++j) {
+      const int st = j % C::STAGES, sn = (j + 1) % C::STAGES;
+      const bool more = j + 1 < nkt;
+      if (more) {
+        if (!look_over(j + 1)) break;
+        if (!wwait(&s_free, j & 1, p.status, abort)) break;
+        tc_fence_after();
+        if (elect_one()) {
+          score(dQ, kSt + sn * ST, C::C_S);
+          mma_commit(&s_full);
+        }
+        __syncwarp();
+      }
+      if (!wwait(&ds_full, j & 1, p.status, abort)) break;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t mK = mSt + st * ST;
+#pragma unroll
+        for (int kk = 0; kk < BT / 16; ++kk) {
+          const uint32_t ac = C::C_DP + (kk / (CW / 16)) * CW + (kk % (CW / 16)) * 8;
+          const uint32_t acc = (j > 0 || kk > 0) ? 1u : 0u;
+          mma_ts(tb + C::C_A, tb + ac, mK + 128 * kk, DUAL ? idA2 : idA, acc);
+          if (DUAL) mma_ts(tb + C::C_A + HDP, tb + ac + BT, mK + 128 * kk, idA, 1);
+        }
+        mma_commit(&st_empty[st]);
+        if (more) {
+          score(dO, kSt + sn * ST + VO, C::C_DP);
+          mma_commit(&dp_full);
+        }
+      }
+      __syncwarp();
+    }
+    if (elect_one()) mma_commit(&drain);
+    __syncwarp();
+    mbar_wait(&drain, 0, p.status, FTC_WAIT_NS);
+  } else {
+    // ---- rows: query row r (TMEM lane r), key columns cb .. cb + CW - 1 ---------------------------------
+    const int q4 = warp & 3;
+    const int r = q4 * 32 + lane;
+    const int half = (warp - 2) >> 2, cb = half * CW;
+    const uint32_t lane_base = tb + (static_cast<uint32_t>(q4 * 32) << 16) + cb;
+    const int lo = tile_lo(st_rows, row0, r);
+    const int64_t row = row0 + r, si = static_cast<int64_t>(h) * p.seq.rows + row;
+    const bool on = r < nvalid;
+    // D of the row, half by each of its two threads
+    sD[half][r] = on ? row_dots<DUAL>(p, row, h, half * (HDP / 2), (half + 1) * (HDP / 2))
+                     : make_float2(0.f, 0.f);
+    row_bar();
+    const float Dv = sD[0][r].x + sD[1][r].x, Dd = sD[0][r].y + sD[1][r].y;
+    if (on && half == 0) {
+      p.Dr[si] = Dv;
+      if (DUAL) p.Drd[si] = Dd;
+    }
+    const float lse2 = on ? p.lse[si] * LOG2E : 0.f, rb = DUAL && on ? p.rbar[si] : 0.f;
+    const uint64_t c2p = pair(p.c2, p.c2), nl = pair(-lse2, -lse2), nD = pair(-Dv, -Dv);
+    const uint64_t nr = pair(-rb, -rb), nDd = pair(-Dd, -Dd), sc = pair(p.scale, p.scale);
+    bool ok = true;
+    for (int j = 0; j < nkt; ++j) {
+      const int st = j % C::STAGES;
+      const bool mx = mixed(j);
+      const int a = lo - (k0 + j * BT), b = row0 + r - (k0 + j * BT);
+      uint32_t badw[CW / 32];
+      bool any_bad = false;
+      if (mx) {
+        if (!wwait(&st_clean[st], (j / C::STAGES) & 1, p.status, abort)) { ok = false; break; }
+#pragma unroll
+        for (int w = 0; w < CW / 32; ++w) { badw[w] = bad[st][cb / 32 + w]; any_bad |= badw[w] != 0; }
+      }
+      if (!wwait(&s_full, j & 1, p.status, abort)) { ok = false; break; }
+      tc_fence_after();
+      auto own = [&](int c) { return cb + c >= a && cb + c <= b; };
+      float pr[CW], pd[DUAL ? CW : 1];
+      auto probs = [&](auto masked) {
+        constexpr bool MASK = decltype(masked)::value;
+#pragma unroll
+        for (int c0 = 0; c0 < CW; c0 += 16) {
+          float sv[16], sd[16];
+          tmem_ld16_nowait(lane_base + C::C_S + c0, sv);
+          if (DUAL) tmem_ld16_nowait(lane_base + C::C_SD + c0, sd);
+          tmem_wait_ld();
+#pragma unroll
+          for (int f = 0; f < 16; f += 2) {
+            const int c = c0 + f;
+            const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, nl));
+            pr[c] = ex2(x.x);
+            pr[c + 1] = ex2(x.y);
+            if (MASK && !own(c)) pr[c] = 0.f;
+            if (MASK && !own(c + 1)) pr[c + 1] = 0.f;
+            if (DUAL) {
+              const float2 y = halves(mul2(pair(pr[c], pr[c + 1]), fma2(pair(sd[f], sd[f + 1]), sc, nr)));
+              pd[c] = y.x;
+              pd[DUAL ? c + 1 : 0] = y.y;
+            }
+          }
+        }
+      };
+      if (mx) probs(std::true_type{});
+      else probs(std::false_type{});
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(&s_free);
+      if (!wwait(&dp_full, j & 1, p.status, abort)) { ok = false; break; }
+      tc_fence_after();
+      auto scores = [&](auto masked) {
+        constexpr bool MASK = decltype(masked)::value;
+#pragma unroll
+        for (int c0 = 0; c0 < CW; c0 += 16) {
+          float dp[16], dd[16];
+          uint32_t sk[8], sdk[8];
+          tmem_ld16_nowait(lane_base + C::C_DP + c0, dp);
+          if (DUAL) tmem_ld16_nowait(lane_base + C::C_DPD + c0, dd);
+          tmem_wait_ld();
+#pragma unroll
+          for (int f = 0; f < 16; f += 2) {
+            const int c = c0 + f;
+            const uint64_t pp = pair(pr[c], pr[c + 1]);
+            const uint64_t x = add2(pair(dp[f], dp[f + 1]), nD);
+            float2 s = halves(mul2(pp, x));
+            const bool o0 = !MASK || own(c), o1 = !MASK || own(c + 1);
+            if (!o0) s.x = 0.f;
+            if (!o1) s.y = 0.f;
+            sk[f / 2] = pack_bf16x2(s.x, s.y);
+            if (DUAL) {
+              const uint64_t y = add2(pair(dd[f], dd[f + 1]), nDd);
+              float2 z = halves(fma2(pair(pd[c], pd[DUAL ? c + 1 : 0]), x, mul2(pp, y)));
+              if (!o0) z.x = 0.f;
+              if (!o1) z.y = 0.f;
+              sdk[f / 2] = pack_bf16x2(z.x, z.y);
+            }
+            if (MASK && any_bad) {
+              const uint32_t n = nan_pair(badw[c >> 5] >> (c & 31), o0, o1);
+              sk[f / 2] |= n;
+              if (DUAL) sdk[f / 2] |= n;
+            }
+          }
+          tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
+          if (DUAL) tmem_st8(lane_base + C::C_DPD + c0 / 2, sdk);
+        }
+      };
+      if (mx) scores(std::true_type{});
+      else scores(std::false_type{});
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(&ds_full);
+    }
+    if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
+      tc_fence_after();
+      const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16);
+      auto put = [&](uint32_t c, __nv_bfloat16* dst) {
+#pragma unroll 1
+        for (int c0 = half * (HDP / 2); c0 < (half + 1) * (HDP / 2); c0 += 16) {
+          if (c0 >= p.D) break;
+          float v[16];
+          tmem_ld16(acc + c + c0, v);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] *= p.scale;
+          if (on) put16(dst, c0, p.D, v);
+        }
+      };
+      put(C::C_A, p.dq + row * p.lddq + h * p.D);
+      if (DUAL) put(C::C_A + HDP, p.dqd + row * p.lddq + h * p.D);
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
+                 "r"(C::COLS_Q));
+  }
+}
+
+template <bool DUAL, int HDP>
+cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
+  using C = BwdCfg<DUAL, HDP>;
+  const int N = a.seq.rows;
+  // {q, dO} and {k, v} with their tangents, as 128-row and as streamed boxes
+  CUtensorMap qr[4], qs[4], kr[4], ks[4];
+  const __nv_bfloat16* qo[4] = {a.q, a.d_o, DUAL ? a.qd : nullptr, DUAL ? a.d_od : nullptr};
+  const __nv_bfloat16* kv[4] = {a.k, a.v, DUAL ? a.kd : nullptr, DUAL ? a.vd : nullptr};
+  for (int i = 0; i < 4; ++i) {
+    const int64_t lq = i & 1 ? a.lddo : a.ldq, lk = i & 1 ? a.ldv : a.ldk;
+    if (!head_map(&qr[i], qo[i], a.D, N, lq, a.Hq, TR) || !head_map(&qs[i], qo[i], a.D, N, lq, a.Hq, C::BT) ||
+        !head_map(&kr[i], kv[i], a.D, N, lk, a.Hkv, TR) || !head_map(&ks[i], kv[i], a.D, N, lk, a.Hkv, C::BT))
+      return cudaErrorInvalidValue;
+  }
+  static PerDeviceOnce once;
+  cudaError_t e = once.run([](int&) {
+    cudaError_t r = cudaFuncSetAttribute(attn_tc_bwd_kv_kernel<DUAL, HDP>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_KV);
+    if (r != cudaSuccess) return r;
+    return cudaFuncSetAttribute(attn_tc_bwd_q_kernel<DUAL, HDP>,
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_Q);
+  });
+  if (e != cudaSuccess) return e;
+  const TcParams2 p = tc_params(a);
+  const int64_t grid = static_cast<int64_t>(p.tiles) * a.Hq;
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  e = launch_k(attn_tc_bwd_q_kernel<DUAL, HDP>, dim3(static_cast<unsigned>(grid)), dim3(C::THREADS),
+               C::SMEM_Q, s, qr[0], qr[1], qr[2], qr[3], ks[0], ks[1], ks[2], ks[3], p);
+  if (e != cudaSuccess) return e;
+  return launch_k(attn_tc_bwd_kv_kernel<DUAL, HDP>, dim3(static_cast<unsigned>(p.tiles * a.Hkv)),
+                  dim3(C::THREADS), C::SMEM_KV, s, kr[0], kr[1], kr[2], kr[3], qs[0], qs[1], qs[2],
+                  qs[3], p);
+}
+
 }  // namespace
+
+cudaError_t attn_tc_bwd(const AttnParams& a, bool dual, cudaStream_t s) {
+  if (dual) return launch_bwd<true, 64>(a, s);
+  return a.D <= 64 ? launch_bwd<false, 64>(a, s) : launch_bwd<false, 128>(a, s);
+}
 
 cudaError_t attn_tc_fwd(const AttnParams& a, bool dual, cudaStream_t s) {
   if (dual) return launch_fwd<true, 64>(a, s);

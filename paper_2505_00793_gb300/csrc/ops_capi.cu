@@ -262,7 +262,7 @@ mf_status mf_attn_bwd(const mf_attn_args* args, void* stream) {
   AttnParams p;
   const mf_status st = attn_params(*args, true, &p);
   if (st != MF_OK || args->n_rows == 0) return st;
-  return done(mf::attn_rows_bwd(p, args->qd != nullptr, static_cast<cudaStream_t>(stream)));
+  return done(mf::attn_tc_bwd(p, args->qd != nullptr, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"
