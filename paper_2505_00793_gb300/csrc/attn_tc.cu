@@ -76,23 +76,34 @@ struct SeqTile {
   uint32_t bits[4];
 };
 
-// Row count of the batch that belongs to sequences is read by every thread; the table is filled
-// by all threads of the block between two barriers.
-__device__ __forceinline__ void seq_tile_init(const SeqRows& s, int row0, SeqTile& t) {
-  if (threadIdx.x < 4) t.bits[threadIdx.x] = 0;
-  if (threadIdx.x == 4) t.lo0 = s.start ? 0 : row0 - row0 % s.len;
-  if (threadIdx.x == 5) t.hi1 = s.start ? s.rows : (row0 + TR - 1) - (row0 + TR - 1) % s.len + s.len;
+// The table is filled by all threads of the block: each reads its first start (SeqLoad) before
+// the block's first barrier, so that the reads of the prologue are in flight together.
+struct SeqLoad {
+  int first, v;
+};
+__device__ __forceinline__ SeqLoad seq_tile_load(const SeqRows& s, int row0) {
+  SeqLoad l{0, 0};
+  if (!s.start) return l;
+  if (s.n > 2048) l.first = seq_find(s, row0);   // long tables: from the first row's sequence on
+  const int i = l.first + static_cast<int>(threadIdx.x);
+  if (i <= s.n) l.v = s.start[i];
+  return l;
 }
-__device__ __forceinline__ void seq_tile_fill(const SeqRows& s, int row0, SeqTile& t, int threads) {
+__device__ __forceinline__ void seq_tile_init(const SeqRows& s, int row0, SeqTile& t) {
+  const int e = static_cast<int>(threadIdx.x) - 64;
+  if (e >= 0 && e < 4) t.bits[e] = 0;
+  if (e == 4) t.lo0 = s.start ? 0 : row0 - row0 % s.len;
+  if (e == 5) t.hi1 = s.start ? s.rows : (row0 + TR - 1) - (row0 + TR - 1) % s.len + s.len;
+}
+__device__ __forceinline__ void seq_tile_fill(const SeqRows& s, int row0, SeqTile& t, int threads,
+                                              const SeqLoad& l) {
   if (!s.start) {
     const int p = threadIdx.x;
     if (p > 0 && p < TR && (row0 + p) % s.len == 0) atomicOr(&t.bits[p >> 5], 1u << (p & 31));
     return;
   }
-  // long tables: from the first row's sequence on
-  const int first = s.n > 2048 ? seq_find(s, row0) : 0;
-  for (int i = first + static_cast<int>(threadIdx.x); i <= s.n; i += threads) {
-    const int v = s.start[i];
+  int v = l.v;
+  for (int i = l.first + static_cast<int>(threadIdx.x); i <= s.n;) {
     if (v <= row0) {
       atomicMax(&t.lo0, v);
     } else if (v - row0 < TR) {
@@ -101,6 +112,8 @@ __device__ __forceinline__ void seq_tile_fill(const SeqRows& s, int row0, SeqTil
       atomicMin(&t.hi1, v);
       break;
     }
+    i += threads;
+    if (i <= s.n) v = s.start[i];
   }
 }
 // First row of row0 + r's sequence, and the row behind its last.
@@ -115,6 +128,17 @@ __device__ __forceinline__ int tile_hi(const SeqTile& t, int row0, int r) {
   uint32_t m = (r & 31) == 31 ? 0u : t.bits[w] & (0xffffffffu << ((r & 31) + 1));
   while (!m && w < 3) m = t.bits[++w];
   return m ? row0 + w * 32 + __ffs(m) - 1 : t.hi1;
+}
+
+// Bits lo .. hi of a word of 32 columns.
+__device__ __forceinline__ uint32_t col_bits(int lo, int hi) {
+  lo = max(lo, 0);
+  hi = min(hi, 31);
+  return lo > hi ? 0u : (0xffffffffu << lo) & (0xffffffffu >> (31 - hi));
+}
+// bf16 pair with NaN in the halves whose bits of w are set.
+__device__ __forceinline__ uint32_t nan_pair(uint32_t w) {
+  return (w & 1 ? 0x7fffu : 0u) | (w & 2 ? 0x7fff0000u : 0u);
 }
 
 // ---- non-finite values of a mixed tile --------------------------------------------------------
@@ -160,8 +184,8 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 
 // ---- forward ------------------------------------------------------------------------------------
 // One CTA per (query head, 128 rows): warp 0 loads (Q once, then key tiles into a ring of K and a
-// ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..5 hold
-// a row a thread.  The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T
+// ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..9 hold
+// the rows, two threads a row, each half of a tile's keys.  The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T
 // into S'; P [V | V'] -> [O | T], then (P (*) S') V into T; o' = T / l - rbar o.
 template <bool DUAL, int HDP>
 struct FwdCfg {
@@ -173,7 +197,9 @@ struct FwdCfg {
   static constexpr int TILE_B = NT * NA * KATOM;           // K (K') or V (V') of a tile
   static constexpr int STAGES = HDP == 128 ? 1 : 2;
   static constexpr int SMEM = Q_B + 2 * STAGES * TILE_B + 1024;
-  static constexpr int THREADS = 192;
+  static constexpr int EW = 8;                             // row warps: two threads a row
+  static constexpr int THREADS = 64 + 32 * EW;
+  static constexpr int HC = TK / 2;                        // keys of a row thread
   static constexpr int CTAS = 2;
   static constexpr uint32_t TMEM_COLS = 256;
   static constexpr uint32_t C_S = 0, C_SD = 64, C_O = 128, C_T = 192;
@@ -213,6 +239,8 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   __shared__ __align__(8) uint64_t k_full[C::STAGES], k_empty[C::STAGES];
   __shared__ __align__(8) uint64_t v_full[C::STAGES], v_empty[C::STAGES], v_clean[C::STAGES];
   __shared__ uint32_t bad[C::STAGES][4];
+  __shared__ float row_max[2][2][TR];
+  __shared__ float2 row_sum[2][TR];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
@@ -230,13 +258,14 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_entry();
+  const SeqLoad sl = seq_tile_load(p.seq, row0);
   const int nvalid = min(seq_total(p.seq) - row0, TR);
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
   if (threadIdx.x == 0) {
     mbar_init(&q_full, 1);
     mbar_init(&s_full, 1);
-    mbar_init(&p_full, 4);
+    mbar_init(&p_full, C::EW);
     mbar_init(&drain, 1);
     for (int i = 0; i < C::STAGES; ++i) {
       mbar_init(&k_full[i], 1);
@@ -247,6 +276,13 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
     }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    // the rows' own operands need nothing of the sequences
+    mbar_expect_tx(&q_full, C::Q_B);
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+      tma_load_3d(sQ + a * ATOM128, &tmQ, &q_full, 64 * a, row0, h);
+      if (DUAL) tma_load_3d(sQ + (NA + a) * ATOM128, &tmQd, &q_full, 64 * a, row0, h);
+    }
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -255,7 +291,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   __syncthreads();
-  seq_tile_fill(p.seq, row0, st_rows, C::THREADS);
+  seq_tile_fill(p.seq, row0, st_rows, C::THREADS, sl);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -269,12 +305,6 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   if (warp == 0) {
     if (elect_one()) {
       // ---- TMA producer ---------------------------------------------------------------------
-      mbar_expect_tx(&q_full, C::Q_B);
-#pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        tma_load_3d(sQ + a * ATOM128, &tmQ, &q_full, 64 * a, row0, h);
-        if (DUAL) tma_load_3d(sQ + (NA + a) * ATOM128, &tmQd, &q_full, 64 * a, row0, h);
-      }
       int nk = 0, nv = 0;
       for (int j = 0; j < nkt; ++j) {
         const int st = j % C::STAGES;
@@ -352,8 +382,8 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
 #pragma unroll
         for (int kk = 0; kk < TK / 16; ++kk) {
           const uint32_t acc = (j > 0 || kk > 0) ? 1u : 0u;
-          // keys 64.. of a tile sit 64 columns on, where their scores were
-          const uint32_t pc = (kk >> 2) * 64 + 8 * (kk & 3);
+          // each 32 keys' P begins where their scores did
+          const uint32_t pc = (kk >> 1) * 32 + 8 * (kk & 1);
           if (DUAL) {
             mma_ts(tb + C::C_O, tb + C::C_S + pc, mV + 128 * kk, idO2, acc);
             mma_ts(tb + C::C_T, tb + C::C_SD + pc, mV + 128 * kk, idO, 1);
@@ -371,51 +401,61 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
     __syncwarp();
     mbar_wait(&drain, 0, p.status, FTC_WAIT_NS);
   } else {
-    // ---- rows: thread r owns row row0 + r (TMEM lane r) ------------------------------------------
+    // ---- rows: row row0 + r (TMEM lane r), keys cb .. cb + HC - 1 of each tile ------------------------
+    constexpr int HC = C::HC;
     const int q4 = warp & 3;
     const int r = q4 * 32 + lane;
-    const uint32_t lane_base = tb + (static_cast<uint32_t>(q4 * 32) << 16);
+    const int half = (warp - 2) >> 2, cb = half * HC;
+    const uint32_t lanes = tb + (static_cast<uint32_t>(q4 * 32) << 16);
+    const uint32_t aS = lanes + C::C_S + cb, aSd = lanes + C::C_SD + cb;
     const int lo = tile_lo(st_rows, row0, r);
+    const uint64_t c2p = pair(p.c2, p.c2), scp = pair(p.scale, p.scale);
     float m2 = -INFINITY, l = 0.f, rs = 0.f;
     bool ok = true;
     for (int j = 0; j < nkt; ++j) {
       const int st = j % C::STAGES;
       const bool mx_tile = mixed(j);
-      if (!wwait(&s_full, j & 1, p.status, abort)) { ok = false; break; }
-      uint32_t badw[TK / 32];
-      bool any_bad = false;
+      // a thread that gives up still meets its row's other thread once a tile
+      ok = ok && wwait(&s_full, j & 1, p.status, abort);
+      // the row's own keys among this thread's, and those of them whose V is not finite
+      uint32_t own[HC / 32], bads[HC / 32];
       if (mx_tile) {
-        if (!wwait(&v_clean[st], (j / C::STAGES) & 1, p.status, abort)) { ok = false; break; }
+        ok = ok && wwait(&v_clean[st], (j / C::STAGES) & 1, p.status, abort);
+        const int kb = k0 + j * TK + cb;
 #pragma unroll
-        for (int i = 0; i < TK / 32; ++i) { badw[i] = bad[st][i]; any_bad |= badw[i] != 0; }
+        for (int c = 0; c < HC / 32; ++c) {
+          own[c] = col_bits(lo - kb - 32 * c, row0 + r - kb - 32 * c);
+          bads[c] = own[c] & bad[st][cb / 32 + c];
+        }
       }
       tc_fence_after();
-      // keys a .. b of this tile are the row's own
-      const int a = lo - (k0 + j * TK), b = row0 + r - (k0 + j * TK);
-      float sv[64];
-      auto own = [&](int i) { return i >= a && i <= b; };
-      auto tile_max = [&](int c0, float mx) {
-        tmem_ld32_nowait(lane_base + C::C_S + c0, sv);
-        tmem_ld32_nowait(lane_base + C::C_S + c0 + 32, sv + 32);
+      float sv[32];
+      auto load_scores = [&](int c) {
+        tmem_ld32_nowait(aS + 32 * c, sv);
         tmem_wait_ld();
         if (mx_tile) {
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (own(c0 + i)) mx = fmaxf(mx, sv[i]);
-        } else {
-          float y0 = mx, y1 = sv[0];
-#pragma unroll
-          for (int i = 0; i < 64; i += 4) {
-            y0 = fmaxf(fmaxf(y0, sv[i]), sv[i + 1]);
-            y1 = fmaxf(fmaxf(y1, sv[i + 2]), sv[i + 3]);
-          }
-          mx = fmaxf(y0, y1);
+          for (int i = 0; i < 32; ++i) sv[i] = own[c] >> i & 1 ? sv[i] : -INFINITY;
         }
-        return mx;
       };
       float mx = -INFINITY;
 #pragma unroll
-      for (int c0 = 0; c0 < TK; c0 += 64) mx = tile_max(c0, mx);
+      for (int c = 0; c < HC / 32; ++c) {
+        if (!ok) break;
+        load_scores(c);
+        float y0 = mx, y1 = sv[0];
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          y0 = fmaxf(fmaxf(y0, sv[i]), sv[i + 1]);
+          y1 = fmaxf(fmaxf(y1, sv[i + 2]), sv[i + 3]);
+        }
+        mx = fmaxf(y0, y1);
+      }
+      // the row's other thread has the other half of the keys
+      row_max[j & 1][half][r] = mx;
+      asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+      if (!ok) continue;
+      mx = fmaxf(mx, row_max[j & 1][half ^ 1][r]);
       const float t2 = mx * p.c2;
       float f = 1.f;
       if (t2 > m2 + TAU) {
@@ -427,65 +467,53 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
         // scores j were issued behind the products of tile j - 1, which are done
 #pragma unroll 1
-        for (int c0 = 0; c0 < HDP * C::NT; c0 += 16) {
+        for (int c0 = 0; c0 < HDP * C::NT / 2; c0 += 16) {
           float v[16];
-          tmem_ld16(lane_base + C::C_O + c0, v);
+          const uint32_t at = lanes + C::C_O + half * (HDP * C::NT / 2) + c0;
+          tmem_ld16(at, v);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] *= f;
-          tmem_st16(lane_base + C::C_O + c0, v);
+          tmem_st16(at, v);
         }
       }
       const float base = m2 == -INFINITY ? 0.f : m2;     // no key of the row so far: P = 0
-      const uint64_t c2p = pair(p.c2, p.c2), nm = pair(-base, -base);
+      const uint64_t nm = pair(-base, -base);
       uint64_t l2 = 0, r2 = 0;
-      auto probs = [&](int c0, auto masked) {
-        constexpr bool MASK = decltype(masked)::value;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          uint32_t pk[16], psk[16];
-          float sd[32];
-          if (DUAL) {
-            tmem_ld32_nowait(lane_base + C::C_SD + c0 + 32 * g, sd);
-            tmem_wait_ld();
-          }
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const int e = 32 * g + i;
-            const float2 x = halves(fma2(pair(sv[e], sv[e + 1]), c2p, nm));
-            float p0 = ex2(x.x), p1 = ex2(x.y);
-            const bool o0 = !MASK || own(c0 + e), o1 = !MASK || own(c0 + e + 1);
-            if (!o0) p0 = 0.f;
-            if (!o1) p1 = 0.f;
-            const uint64_t pp = pair(p0, p1);
-            l2 = add2(l2, pp);
-            pk[i / 2] = pack_bf16x2(p0, p1);
-            if (DUAL) {
-              float2 ps = halves(mul2(pp, pair(sd[i], sd[i + 1])));
-              if (!o0) ps.x = 0.f;      // the tangent's score may be anything there
-              if (!o1) ps.y = 0.f;
-              r2 = add2(r2, pair(ps.x, ps.y));
-              psk[i / 2] = pack_bf16x2(ps.x * p.scale, ps.y * p.scale);
-            }
-            if (MASK && any_bad) {
-              const uint32_t w = badw[(c0 + e) >> 5] >> (e & 31);
-              const uint32_t nan2 = (o0 && (w & 1) ? 0x7fffu : 0u) | (o1 && (w & 2) ? 0x7fff0000u : 0u);
-              pk[i / 2] |= nan2;
-              if (DUAL) psk[i / 2] |= nan2;
-            }
-          }
-          tmem_st16u(lane_base + C::C_S + c0 + 16 * g, pk);
-          if (DUAL) tmem_st16u(lane_base + C::C_SD + c0 + 16 * g, psk);
-        }
-      };
-#pragma unroll
-      for (int c0 = TK - 64; c0 >= 0; c0 -= 64) {
-        if (c0 != TK - 64) {   // the last 64 keys' scores are still in registers
-          tmem_ld32_nowait(lane_base + C::C_S + c0, sv);
-          tmem_ld32_nowait(lane_base + C::C_S + c0 + 32, sv + 32);
+      for (int c = HC / 32 - 1; c >= 0; --c) {
+        if (c != HC / 32 - 1) load_scores(c);            // the last ones are still here
+        float sd[32];
+        if (DUAL) {
+          tmem_ld32_nowait(aSd + 32 * c, sd);
           tmem_wait_ld();
+          if (mx_tile) {   // the tangent of a masked score may be anything
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sd[i] = own[c] >> i & 1 ? sd[i] : 0.f;
+          }
         }
-        if (mx_tile) probs(c0, std::true_type{});
-        else probs(c0, std::false_type{});
+        uint32_t pk[16], psk[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          const float2 x = halves(fma2(pair(sv[i], sv[i + 1]), c2p, nm));
+          const float p0 = ex2(x.x), p1 = ex2(x.y);
+          const uint64_t pp = pair(p0, p1);
+          l2 = add2(l2, pp);
+          pk[i / 2] = pack_bf16x2(p0, p1);
+          if (DUAL) {
+            const uint64_t ps = mul2(mul2(pp, scp), pair(sd[i], sd[i + 1]));
+            r2 = add2(r2, ps);
+            psk[i / 2] = pack2(ps);
+          }
+        }
+        if (mx_tile && bads[c]) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            pk[i] |= nan_pair(bads[c] >> (2 * i));
+            if (DUAL) psk[i] |= nan_pair(bads[c] >> (2 * i));
+          }
+        }
+        tmem_st16u(aS + 32 * c, pk);
+        if (DUAL) tmem_st16u(aSd + 32 * c, psk);
       }
       const float2 lh = halves(l2), rh = halves(r2);
       l += lh.x + lh.y;
@@ -495,20 +523,25 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       __syncwarp();
       if (lane == 0) mbar_arrive_local(&p_full);
     }
+    // the row's sums over both threads (every row thread meets the barrier)
+    row_sum[half][r] = make_float2(l, rs);
+    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+    l = row_sum[0][r].x + row_sum[1][r].x;
+    rs = row_sum[0][r].y + row_sum[1][r].y;
     if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const float inv = 1.f / l;
-      const float rb = DUAL ? rs * p.scale * inv : 0.f;
+      const float rb = DUAL ? rs * inv : 0.f;
       const int64_t row = row0 + r;
       const bool on = r < nvalid;
       __nv_bfloat16* orow = p.ow + row * p.ldo + h * p.D;
       __nv_bfloat16* drow = DUAL ? p.owd + row * p.ldo + h * p.D : nullptr;
 #pragma unroll 1
-      for (int c0 = 0; c0 < HDP; c0 += 16) {
+      for (int c0 = half * (HDP / 2); c0 < (half + 1) * (HDP / 2); c0 += 16) {
         if (c0 >= p.D) break;
         float o[16], t[16];
-        tmem_ld16(lane_base + C::C_O + c0, o);
-        if (DUAL) tmem_ld16(lane_base + C::C_T + c0, t);
+        tmem_ld16(lanes + C::C_O + c0, o);
+        if (DUAL) tmem_ld16(lanes + C::C_T + c0, t);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           o[i] *= inv;
@@ -517,7 +550,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
         if (on) put16(orow, c0, p.D, o);
         if (DUAL && on) put16(drow, c0, p.D, t);
       }
-      if (on) {
+      if (on && half == 0) {
         const int64_t si = static_cast<int64_t>(h) * p.seq.rows + row;
         p.lse[si] = (m2 + log2f(l)) * LN2;
         if (DUAL) p.rbar[si] = rb;
@@ -660,11 +693,6 @@ __device__ __forceinline__ float2 row_dots(const TcParams2& p, int64_t row, int 
   return make_float2(s, sd);
 }
 
-// bf16 pair that is NaN where its row is noted as not finite and attends.
-__device__ __forceinline__ uint32_t nan_pair(uint32_t w, bool o0, bool o1) {
-  return (o0 && (w & 1) ? 0x7fffu : 0u) | (o1 && (w & 2) ? 0x7fff0000u : 0u);
-}
-
 template <bool DUAL, int HDP>
 __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>::CTAS)
     attn_tc_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -694,6 +722,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_entry();
+  const SeqLoad sl = seq_tile_load(p.seq, row0);
   const int nvalid = min(seq_total(p.seq) - row0, TR);
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
@@ -711,6 +740,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_expect_tx(&res_full, 2 * C::RES1);
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+      tma_load_3d(sRes + a * ATOM128, &tmK, &res_full, 64 * a, row0, hk);
+      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmV, &res_full, 64 * a, row0, hk);
+      if (DUAL) {
+        tma_load_3d(sRes + (NA + a) * ATOM128, &tmKd, &res_full, 64 * a, row0, hk);
+        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmVd, &res_full, 64 * a, row0, hk);
+      }
+    }
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -719,7 +758,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   __syncthreads();
-  seq_tile_fill(p.seq, row0, st_rows, C::THREADS);
+  seq_tile_fill(p.seq, row0, st_rows, C::THREADS, sl);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -733,19 +772,6 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 
   if (warp == 0) {
     // ---- loads: TMA by one lane, row statistics by all -------------------------------------------
-    if (elect_one()) {
-      mbar_expect_tx(&res_full, 2 * C::RES1);
-#pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        tma_load_3d(sRes + a * ATOM128, &tmK, &res_full, 64 * a, row0, hk);
-        tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmV, &res_full, 64 * a, row0, hk);
-        if (DUAL) {
-          tma_load_3d(sRes + (NA + a) * ATOM128, &tmKd, &res_full, 64 * a, row0, hk);
-          tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmVd, &res_full, 64 * a, row0, hk);
-        }
-      }
-    }
-    __syncwarp();
     int issued = 0, t = 0, h = hk * G;
     for (int i = 0; i < ntile; ++i) {
       const int st = i % C::STAGES;
@@ -890,17 +916,18 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int a = r - t * BT, b = hi - (row0 + t * BT);
       if (++t == nqt) t = 0;
       if (!wwait(&st_full[st], ph, p.status, abort)) { ok = false; break; }   // the statistics
-      uint32_t badw[CW / 32];
-      bool any_bad = false;
+      uint32_t own[CW / 32], bads[CW / 32];
       if (mx) {
         if (!wwait(&st_clean[st], ph, p.status, abort)) { ok = false; break; }
 #pragma unroll
-        for (int w = 0; w < CW / 32; ++w) { badw[w] = bad[st][cb / 32 + w]; any_bad |= badw[w] != 0; }
+        for (int w = 0; w < CW / 32; ++w) {
+          own[w] = col_bits(a - cb - 32 * w, b - 1 - cb - 32 * w);
+          bads[w] = own[w] & bad[st][cb / 32 + w];
+        }
       }
       const float4* stat = reinterpret_cast<const float4*>(sStat + st * C::STAT_F + cb);
       if (!wwait(&s_full, i & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
-      auto own = [&](int c) { return cb + c >= a && cb + c < b; };
       float pr[CW], pd[DUAL ? CW : 1];
       auto probs = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
@@ -923,7 +950,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               const int f = e + 2 * u, c = c0 + f;
               const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, mul2(lv[u], neg1)));
               float p0 = ex2(x.x), p1 = ex2(x.y);
-              const bool o0 = !MASK || own(c), o1 = !MASK || own(c + 1);
+              const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
+              const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
               if (!o0) p0 = 0.f;
               if (!o1) p1 = 0.f;
               pr[c] = p0;
@@ -938,11 +966,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
                 pd[DUAL ? c + 1 : 0] = y.y;
                 pdk[f / 2] = pack_bf16x2(y.x, y.y);
               }
-              if (MASK && any_bad) {
-                const uint32_t n = nan_pair(badw[c >> 5] >> (c & 31), o0, o1);
-                pk[f / 2] |= n;
-                if (DUAL) pdk[f / 2] |= n;
-              }
+            }
+          }
+          if (MASK && bads[c0 >> 5]) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              pk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) pdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_S + c0 / 2, pk);
@@ -979,7 +1009,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               const uint64_t pp = pair(pr[c], pr[c + 1]);
               const uint64_t x = fma2(dv[u], neg1, pair(dp[f], dp[f + 1]));
               float2 s = halves(mul2(pp, x));
-              const bool o0 = !MASK || own(c), o1 = !MASK || own(c + 1);
+              const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
+              const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
               if (!o0) s.x = 0.f;
               if (!o1) s.y = 0.f;
               sk[f / 2] = pack_bf16x2(s.x, s.y);
@@ -990,11 +1021,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
                 if (!o1) z.y = 0.f;
                 sdk[f / 2] = pack_bf16x2(z.x, z.y);
               }
-              if (MASK && any_bad) {
-                const uint32_t n = nan_pair(badw[c >> 5] >> (c & 31), o0, o1);
-                sk[f / 2] |= n;
-                if (DUAL) sdk[f / 2] |= n;
-              }
+            }
+          }
+          if (MASK && bads[c0 >> 5]) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
@@ -1069,6 +1102,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_entry();
+  const SeqLoad sl = seq_tile_load(p.seq, row0);
   const int nvalid = min(seq_total(p.seq) - row0, TR);
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
@@ -1086,6 +1120,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_expect_tx(&res_full, 2 * C::RES1);
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+      tma_load_3d(sRes + a * ATOM128, &tmQ, &res_full, 64 * a, row0, h);
+      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmO, &res_full, 64 * a, row0, h);
+      if (DUAL) {
+        tma_load_3d(sRes + (NA + a) * ATOM128, &tmQd, &res_full, 64 * a, row0, h);
+        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmOd, &res_full, 64 * a, row0, h);
+      }
+    }
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -1094,7 +1138,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   __syncthreads();
-  seq_tile_fill(p.seq, row0, st_rows, C::THREADS);
+  seq_tile_fill(p.seq, row0, st_rows, C::THREADS, sl);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1107,16 +1151,6 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   if (warp == 0) {
     if (elect_one()) {
       // ---- TMA producer ---------------------------------------------------------------------------
-      mbar_expect_tx(&res_full, 2 * C::RES1);
-#pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        tma_load_3d(sRes + a * ATOM128, &tmQ, &res_full, 64 * a, row0, h);
-        tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmO, &res_full, 64 * a, row0, h);
-        if (DUAL) {
-          tma_load_3d(sRes + (NA + a) * ATOM128, &tmQd, &res_full, 64 * a, row0, h);
-          tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmOd, &res_full, 64 * a, row0, h);
-        }
-      }
       int issued = 0;
       for (int j = 0; j < nkt; ++j) {
         const int st = j % C::STAGES;
@@ -1239,16 +1273,17 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int st = j % C::STAGES;
       const bool mx = mixed(j);
       const int a = lo - (k0 + j * BT), b = row0 + r - (k0 + j * BT);
-      uint32_t badw[CW / 32];
-      bool any_bad = false;
+      uint32_t own[CW / 32], bads[CW / 32];
       if (mx) {
         if (!wwait(&st_clean[st], (j / C::STAGES) & 1, p.status, abort)) { ok = false; break; }
 #pragma unroll
-        for (int w = 0; w < CW / 32; ++w) { badw[w] = bad[st][cb / 32 + w]; any_bad |= badw[w] != 0; }
+        for (int w = 0; w < CW / 32; ++w) {
+          own[w] = col_bits(a - cb - 32 * w, b - cb - 32 * w);
+          bads[w] = own[w] & bad[st][cb / 32 + w];
+        }
       }
       if (!wwait(&s_full, j & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
-      auto own = [&](int c) { return cb + c >= a && cb + c <= b; };
       float pr[CW], pd[DUAL ? CW : 1];
       auto probs = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
@@ -1264,8 +1299,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, nl));
             pr[c] = ex2(x.x);
             pr[c + 1] = ex2(x.y);
-            if (MASK && !own(c)) pr[c] = 0.f;
-            if (MASK && !own(c + 1)) pr[c + 1] = 0.f;
+            if (MASK && !(own[c >> 5] >> (c & 31) & 1)) pr[c] = 0.f;
+            if (MASK && !(own[c >> 5] >> (c & 31) & 2)) pr[c + 1] = 0.f;
             if (DUAL) {
               const float2 y = halves(mul2(pair(pr[c], pr[c + 1]), fma2(pair(sd[f], sd[f + 1]), sc, nr)));
               pd[c] = y.x;
@@ -1296,7 +1331,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             const uint64_t pp = pair(pr[c], pr[c + 1]);
             const uint64_t x = add2(pair(dp[f], dp[f + 1]), nD);
             float2 s = halves(mul2(pp, x));
-            const bool o0 = !MASK || own(c), o1 = !MASK || own(c + 1);
+            const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
+            const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
             if (!o0) s.x = 0.f;
             if (!o1) s.y = 0.f;
             sk[f / 2] = pack_bf16x2(s.x, s.y);
@@ -1307,10 +1343,12 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               if (!o1) z.y = 0.f;
               sdk[f / 2] = pack_bf16x2(z.x, z.y);
             }
-            if (MASK && any_bad) {
-              const uint32_t n = nan_pair(badw[c >> 5] >> (c & 31), o0, o1);
-              sk[f / 2] |= n;
-              if (DUAL) sdk[f / 2] |= n;
+          }
+          if (MASK && bads[c0 >> 5]) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
