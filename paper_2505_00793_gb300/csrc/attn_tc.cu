@@ -62,6 +62,12 @@ __device__ __forceinline__ void tmem_st16u(uint32_t t, const uint32_t* v) {
 __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -208,6 +214,7 @@ struct FwdCfg {
 struct TcParams2 {
   SeqRows seq;
   int Hq, Hkv, D, tiles;
+  int share;                      // CTAs that share a group's query heads (key-row kernel)
   float c2, scale;                // scale log2 e, scale
   int64_t ldo, lddo, lddq, lddk, lddv;
   const __nv_bfloat16 *o, *od, *d_o, *d_od;
@@ -216,14 +223,25 @@ struct TcParams2 {
   int* status;
 };
 
-// Columns c0 .. c0+15 of a row of a head of D columns, as bf16.
-__device__ __forceinline__ void put16(__nv_bfloat16* row, int c0, int D, const float* v) {
+// Results leave through shared memory, so that global rows are written whole: a tile of 128
+// rows of W bf16, 16-byte chunk c of row r at place c ^ (r & 7).
+template <int W>
+__device__ __forceinline__ void stage16(uint8_t* buf, int r, int c0, const float* v) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)
-    if (c0 + 8 * h < D)
-      *reinterpret_cast<uint4*>(row + c0 + 8 * h) =
-          make_uint4(pack_bf16x2(v[8 * h], v[8 * h + 1]), pack_bf16x2(v[8 * h + 2], v[8 * h + 3]),
-                     pack_bf16x2(v[8 * h + 4], v[8 * h + 5]), pack_bf16x2(v[8 * h + 6], v[8 * h + 7]));
+    *reinterpret_cast<uint4*>(buf + r * (2 * W) + (((c0 / 8 + h) ^ (r & 7)) << 4)) =
+        make_uint4(pack_bf16x2(v[8 * h], v[8 * h + 1]), pack_bf16x2(v[8 * h + 2], v[8 * h + 3]),
+                   pack_bf16x2(v[8 * h + 4], v[8 * h + 5]), pack_bf16x2(v[8 * h + 6], v[8 * h + 7]));
+}
+template <int W>
+__device__ __forceinline__ void stage_out(const uint8_t* buf, int nvalid, int D, __nv_bfloat16* dst,
+                                          int64_t ld, int t, int threads) {
+  for (int i = t; i < TR * (W / 8); i += threads) {
+    const int r = i / (W / 8), c = i % (W / 8);
+    if (r < nvalid && 8 * c < D)
+      *reinterpret_cast<uint4*>(dst + r * ld + 8 * c) =
+          *reinterpret_cast<const uint4*>(buf + r * (2 * W) + ((c ^ (r & 7)) << 4));
+  }
 }
 
 template <bool DUAL, int HDP>
@@ -532,29 +550,37 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       tc_fence_after();
       const float inv = 1.f / l;
       const float rb = DUAL ? rs * inv : 0.f;
-      const int64_t row = row0 + r;
-      const bool on = r < nvalid;
-      __nv_bfloat16* orow = p.ow + row * p.ldo + h * p.D;
-      __nv_bfloat16* drow = DUAL ? p.owd + row * p.ldo + h * p.D : nullptr;
-#pragma unroll 1
-      for (int c0 = half * (HDP / 2); c0 < (half + 1) * (HDP / 2); c0 += 16) {
-        if (c0 >= p.D) break;
+#pragma unroll
+      for (int c0 = 0; c0 < HDP / 2; c0 += 16) {
+        const int c = half * (HDP / 2) + c0;
         float o[16], t[16];
-        tmem_ld16(lanes + C::C_O + c0, o);
-        if (DUAL) tmem_ld16(lanes + C::C_T + c0, t);
+        tmem_ld16_nowait(lanes + C::C_O + c, o);
+        if (DUAL) tmem_ld16_nowait(lanes + C::C_T + c, t);
+        tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           o[i] *= inv;
           if (DUAL) t[i] = t[i] * inv - rb * o[i];
         }
-        if (on) put16(orow, c0, p.D, o);
-        if (DUAL && on) put16(drow, c0, p.D, t);
+        stage16<HDP>(smem, r, c, o);
+        if (DUAL) stage16<HDP>(smem + TR * HDP * 2, r, c, t);
       }
-      if (on && half == 0) {
-        const int64_t si = static_cast<int64_t>(h) * p.seq.rows + row;
+      if (r < nvalid && half == 0) {
+        const int64_t si = static_cast<int64_t>(h) * p.seq.rows + row0 + r;
         p.lse[si] = (m2 + log2f(l)) * LN2;
         if (DUAL) p.rbar[si] = rb;
       }
+    } else {
+      ok = false;
+    }
+    // rows are staged over the operands, which every product has read; a warp without a result
+    // writes none (the status says so)
+    asm volatile("bar.sync 5, %0;" ::"n"(C::EW * 32) : "memory");
+    if (ok) {
+      const int64_t at = static_cast<int64_t>(row0) * p.ldo + h * p.D;
+      stage_out<HDP>(smem, nvalid, p.D, p.ow + at, p.ldo, threadIdx.x - 64, C::EW * 32);
+      if (DUAL)
+        stage_out<HDP>(smem + TR * HDP * 2, nvalid, p.D, p.owd + at, p.ldo, threadIdx.x - 64, C::EW * 32);
     }
     tc_fence_before();
   }
@@ -638,16 +664,17 @@ struct BwdCfg {
   static constexpr int NA = HDP / 64;
   static constexpr int BT = HDP == 128 ? 128 : 64;         // streamed rows a tile
   static constexpr int NT = DUAL ? 2 : 1;
-  static constexpr int EW = 8;                             // row warps: two threads a row
-  static constexpr int THREADS = 64 + 32 * EW;
-  static constexpr int CW = BT / 2;                        // columns of a row thread
+  static constexpr int CTAS = DUAL || HDP == 128 ? 1 : 2;
+  static constexpr int EW = CTAS == 1 ? 16 : 8;            // row warps
+  static constexpr int THREADS = 96 + 32 * EW;             // loads, products, look-over, rows
+  static constexpr int CW = BT * 4 / EW;                   // columns of a row thread
+  static constexpr int OW = HDP * 4 / EW;                  // accumulator columns it brings out
   static constexpr int RES1 = NT * NA * ATOM128;           // K (K') or V (V'); Q (Q') or dO (dO')
   static constexpr int BATOM = BT * 128;
   static constexpr int TILE_B = NT * NA * BATOM;           // one streamed operand with its tangent
   static constexpr int STAGE_B = 2 * TILE_B;
   static constexpr int STAGES = HDP == 128 ? 2 : DUAL ? 4 : 3;
-  static constexpr int CTAS = DUAL || HDP == 128 ? 1 : 2;
-  static constexpr int NSTAT = DUAL ? 4 : 2;               // lse, D (rbar, D')
+  static constexpr int NSTAT = DUAL ? 4 : 2;               // -lse log2 e, -D (-rbar, -D')
   static constexpr int STAT_F = NSTAT * BT;
   static constexpr int SMEM_Q = 2 * RES1 + STAGES * STAGE_B + 1024;
   static constexpr int SMEM_KV = SMEM_Q + STAGES * STAT_F * 4;
@@ -660,7 +687,11 @@ struct BwdCfg {
   static constexpr uint32_t COLS_Q = C_B <= 256 ? 256 : 512;
 };
 
-__device__ __forceinline__ void row_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// The row warps' barrier.
+template <int EW>
+__device__ __forceinline__ void row_bar() {
+  asm volatile("bar.sync 1, %0;" ::"n"(EW * 32) : "memory");
+}
 
 // Column sums of a row's dO (*) O over this thread's half of the head, with the tangent.
 template <bool DUAL>
@@ -715,10 +746,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   uint8_t* sRes = smem;                        // K (K'), V (V')
   uint8_t* sSt = smem + 2 * C::RES1;           // stage: Q (Q'), dO (dO')
   float* sStat = reinterpret_cast<float*>(sSt + C::STAGES * C::STAGE_B);
-  // heads fastest; the first rows of a long sequence (the longest walks) come first
-  const int hk = static_cast<int>(blockIdx.x % p.Hkv);
-  const int row0 = static_cast<int>(blockIdx.x / p.Hkv) * TR;
-  const int G = p.Hq / p.Hkv;
+  // a cluster shares the query heads of a group; heads fastest; the first rows of a long
+  // sequence (the longest walks) come first
+  const int rank = static_cast<int>(blockIdx.x % p.share);
+  const int hk = static_cast<int>(blockIdx.x / p.share % p.Hkv);
+  const int row0 = static_cast<int>(blockIdx.x / (p.share * p.Hkv)) * TR;
+  const int G = p.Hq / p.Hkv / p.share;
+  const int h0 = (hk * p.share + rank) * G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_entry();
@@ -734,7 +768,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     mbar_init(&ds_full, C::EW);
     mbar_init(&drain, 1);
     for (int i = 0; i < C::STAGES; ++i) {
-      mbar_init(&st_full[i], 2);
+      mbar_init(&st_full[i], 1);
       mbar_init(&st_empty[i], 1);
       mbar_init(&st_clean[i], 1);
     }
@@ -771,13 +805,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   auto mixed = [&](int t) { return t * BT < nvalid - 1 || row0 + t * BT + BT > hi0; };
 
   if (warp == 0) {
-    // ---- loads: TMA by one lane, row statistics by all -------------------------------------------
-    int issued = 0, t = 0, h = hk * G;
-    for (int i = 0; i < ntile; ++i) {
-      const int st = i % C::STAGES;
-      if (!wwait(&st_empty[st], ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
-      const int qr = row0 + t * BT;
-      if (elect_one()) {
+    if (elect_one()) {
+      // ---- TMA producer ---------------------------------------------------------------------------
+      int issued = 0, t = 0, h = h0;
+      for (int i = 0; i < ntile; ++i) {
+        const int st = i % C::STAGES;
+        if (!fwait(&st_empty[st], ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+        const int qr = row0 + t * BT;
         mbar_expect_tx(&st_full[st], C::STAGE_B);
         uint8_t* b = sSt + st * C::STAGE_B;
 #pragma unroll
@@ -789,34 +823,47 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmOd, &st_full[st], 64 * a, qr, h);
           }
         }
+        ++issued;
+        if (++t == nqt) { t = 0; ++h; }
       }
-      __syncwarp();
-      float* sst = sStat + st * C::STAT_F;
+      mbar_wait(&res_full, 0, p.status, FTC_WAIT_NS);
+      drain_loads(st_full, issued, C::STAGES, p.status);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // ---- look-over: row statistics (negated, read a tile ahead) and mixed tiles ----------------------
+    float v[C::NSTAT][BT / 32];
+    auto read = [&](int t, int h) {
       const int64_t base = static_cast<int64_t>(h) * p.seq.rows;
-      float v[C::NSTAT][BT / 32];
 #pragma unroll
       for (int e = 0; e < BT / 32; ++e) {
-        const int row = qr + 32 * e + lane;
+        const int row = row0 + t * BT + 32 * e + lane;
         const bool in = row < p.seq.rows;
-        v[0][e] = in ? p.lse[base + row] * LOG2E : 0.f;
-        v[1][e] = in ? p.Dr[base + row] : 0.f;
+        v[0][e] = in ? p.lse[base + row] * -LOG2E : 0.f;
+        v[1][e] = in ? -p.Dr[base + row] : 0.f;
         if (DUAL) {
-          v[2][e] = in ? p.rbar[base + row] : 0.f;
-          v[3][e] = in ? p.Drd[base + row] : 0.f;
+          v[2][e] = in ? -p.rbar[base + row] : 0.f;
+          v[3][e] = in ? -p.Drd[base + row] : 0.f;
         }
       }
+    };
+    int t = 0, h = h0;
+    read(0, h0);
+    for (int i = 0; i < ntile; ++i) {
+      const int st = i % C::STAGES;
+      const bool mx = mixed(t);
+      if (!wwait(&st_full[st], (i / C::STAGES) & 1, p.status, abort)) break;
+      float* sst = sStat + st * C::STAT_F;
 #pragma unroll
       for (int k = 0; k < C::NSTAT; ++k)
 #pragma unroll
         for (int e = 0; e < BT / 32; ++e) sst[k * BT + 32 * e + lane] = v[k][e];
-      __syncwarp();
-      if (lane == 0) mbar_arrive_local(&st_full[st]);
-      ++issued;
       if (++t == nqt) { t = 0; ++h; }
+      if (i + 1 < ntile) read(t, h);
+      if (mx) scrub(sSt + st * C::STAGE_B, BT, 2 * C::NT * NA, bad[st], lane);
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(&st_clean[st]);
     }
-    __syncwarp();
-    mbar_wait(&res_full, 0, p.status, FTC_WAIT_NS);
-    drain_loads(st_full, issued, C::STAGES, p.status);
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
     constexpr uint32_t idS = idesc_bf16(TR, BT), idS2 = idesc_bf16(TR, 2 * BT);
@@ -848,17 +895,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
         if (DUAL) mma_ts(tb + c + HDP, tb + ac + BT, y + 128 * kk, idA, 1);
       }
     };
-    int t = 0;      // query tile of the tile being looked over
-    auto look_over = [&](int i) -> bool {
-      const int st = i % C::STAGES;
-      if (!wwait(&st_full[st], (i / C::STAGES) & 1, p.status, abort)) return false;
-      if (mixed(t)) scrub(sSt + st * C::STAGE_B, BT, 2 * C::NT * NA, bad[st], lane);
-      if (++t == nqt) t = 0;
-      if (lane == 0) mbar_arrive_local(&st_clean[st]);
-      __syncwarp();
-      return true;
+    auto ready = [&](int i) {
+      return wwait(&st_clean[i % C::STAGES], (i / C::STAGES) & 1, p.status, abort);
     };
-    bool ok = wwait(&res_full, 0, p.status, abort) && look_over(0);
+    bool ok = wwait(&res_full, 0, p.status, abort) && ready(0);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
@@ -872,7 +912,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     for (int i = 0; ok && i < ntile; ++i) {
       const int st = i % C::STAGES, sn = (i + 1) % C::STAGES;
       const bool more = i + 1 < ntile;
-      if (more && !look_over(i + 1)) break;
+      if (more && !ready(i + 1)) break;
       if (!wwait(&p_full, i & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
@@ -902,10 +942,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     // ---- rows: key row r (TMEM lane r), query columns cb .. cb + CW - 1 ---------------------------------
     const int q4 = warp & 3;
     const int r = q4 * 32 + lane;
-    const int half = (warp - 2) >> 2, cb = half * CW;
+    const int part = (warp - 3) >> 2, cb = part * CW;
     const uint32_t lane_base = tb + (static_cast<uint32_t>(q4 * 32) << 16) + cb;
     const int hi = tile_hi(st_rows, row0, r);
-    const uint64_t c2p = pair(p.c2, p.c2), neg1 = pair(-1.f, -1.f), sc = pair(p.scale, p.scale);
+    const uint64_t c2p = pair(p.c2, p.c2), sc = pair(p.scale, p.scale);
     bool ok = true;
     int t = 0;
     for (int i = 0; i < ntile; ++i) {
@@ -915,15 +955,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       // columns a .. b - 1 (of the tile) attend to this key
       const int a = r - t * BT, b = hi - (row0 + t * BT);
       if (++t == nqt) t = 0;
-      if (!wwait(&st_full[st], ph, p.status, abort)) { ok = false; break; }   // the statistics
-      uint32_t own[CW / 32], bads[CW / 32];
+      if (!wwait(&st_clean[st], ph, p.status, abort)) { ok = false; break; }   // the statistics
+      uint32_t own = 0, bads = 0;
       if (mx) {
-        if (!wwait(&st_clean[st], ph, p.status, abort)) { ok = false; break; }
-#pragma unroll
-        for (int w = 0; w < CW / 32; ++w) {
-          own[w] = col_bits(a - cb - 32 * w, b - 1 - cb - 32 * w);
-          bads[w] = own[w] & bad[st][cb / 32 + w];
-        }
+        own = col_bits(a - cb, b - 1 - cb);
+        bads = own & (bad[st][cb >> 5] >> (cb & 31));
       }
       const float4* stat = reinterpret_cast<const float4*>(sStat + st * C::STAT_F + cb);
       if (!wwait(&s_full, i & 1, p.status, abort)) { ok = false; break; }
@@ -948,10 +984,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               const int f = e + 2 * u, c = c0 + f;
-              const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, mul2(lv[u], neg1)));
+              const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, lv[u]));
               float p0 = ex2(x.x), p1 = ex2(x.y);
-              const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
-              const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
+              const bool o0 = !MASK || (own >> c & 1);
+              const bool o1 = !MASK || (own >> c & 2);
               if (!o0) p0 = 0.f;
               if (!o1) p1 = 0.f;
               pr[c] = p0;
@@ -959,7 +995,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               pk[f / 2] = pack_bf16x2(p0, p1);
               if (DUAL) {
                 float2 y = halves(mul2(pair(p0, p1),
-                                       fma2(pair(sd[f], sd[f + 1]), sc, mul2(rv[u], neg1))));
+                                       fma2(pair(sd[f], sd[f + 1]), sc, rv[u])));
                 if (!o0) y.x = 0.f;
                 if (!o1) y.y = 0.f;
                 pd[c] = y.x;
@@ -968,11 +1004,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               }
             }
           }
-          if (MASK && bads[c0 >> 5]) {
+          if (MASK && bads) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              pk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
-              if (DUAL) pdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              pk[k] |= nan_pair(bads >> (c0 + 2 * k));
+              if (DUAL) pdk[k] |= nan_pair(bads >> (c0 + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_S + c0 / 2, pk);
@@ -1007,15 +1043,15 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             for (int u = 0; u < 2; ++u) {
               const int f = e + 2 * u, c = c0 + f;
               const uint64_t pp = pair(pr[c], pr[c + 1]);
-              const uint64_t x = fma2(dv[u], neg1, pair(dp[f], dp[f + 1]));
+              const uint64_t x = add2(dv[u], pair(dp[f], dp[f + 1]));
               float2 s = halves(mul2(pp, x));
-              const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
-              const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
+              const bool o0 = !MASK || (own >> c & 1);
+              const bool o1 = !MASK || (own >> c & 2);
               if (!o0) s.x = 0.f;
               if (!o1) s.y = 0.f;
               sk[f / 2] = pack_bf16x2(s.x, s.y);
               if (DUAL) {
-                const uint64_t y = fma2(gv[u], neg1, pair(dd[f], dd[f + 1]));
+                const uint64_t y = add2(gv[u], pair(dd[f], dd[f + 1]));
                 float2 z = halves(fma2(pair(pd[c], pd[DUAL ? c + 1 : 0]), x, mul2(pp, y)));
                 if (!o0) z.x = 0.f;
                 if (!o1) z.y = 0.f;
@@ -1023,11 +1059,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               }
             }
           }
-          if (MASK && bads[c0 >> 5]) {
+          if (MASK && bads) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
-              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              sk[k] |= nan_pair(bads >> (c0 + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(bads >> (c0 + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
@@ -1041,32 +1077,59 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       __syncwarp();
       if (lane == 0) mbar_arrive_local(&ds_full);
     }
+    // accumulators to shared memory, over the operands, which every product has read: a tile of
+    // float32 rows each, 16-byte chunk c of row r at place c ^ (r & 7)
     if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
       tc_fence_after();
-      const int64_t row = row0 + r;
-      const bool on = r < nvalid;
-      const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16);
-      auto put = [&](uint32_t c, __nv_bfloat16* dst, float f) {
-#pragma unroll 1
-        for (int c0 = half * (HDP / 2); c0 < (half + 1) * (HDP / 2); c0 += 16) {
-          if (c0 >= p.D) break;
-          float v[16];
-          tmem_ld16(acc + c + c0, v);
+      const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16) + part * C::OW;
 #pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] *= f;
-          if (on) put16(dst, c0, p.D, v);
+      for (int k = 0; k < 2 * C::NT; ++k)
+#pragma unroll
+        for (int c0 = 0; c0 < C::OW; c0 += 16) {
+          float v[16];
+          tmem_ld16(acc + C::C_A + k * HDP + c0, v);
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4*>(smem + (k * TR + r) * (4 * HDP) +
+                                       ((((part * C::OW + c0 + e) / 4) ^ (r & 7)) << 4)) =
+                make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
-      };
-      put(C::C_A, p.dv + row * p.lddv + hk * p.D, 1.f);
-      put(C::C_B, p.dk + row * p.lddk + hk * p.D, p.scale);
-      if (DUAL) {
-        put(C::C_A + HDP, p.dvd + row * p.lddv + hk * p.D, 1.f);
-        put(C::C_B + HDP, p.dkd + row * p.lddk + hk * p.D, p.scale);
-      }
     }
     tc_fence_before();
   }
-  __syncthreads();
+  // the cluster's sums, rank by rank in order, each CTA its part of the rows; the second barrier
+  // keeps a CTA's shared memory until the others have read it
+  cluster_sync_all();
+  if (warp >= 3 && !*abort) {
+    const int rows = (TR + p.share - 1) / p.share;
+    const int r0 = rank * rows, r1 = min(min(r0 + rows, TR), nvalid);
+    constexpr int CH = HDP / 8;
+    for (int i = static_cast<int>(threadIdx.x) - 96 + r0 * CH; i < r1 * CH; i += 32 * C::EW) {
+      const int r = i / CH, c = i % CH;
+      if (8 * c >= p.D) continue;
+      const int64_t row = row0 + r;
+#pragma unroll
+      for (int k = 0; k < 2 * C::NT; ++k) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const uint32_t at = smem_u32(smem) + (k * TR + r) * (4 * HDP);
+        for (int j = 0; j < p.share; ++j) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float4 x = ld_cluster4(dsmem_addr(at + (((2 * c + u) ^ (r & 7)) << 4), j));
+            v[4 * u] += x.x; v[4 * u + 1] += x.y; v[4 * u + 2] += x.z; v[4 * u + 3] += x.w;
+          }
+        }
+        // dV (dV') as they are, dK (dK') with the scale of the scores
+        const bool isv = k < C::NT;
+        const float f = isv ? 1.f : p.scale;
+        __nv_bfloat16* dst = k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd;
+        *reinterpret_cast<uint4*>(dst + row * (isv ? p.lddv : p.lddk) + hk * p.D + 8 * c) =
+            make_uint4(pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f),
+                       pack_bf16x2(v[4] * f, v[5] * f), pack_bf16x2(v[6] * f, v[7] * f));
+      }
+    }
+  }
+  cluster_sync_all();
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
@@ -1087,7 +1150,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   __shared__ __align__(8) uint64_t res_full, s_full, s_free, dp_full, ds_full, drain;
   __shared__ __align__(8) uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
   __shared__ uint32_t bad[C::STAGES][4];
-  __shared__ float2 sD[2][TR];
+  __shared__ float2 sD[C::EW / 4][TR];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
@@ -1173,6 +1236,15 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       drain_loads(st_full, issued, C::STAGES, p.status);
     }
     __syncwarp();
+  } else if (warp == 2) {
+    // ---- look-over of mixed tiles: K (K') multiplies dS; V (V') only meets dO, whose product with a
+    // masked key is dropped
+    for (int j = 0; j < nkt; ++j) {
+      const int st = j % C::STAGES;
+      if (!wwait(&st_full[st], (j / C::STAGES) & 1, p.status, abort)) break;
+      if (mixed(j)) scrub(sSt + st * C::STAGE_B, BT, C::NT * NA, bad[st], lane);
+      if (lane == 0) mbar_arrive_local(&st_clean[st]);
+    }
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
     constexpr uint32_t idS = idesc_bf16(TR, BT), idS2 = idesc_bf16(TR, 2 * BT);
@@ -1192,16 +1264,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           mma_bf16(tb + c + BT, x + RD + 2 * kk, y + 2 * kk, idS, 1);
       }
     };
-    auto look_over = [&](int j) -> bool {
-      const int st = j % C::STAGES;
-      if (!wwait(&st_full[st], (j / C::STAGES) & 1, p.status, abort)) return false;
-      // K (K') multiplies dS; V (V') only meets dO, whose product with a masked key is dropped
-      if (mixed(j)) scrub(sSt + st * C::STAGE_B, BT, C::NT * NA, bad[st], lane);
-      if (lane == 0) mbar_arrive_local(&st_clean[st]);
-      __syncwarp();
-      return true;
+    auto ready = [&](int j) {
+      return wwait(&st_clean[j % C::STAGES], (j / C::STAGES) & 1, p.status, abort);
     };
-    bool ok = wwait(&res_full, 0, p.status, abort) && look_over(0);
+    bool ok = wwait(&res_full, 0, p.status, abort) && ready(0);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
@@ -1216,7 +1282,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int st = j % C::STAGES, sn = (j + 1) % C::STAGES;
       const bool more = j + 1 < nkt;
       if (more) {
-        if (!look_over(j + 1)) break;
+        if (!ready(j + 1)) break;
         if (!wwait(&s_free, j & 1, p.status, abort)) break;
         tc_fence_after();
         if (elect_one()) {
@@ -1251,17 +1317,21 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     // ---- rows: query row r (TMEM lane r), key columns cb .. cb + CW - 1 ---------------------------------
     const int q4 = warp & 3;
     const int r = q4 * 32 + lane;
-    const int half = (warp - 2) >> 2, cb = half * CW;
+    const int part = (warp - 3) >> 2, cb = part * CW;
     const uint32_t lane_base = tb + (static_cast<uint32_t>(q4 * 32) << 16) + cb;
     const int lo = tile_lo(st_rows, row0, r);
     const int64_t row = row0 + r, si = static_cast<int64_t>(h) * p.seq.rows + row;
     const bool on = r < nvalid;
-    // D of the row, half by each of its two threads
-    sD[half][r] = on ? row_dots<DUAL>(p, row, h, half * (HDP / 2), (half + 1) * (HDP / 2))
-                     : make_float2(0.f, 0.f);
-    row_bar();
-    const float Dv = sD[0][r].x + sD[1][r].x, Dd = sD[0][r].y + sD[1][r].y;
-    if (on && half == 0) {
+    // D of the row, a part of the head by each of its threads
+    sD[part][r] = on ? row_dots<DUAL>(p, row, h, part * C::OW, (part + 1) * C::OW) : make_float2(0.f, 0.f);
+    row_bar<C::EW>();
+    float Dv = 0.f, Dd = 0.f;
+#pragma unroll
+    for (int i = 0; i < C::EW / 4; ++i) {
+      Dv += sD[i][r].x;
+      Dd += sD[i][r].y;
+    }
+    if (on && part == 0) {
       p.Dr[si] = Dv;
       if (DUAL) p.Drd[si] = Dd;
     }
@@ -1273,14 +1343,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int st = j % C::STAGES;
       const bool mx = mixed(j);
       const int a = lo - (k0 + j * BT), b = row0 + r - (k0 + j * BT);
-      uint32_t own[CW / 32], bads[CW / 32];
+      uint32_t own = 0, bads = 0;
       if (mx) {
         if (!wwait(&st_clean[st], (j / C::STAGES) & 1, p.status, abort)) { ok = false; break; }
-#pragma unroll
-        for (int w = 0; w < CW / 32; ++w) {
-          own[w] = col_bits(a - cb - 32 * w, b - cb - 32 * w);
-          bads[w] = own[w] & bad[st][cb / 32 + w];
-        }
+        own = col_bits(a - cb, b - cb);
+        bads = own & (bad[st][cb >> 5] >> (cb & 31));
       }
       if (!wwait(&s_full, j & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
@@ -1299,8 +1366,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, nl));
             pr[c] = ex2(x.x);
             pr[c + 1] = ex2(x.y);
-            if (MASK && !(own[c >> 5] >> (c & 31) & 1)) pr[c] = 0.f;
-            if (MASK && !(own[c >> 5] >> (c & 31) & 2)) pr[c + 1] = 0.f;
+            if (MASK && !(own >> c & 1)) pr[c] = 0.f;
+            if (MASK && !(own >> c & 2)) pr[c + 1] = 0.f;
             if (DUAL) {
               const float2 y = halves(mul2(pair(pr[c], pr[c + 1]), fma2(pair(sd[f], sd[f + 1]), sc, nr)));
               pd[c] = y.x;
@@ -1331,8 +1398,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             const uint64_t pp = pair(pr[c], pr[c + 1]);
             const uint64_t x = add2(pair(dp[f], dp[f + 1]), nD);
             float2 s = halves(mul2(pp, x));
-            const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
-            const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
+            const bool o0 = !MASK || (own >> c & 1);
+            const bool o1 = !MASK || (own >> c & 2);
             if (!o0) s.x = 0.f;
             if (!o1) s.y = 0.f;
             sk[f / 2] = pack_bf16x2(s.x, s.y);
@@ -1344,11 +1411,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               sdk[f / 2] = pack_bf16x2(z.x, z.y);
             }
           }
-          if (MASK && bads[c0 >> 5]) {
+          if (MASK && bads) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
-              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              sk[k] |= nan_pair(bads >> (c0 + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(bads >> (c0 + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
@@ -1364,20 +1431,26 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     }
     if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
       tc_fence_after();
-      const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16);
-      auto put = [&](uint32_t c, __nv_bfloat16* dst) {
-#pragma unroll 1
-        for (int c0 = half * (HDP / 2); c0 < (half + 1) * (HDP / 2); c0 += 16) {
-          if (c0 >= p.D) break;
-          float v[16];
-          tmem_ld16(acc + c + c0, v);
+      const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16) + part * C::OW;
 #pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] *= p.scale;
-          if (on) put16(dst, c0, p.D, v);
+      for (int k = 0; k < C::NT; ++k)
+#pragma unroll
+        for (int c0 = 0; c0 < C::OW; c0 += 16) {
+          float v[16];
+          tmem_ld16(acc + C::C_A + k * HDP + c0, v);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] *= p.scale;
+          stage16<HDP>(smem + k * TR * HDP * 2, r, part * C::OW + c0, v);
         }
-      };
-      put(C::C_A, p.dq + row * p.lddq + h * p.D);
-      if (DUAL) put(C::C_A + HDP, p.dqd + row * p.lddq + h * p.D);
+    } else {
+      ok = false;
+    }
+    row_bar<C::EW>();
+    if (ok) {
+      const int64_t at = static_cast<int64_t>(row0) * p.lddq + h * p.D;
+      stage_out<HDP>(smem, nvalid, p.D, p.dq + at, p.lddq, threadIdx.x - 96, C::EW * 32);
+      if (DUAL)
+        stage_out<HDP>(smem + TR * HDP * 2, nvalid, p.D, p.dqd + at, p.lddq, threadIdx.x - 96, C::EW * 32);
     }
     tc_fence_before();
   }
@@ -1387,6 +1460,37 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
                  "r"(C::COLS_Q));
   }
+}
+
+// CTAs of a cluster that share the query heads of a group in the key-row kernel: the fewest
+// (dividing the group, at most 8) that fill the GPU's places four times over.
+int kv_share(int group, int64_t ctas, int per_sm) {
+  int best = 1;
+  for (int n = 1; n <= 8 && n <= group; ++n) {
+    if (group % n) continue;
+    best = n;
+    if (ctas * n >= 4ll * 152 * per_sm) break;
+  }
+  return best;
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_cluster(void (*kernel)(KArgs...), int grid, int cluster, int threads, size_t smem,
+                           cudaStream_t s, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = g_pdl ? 1 : 0;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
 
 template <bool DUAL, int HDP>
@@ -1412,15 +1516,15 @@ cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_Q);
   });
   if (e != cudaSuccess) return e;
-  const TcParams2 p = tc_params(a);
+  TcParams2 p = tc_params(a);
   const int64_t grid = static_cast<int64_t>(p.tiles) * a.Hq;
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  p.share = kv_share(a.Hq / a.Hkv, static_cast<int64_t>(p.tiles) * a.Hkv, C::CTAS);
   e = launch_k(attn_tc_bwd_q_kernel<DUAL, HDP>, dim3(static_cast<unsigned>(grid)), dim3(C::THREADS),
                C::SMEM_Q, s, qr[0], qr[1], qr[2], qr[3], ks[0], ks[1], ks[2], ks[3], p);
   if (e != cudaSuccess) return e;
-  return launch_k(attn_tc_bwd_kv_kernel<DUAL, HDP>, dim3(static_cast<unsigned>(p.tiles * a.Hkv)),
-                  dim3(C::THREADS), C::SMEM_KV, s, kr[0], kr[1], kr[2], kr[3], qs[0], qs[1], qs[2],
-                  qs[3], p);
+  return launch_cluster(attn_tc_bwd_kv_kernel<DUAL, HDP>, p.tiles * a.Hkv * p.share, p.share, C::THREADS,
+                        C::SMEM_KV, s, kr[0], kr[1], kr[2], kr[3], qs[0], qs[1], qs[2], qs[3], p);
 }
 
 }  // namespace
