@@ -14,10 +14,12 @@
 // memory is moved for it, and the products of one CTA, issued by one thread in order, need no
 // barrier between reading P and overwriting it with the next scores.
 //
-// Values of masked places: a product with a zero of P still meets them (0 * inf = NaN).  In
-// mixed tiles the warp that issues the products first looks over the rows that P or dS will
-// multiply, puts zeros in place of what is not finite and notes those rows; rows that attend to
-// a noted one get NaN, others are as if it was not there.
+// Values of masked places: a product with a zero of P still meets them (0 * inf = NaN).  So a
+// CTA whose results are all finite is done; one that finds a NaN or an infinity in them walks its
+// tiles a second time, carefully: in mixed tiles the rows that P or dS will multiply are looked
+// over first, what is not finite in them becomes zero, and rows that do attend to such a row get
+// NaN.  Others come out as if it was not there, bit for bit, and a call without such values pays
+// for a check of its results.
 //
 // Every wait is bounded (2 s), as in flash_tc.cu.
 #include "attn_ops.h"
@@ -73,6 +75,37 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+
+// A warp's bounded wait: one vote when the phase is complete.
+__device__ __forceinline__ bool warp_try(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "vote.sync.all.pred q, p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool rwait(uint64_t* bar, uint32_t parity, int* status,
+                                      volatile int* abort) {
+  if (warp_try(bar, parity)) return true;
+  const long long t0 = global_ns();
+  while (!warp_try(bar, parity)) {
+    if (__any_sync(0xffffffffu, *abort != 0)) return false;
+    if (__any_sync(0xffffffffu, global_ns() - t0 > FTC_WAIT_NS)) {
+      if (status) atomicMax(status, DEV_TIMEOUT);
+      *abort = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+// Zero while everything added so far was finite, else NaN (0 x is NaN for a NaN or an infinity).
+__device__ __forceinline__ void add_check(float& z, float x) { z = fmaf(x, 0.f, z); }
 
 // ---- sequences of a tile's rows -------------------------------------------------------------
 // Borders inside the tile as a bit per row (a sequence starts there), the start of the first
@@ -253,15 +286,18 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   using C = FwdCfg<DUAL, HDP>;
   constexpr int TK = C::TK, NA = C::NA;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t q_full, s_full, p_full, drain;
-  __shared__ __align__(8) uint64_t k_full[C::STAGES], k_empty[C::STAGES];
-  __shared__ __align__(8) uint64_t v_full[C::STAGES], v_empty[C::STAGES], v_clean[C::STAGES];
+  struct Bars {
+    uint64_t q_full, s_full, p_full, drain;
+    uint64_t k_full[C::STAGES], k_empty[C::STAGES], v_full[C::STAGES], v_empty[C::STAGES],
+        v_clean[C::STAGES];
+  };
+  __shared__ __align__(8) Bars bars[2];      // one set per walk
   __shared__ uint32_t bad[C::STAGES][4];
   __shared__ float row_max[2][2][TR];
   __shared__ float2 row_sum[2][TR];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, redo_flag;
 
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -274,6 +310,14 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   const int row0 = (p.tiles - 1 - static_cast<int>(blockIdx.x / p.Hq)) * TR;
   const int hk = h / (p.Hq / p.Hkv);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto load_rows = [&](uint64_t& bar) {
+    mbar_expect_tx(&bar, C::Q_B);
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+      tma_load_3d(sQ + a * ATOM128, &tmQ, &bar, 64 * a, row0, h);
+      if (DUAL) tma_load_3d(sQ + (NA + a) * ATOM128, &tmQd, &bar, 64 * a, row0, h);
+    }
+  };
 
   pdl_entry();
   const SeqLoad sl = seq_tile_load(p.seq, row0);
@@ -281,26 +325,22 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
   if (threadIdx.x == 0) {
-    mbar_init(&q_full, 1);
-    mbar_init(&s_full, 1);
-    mbar_init(&p_full, C::EW);
-    mbar_init(&drain, 1);
-    for (int i = 0; i < C::STAGES; ++i) {
-      mbar_init(&k_full[i], 1);
-      mbar_init(&k_empty[i], 1);
-      mbar_init(&v_full[i], 1);
-      mbar_init(&v_empty[i], 1);
-      mbar_init(&v_clean[i], 1);
+    for (Bars& B : bars) {
+      mbar_init(&B.q_full, 1);
+      mbar_init(&B.s_full, 1);
+      mbar_init(&B.p_full, C::EW);
+      mbar_init(&B.drain, 1);
+      for (int i = 0; i < C::STAGES; ++i) {
+        mbar_init(&B.k_full[i], 1);
+        mbar_init(&B.k_empty[i], 1);
+        mbar_init(&B.v_full[i], 1);
+        mbar_init(&B.v_empty[i], 1);
+        mbar_init(&B.v_clean[i], 1);
+      }
     }
-    abort_flag = 0;
+    abort_flag = redo_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    // the rows' own operands need nothing of the sequences
-    mbar_expect_tx(&q_full, C::Q_B);
-#pragma unroll
-    for (int a = 0; a < NA; ++a) {
-      tma_load_3d(sQ + a * ATOM128, &tmQ, &q_full, 64 * a, row0, h);
-      if (DUAL) tma_load_3d(sQ + (NA + a) * ATOM128, &tmQd, &q_full, 64 * a, row0, h);
-    }
+    load_rows(bars[0].q_full);   // the rows' own operands need nothing of the sequences
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -320,36 +360,40 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   // whether some row does not attend to the whole of key tile j
   auto mixed = [&](int j) { return k0 + j * TK + TK - 1 > row0 || k0 + j * TK < lo1; };
 
+  for (int walk = 0;; ++walk) {
+  const bool careful = walk > 0;
+  Bars& B = bars[walk];
   if (warp == 0) {
     if (elect_one()) {
       // ---- TMA producer ---------------------------------------------------------------------
+      if (walk) load_rows(B.q_full);
       int nk = 0, nv = 0;
       for (int j = 0; j < nkt; ++j) {
         const int st = j % C::STAGES;
         const uint32_t ph = ((j / C::STAGES) & 1) ^ 1;
         const int kr = k0 + j * TK;
-        if (!fwait(&k_empty[st], ph, p.status, abort)) break;
-        mbar_expect_tx(&k_full[st], C::TILE_B);
+        if (!fwait(&B.k_empty[st], ph, p.status, abort)) break;
+        mbar_expect_tx(&B.k_full[st], C::TILE_B);
         uint8_t* b = sK + st * C::TILE_B;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::KATOM, &tmK, &k_full[st], 64 * a, kr, hk);
-          if (DUAL) tma_load_3d(b + (NA + a) * C::KATOM, &tmKd, &k_full[st], 64 * a, kr, hk);
+          tma_load_3d(b + a * C::KATOM, &tmK, &B.k_full[st], 64 * a, kr, hk);
+          if (DUAL) tma_load_3d(b + (NA + a) * C::KATOM, &tmKd, &B.k_full[st], 64 * a, kr, hk);
         }
         ++nk;
-        if (!fwait(&v_empty[st], ph, p.status, abort)) break;
-        mbar_expect_tx(&v_full[st], C::TILE_B);
+        if (!fwait(&B.v_empty[st], ph, p.status, abort)) break;
+        mbar_expect_tx(&B.v_full[st], C::TILE_B);
         b = sV + st * C::TILE_B;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::KATOM, &tmV, &v_full[st], 64 * a, kr, hk);
-          if (DUAL) tma_load_3d(b + (NA + a) * C::KATOM, &tmVd, &v_full[st], 64 * a, kr, hk);
+          tma_load_3d(b + a * C::KATOM, &tmV, &B.v_full[st], 64 * a, kr, hk);
+          if (DUAL) tma_load_3d(b + (NA + a) * C::KATOM, &tmVd, &B.v_full[st], 64 * a, kr, hk);
         }
         ++nv;
       }
-      mbar_wait(&q_full, 0, p.status, FTC_WAIT_NS);
-      drain_loads(k_full, nk, C::STAGES, p.status);
-      drain_loads(v_full, nv, C::STAGES, p.status);
+      mbar_wait(&B.q_full, 0, p.status, FTC_WAIT_NS);
+      drain_loads(B.k_full, nk, C::STAGES, p.status);
+      drain_loads(B.v_full, nv, C::STAGES, p.status);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -361,7 +405,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
     constexpr uint64_t ST = C::TILE_B >> 4;
     auto scores = [&](int j) -> bool {
       const int st = j % C::STAGES;
-      if (!wwait(&k_full[st], (j / C::STAGES) & 1, p.status, abort)) return false;
+      if (!rwait(&B.k_full[st], (j / C::STAGES) & 1, p.status, abort)) return false;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t dK = dKs + st * ST;
@@ -376,24 +420,24 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
           for (int kk = 0; kk < HDP / 16; ++kk)
             mma_bf16(tb + C::C_SD, dQd + 2 * kk, dK + 2 * kk, idS, 1);
         }
-        mma_commit(&s_full);
-        mma_commit(&k_empty[st]);
+        mma_commit(&B.s_full);
+        mma_commit(&B.k_empty[st]);
       }
       __syncwarp();
       return true;
     };
-    bool ok = wwait(&q_full, 0, p.status, abort) && scores(0);
+    bool ok = rwait(&B.q_full, 0, p.status, abort) && scores(0);
     for (int j = 0; ok && j < nkt; ++j) {
       const int st = j % C::STAGES;
       const uint32_t ph = (j / C::STAGES) & 1;
-      if (mixed(j)) {
-        if (!wwait(&v_full[st], ph, p.status, abort)) break;
-        scrub(sV + st * C::TILE_B, TK, C::NT * NA, bad[st], lane);
+      if (careful) {
+        if (!rwait(&B.v_full[st], ph, p.status, abort)) break;
+        if (mixed(j)) scrub(sV + st * C::TILE_B, TK, C::NT * NA, bad[st], lane);
+        if (lane == 0) mbar_arrive_local(&B.v_clean[st]);
+        __syncwarp();
       }
-      if (lane == 0) mbar_arrive_local(&v_clean[st]);
-      __syncwarp();
-      if (!wwait(&v_full[st], ph, p.status, abort)) break;
-      if (!wwait(&p_full, j & 1, p.status, abort)) break;
+      if (!rwait(&B.v_full[st], ph, p.status, abort)) break;
+      if (!rwait(&B.p_full, j & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t mV = mVs + st * ST;
@@ -409,15 +453,15 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
             mma_ts(tb + C::C_O, tb + C::C_S + pc, mV + 128 * kk, idO, acc);
           }
         }
-        mma_commit(&v_empty[st]);
+        mma_commit(&B.v_empty[st]);
       }
       __syncwarp();
       if (j + 1 < nkt && !scores(j + 1)) break;
     }
     // every product issued here has completed before the rows are read and TMEM is released
-    if (elect_one()) mma_commit(&drain);
+    if (elect_one()) mma_commit(&B.drain);
     __syncwarp();
-    mbar_wait(&drain, 0, p.status, FTC_WAIT_NS);
+    mbar_wait(&B.drain, 0, p.status, FTC_WAIT_NS);
   } else {
     // ---- rows: row row0 + r (TMEM lane r), keys cb .. cb + HC - 1 of each tile ------------------------
     constexpr int HC = C::HC;
@@ -434,16 +478,16 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       const int st = j % C::STAGES;
       const bool mx_tile = mixed(j);
       // a thread that gives up still meets its row's other thread once a tile
-      ok = ok && wwait(&s_full, j & 1, p.status, abort);
+      ok = ok && rwait(&B.s_full, j & 1, p.status, abort);
       // the row's own keys among this thread's, and those of them whose V is not finite
       uint32_t own[HC / 32], bads[HC / 32];
       if (mx_tile) {
-        ok = ok && wwait(&v_clean[st], (j / C::STAGES) & 1, p.status, abort);
+        if (careful) ok = ok && rwait(&B.v_clean[st], (j / C::STAGES) & 1, p.status, abort);
         const int kb = k0 + j * TK + cb;
 #pragma unroll
         for (int c = 0; c < HC / 32; ++c) {
           own[c] = col_bits(lo - kb - 32 * c, row0 + r - kb - 32 * c);
-          bads[c] = own[c] & bad[st][cb / 32 + c];
+          bads[c] = careful ? own[c] & bad[st][cb / 32 + c] : 0u;
         }
       }
       tc_fence_after();
@@ -523,7 +567,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
             psk[i / 2] = pack2(ps);
           }
         }
-        if (mx_tile && bads[c]) {
+        if (careful && mx_tile && bads[c]) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             pk[i] |= nan_pair(bads[c] >> (2 * i));
@@ -539,17 +583,18 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&p_full);
+      if (lane == 0) mbar_arrive_local(&B.p_full);
     }
     // the row's sums over both threads (every row thread meets the barrier)
     row_sum[half][r] = make_float2(l, rs);
     asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
     l = row_sum[0][r].x + row_sum[1][r].x;
     rs = row_sum[0][r].y + row_sum[1][r].y;
-    if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
+    if (ok && rwait(&B.drain, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const float inv = 1.f / l;
       const float rb = DUAL ? rs * inv : 0.f;
+      float z = 0.f;
 #pragma unroll
       for (int c0 = 0; c0 < HDP / 2; c0 += 16) {
         const int c = half * (HDP / 2) + c0;
@@ -562,9 +607,15 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
           o[i] *= inv;
           if (DUAL) t[i] = t[i] * inv - rb * o[i];
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          add_check(z, o[i]);
+          if (DUAL) add_check(z, t[i]);
+        }
         stage16<HDP>(smem, r, c, o);
         if (DUAL) stage16<HDP>(smem + TR * HDP * 2, r, c, t);
       }
+      if (r < nvalid && z != 0.f) redo_flag = 1;
       if (r < nvalid && half == 0) {
         const int64_t si = static_cast<int64_t>(h) * p.seq.rows + row0 + r;
         p.lse[si] = (m2 + log2f(l)) * LN2;
@@ -583,8 +634,13 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
         stage_out<HDP>(smem + TR * HDP * 2, nvalid, p.D, p.owd + at, p.ldo, threadIdx.x - 64, C::EW * 32);
     }
     tc_fence_before();
+    fence_async_smem();
   }
   __syncthreads();
+  tc_fence_after();
+  // NaN is what z != 0 sees; a careful walk's result stands
+  if (careful || !redo_flag || *abort) break;
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
@@ -693,35 +749,46 @@ __device__ __forceinline__ void row_bar() {
   asm volatile("bar.sync 1, %0;" ::"n"(EW * 32) : "memory");
 }
 
-// Column sums of a row's dO (*) O over this thread's half of the head, with the tangent.
-template <bool DUAL>
-__device__ __forceinline__ float2 row_dots(const TcParams2& p, int64_t row, int h, int c0, int c1) {
-  float s = 0.f, sd = 0.f;
-  const int64_t oo = row * p.ldo + h * p.D, og = row * p.lddo + h * p.D;
-  auto f8 = [](const __nv_bfloat16* x, float (&v)[8]) {
-    const uint4 w = *reinterpret_cast<const uint4*>(x);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+// D = rowsum(dO (*) O) of the tile's rows, and its tangent rowsum(dO' (*) O + dO (*) O'), by the
+// row warps: the lanes of a row read its 16-byte chunks side by side.
+template <bool DUAL, int HDP, int EW>
+__device__ __forceinline__ void row_dots(const TcParams2& p, int row0, int nvalid, int h, int w,
+                                         int lane, float2* out) {
+  constexpr int LPR = HDP / 8, STEP = EW * (32 / LPR);
+  auto f8 = [](const __nv_bfloat16* x, bool on, float (&v)[8]) {
+    const uint4 w4 = on ? *reinterpret_cast<const uint4*>(x) : make_uint4(0, 0, 0, 0);
+    const uint32_t u[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[2 * i] = __uint_as_float(u[i] << 16);
       v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
     }
   };
-  for (int c = c0; c < c1 && c < p.D; c += 8) {
-    float o[8], g[8], od[8], gd[8];
-    f8(p.o + oo + c, o);
-    f8(p.d_o + og + c, g);
+  const int c = 8 * (lane % LPR);
+#pragma unroll
+  for (int r = w * (32 / LPR) + lane / LPR; r < TR; r += STEP) {
+    const bool on = r < nvalid && c < p.D;
+    const int64_t oo = (static_cast<int64_t>(row0) + r) * p.ldo + h * p.D + c;
+    const int64_t og = (static_cast<int64_t>(row0) + r) * p.lddo + h * p.D + c;
+    float o[8], g[8], od[8], gd[8], s = 0.f, sd = 0.f;
+    f8(p.o + oo, on, o);
+    f8(p.d_o + og, on, g);
     if (DUAL) {
-      f8(p.od + oo + c, od);
-      f8(p.d_od + og + c, gd);
+      f8(p.od + oo, on, od);
+      f8(p.d_od + og, on, gd);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       s += o[i] * g[i];
       if (DUAL) sd += o[i] * gd[i] + od[i] * g[i];
     }
+#pragma unroll
+    for (int k = LPR / 2; k > 0; k >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, k);
+      if (DUAL) sd += __shfl_xor_sync(0xffffffffu, sd, k);
+    }
+    if (lane % LPR == 0) out[r] = make_float2(s, sd);
   }
-  return make_float2(s, sd);
 }
 
 template <bool DUAL, int HDP>
@@ -734,12 +801,15 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   using C = BwdCfg<DUAL, HDP>;
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t res_full, s_full, dp_full, p_full, ds_full, drain;
-  __shared__ __align__(8) uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
+  struct Bars {
+    uint64_t res_full, s_full, dp_full, p_full, ds_full, drain;
+    uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
+  };
+  __shared__ __align__(8) Bars bars[2];      // one set per walk
   __shared__ uint32_t bad[C::STAGES][4];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, redo_flag;
 
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -754,6 +824,18 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   const int G = p.Hq / p.Hkv / p.share;
   const int h0 = (hk * p.share + rank) * G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto load_rows = [&](uint64_t& bar) {
+    mbar_expect_tx(&bar, 2 * C::RES1);
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+      tma_load_3d(sRes + a * ATOM128, &tmK, &bar, 64 * a, row0, hk);
+      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmV, &bar, 64 * a, row0, hk);
+      if (DUAL) {
+        tma_load_3d(sRes + (NA + a) * ATOM128, &tmKd, &bar, 64 * a, row0, hk);
+        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmVd, &bar, 64 * a, row0, hk);
+      }
+    }
+  };
 
   pdl_entry();
   const SeqLoad sl = seq_tile_load(p.seq, row0);
@@ -761,29 +843,22 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
   if (threadIdx.x == 0) {
-    mbar_init(&res_full, 1);
-    mbar_init(&s_full, 1);
-    mbar_init(&dp_full, 1);
-    mbar_init(&p_full, C::EW);
-    mbar_init(&ds_full, C::EW);
-    mbar_init(&drain, 1);
-    for (int i = 0; i < C::STAGES; ++i) {
-      mbar_init(&st_full[i], 1);
-      mbar_init(&st_empty[i], 1);
-      mbar_init(&st_clean[i], 1);
-    }
-    abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    mbar_expect_tx(&res_full, 2 * C::RES1);
-#pragma unroll
-    for (int a = 0; a < NA; ++a) {
-      tma_load_3d(sRes + a * ATOM128, &tmK, &res_full, 64 * a, row0, hk);
-      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmV, &res_full, 64 * a, row0, hk);
-      if (DUAL) {
-        tma_load_3d(sRes + (NA + a) * ATOM128, &tmKd, &res_full, 64 * a, row0, hk);
-        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmVd, &res_full, 64 * a, row0, hk);
+    for (Bars& B : bars) {
+      mbar_init(&B.res_full, 1);
+      mbar_init(&B.s_full, 1);
+      mbar_init(&B.dp_full, 1);
+      mbar_init(&B.p_full, C::EW);
+      mbar_init(&B.ds_full, C::EW);
+      mbar_init(&B.drain, 1);
+      for (int i = 0; i < C::STAGES; ++i) {
+        mbar_init(&B.st_full[i], 1);
+        mbar_init(&B.st_empty[i], 1);
+        mbar_init(&B.st_clean[i], 1);
       }
     }
+    abort_flag = redo_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    load_rows(bars[0].res_full);   // the rows' own operands need nothing of the sequences
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -804,30 +879,34 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   // whether some key row is not attended to by the whole of query tile t
   auto mixed = [&](int t) { return t * BT < nvalid - 1 || row0 + t * BT + BT > hi0; };
 
+  for (int walk = 0;; ++walk) {
+  const bool careful = walk > 0;
+  Bars& B = bars[walk];
   if (warp == 0) {
     if (elect_one()) {
+      if (walk) load_rows(B.res_full);
       // ---- TMA producer ---------------------------------------------------------------------------
       int issued = 0, t = 0, h = h0;
       for (int i = 0; i < ntile; ++i) {
         const int st = i % C::STAGES;
-        if (!fwait(&st_empty[st], ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+        if (!fwait(&B.st_empty[st], ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
         const int qr = row0 + t * BT;
-        mbar_expect_tx(&st_full[st], C::STAGE_B);
+        mbar_expect_tx(&B.st_full[st], C::STAGE_B);
         uint8_t* b = sSt + st * C::STAGE_B;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::BATOM, &tmQ, &st_full[st], 64 * a, qr, h);
-          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmO, &st_full[st], 64 * a, qr, h);
+          tma_load_3d(b + a * C::BATOM, &tmQ, &B.st_full[st], 64 * a, qr, h);
+          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmO, &B.st_full[st], 64 * a, qr, h);
           if (DUAL) {
-            tma_load_3d(b + (NA + a) * C::BATOM, &tmQd, &st_full[st], 64 * a, qr, h);
-            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmOd, &st_full[st], 64 * a, qr, h);
+            tma_load_3d(b + (NA + a) * C::BATOM, &tmQd, &B.st_full[st], 64 * a, qr, h);
+            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmOd, &B.st_full[st], 64 * a, qr, h);
           }
         }
         ++issued;
         if (++t == nqt) { t = 0; ++h; }
       }
-      mbar_wait(&res_full, 0, p.status, FTC_WAIT_NS);
-      drain_loads(st_full, issued, C::STAGES, p.status);
+      mbar_wait(&B.res_full, 0, p.status, FTC_WAIT_NS);
+      drain_loads(B.st_full, issued, C::STAGES, p.status);
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -852,7 +931,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     for (int i = 0; i < ntile; ++i) {
       const int st = i % C::STAGES;
       const bool mx = mixed(t);
-      if (!wwait(&st_full[st], (i / C::STAGES) & 1, p.status, abort)) break;
+      if (!rwait(&B.st_full[st], (i / C::STAGES) & 1, p.status, abort)) break;
       float* sst = sStat + st * C::STAT_F;
 #pragma unroll
       for (int k = 0; k < C::NSTAT; ++k)
@@ -860,9 +939,9 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
         for (int e = 0; e < BT / 32; ++e) sst[k * BT + 32 * e + lane] = v[k][e];
       if (++t == nqt) { t = 0; ++h; }
       if (i + 1 < ntile) read(t, h);
-      if (mx) scrub(sSt + st * C::STAGE_B, BT, 2 * C::NT * NA, bad[st], lane);
+      if (careful && mx) scrub(sSt + st * C::STAGE_B, BT, 2 * C::NT * NA, bad[st], lane);
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&st_clean[st]);
+      if (lane == 0) mbar_arrive_local(&B.st_clean[st]);
     }
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
@@ -896,16 +975,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       }
     };
     auto ready = [&](int i) {
-      return wwait(&st_clean[i % C::STAGES], (i / C::STAGES) & 1, p.status, abort);
+      return rwait(&B.st_clean[i % C::STAGES], (i / C::STAGES) & 1, p.status, abort);
     };
-    bool ok = wwait(&res_full, 0, p.status, abort) && ready(0);
+    bool ok = rwait(&B.res_full, 0, p.status, abort) && ready(0);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
         score(dK, kSt, C::C_S);
-        mma_commit(&s_full);
+        mma_commit(&B.s_full);
         score(dV, kSt + DO, C::C_DP);
-        mma_commit(&dp_full);
+        mma_commit(&B.dp_full);
       }
       __syncwarp();
     }
@@ -913,31 +992,31 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int st = i % C::STAGES, sn = (i + 1) % C::STAGES;
       const bool more = i + 1 < ntile;
       if (more && !ready(i + 1)) break;
-      if (!wwait(&p_full, i & 1, p.status, abort)) break;
+      if (!rwait(&B.p_full, i & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         accum(C::C_A, C::C_S, mSt + st * ST + DO, i == 0);
         if (more) {
           score(dK, kSt + sn * ST, C::C_S);
-          mma_commit(&s_full);
+          mma_commit(&B.s_full);
         }
       }
       __syncwarp();
-      if (!wwait(&ds_full, i & 1, p.status, abort)) break;
+      if (!rwait(&B.ds_full, i & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         accum(C::C_B, C::C_DP, mSt + st * ST, i == 0);
-        mma_commit(&st_empty[st]);
+        mma_commit(&B.st_empty[st]);
         if (more) {
           score(dV, kSt + sn * ST + DO, C::C_DP);
-          mma_commit(&dp_full);
+          mma_commit(&B.dp_full);
         }
       }
       __syncwarp();
     }
-    if (elect_one()) mma_commit(&drain);
+    if (elect_one()) mma_commit(&B.drain);
     __syncwarp();
-    mbar_wait(&drain, 0, p.status, FTC_WAIT_NS);
+    mbar_wait(&B.drain, 0, p.status, FTC_WAIT_NS);
   } else {
     // ---- rows: key row r (TMEM lane r), query columns cb .. cb + CW - 1 ---------------------------------
     const int q4 = warp & 3;
@@ -955,14 +1034,14 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       // columns a .. b - 1 (of the tile) attend to this key
       const int a = r - t * BT, b = hi - (row0 + t * BT);
       if (++t == nqt) t = 0;
-      if (!wwait(&st_clean[st], ph, p.status, abort)) { ok = false; break; }   // the statistics
+      if (!rwait(&B.st_clean[st], ph, p.status, abort)) { ok = false; break; }   // the statistics
       uint32_t own = 0, bads = 0;
       if (mx) {
         own = col_bits(a - cb, b - 1 - cb);
-        bads = own & (bad[st][cb >> 5] >> (cb & 31));
+        if (careful) bads = own & (bad[st][cb >> 5] >> (cb & 31));
       }
       const float4* stat = reinterpret_cast<const float4*>(sStat + st * C::STAT_F + cb);
-      if (!wwait(&s_full, i & 1, p.status, abort)) { ok = false; break; }
+      if (!rwait(&B.s_full, i & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       float pr[CW], pd[DUAL ? CW : 1];
       auto probs = [&](auto masked) {
@@ -1020,8 +1099,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&p_full);
-      if (!wwait(&dp_full, i & 1, p.status, abort)) { ok = false; break; }
+      if (lane == 0) mbar_arrive_local(&B.p_full);
+      if (!rwait(&B.dp_full, i & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       auto scores = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
@@ -1075,13 +1154,14 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&ds_full);
+      if (lane == 0) mbar_arrive_local(&B.ds_full);
     }
     // accumulators to shared memory, over the operands, which every product has read: a tile of
     // float32 rows each, 16-byte chunk c of row r at place c ^ (r & 7)
-    if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
+    if (ok && rwait(&B.drain, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16) + part * C::OW;
+      float z = 0.f;
 #pragma unroll
       for (int k = 0; k < 2 * C::NT; ++k)
 #pragma unroll
@@ -1089,13 +1169,21 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           float v[16];
           tmem_ld16(acc + C::C_A + k * HDP + c0, v);
 #pragma unroll
+          for (int e = 0; e < 16; ++e) add_check(z, v[e]);
+#pragma unroll
           for (int e = 0; e < 16; e += 4)
             *reinterpret_cast<float4*>(smem + (k * TR + r) * (4 * HDP) +
                                        ((((part * C::OW + c0 + e) / 4) ^ (r & 7)) << 4)) =
                 make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
+      if (r < nvalid && z != 0.f) redo_flag = 1;
     }
     tc_fence_before();
+    fence_async_smem();
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (careful || !redo_flag || *abort) break;
   }
   // the cluster's sums, rank by rank in order, each CTA its part of the rows; the second barrier
   // keeps a CTA's shared memory until the others have read it
@@ -1131,7 +1219,6 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   }
   cluster_sync_all();
   if (warp == 1) {
-    tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
                  "r"(C::COLS_KV));
   }
@@ -1147,13 +1234,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   using C = BwdCfg<DUAL, HDP>;
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t res_full, s_full, s_free, dp_full, ds_full, drain;
-  __shared__ __align__(8) uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
+  struct Bars {
+    uint64_t res_full, s_full, s_free, dp_full, ds_full, drain;
+    uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
+  };
+  __shared__ __align__(8) Bars bars[2];      // one set per walk
   __shared__ uint32_t bad[C::STAGES][4];
-  __shared__ float2 sD[C::EW / 4][TR];
+  __shared__ float2 sD[TR];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, redo_flag;
 
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -1163,6 +1253,18 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   const int row0 = (p.tiles - 1 - static_cast<int>(blockIdx.x / p.Hq)) * TR;
   const int hk = h / (p.Hq / p.Hkv);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto load_rows = [&](uint64_t& bar) {
+    mbar_expect_tx(&bar, 2 * C::RES1);
+#pragma unroll
+    for (int a = 0; a < NA; ++a) {
+      tma_load_3d(sRes + a * ATOM128, &tmQ, &bar, 64 * a, row0, h);
+      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmO, &bar, 64 * a, row0, h);
+      if (DUAL) {
+        tma_load_3d(sRes + (NA + a) * ATOM128, &tmQd, &bar, 64 * a, row0, h);
+        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmOd, &bar, 64 * a, row0, h);
+      }
+    }
+  };
 
   pdl_entry();
   const SeqLoad sl = seq_tile_load(p.seq, row0);
@@ -1170,29 +1272,22 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
   if (threadIdx.x == 0) {
-    mbar_init(&res_full, 1);
-    mbar_init(&s_full, 1);
-    mbar_init(&s_free, C::EW);
-    mbar_init(&dp_full, 1);
-    mbar_init(&ds_full, C::EW);
-    mbar_init(&drain, 1);
-    for (int i = 0; i < C::STAGES; ++i) {
-      mbar_init(&st_full[i], 1);
-      mbar_init(&st_empty[i], 1);
-      mbar_init(&st_clean[i], 1);
-    }
-    abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    mbar_expect_tx(&res_full, 2 * C::RES1);
-#pragma unroll
-    for (int a = 0; a < NA; ++a) {
-      tma_load_3d(sRes + a * ATOM128, &tmQ, &res_full, 64 * a, row0, h);
-      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmO, &res_full, 64 * a, row0, h);
-      if (DUAL) {
-        tma_load_3d(sRes + (NA + a) * ATOM128, &tmQd, &res_full, 64 * a, row0, h);
-        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmOd, &res_full, 64 * a, row0, h);
+    for (Bars& B : bars) {
+      mbar_init(&B.res_full, 1);
+      mbar_init(&B.s_full, 1);
+      mbar_init(&B.s_free, C::EW);
+      mbar_init(&B.dp_full, 1);
+      mbar_init(&B.ds_full, C::EW);
+      mbar_init(&B.drain, 1);
+      for (int i = 0; i < C::STAGES; ++i) {
+        mbar_init(&B.st_full[i], 1);
+        mbar_init(&B.st_empty[i], 1);
+        mbar_init(&B.st_clean[i], 1);
       }
     }
+    abort_flag = redo_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    load_rows(bars[0].res_full);   // the rows' own operands need nothing of the sequences
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -1211,29 +1306,33 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   const int nkt = (row0 + nvalid - k0 + BT - 1) / BT;
   auto mixed = [&](int j) { return k0 + j * BT + BT - 1 > row0 || k0 + j * BT < lo1; };
 
+  for (int walk = 0;; ++walk) {
+  const bool careful = walk > 0;
+  Bars& B = bars[walk];
   if (warp == 0) {
     if (elect_one()) {
+      if (walk) load_rows(B.res_full);
       // ---- TMA producer ---------------------------------------------------------------------------
       int issued = 0;
       for (int j = 0; j < nkt; ++j) {
         const int st = j % C::STAGES;
-        if (!fwait(&st_empty[st], ((j / C::STAGES) & 1) ^ 1, p.status, abort)) break;
-        mbar_expect_tx(&st_full[st], C::STAGE_B);
+        if (!fwait(&B.st_empty[st], ((j / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+        mbar_expect_tx(&B.st_full[st], C::STAGE_B);
         uint8_t* b = sSt + st * C::STAGE_B;
         const int kr = k0 + j * BT;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::BATOM, &tmK, &st_full[st], 64 * a, kr, hk);
-          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmV, &st_full[st], 64 * a, kr, hk);
+          tma_load_3d(b + a * C::BATOM, &tmK, &B.st_full[st], 64 * a, kr, hk);
+          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmV, &B.st_full[st], 64 * a, kr, hk);
           if (DUAL) {
-            tma_load_3d(b + (NA + a) * C::BATOM, &tmKd, &st_full[st], 64 * a, kr, hk);
-            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmVd, &st_full[st], 64 * a, kr, hk);
+            tma_load_3d(b + (NA + a) * C::BATOM, &tmKd, &B.st_full[st], 64 * a, kr, hk);
+            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmVd, &B.st_full[st], 64 * a, kr, hk);
           }
         }
         ++issued;
       }
-      mbar_wait(&res_full, 0, p.status, FTC_WAIT_NS);
-      drain_loads(st_full, issued, C::STAGES, p.status);
+      mbar_wait(&B.res_full, 0, p.status, FTC_WAIT_NS);
+      drain_loads(B.st_full, issued, C::STAGES, p.status);
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -1241,9 +1340,9 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     // masked key is dropped
     for (int j = 0; j < nkt; ++j) {
       const int st = j % C::STAGES;
-      if (!wwait(&st_full[st], (j / C::STAGES) & 1, p.status, abort)) break;
-      if (mixed(j)) scrub(sSt + st * C::STAGE_B, BT, C::NT * NA, bad[st], lane);
-      if (lane == 0) mbar_arrive_local(&st_clean[st]);
+      if (!rwait(&B.st_full[st], (j / C::STAGES) & 1, p.status, abort)) break;
+      if (careful && mixed(j)) scrub(sSt + st * C::STAGE_B, BT, C::NT * NA, bad[st], lane);
+      if (lane == 0) mbar_arrive_local(&B.st_clean[st]);
     }
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
@@ -1265,16 +1364,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       }
     };
     auto ready = [&](int j) {
-      return wwait(&st_clean[j % C::STAGES], (j / C::STAGES) & 1, p.status, abort);
+      return rwait(&B.st_clean[j % C::STAGES], (j / C::STAGES) & 1, p.status, abort);
     };
-    bool ok = wwait(&res_full, 0, p.status, abort) && ready(0);
+    bool ok = rwait(&B.res_full, 0, p.status, abort) && ready(0);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
         score(dQ, kSt, C::C_S);
-        mma_commit(&s_full);
+        mma_commit(&B.s_full);
         score(dO, kSt + VO, C::C_DP);
-        mma_commit(&dp_full);
+        mma_commit(&B.dp_full);
       }
       __syncwarp();
     }
@@ -1283,15 +1382,15 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const bool more = j + 1 < nkt;
       if (more) {
         if (!ready(j + 1)) break;
-        if (!wwait(&s_free, j & 1, p.status, abort)) break;
+        if (!rwait(&B.s_free, j & 1, p.status, abort)) break;
         tc_fence_after();
         if (elect_one()) {
           score(dQ, kSt + sn * ST, C::C_S);
-          mma_commit(&s_full);
+          mma_commit(&B.s_full);
         }
         __syncwarp();
       }
-      if (!wwait(&ds_full, j & 1, p.status, abort)) break;
+      if (!rwait(&B.ds_full, j & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t mK = mSt + st * ST;
@@ -1302,17 +1401,17 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           mma_ts(tb + C::C_A, tb + ac, mK + 128 * kk, DUAL ? idA2 : idA, acc);
           if (DUAL) mma_ts(tb + C::C_A + HDP, tb + ac + BT, mK + 128 * kk, idA, 1);
         }
-        mma_commit(&st_empty[st]);
+        mma_commit(&B.st_empty[st]);
         if (more) {
           score(dO, kSt + sn * ST + VO, C::C_DP);
-          mma_commit(&dp_full);
+          mma_commit(&B.dp_full);
         }
       }
       __syncwarp();
     }
-    if (elect_one()) mma_commit(&drain);
+    if (elect_one()) mma_commit(&B.drain);
     __syncwarp();
-    mbar_wait(&drain, 0, p.status, FTC_WAIT_NS);
+    mbar_wait(&B.drain, 0, p.status, FTC_WAIT_NS);
   } else {
     // ---- rows: query row r (TMEM lane r), key columns cb .. cb + CW - 1 ---------------------------------
     const int q4 = warp & 3;
@@ -1322,15 +1421,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     const int lo = tile_lo(st_rows, row0, r);
     const int64_t row = row0 + r, si = static_cast<int64_t>(h) * p.seq.rows + row;
     const bool on = r < nvalid;
-    // D of the row, a part of the head by each of its threads
-    sD[part][r] = on ? row_dots<DUAL>(p, row, h, part * C::OW, (part + 1) * C::OW) : make_float2(0.f, 0.f);
+    // D of the rows, a row's chunks of 16 bytes in neighbouring lanes
+    if (!careful) row_dots<DUAL, HDP, C::EW>(p, row0, nvalid, h, warp - 3, lane, sD);
     row_bar<C::EW>();
-    float Dv = 0.f, Dd = 0.f;
-#pragma unroll
-    for (int i = 0; i < C::EW / 4; ++i) {
-      Dv += sD[i][r].x;
-      Dd += sD[i][r].y;
-    }
+    const float Dv = sD[r].x, Dd = sD[r].y;
     if (on && part == 0) {
       p.Dr[si] = Dv;
       if (DUAL) p.Drd[si] = Dd;
@@ -1345,11 +1439,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int a = lo - (k0 + j * BT), b = row0 + r - (k0 + j * BT);
       uint32_t own = 0, bads = 0;
       if (mx) {
-        if (!wwait(&st_clean[st], (j / C::STAGES) & 1, p.status, abort)) { ok = false; break; }
         own = col_bits(a - cb, b - cb);
-        bads = own & (bad[st][cb >> 5] >> (cb & 31));
+        if (careful) {
+          if (!rwait(&B.st_clean[st], (j / C::STAGES) & 1, p.status, abort)) { ok = false; break; }
+          bads = own & (bad[st][cb >> 5] >> (cb & 31));
+        }
       }
-      if (!wwait(&s_full, j & 1, p.status, abort)) { ok = false; break; }
+      if (!rwait(&B.s_full, j & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       float pr[CW], pd[DUAL ? CW : 1];
       auto probs = [&](auto masked) {
@@ -1380,8 +1476,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       else probs(std::false_type{});
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&s_free);
-      if (!wwait(&dp_full, j & 1, p.status, abort)) { ok = false; break; }
+      if (lane == 0) mbar_arrive_local(&B.s_free);
+      if (!rwait(&B.dp_full, j & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       auto scores = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
@@ -1427,11 +1523,12 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&ds_full);
+      if (lane == 0) mbar_arrive_local(&B.ds_full);
     }
-    if (ok && wwait(&drain, 0, p.status, abort) && !*abort) {
+    if (ok && rwait(&B.drain, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16) + part * C::OW;
+      float z = 0.f;
 #pragma unroll
       for (int k = 0; k < C::NT; ++k)
 #pragma unroll
@@ -1439,9 +1536,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           float v[16];
           tmem_ld16(acc + C::C_A + k * HDP + c0, v);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] *= p.scale;
+          for (int e = 0; e < 16; ++e) {
+            v[e] *= p.scale;
+            add_check(z, v[e]);
+          }
           stage16<HDP>(smem + k * TR * HDP * 2, r, part * C::OW + c0, v);
         }
+      if (on && z != 0.f) redo_flag = 1;
     } else {
       ok = false;
     }
@@ -1453,10 +1554,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
         stage_out<HDP>(smem + TR * HDP * 2, nvalid, p.D, p.dqd + at, p.lddq, threadIdx.x - 96, C::EW * 32);
     }
     tc_fence_before();
+    fence_async_smem();
   }
   __syncthreads();
+  tc_fence_after();
+  if (careful || !redo_flag || *abort) break;
+  }
   if (warp == 1) {
-    tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
                  "r"(C::COLS_Q));
   }
