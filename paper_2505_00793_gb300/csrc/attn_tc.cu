@@ -53,14 +53,6 @@ __device__ __forceinline__ void tmem_st8(uint32_t t, const uint32_t* v) {
                "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-__device__ __forceinline__ void tmem_st16u(uint32_t t, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(t),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-      "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-      : "memory");
-}
 __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
@@ -70,14 +62,28 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
                : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
+// The cluster's last barrier: what was read of other CTAs has arrived, and nothing is published
+// (a releasing arrive would wait for the rows just written to be acknowledged).
+__device__ __forceinline__ void cluster_leave() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\t"
+               "barrier.cluster.wait.aligned;" ::: "memory");
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
-// A warp's bounded wait: one vote when the phase is complete.
-__device__ __forceinline__ bool warp_try(uint64_t* bar, uint32_t parity) {
+// Barriers are shared-memory addresses.  Waits are bounded by the SM's clock: 2 s at 2 GHz.
+constexpr long long WAIT_CLOCKS = 4000000000LL;
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// One vote of a warp on whether the phase is complete.
+__device__ __forceinline__ bool warp_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
@@ -85,23 +91,45 @@ __device__ __forceinline__ bool warp_try(uint64_t* bar, uint32_t parity) {
       "vote.sync.all.pred q, p, 0xffffffff;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
+      : "r"(bar), "r"(parity)
       : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ bool rwait(uint64_t* bar, uint32_t parity, int* status,
+// A warp's bounded wait: all of it goes on, or none.
+__device__ __forceinline__ bool rwait(uint32_t bar, uint32_t parity, int* status,
                                       volatile int* abort) {
   if (warp_try(bar, parity)) return true;
-  const long long t0 = global_ns();
+  const long long t0 = clock64();
   while (!warp_try(bar, parity)) {
     if (__any_sync(0xffffffffu, *abort != 0)) return false;
-    if (__any_sync(0xffffffffu, global_ns() - t0 > FTC_WAIT_NS)) {
+    if (__any_sync(0xffffffffu, clock64() - t0 > WAIT_CLOCKS)) {
       if (status) atomicMax(status, DEV_TIMEOUT);
       *abort = 1;
       return false;
     }
   }
   return true;
+}
+// The same for one thread.
+__device__ __forceinline__ bool twait(uint32_t bar, uint32_t parity, int* status,
+                                      volatile int* abort) {
+  if (mbar_try_wait_addr(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait_addr(bar, parity)) {
+    if (*abort) return false;
+    if (clock64() - t0 > WAIT_CLOCKS) {
+      if (status) atomicMax(status, DEV_TIMEOUT);
+      *abort = 1;
+      return false;
+    }
+  }
+  return true;
+}
+// Waits for the loads that were issued, `n` of them round a ring: nothing may still arrive when
+// the CTA ends, given up or not.
+__device__ __forceinline__ void drain_ring(uint32_t full, int n, int stages, int* status) {
+  for (int j = n - stages > 0 ? n - stages : 0; j < n; ++j)
+    if (!mbar_wait_addr(full + 8 * (j % stages), (j / stages) & 1, status, FTC_WAIT_NS)) return;
 }
 
 // Zero while everything added so far was finite, else NaN (0 x is NaN for a NaN or an infinity).
@@ -223,8 +251,8 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 
 // ---- forward ------------------------------------------------------------------------------------
 // One CTA per (query head, 128 rows): warp 0 loads (Q once, then key tiles into a ring of K and a
-// ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..9 hold
-// the rows, two threads a row, each half of a tile's keys.  The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T
+// ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..5 hold
+// the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).  The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T
 // into S'; P [V | V'] -> [O | T], then (P (*) S') V into T; o' = T / l - rbar o.
 template <bool DUAL, int HDP>
 struct FwdCfg {
@@ -236,9 +264,8 @@ struct FwdCfg {
   static constexpr int TILE_B = NT * NA * KATOM;           // K (K') or V (V') of a tile
   static constexpr int STAGES = HDP == 128 ? 1 : 2;
   static constexpr int SMEM = Q_B + 2 * STAGES * TILE_B + 1024;
-  static constexpr int EW = 8;                             // row warps: two threads a row
+  static constexpr int EW = 4;                             // row warps: a thread a row
   static constexpr int THREADS = 64 + 32 * EW;
-  static constexpr int HC = TK / 2;                        // keys of a row thread
   static constexpr int CTAS = 2;
   static constexpr uint32_t TMEM_COLS = 256;
   static constexpr uint32_t C_S = 0, C_SD = 64, C_O = 128, C_T = 192;
@@ -247,7 +274,8 @@ struct FwdCfg {
 struct TcParams2 {
   SeqRows seq;
   int Hq, Hkv, D, tiles;
-  int share;                      // CTAs that share a group's query heads (key-row kernel)
+  int G;                          // query heads of a group
+  int share, Gs;                  // key-row kernel: CTAs that share a group, query heads of each
   float c2, scale;                // scale log2 e, scale
   int64_t ldo, lddo, lddq, lddk, lddv;
   const __nv_bfloat16 *o, *od, *d_o, *d_od;
@@ -255,6 +283,12 @@ struct TcParams2 {
   float *lse, *rbar, *Dr, *Drd;
   int* status;
 };
+
+// Tile of this CTA: grid y, continued along z.
+constexpr int GRID_Y = 65535;
+__device__ __forceinline__ int tile_index() {
+  return static_cast<int>(blockIdx.y) + GRID_Y * static_cast<int>(blockIdx.z);
+}
 
 // Results leave through shared memory, so that global rows are written whole: a tile of 128
 // rows of W bf16, 16-byte chunk c of row r at place c ^ (r & 7).
@@ -286,15 +320,14 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   using C = FwdCfg<DUAL, HDP>;
   constexpr int TK = C::TK, NA = C::NA;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  struct Bars {
-    uint64_t q_full, s_full, p_full, drain;
-    uint64_t k_full[C::STAGES], k_empty[C::STAGES], v_full[C::STAGES], v_empty[C::STAGES],
-        v_clean[C::STAGES];
-  };
-  __shared__ __align__(8) Bars bars[2];      // one set per walk
+  // barriers, as byte offsets in a set; one set per walk
+  constexpr uint32_t B_Q_FULL = 0, B_S_FULL = 8, B_P_FULL = 16, B_DRAIN = 24;
+  constexpr uint32_t B_K_FULL = 32 + 0 * C::STAGES, B_K_EMPTY = 32 + 8 * C::STAGES,
+      B_V_FULL = 32 + 16 * C::STAGES, B_V_EMPTY = 32 + 24 * C::STAGES,
+      B_V_CLEAN = 32 + 32 * C::STAGES;
+  constexpr int NBARS = 4 + 5 * C::STAGES;
+  __shared__ __align__(8) uint64_t bars[2][NBARS];
   __shared__ uint32_t bad[C::STAGES][4];
-  __shared__ float row_max[2][2][TR];
-  __shared__ float2 row_sum[2][TR];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, redo_flag;
@@ -306,16 +339,17 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   uint8_t* sV = sK + C::STAGES * C::TILE_B;
   // heads fastest (a group's heads share K and V), the last rows first (the longest walks of a
   // long sequence)
-  const int h = static_cast<int>(blockIdx.x % p.Hq);
-  const int row0 = (p.tiles - 1 - static_cast<int>(blockIdx.x / p.Hq)) * TR;
-  const int hk = h / (p.Hq / p.Hkv);
+  const int h = static_cast<int>(blockIdx.x), tile = tile_index();
+  if (tile >= p.tiles) return;
+  const int row0 = (p.tiles - 1 - tile) * TR;
+  const int hk = h / p.G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto load_rows = [&](uint64_t& bar) {
-    mbar_expect_tx(&bar, C::Q_B);
+  auto load_rows = [&](uint32_t bar) {
+    mbar_expect_tx_addr(bar, C::Q_B);
 #pragma unroll
     for (int a = 0; a < NA; ++a) {
-      tma_load_3d(sQ + a * ATOM128, &tmQ, &bar, 64 * a, row0, h);
-      if (DUAL) tma_load_3d(sQ + (NA + a) * ATOM128, &tmQd, &bar, 64 * a, row0, h);
+      tma_load_at<false>(smem_u32(sQ + a * ATOM128), &tmQ, bar, 64 * a, row0, h);
+      if (DUAL) tma_load_at<false>(smem_u32(sQ + (NA + a) * ATOM128), &tmQd, bar, 64 * a, row0, h);
     }
   };
 
@@ -324,23 +358,15 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
   const int nvalid = min(seq_total(p.seq) - row0, TR);
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
-  if (threadIdx.x == 0) {
-    for (Bars& B : bars) {
-      mbar_init(&B.q_full, 1);
-      mbar_init(&B.s_full, 1);
-      mbar_init(&B.p_full, C::EW);
-      mbar_init(&B.drain, 1);
-      for (int i = 0; i < C::STAGES; ++i) {
-        mbar_init(&B.k_full[i], 1);
-        mbar_init(&B.k_empty[i], 1);
-        mbar_init(&B.v_full[i], 1);
-        mbar_init(&B.v_empty[i], 1);
-        mbar_init(&B.v_clean[i], 1);
-      }
-    }
-    abort_flag = redo_flag = 0;
+  // a barrier a thread; the first thread's own is the one that its loads complete
+  if (threadIdx.x < 2 * NBARS) {
+    const uint32_t b = threadIdx.x % NBARS;
+    bar_init(smem_u32(&bars[0][0]) + 8 * threadIdx.x, 8 * b == B_P_FULL ? C::EW : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    load_rows(bars[0].q_full);   // the rows' own operands need nothing of the sequences
+  }
+  if (threadIdx.x == 0) {
+    abort_flag = redo_flag = 0;
+    load_rows(smem_u32(&bars[0][0]) + B_Q_FULL);   // the rows' own operands need nothing of the sequences
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -362,38 +388,38 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
 
   for (int walk = 0;; ++walk) {
   const bool careful = walk > 0;
-  Bars& B = bars[walk];
+  const uint32_t bb = smem_u32(&bars[walk][0]);
   if (warp == 0) {
     if (elect_one()) {
       // ---- TMA producer ---------------------------------------------------------------------
-      if (walk) load_rows(B.q_full);
+      if (walk) load_rows(bb + B_Q_FULL);
       int nk = 0, nv = 0;
       for (int j = 0; j < nkt; ++j) {
         const int st = j % C::STAGES;
         const uint32_t ph = ((j / C::STAGES) & 1) ^ 1;
         const int kr = k0 + j * TK;
-        if (!fwait(&B.k_empty[st], ph, p.status, abort)) break;
-        mbar_expect_tx(&B.k_full[st], C::TILE_B);
+        if (!twait(bb + B_K_EMPTY + 8 * st, ph, p.status, abort)) break;
+        mbar_expect_tx_addr(bb + B_K_FULL + 8 * st, C::TILE_B);
         uint8_t* b = sK + st * C::TILE_B;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::KATOM, &tmK, &B.k_full[st], 64 * a, kr, hk);
-          if (DUAL) tma_load_3d(b + (NA + a) * C::KATOM, &tmKd, &B.k_full[st], 64 * a, kr, hk);
+          tma_load_at<false>(smem_u32(b + a * C::KATOM), &tmK, bb + B_K_FULL + 8 * st, 64 * a, kr, hk);
+          if (DUAL) tma_load_at<false>(smem_u32(b + (NA + a) * C::KATOM), &tmKd, bb + B_K_FULL + 8 * st, 64 * a, kr, hk);
         }
         ++nk;
-        if (!fwait(&B.v_empty[st], ph, p.status, abort)) break;
-        mbar_expect_tx(&B.v_full[st], C::TILE_B);
+        if (!twait(bb + B_V_EMPTY + 8 * st, ph, p.status, abort)) break;
+        mbar_expect_tx_addr(bb + B_V_FULL + 8 * st, C::TILE_B);
         b = sV + st * C::TILE_B;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::KATOM, &tmV, &B.v_full[st], 64 * a, kr, hk);
-          if (DUAL) tma_load_3d(b + (NA + a) * C::KATOM, &tmVd, &B.v_full[st], 64 * a, kr, hk);
+          tma_load_at<false>(smem_u32(b + a * C::KATOM), &tmV, bb + B_V_FULL + 8 * st, 64 * a, kr, hk);
+          if (DUAL) tma_load_at<false>(smem_u32(b + (NA + a) * C::KATOM), &tmVd, bb + B_V_FULL + 8 * st, 64 * a, kr, hk);
         }
         ++nv;
       }
-      mbar_wait(&B.q_full, 0, p.status, FTC_WAIT_NS);
-      drain_loads(B.k_full, nk, C::STAGES, p.status);
-      drain_loads(B.v_full, nv, C::STAGES, p.status);
+      mbar_wait_addr(bb + B_Q_FULL, 0, p.status, FTC_WAIT_NS);
+      drain_ring(bb + B_K_FULL, nk, C::STAGES, p.status);
+      drain_ring(bb + B_V_FULL, nv, C::STAGES, p.status);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -405,7 +431,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
     constexpr uint64_t ST = C::TILE_B >> 4;
     auto scores = [&](int j) -> bool {
       const int st = j % C::STAGES;
-      if (!rwait(&B.k_full[st], (j / C::STAGES) & 1, p.status, abort)) return false;
+      if (!rwait(bb + B_K_FULL + 8 * st, (j / C::STAGES) & 1, p.status, abort)) return false;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t dK = dKs + st * ST;
@@ -420,24 +446,24 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
           for (int kk = 0; kk < HDP / 16; ++kk)
             mma_bf16(tb + C::C_SD, dQd + 2 * kk, dK + 2 * kk, idS, 1);
         }
-        mma_commit(&B.s_full);
-        mma_commit(&B.k_empty[st]);
+        mma_commit_addr(bb + B_S_FULL);
+        mma_commit_addr(bb + B_K_EMPTY + 8 * st);
       }
       __syncwarp();
       return true;
     };
-    bool ok = rwait(&B.q_full, 0, p.status, abort) && scores(0);
+    bool ok = rwait(bb + B_Q_FULL, 0, p.status, abort) && scores(0);
     for (int j = 0; ok && j < nkt; ++j) {
       const int st = j % C::STAGES;
       const uint32_t ph = (j / C::STAGES) & 1;
       if (careful) {
-        if (!rwait(&B.v_full[st], ph, p.status, abort)) break;
+        if (!rwait(bb + B_V_FULL + 8 * st, ph, p.status, abort)) break;
         if (mixed(j)) scrub(sV + st * C::TILE_B, TK, C::NT * NA, bad[st], lane);
-        if (lane == 0) mbar_arrive_local(&B.v_clean[st]);
+        if (lane == 0) bar_arrive(bb + B_V_CLEAN + 8 * st);
         __syncwarp();
       }
-      if (!rwait(&B.v_full[st], ph, p.status, abort)) break;
-      if (!rwait(&B.p_full, j & 1, p.status, abort)) break;
+      if (!rwait(bb + B_V_FULL + 8 * st, ph, p.status, abort)) break;
+      if (!rwait(bb + B_P_FULL, j & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t mV = mVs + st * ST;
@@ -453,23 +479,21 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
             mma_ts(tb + C::C_O, tb + C::C_S + pc, mV + 128 * kk, idO, acc);
           }
         }
-        mma_commit(&B.v_empty[st]);
+        mma_commit_addr(bb + B_V_EMPTY + 8 * st);
       }
       __syncwarp();
       if (j + 1 < nkt && !scores(j + 1)) break;
     }
     // every product issued here has completed before the rows are read and TMEM is released
-    if (elect_one()) mma_commit(&B.drain);
+    if (elect_one()) mma_commit_addr(bb + B_DRAIN);
     __syncwarp();
-    mbar_wait(&B.drain, 0, p.status, FTC_WAIT_NS);
+    mbar_wait_addr(bb + B_DRAIN, 0, p.status, FTC_WAIT_NS);
   } else {
-    // ---- rows: row row0 + r (TMEM lane r), keys cb .. cb + HC - 1 of each tile ------------------------
-    constexpr int HC = C::HC;
+    // ---- rows: thread r owns row row0 + r (TMEM lane r) ----------------------------------------------
     const int q4 = warp & 3;
     const int r = q4 * 32 + lane;
-    const int half = (warp - 2) >> 2, cb = half * HC;
     const uint32_t lanes = tb + (static_cast<uint32_t>(q4 * 32) << 16);
-    const uint32_t aS = lanes + C::C_S + cb, aSd = lanes + C::C_SD + cb;
+    const uint32_t aS = lanes + C::C_S, aSd = lanes + C::C_SD;
     const int lo = tile_lo(st_rows, row0, r);
     const uint64_t c2p = pair(p.c2, p.c2), scp = pair(p.scale, p.scale);
     float m2 = -INFINITY, l = 0.f, rs = 0.f;
@@ -477,47 +501,44 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
     for (int j = 0; j < nkt; ++j) {
       const int st = j % C::STAGES;
       const bool mx_tile = mixed(j);
-      // a thread that gives up still meets its row's other thread once a tile
-      ok = ok && rwait(&B.s_full, j & 1, p.status, abort);
-      // the row's own keys among this thread's, and those of them whose V is not finite
-      uint32_t own[HC / 32], bads[HC / 32];
+      if (!rwait(bb + B_S_FULL, j & 1, p.status, abort)) { ok = false; break; }
+      uint32_t own[TK / 32];      // the row's own keys of the tile
       if (mx_tile) {
-        if (careful) ok = ok && rwait(&B.v_clean[st], (j / C::STAGES) & 1, p.status, abort);
-        const int kb = k0 + j * TK + cb;
-#pragma unroll
-        for (int c = 0; c < HC / 32; ++c) {
-          own[c] = col_bits(lo - kb - 32 * c, row0 + r - kb - 32 * c);
-          bads[c] = careful ? own[c] & bad[st][cb / 32 + c] : 0u;
+        if (careful && !rwait(bb + B_V_CLEAN + 8 * st, (j / C::STAGES) & 1, p.status, abort)) {
+          ok = false;
+          break;
         }
+        const int kb = k0 + j * TK;
+#pragma unroll
+        for (int c = 0; c < TK / 32; ++c) own[c] = col_bits(lo - kb - 32 * c, row0 + r - kb - 32 * c);
       }
       tc_fence_after();
-      float sv[32];
-      auto load_scores = [&](int c) {
+      // mixed tiles have code of their own: selects in the common one would be issued for every
+      // element, taken or not
+      float sv[32], mx = -INFINITY;
+      auto load_scores = [&](int c, auto masked) {
         tmem_ld32_nowait(aS + 32 * c, sv);
         tmem_wait_ld();
-        if (mx_tile) {
+        if constexpr (decltype(masked)::value) {
 #pragma unroll
           for (int i = 0; i < 32; ++i) sv[i] = own[c] >> i & 1 ? sv[i] : -INFINITY;
         }
       };
-      float mx = -INFINITY;
+      auto find_max = [&](auto masked) {
 #pragma unroll
-      for (int c = 0; c < HC / 32; ++c) {
-        if (!ok) break;
-        load_scores(c);
-        float y0 = mx, y1 = sv[0];
+        for (int c = 0; c < TK / 32; ++c) {
+          load_scores(c, masked);
+          float y0 = mx, y1 = sv[0];
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          y0 = fmaxf(fmaxf(y0, sv[i]), sv[i + 1]);
-          y1 = fmaxf(fmaxf(y1, sv[i + 2]), sv[i + 3]);
+          for (int i = 0; i < 32; i += 4) {
+            y0 = fmaxf(fmaxf(y0, sv[i]), sv[i + 1]);
+            y1 = fmaxf(fmaxf(y1, sv[i + 2]), sv[i + 3]);
+          }
+          mx = fmaxf(y0, y1);
         }
-        mx = fmaxf(y0, y1);
-      }
-      // the row's other thread has the other half of the keys
-      row_max[j & 1][half][r] = mx;
-      asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
-      if (!ok) continue;
-      mx = fmaxf(mx, row_max[j & 1][half ^ 1][r]);
+      };
+      if (mx_tile) find_max(std::true_type{});
+      else find_max(std::false_type{});
       const float t2 = mx * p.c2;
       float f = 1.f;
       if (t2 > m2 + TAU) {
@@ -529,9 +550,9 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
         // scores j were issued behind the products of tile j - 1, which are done
 #pragma unroll 1
-        for (int c0 = 0; c0 < HDP * C::NT / 2; c0 += 16) {
+        for (int c0 = 0; c0 < HDP * C::NT; c0 += 16) {
           float v[16];
-          const uint32_t at = lanes + C::C_O + half * (HDP * C::NT / 2) + c0;
+          const uint32_t at = lanes + C::C_O + c0;
           tmem_ld16(at, v);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] *= f;
@@ -541,63 +562,67 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       const float base = m2 == -INFINITY ? 0.f : m2;     // no key of the row so far: P = 0
       const uint64_t nm = pair(-base, -base);
       uint64_t l2 = 0, r2 = 0;
+      auto probs = [&](auto masked) {
+        constexpr bool MASK = decltype(masked)::value;
 #pragma unroll
-      for (int c = HC / 32 - 1; c >= 0; --c) {
-        if (c != HC / 32 - 1) load_scores(c);            // the last ones are still here
-        float sd[32];
-        if (DUAL) {
-          tmem_ld32_nowait(aSd + 32 * c, sd);
-          tmem_wait_ld();
-          if (mx_tile) {   // the tangent of a masked score may be anything
+        for (int c = TK / 32 - 1; c >= 0; --c) {
+          if (c != TK / 32 - 1) load_scores(c, masked);    // the last ones are still here
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sd[i] = own[c] >> i & 1 ? sd[i] : 0.f;
+          for (int g = 0; g < 2; ++g) {
+            float sd[16];
+            if (DUAL) {
+              tmem_ld16(aSd + 32 * c + 16 * g, sd);
+              if (MASK) {   // the tangent of a masked score may be anything
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sd[i] = own[c] >> (16 * g + i) & 1 ? sd[i] : 0.f;
+              }
+            }
+            uint32_t pk[8], psk[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float2 x = halves(fma2(pair(sv[16 * g + i], sv[16 * g + i + 1]), c2p, nm));
+              const float p0 = ex2(x.x), p1 = ex2(x.y);
+              const uint64_t pp = pair(p0, p1);
+              l2 = add2(l2, pp);
+              pk[i / 2] = pack_bf16x2(p0, p1);
+              if (DUAL) {
+                const uint64_t ps = mul2(mul2(pp, scp), pair(sd[i], sd[i + 1]));
+                r2 = add2(r2, ps);
+                psk[i / 2] = pack2(ps);
+              }
+            }
+            if (MASK && careful) {
+              const uint32_t w = (own[c] & bad[st][c]) >> (16 * g);
+              if (w & 0xffffu) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  pk[i] |= nan_pair(w >> (2 * i));
+                  if (DUAL) psk[i] |= nan_pair(w >> (2 * i));
+                }
+              }
+            }
+            tmem_st8(aS + 32 * c + 8 * g, pk);
+            if (DUAL) tmem_st8(aSd + 32 * c + 8 * g, psk);
           }
         }
-        uint32_t pk[16], psk[16];
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          const float2 x = halves(fma2(pair(sv[i], sv[i + 1]), c2p, nm));
-          const float p0 = ex2(x.x), p1 = ex2(x.y);
-          const uint64_t pp = pair(p0, p1);
-          l2 = add2(l2, pp);
-          pk[i / 2] = pack_bf16x2(p0, p1);
-          if (DUAL) {
-            const uint64_t ps = mul2(mul2(pp, scp), pair(sd[i], sd[i + 1]));
-            r2 = add2(r2, ps);
-            psk[i / 2] = pack2(ps);
-          }
-        }
-        if (careful && mx_tile && bads[c]) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            pk[i] |= nan_pair(bads[c] >> (2 * i));
-            if (DUAL) psk[i] |= nan_pair(bads[c] >> (2 * i));
-          }
-        }
-        tmem_st16u(aS + 32 * c, pk);
-        if (DUAL) tmem_st16u(aSd + 32 * c, psk);
-      }
+      };
+      if (mx_tile) probs(std::true_type{});
+      else probs(std::false_type{});
       const float2 lh = halves(l2), rh = halves(r2);
       l += lh.x + lh.y;
       rs += rh.x + rh.y;
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&B.p_full);
+      if (lane == 0) bar_arrive(bb + B_P_FULL);
     }
-    // the row's sums over both threads (every row thread meets the barrier)
-    row_sum[half][r] = make_float2(l, rs);
-    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
-    l = row_sum[0][r].x + row_sum[1][r].x;
-    rs = row_sum[0][r].y + row_sum[1][r].y;
-    if (ok && rwait(&B.drain, 0, p.status, abort) && !*abort) {
+    if (ok && rwait(bb + B_DRAIN, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const float inv = 1.f / l;
       const float rb = DUAL ? rs * inv : 0.f;
       float z = 0.f;
 #pragma unroll
-      for (int c0 = 0; c0 < HDP / 2; c0 += 16) {
-        const int c = half * (HDP / 2) + c0;
+      for (int c = 0; c < HDP; c += 16) {
         float o[16], t[16];
         tmem_ld16_nowait(lanes + C::C_O + c, o);
         if (DUAL) tmem_ld16_nowait(lanes + C::C_T + c, t);
@@ -616,7 +641,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
         if (DUAL) stage16<HDP>(smem + TR * HDP * 2, r, c, t);
       }
       if (r < nvalid && z != 0.f) redo_flag = 1;
-      if (r < nvalid && half == 0) {
+      if (r < nvalid) {
         const int64_t si = static_cast<int64_t>(h) * p.seq.rows + row0 + r;
         p.lse[si] = (m2 + log2f(l)) * LN2;
         if (DUAL) p.rbar[si] = rb;
@@ -657,12 +682,18 @@ bool head_map(CUtensorMap* m, const __nv_bfloat16* t, int D, int rows, int64_t l
   return make_head_map(m, t, D, rows, ld, heads, box);
 }
 
+dim3 tile_grid(int x, int tiles) {
+  return dim3(static_cast<unsigned>(x), static_cast<unsigned>(tiles < GRID_Y ? tiles : GRID_Y),
+              static_cast<unsigned>((tiles + GRID_Y - 1) / GRID_Y));
+}
+
 TcParams2 tc_params(const AttnParams& a) {
   TcParams2 p;
   memset(&p, 0, sizeof(p));
   p.seq = a.seq;
   p.Hq = a.Hq; p.Hkv = a.Hkv; p.D = a.D;
   p.tiles = (a.seq.rows + TR - 1) / TR;
+  p.G = a.Hq / a.Hkv;
   p.scale = a.scale;
   p.c2 = a.scale * LOG2E;
   p.ldo = a.ldo; p.lddo = a.lddo; p.lddq = a.lddq; p.lddk = a.lddk; p.lddv = a.lddv;
@@ -692,9 +723,7 @@ cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
   });
   if (e != cudaSuccess) return e;
   const TcParams2 p = tc_params(a);
-  const int64_t grid = static_cast<int64_t>(p.tiles) * a.Hq;
-  if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_k(attn_tc_fwd_kernel<DUAL, HDP>, dim3(static_cast<unsigned>(grid)), dim3(C::THREADS),
+  return launch_k(attn_tc_fwd_kernel<DUAL, HDP>, tile_grid(a.Hq, p.tiles), dim3(C::THREADS),
                   C::SMEM, s, q, k, v, qd, kd, vd, p);
 }
 
@@ -714,16 +743,21 @@ cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
 // into dS(i), the tensor cores work on dV(i) and S(i+1); while they turn S(i+1) into P(i+1), on
 // dK(i) and dP(i+1).
 // Query-row kernel, per key tile:  dS as above, untransposed, over dP;  dQ += dS K,
-// dQ' += dS' K + dS K',  in the order  S(j+1) | dQ(j) dP(j+1).
+// dQ' += dS' K + dS K'.  dP has two buffers, so that S(j+1) and dP(j+1) run while the row warps
+// work on tile j.
 template <bool DUAL, int HDP>
 struct BwdCfg {
   static constexpr int NA = HDP / 64;
   static constexpr int BT = HDP == 128 ? 128 : 64;         // streamed rows a tile
   static constexpr int NT = DUAL ? 2 : 1;
   static constexpr int CTAS = DUAL || HDP == 128 ? 1 : 2;
-  static constexpr int EW = CTAS == 1 ? 16 : 8;            // row warps
+#ifndef BWD_EW
+#define BWD_EW 8
+#endif
+  static constexpr int EW = CTAS == 1 ? BWD_EW : 8;            // row warps
   static constexpr int THREADS = 96 + 32 * EW;             // loads, products, look-over, rows
   static constexpr int CW = BT * 4 / EW;                   // columns of a row thread
+  static constexpr int OWN = (CW + 31) / 32;               // words of a bit a column
   static constexpr int OW = HDP * 4 / EW;                  // accumulator columns it brings out
   static constexpr int RES1 = NT * NA * ATOM128;           // K (K') or V (V'); Q (Q') or dO (dO')
   static constexpr int BATOM = BT * 128;
@@ -737,10 +771,12 @@ struct BwdCfg {
   static_assert(SMEM_KV + 1024 <= 227 * 1024, "a CTA's shared memory");
   // TMEM: S (S'), dP (dP'), then the accumulators, tangents behind their primal
   static constexpr uint32_t C_S = 0, C_SD = BT, C_DP = NT * BT, C_DPD = C_DP + BT;
-  static constexpr uint32_t C_A = 2 * NT * BT;             // dV (dV') or dQ (dQ')
+  static constexpr uint32_t C_A = 2 * NT * BT;             // dV (dV')
   static constexpr uint32_t C_B = C_A + NT * HDP;          // dK (dK')
-  static constexpr uint32_t COLS_KV = C_B + NT * HDP <= 256 ? 256 : 512;
-  static constexpr uint32_t COLS_Q = C_B <= 256 ? 256 : 512;
+  static constexpr uint32_t COLS = C_B + NT * HDP;         // 256 or 512, all of it
+  // query-row kernel: two buffers of dP (dP') behind each other, then dQ (dQ')
+  static constexpr uint32_t DP_STEP = NT * BT, C_Q = 3 * NT * BT;
+  static_assert((COLS == 256 || COLS == 512) && C_Q + NT * HDP == COLS, "TMEM columns");
 };
 
 // The row warps' barrier.
@@ -801,11 +837,12 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   using C = BwdCfg<DUAL, HDP>;
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  struct Bars {
-    uint64_t res_full, s_full, dp_full, p_full, ds_full, drain;
-    uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
-  };
-  __shared__ __align__(8) Bars bars[2];      // one set per walk
+  // barriers, as byte offsets in a set; one set per walk
+  constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_DP_FULL = 16, B_P_FULL = 24, B_DS_FULL = 32, B_DRAIN = 40;
+  constexpr uint32_t B_ST_FULL = 48 + 0 * C::STAGES, B_ST_EMPTY = 48 + 8 * C::STAGES,
+      B_ST_CLEAN = 48 + 16 * C::STAGES;
+  constexpr int NBARS = 6 + 3 * C::STAGES;
+  __shared__ __align__(8) uint64_t bars[2][NBARS];
   __shared__ uint32_t bad[C::STAGES][4];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
@@ -818,21 +855,23 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   float* sStat = reinterpret_cast<float*>(sSt + C::STAGES * C::STAGE_B);
   // a cluster shares the query heads of a group; heads fastest; the first rows of a long
   // sequence (the longest walks) come first
-  const int rank = static_cast<int>(blockIdx.x % p.share);
-  const int hk = static_cast<int>(blockIdx.x / p.share % p.Hkv);
-  const int row0 = static_cast<int>(blockIdx.x / (p.share * p.Hkv)) * TR;
-  const int G = p.Hq / p.Hkv / p.share;
-  const int h0 = (hk * p.share + rank) * G;
+  int rank, hk;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(hk));
+  const int tile = tile_index();
+  if (tile >= p.tiles) return;
+  const int row0 = tile * TR;
+  const int G = p.Gs, h0 = (hk * p.share + rank) * G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto load_rows = [&](uint64_t& bar) {
-    mbar_expect_tx(&bar, 2 * C::RES1);
+  auto load_rows = [&](uint32_t bar) {
+    mbar_expect_tx_addr(bar, 2 * C::RES1);
 #pragma unroll
     for (int a = 0; a < NA; ++a) {
-      tma_load_3d(sRes + a * ATOM128, &tmK, &bar, 64 * a, row0, hk);
-      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmV, &bar, 64 * a, row0, hk);
+      tma_load_at<false>(smem_u32(sRes + a * ATOM128), &tmK, bar, 64 * a, row0, hk);
+      tma_load_at<false>(smem_u32(sRes + C::RES1 + a * ATOM128), &tmV, bar, 64 * a, row0, hk);
       if (DUAL) {
-        tma_load_3d(sRes + (NA + a) * ATOM128, &tmKd, &bar, 64 * a, row0, hk);
-        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmVd, &bar, 64 * a, row0, hk);
+        tma_load_at<false>(smem_u32(sRes + (NA + a) * ATOM128), &tmKd, bar, 64 * a, row0, hk);
+        tma_load_at<false>(smem_u32(sRes + C::RES1 + (NA + a) * ATOM128), &tmVd, bar, 64 * a, row0, hk);
       }
     }
   };
@@ -842,28 +881,20 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   const int nvalid = min(seq_total(p.seq) - row0, TR);
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
-  if (threadIdx.x == 0) {
-    for (Bars& B : bars) {
-      mbar_init(&B.res_full, 1);
-      mbar_init(&B.s_full, 1);
-      mbar_init(&B.dp_full, 1);
-      mbar_init(&B.p_full, C::EW);
-      mbar_init(&B.ds_full, C::EW);
-      mbar_init(&B.drain, 1);
-      for (int i = 0; i < C::STAGES; ++i) {
-        mbar_init(&B.st_full[i], 1);
-        mbar_init(&B.st_empty[i], 1);
-        mbar_init(&B.st_clean[i], 1);
-      }
-    }
-    abort_flag = redo_flag = 0;
+  // a barrier a thread; the first thread's own is the one that its loads complete
+  if (threadIdx.x < 2 * NBARS) {
+    const uint32_t b = threadIdx.x % NBARS;
+    bar_init(smem_u32(&bars[0][0]) + 8 * threadIdx.x, 8 * b == B_P_FULL || 8 * b == B_DS_FULL ? C::EW : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    load_rows(bars[0].res_full);   // the rows' own operands need nothing of the sequences
+  }
+  if (threadIdx.x == 0) {
+    abort_flag = redo_flag = 0;
+    load_rows(smem_u32(&bars[0][0]) + B_RES_FULL);   // the rows' own operands need nothing of the sequences
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                      smem_u32(&tmem_slot)),
-                 "r"(C::COLS_KV));
+                 "r"(C::COLS));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   __syncthreads();
@@ -881,32 +912,32 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 
   for (int walk = 0;; ++walk) {
   const bool careful = walk > 0;
-  Bars& B = bars[walk];
+  const uint32_t bb = smem_u32(&bars[walk][0]);
   if (warp == 0) {
     if (elect_one()) {
-      if (walk) load_rows(B.res_full);
+      if (walk) load_rows(bb + B_RES_FULL);
       // ---- TMA producer ---------------------------------------------------------------------------
       int issued = 0, t = 0, h = h0;
       for (int i = 0; i < ntile; ++i) {
         const int st = i % C::STAGES;
-        if (!fwait(&B.st_empty[st], ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+        if (!twait(bb + B_ST_EMPTY + 8 * st, ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
         const int qr = row0 + t * BT;
-        mbar_expect_tx(&B.st_full[st], C::STAGE_B);
+        mbar_expect_tx_addr(bb + B_ST_FULL + 8 * st, C::STAGE_B);
         uint8_t* b = sSt + st * C::STAGE_B;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::BATOM, &tmQ, &B.st_full[st], 64 * a, qr, h);
-          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmO, &B.st_full[st], 64 * a, qr, h);
+          tma_load_at<false>(smem_u32(b + a * C::BATOM), &tmQ, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
+          tma_load_at<false>(smem_u32(b + C::TILE_B + a * C::BATOM), &tmO, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
           if (DUAL) {
-            tma_load_3d(b + (NA + a) * C::BATOM, &tmQd, &B.st_full[st], 64 * a, qr, h);
-            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmOd, &B.st_full[st], 64 * a, qr, h);
+            tma_load_at<false>(smem_u32(b + (NA + a) * C::BATOM), &tmQd, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
+            tma_load_at<false>(smem_u32(b + C::TILE_B + (NA + a) * C::BATOM), &tmOd, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
           }
         }
         ++issued;
         if (++t == nqt) { t = 0; ++h; }
       }
-      mbar_wait(&B.res_full, 0, p.status, FTC_WAIT_NS);
-      drain_loads(B.st_full, issued, C::STAGES, p.status);
+      mbar_wait_addr(bb + B_RES_FULL, 0, p.status, FTC_WAIT_NS);
+      drain_ring(bb + B_ST_FULL, issued, C::STAGES, p.status);
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -931,7 +962,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     for (int i = 0; i < ntile; ++i) {
       const int st = i % C::STAGES;
       const bool mx = mixed(t);
-      if (!rwait(&B.st_full[st], (i / C::STAGES) & 1, p.status, abort)) break;
+      if (!rwait(bb + B_ST_FULL + 8 * st, (i / C::STAGES) & 1, p.status, abort)) break;
       float* sst = sStat + st * C::STAT_F;
 #pragma unroll
       for (int k = 0; k < C::NSTAT; ++k)
@@ -941,7 +972,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       if (i + 1 < ntile) read(t, h);
       if (careful && mx) scrub(sSt + st * C::STAGE_B, BT, 2 * C::NT * NA, bad[st], lane);
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&B.st_clean[st]);
+      if (lane == 0) bar_arrive(bb + B_ST_CLEAN + 8 * st);
     }
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
@@ -975,16 +1006,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       }
     };
     auto ready = [&](int i) {
-      return rwait(&B.st_clean[i % C::STAGES], (i / C::STAGES) & 1, p.status, abort);
+      return rwait(bb + B_ST_CLEAN + 8 * (i % C::STAGES), (i / C::STAGES) & 1, p.status, abort);
     };
-    bool ok = rwait(&B.res_full, 0, p.status, abort) && ready(0);
+    bool ok = rwait(bb + B_RES_FULL, 0, p.status, abort) && ready(0);
     if (ok) {
       tc_fence_after();
       if (elect_one()) {
         score(dK, kSt, C::C_S);
-        mma_commit(&B.s_full);
+        mma_commit_addr(bb + B_S_FULL);
         score(dV, kSt + DO, C::C_DP);
-        mma_commit(&B.dp_full);
+        mma_commit_addr(bb + B_DP_FULL);
       }
       __syncwarp();
     }
@@ -992,31 +1023,31 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int st = i % C::STAGES, sn = (i + 1) % C::STAGES;
       const bool more = i + 1 < ntile;
       if (more && !ready(i + 1)) break;
-      if (!rwait(&B.p_full, i & 1, p.status, abort)) break;
+      if (!rwait(bb + B_P_FULL, i & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         accum(C::C_A, C::C_S, mSt + st * ST + DO, i == 0);
         if (more) {
           score(dK, kSt + sn * ST, C::C_S);
-          mma_commit(&B.s_full);
+          mma_commit_addr(bb + B_S_FULL);
         }
       }
       __syncwarp();
-      if (!rwait(&B.ds_full, i & 1, p.status, abort)) break;
+      if (!rwait(bb + B_DS_FULL, i & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         accum(C::C_B, C::C_DP, mSt + st * ST, i == 0);
-        mma_commit(&B.st_empty[st]);
+        mma_commit_addr(bb + B_ST_EMPTY + 8 * st);
         if (more) {
           score(dV, kSt + sn * ST + DO, C::C_DP);
-          mma_commit(&B.dp_full);
+          mma_commit_addr(bb + B_DP_FULL);
         }
       }
       __syncwarp();
     }
-    if (elect_one()) mma_commit(&B.drain);
+    if (elect_one()) mma_commit_addr(bb + B_DRAIN);
     __syncwarp();
-    mbar_wait(&B.drain, 0, p.status, FTC_WAIT_NS);
+    mbar_wait_addr(bb + B_DRAIN, 0, p.status, FTC_WAIT_NS);
   } else {
     // ---- rows: key row r (TMEM lane r), query columns cb .. cb + CW - 1 ---------------------------------
     const int q4 = warp & 3;
@@ -1034,14 +1065,17 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       // columns a .. b - 1 (of the tile) attend to this key
       const int a = r - t * BT, b = hi - (row0 + t * BT);
       if (++t == nqt) t = 0;
-      if (!rwait(&B.st_clean[st], ph, p.status, abort)) { ok = false; break; }   // the statistics
-      uint32_t own = 0, bads = 0;
+      if (!rwait(bb + B_ST_CLEAN + 8 * st, ph, p.status, abort)) { ok = false; break; }   // the statistics
+      uint32_t own[C::OWN], bads[C::OWN] = {};   // the row's own columns, the noted ones of them
       if (mx) {
-        own = col_bits(a - cb, b - 1 - cb);
-        if (careful) bads = own & (bad[st][cb >> 5] >> (cb & 31));
+#pragma unroll
+        for (int w = 0; w < C::OWN; ++w) {
+          own[w] = col_bits(a - cb - 32 * w, b - 1 - cb - 32 * w);
+          if (careful) bads[w] = own[w] & (bad[st][(cb >> 5) + w] >> (cb & 31));
+        }
       }
       const float4* stat = reinterpret_cast<const float4*>(sStat + st * C::STAT_F + cb);
-      if (!rwait(&B.s_full, i & 1, p.status, abort)) { ok = false; break; }
+      if (!rwait(bb + B_S_FULL, i & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       float pr[CW], pd[DUAL ? CW : 1];
       auto probs = [&](auto masked) {
@@ -1065,8 +1099,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               const int f = e + 2 * u, c = c0 + f;
               const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, lv[u]));
               float p0 = ex2(x.x), p1 = ex2(x.y);
-              const bool o0 = !MASK || (own >> c & 1);
-              const bool o1 = !MASK || (own >> c & 2);
+              const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
+              const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
               if (!o0) p0 = 0.f;
               if (!o1) p1 = 0.f;
               pr[c] = p0;
@@ -1083,11 +1117,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               }
             }
           }
-          if (MASK && bads) {
+          if (MASK && bads[c0 >> 5]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              pk[k] |= nan_pair(bads >> (c0 + 2 * k));
-              if (DUAL) pdk[k] |= nan_pair(bads >> (c0 + 2 * k));
+              pk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) pdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_S + c0 / 2, pk);
@@ -1099,8 +1133,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&B.p_full);
-      if (!rwait(&B.dp_full, i & 1, p.status, abort)) { ok = false; break; }
+      if (lane == 0) bar_arrive(bb + B_P_FULL);
+      if (!rwait(bb + B_DP_FULL, i & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       auto scores = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
@@ -1124,8 +1158,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               const uint64_t pp = pair(pr[c], pr[c + 1]);
               const uint64_t x = add2(dv[u], pair(dp[f], dp[f + 1]));
               float2 s = halves(mul2(pp, x));
-              const bool o0 = !MASK || (own >> c & 1);
-              const bool o1 = !MASK || (own >> c & 2);
+              const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
+              const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
               if (!o0) s.x = 0.f;
               if (!o1) s.y = 0.f;
               sk[f / 2] = pack_bf16x2(s.x, s.y);
@@ -1138,11 +1172,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               }
             }
           }
-          if (MASK && bads) {
+          if (MASK && bads[c0 >> 5]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              sk[k] |= nan_pair(bads >> (c0 + 2 * k));
-              if (DUAL) sdk[k] |= nan_pair(bads >> (c0 + 2 * k));
+              sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
@@ -1154,11 +1188,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&B.ds_full);
+      if (lane == 0) bar_arrive(bb + B_DS_FULL);
     }
     // accumulators to shared memory, over the operands, which every product has read: a tile of
     // float32 rows each, 16-byte chunk c of row r at place c ^ (r & 7)
-    if (ok && rwait(&B.drain, 0, p.status, abort) && !*abort) {
+    if (ok && rwait(bb + B_DRAIN, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16) + part * C::OW;
       float z = 0.f;
@@ -1190,37 +1224,45 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   cluster_sync_all();
   if (warp >= 3 && !*abort) {
     const int rows = (TR + p.share - 1) / p.share;
-    const int r0 = rank * rows, r1 = min(min(r0 + rows, TR), nvalid);
+    const int r0 = rank * rows, nr = min(min(r0 + rows, TR), nvalid) - r0;
     constexpr int CH = HDP / 8;
-    for (int i = static_cast<int>(threadIdx.x) - 96 + r0 * CH; i < r1 * CH; i += 32 * C::EW) {
-      const int r = i / CH, c = i % CH;
+    // eight columns of one sum at a time; all the ranks' reads in flight together
+    for (int i = static_cast<int>(threadIdx.x) - 96; i < nr * (2 * C::NT * CH); i += 32 * C::EW) {
+      const int c = i % CH, k = i / CH % (2 * C::NT), r = r0 + i / (2 * C::NT * CH);
       if (8 * c >= p.D) continue;
-      const int64_t row = row0 + r;
+      const uint32_t at = (k * TR + r) * (4 * HDP);
+      const uint32_t o0 = at + (((2 * c) ^ (r & 7)) << 4), o1 = at + (((2 * c + 1) ^ (r & 7)) << 4);
+      float4 x = *reinterpret_cast<const float4*>(smem + o0), y = *reinterpret_cast<const float4*>(smem + o1);
+      if (p.share > 1) {
+        float4 xs[8], ys[8];
 #pragma unroll
-      for (int k = 0; k < 2 * C::NT; ++k) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        const uint32_t at = smem_u32(smem) + (k * TR + r) * (4 * HDP);
-        for (int j = 0; j < p.share; ++j) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float4 x = ld_cluster4(dsmem_addr(at + (((2 * c + u) ^ (r & 7)) << 4), j));
-            v[4 * u] += x.x; v[4 * u + 1] += x.y; v[4 * u + 2] += x.z; v[4 * u + 3] += x.w;
+        for (int j = 0; j < 8; ++j)
+          if (j < p.share) {
+            xs[j] = ld_cluster4(dsmem_addr(smem_u32(smem + o0), j));
+            ys[j] = ld_cluster4(dsmem_addr(smem_u32(smem + o1), j));
           }
-        }
-        // dV (dV') as they are, dK (dK') with the scale of the scores
-        const bool isv = k < C::NT;
-        const float f = isv ? 1.f : p.scale;
-        __nv_bfloat16* dst = k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd;
-        *reinterpret_cast<uint4*>(dst + row * (isv ? p.lddv : p.lddk) + hk * p.D + 8 * c) =
-            make_uint4(pack_bf16x2(v[0] * f, v[1] * f), pack_bf16x2(v[2] * f, v[3] * f),
-                       pack_bf16x2(v[4] * f, v[5] * f), pack_bf16x2(v[6] * f, v[7] * f));
+        x = xs[0];
+        y = ys[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j)
+          if (j < p.share) {
+            x.x += xs[j].x; x.y += xs[j].y; x.z += xs[j].z; x.w += xs[j].w;
+            y.x += ys[j].x; y.y += ys[j].y; y.z += ys[j].z; y.w += ys[j].w;
+          }
       }
+      // dV (dV') as they are, dK (dK') with the scale of the scores
+      const bool isv = k < C::NT;
+      const float f = isv ? 1.f : p.scale;
+      __nv_bfloat16* dst = k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd;
+      *reinterpret_cast<uint4*>(dst + (row0 + r) * (isv ? p.lddv : p.lddk) + hk * p.D + 8 * c) =
+          make_uint4(pack_bf16x2(x.x * f, x.y * f), pack_bf16x2(x.z * f, x.w * f),
+                     pack_bf16x2(y.x * f, y.y * f), pack_bf16x2(y.z * f, y.w * f));
     }
   }
-  cluster_sync_all();
+  cluster_leave();
   if (warp == 1) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
-                 "r"(C::COLS_KV));
+                 "r"(C::COLS));
   }
 }
 
@@ -1234,11 +1276,12 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   using C = BwdCfg<DUAL, HDP>;
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  struct Bars {
-    uint64_t res_full, s_full, s_free, dp_full, ds_full, drain;
-    uint64_t st_full[C::STAGES], st_empty[C::STAGES], st_clean[C::STAGES];
-  };
-  __shared__ __align__(8) Bars bars[2];      // one set per walk
+  // barriers, as byte offsets in a set; one set per walk
+  constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_S_FREE = 16, B_DP_FULL = 24, B_DS_FULL = 32, B_DRAIN = 40;
+  constexpr uint32_t B_ST_FULL = 48 + 0 * C::STAGES, B_ST_EMPTY = 48 + 8 * C::STAGES,
+      B_ST_CLEAN = 48 + 16 * C::STAGES;
+  constexpr int NBARS = 6 + 3 * C::STAGES;
+  __shared__ __align__(8) uint64_t bars[2][NBARS];
   __shared__ uint32_t bad[C::STAGES][4];
   __shared__ float2 sD[TR];
   __shared__ SeqTile st_rows;
@@ -1249,19 +1292,20 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* sRes = smem;                        // Q (Q'), dO (dO')
   uint8_t* sSt = smem + 2 * C::RES1;           // stage: K (K'), V (V')
-  const int h = static_cast<int>(blockIdx.x % p.Hq);
-  const int row0 = (p.tiles - 1 - static_cast<int>(blockIdx.x / p.Hq)) * TR;
-  const int hk = h / (p.Hq / p.Hkv);
+  const int h = static_cast<int>(blockIdx.x), tile = tile_index();
+  if (tile >= p.tiles) return;
+  const int row0 = (p.tiles - 1 - tile) * TR;
+  const int hk = h / p.G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto load_rows = [&](uint64_t& bar) {
-    mbar_expect_tx(&bar, 2 * C::RES1);
+  auto load_rows = [&](uint32_t bar) {
+    mbar_expect_tx_addr(bar, 2 * C::RES1);
 #pragma unroll
     for (int a = 0; a < NA; ++a) {
-      tma_load_3d(sRes + a * ATOM128, &tmQ, &bar, 64 * a, row0, h);
-      tma_load_3d(sRes + C::RES1 + a * ATOM128, &tmO, &bar, 64 * a, row0, h);
+      tma_load_at<false>(smem_u32(sRes + a * ATOM128), &tmQ, bar, 64 * a, row0, h);
+      tma_load_at<false>(smem_u32(sRes + C::RES1 + a * ATOM128), &tmO, bar, 64 * a, row0, h);
       if (DUAL) {
-        tma_load_3d(sRes + (NA + a) * ATOM128, &tmQd, &bar, 64 * a, row0, h);
-        tma_load_3d(sRes + C::RES1 + (NA + a) * ATOM128, &tmOd, &bar, 64 * a, row0, h);
+        tma_load_at<false>(smem_u32(sRes + (NA + a) * ATOM128), &tmQd, bar, 64 * a, row0, h);
+        tma_load_at<false>(smem_u32(sRes + C::RES1 + (NA + a) * ATOM128), &tmOd, bar, 64 * a, row0, h);
       }
     }
   };
@@ -1271,28 +1315,20 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   const int nvalid = min(seq_total(p.seq) - row0, TR);
   if (nvalid <= 0) return;
   seq_tile_init(p.seq, row0, st_rows);
-  if (threadIdx.x == 0) {
-    for (Bars& B : bars) {
-      mbar_init(&B.res_full, 1);
-      mbar_init(&B.s_full, 1);
-      mbar_init(&B.s_free, C::EW);
-      mbar_init(&B.dp_full, 1);
-      mbar_init(&B.ds_full, C::EW);
-      mbar_init(&B.drain, 1);
-      for (int i = 0; i < C::STAGES; ++i) {
-        mbar_init(&B.st_full[i], 1);
-        mbar_init(&B.st_empty[i], 1);
-        mbar_init(&B.st_clean[i], 1);
-      }
-    }
-    abort_flag = redo_flag = 0;
+  // a barrier a thread; the first thread's own is the one that its loads complete
+  if (threadIdx.x < 2 * NBARS) {
+    const uint32_t b = threadIdx.x % NBARS;
+    bar_init(smem_u32(&bars[0][0]) + 8 * threadIdx.x, 8 * b == B_S_FREE || 8 * b == B_DS_FULL ? C::EW : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    load_rows(bars[0].res_full);   // the rows' own operands need nothing of the sequences
+  }
+  if (threadIdx.x == 0) {
+    abort_flag = redo_flag = 0;
+    load_rows(smem_u32(&bars[0][0]) + B_RES_FULL);   // the rows' own operands need nothing of the sequences
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                      smem_u32(&tmem_slot)),
-                 "r"(C::COLS_Q));
+                 "r"(C::COLS));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   __syncthreads();
@@ -1308,31 +1344,31 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 
   for (int walk = 0;; ++walk) {
   const bool careful = walk > 0;
-  Bars& B = bars[walk];
+  const uint32_t bb = smem_u32(&bars[walk][0]);
   if (warp == 0) {
     if (elect_one()) {
-      if (walk) load_rows(B.res_full);
+      if (walk) load_rows(bb + B_RES_FULL);
       // ---- TMA producer ---------------------------------------------------------------------------
       int issued = 0;
       for (int j = 0; j < nkt; ++j) {
         const int st = j % C::STAGES;
-        if (!fwait(&B.st_empty[st], ((j / C::STAGES) & 1) ^ 1, p.status, abort)) break;
-        mbar_expect_tx(&B.st_full[st], C::STAGE_B);
+        if (!twait(bb + B_ST_EMPTY + 8 * st, ((j / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+        mbar_expect_tx_addr(bb + B_ST_FULL + 8 * st, C::STAGE_B);
         uint8_t* b = sSt + st * C::STAGE_B;
         const int kr = k0 + j * BT;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_3d(b + a * C::BATOM, &tmK, &B.st_full[st], 64 * a, kr, hk);
-          tma_load_3d(b + C::TILE_B + a * C::BATOM, &tmV, &B.st_full[st], 64 * a, kr, hk);
+          tma_load_at<false>(smem_u32(b + a * C::BATOM), &tmK, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
+          tma_load_at<false>(smem_u32(b + C::TILE_B + a * C::BATOM), &tmV, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
           if (DUAL) {
-            tma_load_3d(b + (NA + a) * C::BATOM, &tmKd, &B.st_full[st], 64 * a, kr, hk);
-            tma_load_3d(b + C::TILE_B + (NA + a) * C::BATOM, &tmVd, &B.st_full[st], 64 * a, kr, hk);
+            tma_load_at<false>(smem_u32(b + (NA + a) * C::BATOM), &tmKd, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
+            tma_load_at<false>(smem_u32(b + C::TILE_B + (NA + a) * C::BATOM), &tmVd, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
           }
         }
         ++issued;
       }
-      mbar_wait(&B.res_full, 0, p.status, FTC_WAIT_NS);
-      drain_loads(B.st_full, issued, C::STAGES, p.status);
+      mbar_wait_addr(bb + B_RES_FULL, 0, p.status, FTC_WAIT_NS);
+      drain_ring(bb + B_ST_FULL, issued, C::STAGES, p.status);
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -1340,9 +1376,9 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     // masked key is dropped
     for (int j = 0; j < nkt; ++j) {
       const int st = j % C::STAGES;
-      if (!rwait(&B.st_full[st], (j / C::STAGES) & 1, p.status, abort)) break;
+      if (!rwait(bb + B_ST_FULL + 8 * st, (j / C::STAGES) & 1, p.status, abort)) break;
       if (careful && mixed(j)) scrub(sSt + st * C::STAGE_B, BT, C::NT * NA, bad[st], lane);
-      if (lane == 0) mbar_arrive_local(&B.st_clean[st]);
+      if (lane == 0) bar_arrive(bb + B_ST_CLEAN + 8 * st);
     }
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
@@ -1364,54 +1400,47 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       }
     };
     auto ready = [&](int j) {
-      return rwait(&B.st_clean[j % C::STAGES], (j / C::STAGES) & 1, p.status, abort);
+      return rwait(bb + B_ST_CLEAN + 8 * (j % C::STAGES), (j / C::STAGES) & 1, p.status, abort);
     };
-    bool ok = rwait(&B.res_full, 0, p.status, abort) && ready(0);
-    if (ok) {
+    // the scores of tile j, ahead of its dP: S waits until the row warps have read the last one
+    auto scores = [&](int j) -> bool {
+      if (!ready(j)) return false;
+      if (j > 0 && !rwait(bb + B_S_FREE, (j - 1) & 1, p.status, abort)) return false;
       tc_fence_after();
       if (elect_one()) {
-        score(dQ, kSt, C::C_S);
-        mma_commit(&B.s_full);
-        score(dO, kSt + VO, C::C_DP);
-        mma_commit(&B.dp_full);
+        const uint64_t k = kSt + (j % C::STAGES) * ST;
+        score(dQ, k, C::C_S);
+        mma_commit_addr(bb + B_S_FULL);
+        // buffer j & 1 held dS of tile j - 2, whose product has been issued
+        score(dO, k + VO, C::C_DP + (j & 1) * C::DP_STEP);
+        mma_commit_addr(bb + B_DP_FULL);
       }
       __syncwarp();
-    }
+      return true;
+    };
+    bool ok = rwait(bb + B_RES_FULL, 0, p.status, abort) && scores(0);
     for (int j = 0; ok && j < nkt; ++j) {
-      const int st = j % C::STAGES, sn = (j + 1) % C::STAGES;
-      const bool more = j + 1 < nkt;
-      if (more) {
-        if (!ready(j + 1)) break;
-        if (!rwait(&B.s_free, j & 1, p.status, abort)) break;
-        tc_fence_after();
-        if (elect_one()) {
-          score(dQ, kSt + sn * ST, C::C_S);
-          mma_commit(&B.s_full);
-        }
-        __syncwarp();
-      }
-      if (!rwait(&B.ds_full, j & 1, p.status, abort)) break;
+      const int st = j % C::STAGES;
+      if (j + 1 < nkt && !scores(j + 1)) break;
+      if (!rwait(bb + B_DS_FULL, j & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t mK = mSt + st * ST;
+        const uint32_t a = tb + C::C_DP + (j & 1) * C::DP_STEP;
 #pragma unroll
         for (int kk = 0; kk < BT / 16; ++kk) {
-          const uint32_t ac = C::C_DP + (kk / (CW / 16)) * CW + (kk % (CW / 16)) * 8;
+          const uint32_t ac = a + (kk / (CW / 16)) * CW + (kk % (CW / 16)) * 8;
           const uint32_t acc = (j > 0 || kk > 0) ? 1u : 0u;
-          mma_ts(tb + C::C_A, tb + ac, mK + 128 * kk, DUAL ? idA2 : idA, acc);
-          if (DUAL) mma_ts(tb + C::C_A + HDP, tb + ac + BT, mK + 128 * kk, idA, 1);
+          mma_ts(tb + C::C_Q, ac, mK + 128 * kk, DUAL ? idA2 : idA, acc);
+          if (DUAL) mma_ts(tb + C::C_Q + HDP, ac + BT, mK + 128 * kk, idA, 1);
         }
-        mma_commit(&B.st_empty[st]);
-        if (more) {
-          score(dO, kSt + sn * ST + VO, C::C_DP);
-          mma_commit(&B.dp_full);
-        }
+        mma_commit_addr(bb + B_ST_EMPTY + 8 * st);
       }
       __syncwarp();
     }
-    if (elect_one()) mma_commit(&B.drain);
+    if (elect_one()) mma_commit_addr(bb + B_DRAIN);
     __syncwarp();
-    mbar_wait(&B.drain, 0, p.status, FTC_WAIT_NS);
+    mbar_wait_addr(bb + B_DRAIN, 0, p.status, FTC_WAIT_NS);
   } else {
     // ---- rows: query row r (TMEM lane r), key columns cb .. cb + CW - 1 ---------------------------------
     const int q4 = warp & 3;
@@ -1437,15 +1466,19 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int st = j % C::STAGES;
       const bool mx = mixed(j);
       const int a = lo - (k0 + j * BT), b = row0 + r - (k0 + j * BT);
-      uint32_t own = 0, bads = 0;
+      uint32_t own[C::OWN], bads[C::OWN] = {};   // the row's own columns, the noted ones of them
       if (mx) {
-        own = col_bits(a - cb, b - cb);
-        if (careful) {
-          if (!rwait(&B.st_clean[st], (j / C::STAGES) & 1, p.status, abort)) { ok = false; break; }
-          bads = own & (bad[st][cb >> 5] >> (cb & 31));
+        if (careful && !rwait(bb + B_ST_CLEAN + 8 * st, (j / C::STAGES) & 1, p.status, abort)) {
+          ok = false;
+          break;
+        }
+#pragma unroll
+        for (int w = 0; w < C::OWN; ++w) {
+          own[w] = col_bits(a - cb - 32 * w, b - cb - 32 * w);
+          if (careful) bads[w] = own[w] & (bad[st][(cb >> 5) + w] >> (cb & 31));
         }
       }
-      if (!rwait(&B.s_full, j & 1, p.status, abort)) { ok = false; break; }
+      if (!rwait(bb + B_S_FULL, j & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       float pr[CW], pd[DUAL ? CW : 1];
       auto probs = [&](auto masked) {
@@ -1462,8 +1495,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             const float2 x = halves(fma2(pair(sv[f], sv[f + 1]), c2p, nl));
             pr[c] = ex2(x.x);
             pr[c + 1] = ex2(x.y);
-            if (MASK && !(own >> c & 1)) pr[c] = 0.f;
-            if (MASK && !(own >> c & 2)) pr[c + 1] = 0.f;
+            if (MASK && !(own[c >> 5] >> (c & 31) & 1)) pr[c] = 0.f;
+            if (MASK && !(own[c >> 5] >> (c & 31) & 2)) pr[c + 1] = 0.f;
             if (DUAL) {
               const float2 y = halves(mul2(pair(pr[c], pr[c + 1]), fma2(pair(sd[f], sd[f + 1]), sc, nr)));
               pd[c] = y.x;
@@ -1476,17 +1509,18 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       else probs(std::false_type{});
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&B.s_free);
-      if (!rwait(&B.dp_full, j & 1, p.status, abort)) { ok = false; break; }
+      if (lane == 0) bar_arrive(bb + B_S_FREE);
+      if (!rwait(bb + B_DP_FULL, j & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
+      const uint32_t aP = lane_base + C::C_DP + (j & 1) * C::DP_STEP;
       auto scores = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
 #pragma unroll
         for (int c0 = 0; c0 < CW; c0 += 16) {
           float dp[16], dd[16];
           uint32_t sk[8], sdk[8];
-          tmem_ld16_nowait(lane_base + C::C_DP + c0, dp);
-          if (DUAL) tmem_ld16_nowait(lane_base + C::C_DPD + c0, dd);
+          tmem_ld16_nowait(aP + c0, dp);
+          if (DUAL) tmem_ld16_nowait(aP + BT + c0, dd);
           tmem_wait_ld();
 #pragma unroll
           for (int f = 0; f < 16; f += 2) {
@@ -1494,8 +1528,8 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
             const uint64_t pp = pair(pr[c], pr[c + 1]);
             const uint64_t x = add2(pair(dp[f], dp[f + 1]), nD);
             float2 s = halves(mul2(pp, x));
-            const bool o0 = !MASK || (own >> c & 1);
-            const bool o1 = !MASK || (own >> c & 2);
+            const bool o0 = !MASK || (own[c >> 5] >> (c & 31) & 1);
+            const bool o1 = !MASK || (own[c >> 5] >> (c & 31) & 2);
             if (!o0) s.x = 0.f;
             if (!o1) s.y = 0.f;
             sk[f / 2] = pack_bf16x2(s.x, s.y);
@@ -1507,15 +1541,15 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               sdk[f / 2] = pack_bf16x2(z.x, z.y);
             }
           }
-          if (MASK && bads) {
+          if (MASK && bads[c0 >> 5]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              sk[k] |= nan_pair(bads >> (c0 + 2 * k));
-              if (DUAL) sdk[k] |= nan_pair(bads >> (c0 + 2 * k));
+              sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
-          tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
-          if (DUAL) tmem_st8(lane_base + C::C_DPD + c0 / 2, sdk);
+          tmem_st8(aP + c0 / 2, sk);
+          if (DUAL) tmem_st8(aP + BT + c0 / 2, sdk);
         }
       };
       if (mx) scores(std::true_type{});
@@ -1523,9 +1557,9 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_local(&B.ds_full);
+      if (lane == 0) bar_arrive(bb + B_DS_FULL);
     }
-    if (ok && rwait(&B.drain, 0, p.status, abort) && !*abort) {
+    if (ok && rwait(bb + B_DRAIN, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16) + part * C::OW;
       float z = 0.f;
@@ -1534,7 +1568,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 #pragma unroll
         for (int c0 = 0; c0 < C::OW; c0 += 16) {
           float v[16];
-          tmem_ld16(acc + C::C_A + k * HDP + c0, v);
+          tmem_ld16(acc + C::C_Q + k * HDP + c0, v);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             v[e] *= p.scale;
@@ -1562,7 +1596,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   }
   if (warp == 1) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
-                 "r"(C::COLS_Q));
+                 "r"(C::COLS));
   }
 }
 
@@ -1579,10 +1613,10 @@ int kv_share(int group, int64_t ctas, int per_sm) {
 }
 
 template <typename... KArgs, typename... Args>
-cudaError_t launch_cluster(void (*kernel)(KArgs...), int grid, int cluster, int threads, size_t smem,
+cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, int cluster, int threads, size_t smem,
                            cudaStream_t s, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -1621,13 +1655,12 @@ cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
   });
   if (e != cudaSuccess) return e;
   TcParams2 p = tc_params(a);
-  const int64_t grid = static_cast<int64_t>(p.tiles) * a.Hq;
-  if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  p.share = kv_share(a.Hq / a.Hkv, static_cast<int64_t>(p.tiles) * a.Hkv, C::CTAS);
-  e = launch_k(attn_tc_bwd_q_kernel<DUAL, HDP>, dim3(static_cast<unsigned>(grid)), dim3(C::THREADS),
+  p.share = kv_share(p.G, static_cast<int64_t>(p.tiles) * a.Hkv, C::CTAS);
+  p.Gs = p.G / p.share;
+  e = launch_k(attn_tc_bwd_q_kernel<DUAL, HDP>, tile_grid(a.Hq, p.tiles), dim3(C::THREADS),
                C::SMEM_Q, s, qr[0], qr[1], qr[2], qr[3], ks[0], ks[1], ks[2], ks[3], p);
   if (e != cudaSuccess) return e;
-  return launch_cluster(attn_tc_bwd_kv_kernel<DUAL, HDP>, p.tiles * a.Hkv * p.share, p.share, C::THREADS,
+  return launch_cluster(attn_tc_bwd_kv_kernel<DUAL, HDP>, tile_grid(a.Hkv * p.share, p.tiles), p.share, C::THREADS,
                         C::SMEM_KV, s, kr[0], kr[1], kr[2], kr[3], qs[0], qs[1], qs[2], qs[3], p);
 }
 
