@@ -33,19 +33,35 @@ constexpr int TR = 128;                       // rows of a CTA's own tile (MMA M
 constexpr int ATOM128 = 128 * 128;            // bytes of [128 rows][64] bf16
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
-// MN-major operand of 64-column boxes of 128-byte rows, `box` bytes apart.
-__device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr, int box) {
-  return (sdesc_mn_sw128(saddr) & ~(0x3FFFull << 16)) | (static_cast<uint64_t>(box >> 4) << 16);
+// Shared-memory operands as the low words of their matrix descriptors (start address >> 4 and
+// leading byte offset >> 4; the high word is the same for all: 128-byte swizzle, 8-row groups of
+// 1024 bytes).  A byte offset moves a low word by offset >> 4.  Kept as 32-bit words: with 64-bit
+// descriptors moved by a ring's stage, nvcc 13.0 built products of the wrong columns.
+constexpr uint32_t DESC_HI = 0x40004040u;
+__device__ __forceinline__ uint32_t kdesc(uint32_t saddr) {        // K-major
+  return ((saddr & 0x3FFFFu) >> 4) | (1u << 16);
+}
+__device__ __forceinline__ uint32_t ndesc(uint32_t saddr, int box) {   // MN-major: 64-column boxes
+  return ((saddr & 0x3FFFFu) >> 4) | (static_cast<uint32_t>(box >> 4) << 16);
+}
+__device__ __forceinline__ uint64_t desc(uint32_t lo) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(DESC_HI));
+  return d;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                       uint32_t acc) {
+  mma_bf16(d, desc(a), desc(b), idesc, acc);
 }
 
 // D[tmem] (+)= A[tmem] B, A bf16: lane = row, two consecutive K elements a column.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bd, uint32_t idesc,
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
                                        uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(bd), "r"(idesc), "r"(acc));
+      "r"(a), "l"(desc(b)), "r"(idesc), "r"(acc));
 }
 
 __device__ __forceinline__ void tmem_st8(uint32_t t, const uint32_t* v) {
@@ -213,7 +229,6 @@ __device__ __forceinline__ uint32_t nan_pair(uint32_t w) {
 // and sets the bit of its row in bad[].  0 * x is zero for every finite x and NaN otherwise, so
 // one multiply-add a pair tells whether there is anything to do.
 __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32_t* bad, int lane) {
-  if (lane < 4) bad[lane] = 0;
   const __nv_bfloat162 z = __float2bfloat162_rn(0.f);
   __nv_bfloat162 acc = z;
   const uint4* p = reinterpret_cast<const uint4*>(base);
@@ -426,25 +441,25 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
     // ---- products -------------------------------------------------------------------------------
     constexpr uint32_t idS = idesc_bf16(TR, TK), idS2 = idesc_bf16(TR, 2 * TK);
     constexpr uint32_t idO = idesc_bf16(TR, HDP) | (1u << 16), idO2 = idesc_bf16(TR, 2 * HDP) | (1u << 16);
-    const uint64_t dQ = sdesc_sw128(smem_u32(sQ)), dQd = dQ + (NA * ATOM128 >> 4);
-    const uint64_t dKs = sdesc_sw128(smem_u32(sK)), mVs = sdesc_mn(smem_u32(sV), C::KATOM);
-    constexpr uint64_t ST = C::TILE_B >> 4;
+    const uint32_t dQ = kdesc(smem_u32(sQ)), dQd = dQ + (NA * ATOM128 >> 4);
+    const uint32_t dKs = kdesc(smem_u32(sK)), mVs = ndesc(smem_u32(sV), C::KATOM);
+    constexpr uint32_t ST = C::TILE_B >> 4;
     auto scores = [&](int j) -> bool {
       const int st = j % C::STAGES;
       if (!rwait(bb + B_K_FULL + 8 * st, (j / C::STAGES) & 1, p.status, abort)) return false;
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t dK = dKs + st * ST;
+        const uint32_t dK = dKs + st * ST;
 #pragma unroll
         for (int kk = 0; kk < HDP / 16; ++kk) {
-          const uint64_t qo = (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3);
-          const uint64_t ko = (kk >> 2) * (C::KATOM >> 4) + 2 * (kk & 3);
-          mma_bf16(tb + C::C_S, dQ + qo, dK + ko, DUAL ? idS2 : idS, kk > 0);
+          const uint32_t qo = (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3);
+          const uint32_t ko = (kk >> 2) * (C::KATOM >> 4) + 2 * (kk & 3);
+          mma_ss(tb + C::C_S, dQ + qo, dK + ko, DUAL ? idS2 : idS, kk > 0);
         }
         if (DUAL) {
 #pragma unroll
           for (int kk = 0; kk < HDP / 16; ++kk)
-            mma_bf16(tb + C::C_SD, dQd + 2 * kk, dK + 2 * kk, idS, 1);
+            mma_ss(tb + C::C_SD, dQd + 2 * kk, dK + 2 * kk, idS, 1);
         }
         mma_commit_addr(bb + B_S_FULL);
         mma_commit_addr(bb + B_K_EMPTY + 8 * st);
@@ -458,6 +473,8 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       const uint32_t ph = (j / C::STAGES) & 1;
       if (careful) {
         if (!rwait(bb + B_V_FULL + 8 * st, ph, p.status, abort)) break;
+        if (lane < 4) bad[st][lane] = 0;
+        __syncwarp();
         if (mixed(j)) scrub(sV + st * C::TILE_B, TK, C::NT * NA, bad[st], lane);
         if (lane == 0) bar_arrive(bb + B_V_CLEAN + 8 * st);
         __syncwarp();
@@ -466,7 +483,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>:
       if (!rwait(bb + B_P_FULL, j & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t mV = mVs + st * ST;
+        const uint32_t mV = mVs + st * ST;
 #pragma unroll
         for (int kk = 0; kk < TK / 16; ++kk) {
           const uint32_t acc = (j > 0 || kk > 0) ? 1u : 0u;
@@ -745,16 +762,26 @@ cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
 // Query-row kernel, per key tile:  dS as above, untransposed, over dP;  dQ += dS K,
 // dQ' += dS' K + dS K'.  dP has two buffers, so that S(j+1) and dP(j+1) run while the row warps
 // work on tile j.
+// Position in a ring of N stages: the stage and the parity of its phase.
+template <int N>
+struct Ring {
+  int st = 0;
+  uint32_t ph = 0;
+  __device__ __forceinline__ void next() {
+    if (++st == N) {
+      st = 0;
+      ph ^= 1;
+    }
+  }
+};
+
 template <bool DUAL, int HDP>
 struct BwdCfg {
   static constexpr int NA = HDP / 64;
   static constexpr int BT = HDP == 128 ? 128 : 64;         // streamed rows a tile
   static constexpr int NT = DUAL ? 2 : 1;
   static constexpr int CTAS = DUAL || HDP == 128 ? 1 : 2;
-#ifndef BWD_EW
-#define BWD_EW 8
-#endif
-  static constexpr int EW = CTAS == 1 ? BWD_EW : 8;            // row warps
+  static constexpr int EW = 8;                             // row warps
   static constexpr int THREADS = 96 + 32 * EW;             // loads, products, look-over, rows
   static constexpr int CW = BT * 4 / EW;                   // columns of a row thread
   static constexpr int OWN = (CW + 31) / 32;               // words of a bit a column
@@ -762,13 +789,18 @@ struct BwdCfg {
   static constexpr int RES1 = NT * NA * ATOM128;           // K (K') or V (V'); Q (Q') or dO (dO')
   static constexpr int BATOM = BT * 128;
   static constexpr int TILE_B = NT * NA * BATOM;           // one streamed operand with its tangent
-  static constexpr int STAGE_B = 2 * TILE_B;
-  static constexpr int STAGES = HDP == 128 ? 2 : DUAL ? 4 : 3;
+  // two rings: X is read to the end of a tile (Q, or K), Y only by its first products (dO, or V),
+  // so X needs a stage more to be loaded ahead
+  static constexpr int XS = HDP == 128 ? 3 : 5, YS = HDP == 128 ? 2 : 4;
   static constexpr int NSTAT = DUAL ? 4 : 2;               // -lse log2 e, -D (-rbar, -D')
   static constexpr int STAT_F = NSTAT * BT;
-  static constexpr int SMEM_Q = 2 * RES1 + STAGES * STAGE_B + 1024;
-  static constexpr int SMEM_KV = SMEM_Q + STAGES * STAT_F * 4;
-  static_assert(SMEM_KV + 1024 <= 227 * 1024, "a CTA's shared memory");
+  static constexpr int OPND_B = 2 * RES1 + XS * TILE_B + YS * TILE_B;
+  // the widest buffers leave no room to round their base up: it begins on a 1024-byte boundary
+  // (the declared alignment), which the kernels check
+  static constexpr int SLACK = HDP == 128 ? 0 : 1024;
+  static constexpr int SMEM_Q = OPND_B + SLACK;
+  static constexpr int SMEM_KV = OPND_B + 2 * STAT_F * 4 + SLACK;
+  static_assert(SMEM_KV + 1024 <= 227 * 1024 && SMEM_Q + 2048 <= 227 * 1024, "a CTA's shared memory");
   // TMEM: S (S'), dP (dP'), then the accumulators, tangents behind their primal
   static constexpr uint32_t C_S = 0, C_SD = BT, C_DP = NT * BT, C_DPD = C_DP + BT;
   static constexpr uint32_t C_A = 2 * NT * BT;             // dV (dV')
@@ -838,12 +870,14 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   // barriers, as byte offsets in a set; one set per walk
-  constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_DP_FULL = 16, B_P_FULL = 24, B_DS_FULL = 32, B_DRAIN = 40;
-  constexpr uint32_t B_ST_FULL = 48 + 0 * C::STAGES, B_ST_EMPTY = 48 + 8 * C::STAGES,
-      B_ST_CLEAN = 48 + 16 * C::STAGES;
-  constexpr int NBARS = 6 + 3 * C::STAGES;
+  // barriers, as byte offsets in a set; one set per walk
+  constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_DP_FULL = 16, B_P_FULL = 24, B_DS_FULL = 32,
+                     B_DRAIN = 40, B_CLEAN = 48, B_READ = 64;
+  constexpr uint32_t B_X_FULL = 80, B_X_EMPTY = B_X_FULL + 8 * C::XS, B_Y_FULL = B_X_EMPTY + 8 * C::XS,
+                     B_Y_EMPTY = B_Y_FULL + 8 * C::YS;
+  constexpr int NBARS = 10 + 2 * C::XS + 2 * C::YS;
   __shared__ __align__(8) uint64_t bars[2][NBARS];
-  __shared__ uint32_t bad[C::STAGES][4];
+  __shared__ uint32_t bad[2][4];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, redo_flag;
@@ -851,8 +885,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* sRes = smem;                        // K (K'), V (V')
-  uint8_t* sSt = smem + 2 * C::RES1;           // stage: Q (Q'), dO (dO')
-  float* sStat = reinterpret_cast<float*>(sSt + C::STAGES * C::STAGE_B);
+  uint8_t* sX = smem + 2 * C::RES1;            // Q (Q')
+  uint8_t* sY = sX + C::XS * C::TILE_B;        // dO (dO')
+  float* sStat = reinterpret_cast<float*>(sY + C::YS * C::TILE_B);   // two tiles' statistics
+  if (C::SLACK == 0 && smem != smem_raw) {     // the whole grid alike, before any barrier
+    if (threadIdx.x == 0 && p.status) atomicMax(p.status, DEV_SMEM_BASE);
+    return;
+  }
   // a cluster shares the query heads of a group; heads fastest; the first rows of a long
   // sequence (the longest walks) come first
   int rank, hk;
@@ -917,27 +956,36 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     if (elect_one()) {
       if (walk) load_rows(bb + B_RES_FULL);
       // ---- TMA producer ---------------------------------------------------------------------------
-      int issued = 0, t = 0, h = h0;
-      for (int i = 0; i < ntile; ++i) {
-        const int st = i % C::STAGES;
-        if (!twait(bb + B_ST_EMPTY + 8 * st, ((i / C::STAGES) & 1) ^ 1, p.status, abort)) break;
+      int n = 0, t = 0, h = h0;
+      Ring<C::XS> x;
+      Ring<C::YS> y;
+      for (; n < ntile; ++n) {
         const int qr = row0 + t * BT;
-        mbar_expect_tx_addr(bb + B_ST_FULL + 8 * st, C::STAGE_B);
-        uint8_t* b = sSt + st * C::STAGE_B;
+        if (!twait(bb + B_X_EMPTY + 8 * x.st, x.ph ^ 1, p.status, abort)) break;
+        // both or neither: the waits at the end count them together
+        if (!twait(bb + B_Y_EMPTY + 8 * y.st, y.ph ^ 1, p.status, abort)) break;
+        uint32_t b = smem_u32(sX + x.st * C::TILE_B), bar = bb + B_X_FULL + 8 * x.st;
+        mbar_expect_tx_addr(bar, C::TILE_B);
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_at<false>(smem_u32(b + a * C::BATOM), &tmQ, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
-          tma_load_at<false>(smem_u32(b + C::TILE_B + a * C::BATOM), &tmO, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
-          if (DUAL) {
-            tma_load_at<false>(smem_u32(b + (NA + a) * C::BATOM), &tmQd, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
-            tma_load_at<false>(smem_u32(b + C::TILE_B + (NA + a) * C::BATOM), &tmOd, bb + B_ST_FULL + 8 * st, 64 * a, qr, h);
-          }
+          tma_load_at<false>(b + a * C::BATOM, &tmQ, bar, 64 * a, qr, h);
+          if (DUAL) tma_load_at<false>(b + (NA + a) * C::BATOM, &tmQd, bar, 64 * a, qr, h);
         }
-        ++issued;
+        b = smem_u32(sY + y.st * C::TILE_B);
+        bar = bb + B_Y_FULL + 8 * y.st;
+        mbar_expect_tx_addr(bar, C::TILE_B);
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+          tma_load_at<false>(b + a * C::BATOM, &tmO, bar, 64 * a, qr, h);
+          if (DUAL) tma_load_at<false>(b + (NA + a) * C::BATOM, &tmOd, bar, 64 * a, qr, h);
+        }
+        x.next();
+        y.next();
         if (++t == nqt) { t = 0; ++h; }
       }
       mbar_wait_addr(bb + B_RES_FULL, 0, p.status, FTC_WAIT_NS);
-      drain_ring(bb + B_ST_FULL, issued, C::STAGES, p.status);
+      drain_ring(bb + B_X_FULL, n, C::XS, p.status);
+      drain_ring(bb + B_Y_FULL, n, C::YS, p.status);
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -959,43 +1007,58 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     };
     int t = 0, h = h0;
     read(0, h0);
+    Ring<C::XS> x;
+    Ring<C::YS> y;
     for (int i = 0; i < ntile; ++i) {
-      const int st = i % C::STAGES;
+      const int sl = i & 1;
       const bool mx = mixed(t);
-      if (!rwait(bb + B_ST_FULL + 8 * st, (i / C::STAGES) & 1, p.status, abort)) break;
-      float* sst = sStat + st * C::STAT_F;
+      // the row warps are done with the tile before the last one
+      if (!rwait(bb + B_READ + 8 * sl, ((i >> 1) & 1) ^ 1, p.status, abort)) break;
+      float* sst = sStat + sl * C::STAT_F;
 #pragma unroll
       for (int k = 0; k < C::NSTAT; ++k)
 #pragma unroll
         for (int e = 0; e < BT / 32; ++e) sst[k * BT + 32 * e + lane] = v[k][e];
       if (++t == nqt) { t = 0; ++h; }
       if (i + 1 < ntile) read(t, h);
-      if (careful && mx) scrub(sSt + st * C::STAGE_B, BT, 2 * C::NT * NA, bad[st], lane);
+      if (careful) {
+        if (!rwait(bb + B_X_FULL + 8 * x.st, x.ph, p.status, abort)) break;
+        if (!rwait(bb + B_Y_FULL + 8 * y.st, y.ph, p.status, abort)) break;
+        if (mx) {
+          if (lane < 4) bad[sl][lane] = 0;
+          __syncwarp();
+          scrub(sX + x.st * C::TILE_B, BT, C::NT * NA, bad[sl], lane);
+          scrub(sY + y.st * C::TILE_B, BT, C::NT * NA, bad[sl], lane);
+        }
+        x.next();
+        y.next();
+      }
       __syncwarp();
-      if (lane == 0) bar_arrive(bb + B_ST_CLEAN + 8 * st);
+      if (lane == 0) bar_arrive(bb + B_CLEAN + 8 * sl);
     }
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
     constexpr uint32_t idS = idesc_bf16(TR, BT), idS2 = idesc_bf16(TR, 2 * BT);
     constexpr uint32_t idA = idesc_bf16(TR, HDP) | (1u << 16), idA2 = idesc_bf16(TR, 2 * HDP) | (1u << 16);
-    const uint64_t dK = sdesc_sw128(smem_u32(sRes)), dV = dK + (C::RES1 >> 4);
-    constexpr uint64_t RD = NA * ATOM128 >> 4;            // a resident operand's tangent
-    const uint64_t kSt = sdesc_sw128(smem_u32(sSt)), mSt = sdesc_mn(smem_u32(sSt), C::BATOM);
-    constexpr uint64_t ST = C::STAGE_B >> 4, DO = C::TILE_B >> 4;
+    const uint32_t dK = kdesc(smem_u32(sRes)), dV = dK + (C::RES1 >> 4);
+    constexpr uint32_t RD = NA * ATOM128 >> 4;            // a resident operand's tangent
+    const uint32_t kX = kdesc(smem_u32(sX)), mX = ndesc(smem_u32(sX), C::BATOM);
+    const uint32_t kY = kdesc(smem_u32(sY)), mY = ndesc(smem_u32(sY), C::BATOM);
+    constexpr uint32_t ST = C::TILE_B >> 4;
     // X Y^T into column c (and the tangent's next to it)
-    auto score = [&](uint64_t x, uint64_t y, uint32_t c) {
+    auto score = [&](uint32_t x, uint32_t y, uint32_t c) {
 #pragma unroll
       for (int kk = 0; kk < HDP / 16; ++kk)
-        mma_bf16(tb + c, x + (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3),
+        mma_ss(tb + c, x + (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3),
                  y + (kk >> 2) * (C::BATOM >> 4) + 2 * (kk & 3), DUAL ? idS2 : idS, kk > 0);
       if (DUAL) {
 #pragma unroll
         for (int kk = 0; kk < HDP / 16; ++kk)
-          mma_bf16(tb + c + BT, x + RD + 2 * kk, y + 2 * kk, idS, 1);
+          mma_ss(tb + c + BT, x + RD + 2 * kk, y + 2 * kk, idS, 1);
       }
     };
     // acc += A^T-rows (TMEM columns a, tangent a + BT) times streamed rows y
-    auto accum = [&](uint32_t c, uint32_t a, uint64_t y, bool first) {
+    auto accum = [&](uint32_t c, uint32_t a, uint32_t y, bool first) {
 #pragma unroll
       for (int kk = 0; kk < BT / 16; ++kk) {
         // the two threads of a row keep their halves apart
@@ -1005,45 +1068,54 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
         if (DUAL) mma_ts(tb + c + HDP, tb + ac + BT, y + 128 * kk, idA, 1);
       }
     };
-    auto ready = [&](int i) {
-      return rwait(bb + B_ST_CLEAN + 8 * (i % C::STAGES), (i / C::STAGES) & 1, p.status, abort);
-    };
-    bool ok = rwait(bb + B_RES_FULL, 0, p.status, abort) && ready(0);
-    if (ok) {
+    Ring<C::XS> x, xd;      // of the tile whose scores are next, and of the one being added up
+    Ring<C::YS> y, yd;
+    // S of tile i, and dP
+    auto s_scores = [&](int i) -> bool {
+      if (careful && !rwait(bb + B_CLEAN + 8 * (i & 1), (i >> 1) & 1, p.status, abort)) return false;
+      if (!rwait(bb + B_X_FULL + 8 * x.st, x.ph, p.status, abort)) return false;
       tc_fence_after();
       if (elect_one()) {
-        score(dK, kSt, C::C_S);
+        score(dK, kX + x.st * ST, C::C_S);
         mma_commit_addr(bb + B_S_FULL);
-        score(dV, kSt + DO, C::C_DP);
+      }
+      __syncwarp();
+      x.next();
+      return true;
+    };
+    auto p_scores = [&]() -> bool {
+      if (!rwait(bb + B_Y_FULL + 8 * y.st, y.ph, p.status, abort)) return false;
+      tc_fence_after();
+      if (elect_one()) {
+        score(dV, kY + y.st * ST, C::C_DP);
         mma_commit_addr(bb + B_DP_FULL);
       }
       __syncwarp();
-    }
+      y.next();
+      return true;
+    };
+    bool ok = rwait(bb + B_RES_FULL, 0, p.status, abort) && s_scores(0) && p_scores();
     for (int i = 0; ok && i < ntile; ++i) {
-      const int st = i % C::STAGES, sn = (i + 1) % C::STAGES;
       const bool more = i + 1 < ntile;
-      if (more && !ready(i + 1)) break;
       if (!rwait(bb + B_P_FULL, i & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
-        accum(C::C_A, C::C_S, mSt + st * ST + DO, i == 0);
-        if (more) {
-          score(dK, kSt + sn * ST, C::C_S);
-          mma_commit_addr(bb + B_S_FULL);
-        }
+        accum(C::C_A, C::C_S, mY + yd.st * ST, i == 0);
+        mma_commit_addr(bb + B_Y_EMPTY + 8 * yd.st);
       }
       __syncwarp();
+      yd.next();
+      if (more && !s_scores(i + 1)) break;
       if (!rwait(bb + B_DS_FULL, i & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
-        accum(C::C_B, C::C_DP, mSt + st * ST, i == 0);
-        mma_commit_addr(bb + B_ST_EMPTY + 8 * st);
-        if (more) {
-          score(dV, kSt + sn * ST + DO, C::C_DP);
-          mma_commit_addr(bb + B_DP_FULL);
-        }
+        accum(C::C_B, C::C_DP, mX + xd.st * ST, i == 0);
+        mma_commit_addr(bb + B_X_EMPTY + 8 * xd.st);
+        bar_arrive(bb + B_READ + 8 * (i & 1));
       }
       __syncwarp();
+      xd.next();
+      if (more && !p_scores()) break;
     }
     if (elect_one()) mma_commit_addr(bb + B_DRAIN);
     __syncwarp();
@@ -1059,22 +1131,22 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     bool ok = true;
     int t = 0;
     for (int i = 0; i < ntile; ++i) {
-      const int st = i % C::STAGES;
-      const uint32_t ph = (i / C::STAGES) & 1;
+      const int sl = i & 1;
       const bool mx = mixed(t);
       // columns a .. b - 1 (of the tile) attend to this key
       const int a = r - t * BT, b = hi - (row0 + t * BT);
       if (++t == nqt) t = 0;
-      if (!rwait(bb + B_ST_CLEAN + 8 * st, ph, p.status, abort)) { ok = false; break; }   // the statistics
+      // the statistics
+      if (!rwait(bb + B_CLEAN + 8 * sl, (i >> 1) & 1, p.status, abort)) { ok = false; break; }
       uint32_t own[C::OWN], bads[C::OWN] = {};   // the row's own columns, the noted ones of them
       if (mx) {
 #pragma unroll
         for (int w = 0; w < C::OWN; ++w) {
           own[w] = col_bits(a - cb - 32 * w, b - 1 - cb - 32 * w);
-          if (careful) bads[w] = own[w] & (bad[st][(cb >> 5) + w] >> (cb & 31));
+          if (careful) bads[w] = own[w] & (bad[sl][(cb >> 5) + w] >> (cb & 31));
         }
       }
-      const float4* stat = reinterpret_cast<const float4*>(sStat + st * C::STAT_F + cb);
+      const float4* stat = reinterpret_cast<const float4*>(sStat + sl * C::STAT_F + cb);
       if (!rwait(bb + B_S_FULL, i & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       float pr[CW], pd[DUAL ? CW : 1];
@@ -1277,12 +1349,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   // barriers, as byte offsets in a set; one set per walk
-  constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_S_FREE = 16, B_DP_FULL = 24, B_DS_FULL = 32, B_DRAIN = 40;
-  constexpr uint32_t B_ST_FULL = 48 + 0 * C::STAGES, B_ST_EMPTY = 48 + 8 * C::STAGES,
-      B_ST_CLEAN = 48 + 16 * C::STAGES;
-  constexpr int NBARS = 6 + 3 * C::STAGES;
+  // barriers, as byte offsets in a set; one set per walk
+  constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_S_FREE = 16, B_DRAIN = 24;
+  // one for each buffer of dP: the next tile's phase may be complete before somebody has come to
+  // wait for this one's, and a barrier tells only two phases apart
+  constexpr uint32_t B_DP_FULL = 32, B_DS_FULL = 48;
+  constexpr uint32_t B_X_FULL = 64, B_X_EMPTY = B_X_FULL + 8 * C::XS, B_CLEAN = B_X_EMPTY + 8 * C::XS,
+                     B_Y_FULL = B_CLEAN + 8 * C::XS, B_Y_EMPTY = B_Y_FULL + 8 * C::YS;
+  constexpr int NBARS = 8 + 3 * C::XS + 2 * C::YS;
   __shared__ __align__(8) uint64_t bars[2][NBARS];
-  __shared__ uint32_t bad[C::STAGES][4];
+  __shared__ uint32_t bad[C::XS][4];
   __shared__ float2 sD[TR];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
@@ -1291,7 +1367,12 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* sRes = smem;                        // Q (Q'), dO (dO')
-  uint8_t* sSt = smem + 2 * C::RES1;           // stage: K (K'), V (V')
+  uint8_t* sX = smem + 2 * C::RES1;            // K (K')
+  uint8_t* sY = sX + C::XS * C::TILE_B;        // V (V')
+  if (C::SLACK == 0 && smem != smem_raw) {     // the whole grid alike, before any barrier
+    if (threadIdx.x == 0 && p.status) atomicMax(p.status, DEV_SMEM_BASE);
+    return;
+  }
   const int h = static_cast<int>(blockIdx.x), tile = tile_index();
   if (tile >= p.tiles) return;
   const int row0 = (p.tiles - 1 - tile) * TR;
@@ -1318,7 +1399,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   // a barrier a thread; the first thread's own is the one that its loads complete
   if (threadIdx.x < 2 * NBARS) {
     const uint32_t b = threadIdx.x % NBARS;
-    bar_init(smem_u32(&bars[0][0]) + 8 * threadIdx.x, 8 * b == B_S_FREE || 8 * b == B_DS_FULL ? C::EW : 1);
+    bar_init(smem_u32(&bars[0][0]) + 8 * threadIdx.x, 8 * b == B_S_FREE || (8 * b & ~8u) == B_DS_FULL ? C::EW : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (threadIdx.x == 0) {
@@ -1349,83 +1430,101 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     if (elect_one()) {
       if (walk) load_rows(bb + B_RES_FULL);
       // ---- TMA producer ---------------------------------------------------------------------------
-      int issued = 0;
-      for (int j = 0; j < nkt; ++j) {
-        const int st = j % C::STAGES;
-        if (!twait(bb + B_ST_EMPTY + 8 * st, ((j / C::STAGES) & 1) ^ 1, p.status, abort)) break;
-        mbar_expect_tx_addr(bb + B_ST_FULL + 8 * st, C::STAGE_B);
-        uint8_t* b = sSt + st * C::STAGE_B;
-        const int kr = k0 + j * BT;
+      int n = 0;
+      Ring<C::XS> x;
+      Ring<C::YS> y;
+      for (; n < nkt; ++n) {
+        const int kr = k0 + n * BT;
+        if (!twait(bb + B_X_EMPTY + 8 * x.st, x.ph ^ 1, p.status, abort)) break;
+        // both or neither: the waits at the end count them together
+        if (!twait(bb + B_Y_EMPTY + 8 * y.st, y.ph ^ 1, p.status, abort)) break;
+        uint32_t b = smem_u32(sX + x.st * C::TILE_B), bar = bb + B_X_FULL + 8 * x.st;
+        mbar_expect_tx_addr(bar, C::TILE_B);
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-          tma_load_at<false>(smem_u32(b + a * C::BATOM), &tmK, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
-          tma_load_at<false>(smem_u32(b + C::TILE_B + a * C::BATOM), &tmV, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
-          if (DUAL) {
-            tma_load_at<false>(smem_u32(b + (NA + a) * C::BATOM), &tmKd, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
-            tma_load_at<false>(smem_u32(b + C::TILE_B + (NA + a) * C::BATOM), &tmVd, bb + B_ST_FULL + 8 * st, 64 * a, kr, hk);
-          }
+          tma_load_at<false>(b + a * C::BATOM, &tmK, bar, 64 * a, kr, hk);
+          if (DUAL) tma_load_at<false>(b + (NA + a) * C::BATOM, &tmKd, bar, 64 * a, kr, hk);
         }
-        ++issued;
+        b = smem_u32(sY + y.st * C::TILE_B);
+        bar = bb + B_Y_FULL + 8 * y.st;
+        mbar_expect_tx_addr(bar, C::TILE_B);
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+          tma_load_at<false>(b + a * C::BATOM, &tmV, bar, 64 * a, kr, hk);
+          if (DUAL) tma_load_at<false>(b + (NA + a) * C::BATOM, &tmVd, bar, 64 * a, kr, hk);
+        }
+        x.next();
+        y.next();
       }
       mbar_wait_addr(bb + B_RES_FULL, 0, p.status, FTC_WAIT_NS);
-      drain_ring(bb + B_ST_FULL, issued, C::STAGES, p.status);
+      drain_ring(bb + B_X_FULL, n, C::XS, p.status);
+      drain_ring(bb + B_Y_FULL, n, C::YS, p.status);
     }
     __syncwarp();
   } else if (warp == 2) {
     // ---- look-over of mixed tiles: K (K') multiplies dS; V (V') only meets dO, whose product with a
     // masked key is dropped
-    for (int j = 0; j < nkt; ++j) {
-      const int st = j % C::STAGES;
-      if (!rwait(bb + B_ST_FULL + 8 * st, (j / C::STAGES) & 1, p.status, abort)) break;
-      if (careful && mixed(j)) scrub(sSt + st * C::STAGE_B, BT, C::NT * NA, bad[st], lane);
-      if (lane == 0) bar_arrive(bb + B_ST_CLEAN + 8 * st);
+    Ring<C::XS> x;
+    for (int j = 0; careful && j < nkt; ++j) {
+      if (!rwait(bb + B_X_FULL + 8 * x.st, x.ph, p.status, abort)) break;
+      if (lane < 4) bad[x.st][lane] = 0;
+      __syncwarp();
+      if (mixed(j)) scrub(sX + x.st * C::TILE_B, BT, C::NT * NA, bad[x.st], lane);
+      if (lane == 0) bar_arrive(bb + B_CLEAN + 8 * x.st);
+      x.next();
     }
   } else if (warp == 1) {
     // ---- products ------------------------------------------------------------------------------------
     constexpr uint32_t idS = idesc_bf16(TR, BT), idS2 = idesc_bf16(TR, 2 * BT);
     constexpr uint32_t idA = idesc_bf16(TR, HDP) | (1u << 16), idA2 = idesc_bf16(TR, 2 * HDP) | (1u << 16);
-    const uint64_t dQ = sdesc_sw128(smem_u32(sRes)), dO = dQ + (C::RES1 >> 4);
-    constexpr uint64_t RD = NA * ATOM128 >> 4;
-    const uint64_t kSt = sdesc_sw128(smem_u32(sSt)), mSt = sdesc_mn(smem_u32(sSt), C::BATOM);
-    constexpr uint64_t ST = C::STAGE_B >> 4, VO = C::TILE_B >> 4;
-    auto score = [&](uint64_t x, uint64_t y, uint32_t c) {
+    const uint32_t dQ = kdesc(smem_u32(sRes)), dO = dQ + (C::RES1 >> 4);
+    constexpr uint32_t RD = NA * ATOM128 >> 4;
+    const uint32_t kX = kdesc(smem_u32(sX)), mX = ndesc(smem_u32(sX), C::BATOM);
+    const uint32_t kY = kdesc(smem_u32(sY));
+    constexpr uint32_t ST = C::TILE_B >> 4;
+    auto score = [&](uint32_t x, uint32_t y, uint32_t c) {
 #pragma unroll
       for (int kk = 0; kk < HDP / 16; ++kk)
-        mma_bf16(tb + c, x + (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3),
+        mma_ss(tb + c, x + (kk >> 2) * (ATOM128 >> 4) + 2 * (kk & 3),
                  y + (kk >> 2) * (C::BATOM >> 4) + 2 * (kk & 3), DUAL ? idS2 : idS, kk > 0);
       if (DUAL) {
 #pragma unroll
         for (int kk = 0; kk < HDP / 16; ++kk)
-          mma_bf16(tb + c + BT, x + RD + 2 * kk, y + 2 * kk, idS, 1);
+          mma_ss(tb + c + BT, x + RD + 2 * kk, y + 2 * kk, idS, 1);
       }
     };
-    auto ready = [&](int j) {
-      return rwait(bb + B_ST_CLEAN + 8 * (j % C::STAGES), (j / C::STAGES) & 1, p.status, abort);
-    };
+    Ring<C::XS> x, xd;      // of the tile whose scores are next, and of the one being added up
+    Ring<C::YS> y;
     // the scores of tile j, ahead of its dP: S waits until the row warps have read the last one
     auto scores = [&](int j) -> bool {
-      if (!ready(j)) return false;
+      if (!rwait(bb + (careful ? B_CLEAN : B_X_FULL) + 8 * x.st, x.ph, p.status, abort)) return false;
       if (j > 0 && !rwait(bb + B_S_FREE, (j - 1) & 1, p.status, abort)) return false;
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t k = kSt + (j % C::STAGES) * ST;
-        score(dQ, k, C::C_S);
+        score(dQ, kX + x.st * ST, C::C_S);
         mma_commit_addr(bb + B_S_FULL);
-        // buffer j & 1 held dS of tile j - 2, whose product has been issued
-        score(dO, k + VO, C::C_DP + (j & 1) * C::DP_STEP);
-        mma_commit_addr(bb + B_DP_FULL);
       }
       __syncwarp();
+      if (!rwait(bb + B_Y_FULL + 8 * y.st, y.ph, p.status, abort)) return false;
+      tc_fence_after();
+      if (elect_one()) {
+        // buffer j & 1 held dS of tile j - 2, whose product has been issued
+        score(dO, kY + y.st * ST, C::C_DP + (j & 1) * C::DP_STEP);
+        mma_commit_addr(bb + B_DP_FULL + 8 * (j & 1));
+        mma_commit_addr(bb + B_Y_EMPTY + 8 * y.st);
+      }
+      __syncwarp();
+      x.next();
+      y.next();
       return true;
     };
     bool ok = rwait(bb + B_RES_FULL, 0, p.status, abort) && scores(0);
     for (int j = 0; ok && j < nkt; ++j) {
-      const int st = j % C::STAGES;
       if (j + 1 < nkt && !scores(j + 1)) break;
-      if (!rwait(bb + B_DS_FULL, j & 1, p.status, abort)) break;
+      if (!rwait(bb + B_DS_FULL + 8 * (j & 1), (j >> 1) & 1, p.status, abort)) break;
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t mK = mSt + st * ST;
+        const uint32_t mK = mX + xd.st * ST;
         const uint32_t a = tb + C::C_DP + (j & 1) * C::DP_STEP;
 #pragma unroll
         for (int kk = 0; kk < BT / 16; ++kk) {
@@ -1434,9 +1533,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           mma_ts(tb + C::C_Q, ac, mK + 128 * kk, DUAL ? idA2 : idA, acc);
           if (DUAL) mma_ts(tb + C::C_Q + HDP, ac + BT, mK + 128 * kk, idA, 1);
         }
-        mma_commit_addr(bb + B_ST_EMPTY + 8 * st);
+        mma_commit_addr(bb + B_X_EMPTY + 8 * xd.st);
       }
       __syncwarp();
+      xd.next();
     }
     if (elect_one()) mma_commit_addr(bb + B_DRAIN);
     __syncwarp();
@@ -1462,20 +1562,20 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     const uint64_t c2p = pair(p.c2, p.c2), nl = pair(-lse2, -lse2), nD = pair(-Dv, -Dv);
     const uint64_t nr = pair(-rb, -rb), nDd = pair(-Dd, -Dd), sc = pair(p.scale, p.scale);
     bool ok = true;
-    for (int j = 0; j < nkt; ++j) {
-      const int st = j % C::STAGES;
+    Ring<C::XS> x;
+    for (int j = 0; j < nkt; ++j, x.next()) {
       const bool mx = mixed(j);
       const int a = lo - (k0 + j * BT), b = row0 + r - (k0 + j * BT);
       uint32_t own[C::OWN], bads[C::OWN] = {};   // the row's own columns, the noted ones of them
       if (mx) {
-        if (careful && !rwait(bb + B_ST_CLEAN + 8 * st, (j / C::STAGES) & 1, p.status, abort)) {
+        if (careful && !rwait(bb + B_CLEAN + 8 * x.st, x.ph, p.status, abort)) {
           ok = false;
           break;
         }
 #pragma unroll
         for (int w = 0; w < C::OWN; ++w) {
           own[w] = col_bits(a - cb - 32 * w, b - cb - 32 * w);
-          if (careful) bads[w] = own[w] & (bad[st][(cb >> 5) + w] >> (cb & 31));
+          if (careful) bads[w] = own[w] & (bad[x.st][(cb >> 5) + w] >> (cb & 31));
         }
       }
       if (!rwait(bb + B_S_FULL, j & 1, p.status, abort)) { ok = false; break; }
@@ -1510,7 +1610,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tc_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive(bb + B_S_FREE);
-      if (!rwait(bb + B_DP_FULL, j & 1, p.status, abort)) { ok = false; break; }
+      if (!rwait(bb + B_DP_FULL + 8 * (j & 1), (j >> 1) & 1, p.status, abort)) { ok = false; break; }
       tc_fence_after();
       const uint32_t aP = lane_base + C::C_DP + (j & 1) * C::DP_STEP;
       auto scores = [&](auto masked) {
@@ -1557,7 +1657,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(bb + B_DS_FULL);
+      if (lane == 0) bar_arrive(bb + B_DS_FULL + 8 * (j & 1));
     }
     if (ok && rwait(bb + B_DRAIN, 0, p.status, abort) && !*abort) {
       tc_fence_after();
