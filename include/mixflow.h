@@ -454,6 +454,7 @@ typedef struct {
  *   dy_ = R(p)^T dy,  dg = sum dy_ x r,  dx = r a - r^3 x mean(x a) with a = g dy_.
  *  work     mf_qk_rope_work_bytes() bytes on a 16-byte boundary, needed with gains; its
  *           contents need not be kept.  Calls that overlap in time need one each.
+ *  status   as for mf_attn_fwd.
  * Errors: MF_ERR_INVALID_ARG, MF_ERR_UNSUPPORTED (a type pair not listed), MF_ERR_CUDA. */
 typedef struct {
   int64_t n_rows;
@@ -476,6 +477,7 @@ typedef struct {
   float *dgq, *dgk, *dgqd, *dgkd;
   void* work;
   size_t work_bytes;
+  int32_t* status;
 } mf_qk_rope_args;
 
 mf_status mf_qk_rope_fwd(const mf_qk_rope_args* args, void* stream);

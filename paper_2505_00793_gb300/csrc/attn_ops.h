@@ -15,8 +15,8 @@ struct SeqRows {
   int n = 0, len = 0, rows = 0;
 };
 
-// Blocks of a head-norm launch (four per SM), which bounds its partial sums.
-constexpr int kRopeMaxBlocks = 4 * 152;
+// Blocks of a head-norm launch (two per SM), which bounds its partial sums.
+constexpr int kRopeMaxBlocks = 2 * 152;
 
 struct RopeParams {
   SeqRows seq;
@@ -33,9 +33,14 @@ struct RopeParams {
   float *dgq = nullptr, *dgk = nullptr, *dgqd = nullptr, *dgkd = nullptr;
   float* part = nullptr;                // [blocks][2 or 4][D] partial gain gradients
   const int* pos = nullptr;
-  // set by qk_rope: lanes a head takes, parts a row is cut into, vector access
-  int lanes = 1, chunks = 1;
+  int* status = nullptr;
+  // set by qk_rope: lanes a head takes, vector access; heads of a part of a row, the parts, units of
+  // work a row is split into and the parts of each; a warp's next unit; shared memory
+  int lanes = 1;
   bool vec = false;
+  int hc = 1, parts = 1, splits = 1, run = 1;
+  int step_row = 0, step_split = 0;
+  int stage_bytes = 0, ring_bytes = 0;
   uint64_t phase[64];                   // 2^-64 turns a position, per rotated pair
 };
 cudaError_t qk_rope(RopeParams p, bool bwd, bool x_bf16, bool y_bf16, cudaStream_t s);

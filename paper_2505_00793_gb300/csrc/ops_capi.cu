@@ -121,6 +121,7 @@ mf_status rope_params(const mf_qk_rope_args& a, RopeParams* p) {
   p->x = a.x; p->xd = a.xd; p->ldx = a.ldx;
   p->gq = a.gq; p->gk = a.gk; p->gqd = a.gqd; p->gkd = a.gkd;
   p->pos = a.pos;
+  p->status = a.status;
   return MF_OK;
 }
 

@@ -8,22 +8,31 @@
 //   dx' = r' a + r a' - (3 r^2 r' m + r^3 m') x - r^3 m x',
 //         a' = g' dy + g dy',  m' = mean(x' a + x a'),  dg' = sum dy' x r + dy (x' r + x r')
 //
-// Layout: a warp walks the heads of one row.  A head is cut into units of eight elements, one
-// unit a lane, so that both elements of every rotated pair are in one lane: in the half layout
-// a rotated unit is four elements of the first half and their four partners, else eight
-// neighbours.  A lane keeps its unit for every head of the row, so each pair's cos and sin are
-// computed once a row, in registers, and no table is read.  A head takes the next power of two
-// of lanes, and the sums over a head are shuffles.
+// Layout.  A head is cut into units of eight elements, one a lane, so that both elements of every
+// rotated pair are in one lane: in the half layout a rotated unit is four elements of the first
+// half and their four partners, else eight neighbours.  A head takes the next power of two of
+// lanes, and sums over a head are shuffles.
+//
+// What bounds it is memory.  Every warp reads ahead of its arithmetic by itself: it copies parts of
+// rows into a ring of its own in shared memory (bulk copies, two stages), so that what is in flight
+// does not depend on registers, and meets no other warp.  Plain loads left the memory idle two
+// thirds of the time; a ring for a whole block cost more in barriers than the heads in arithmetic.
+// The cos and sin of a row's position are computed a pair a lane and kept in registers for all its
+// heads.
 #include "attn_ops.h"
 #include "device_math.cuh"
 #include "launch.cuh"
 #include "packed_rows.cuh"
+#include "pair_math.cuh"
 
 namespace mf {
 namespace {
 
-constexpr int kRopeThreads = 256;
-constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kRopeWarps = 8;
+constexpr int kRopeThreads = 32 * kRopeWarps;
+constexpr int kRopeStages = 2;
+constexpr int kRopeStage = 6 * 1024;                   // bytes of a stage (at most), two a warp
+constexpr int kRopeRing = kRopeWarps * (kRopeStages * kRopeStage + 512);   // of a block, two an SM
 
 // cos and sin of pos * phase, phase in units of 2^-64 turns: the product modulo 2^64 is the
 // angle modulo a turn, exactly, so a far position loses nothing.  The nearest quarter turn is
@@ -39,11 +48,11 @@ __device__ __forceinline__ void turn_cos_sin(int pos, uint64_t phase, float& c, 
   s = (quad & 2) ? -y : y;
 }
 
-// A lane's unit of a head: four pairs (a, b) of elements.
+// A lane's unit of a head: four pairs of elements.
 struct Unit {
-  int oa, ob;      // first element of a and of b (vector form)
+  int oa, ob;      // first elements of its two fours (vector form)
   int u;           // rotated units: first pair is 4 u; others: place 8 u behind the rotated part
-  bool on, rot, mix;   // in use; rotated; a and b alternate in memory
+  bool on, rot;    // in use; rotated
 };
 
 __device__ __forceinline__ Unit make_unit(const RopeParams& p, int lane) {
@@ -53,7 +62,6 @@ __device__ __forceinline__ Unit make_unit(const RopeParams& p, int lane) {
   t.rot = u < nrot;
   t.u = t.rot ? u : u - nrot;
   t.on = t.rot || p.R + 8 * t.u < p.D;
-  t.mix = t.rot && !p.half;
   t.oa = t.rot ? (p.half ? 4 * t.u : 8 * t.u) : p.R + 8 * t.u;
   t.ob = t.rot && p.half ? p.R / 2 + 4 * t.u : t.oa + 4;
   return t;
@@ -71,372 +79,623 @@ __device__ __forceinline__ int unit_elem(const RopeParams& p, const Unit& t, int
   return i < p.D ? i : -1;
 }
 
-__device__ __forceinline__ void load4(const float* s, float (&v)[4]) {
+__device__ __forceinline__ void load4(const float* s, uint64_t& a, uint64_t& b) {
   const float4 f = *reinterpret_cast<const float4*>(s);
-  v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  a = pair(f.x, f.y);
+  b = pair(f.z, f.w);
 }
-__device__ __forceinline__ void load4(const __nv_bfloat16* s, float (&v)[4]) {
+__device__ __forceinline__ void load4(const __nv_bfloat16* s, uint64_t& a, uint64_t& b) {
   const uint2 w = *reinterpret_cast<const uint2*>(s);
-  v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
-  v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+  a = pair(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u));
+  b = pair(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
 }
-__device__ __forceinline__ void store4(float* d, const float (&v)[4]) {
-  *reinterpret_cast<float4*>(d) = make_float4(v[0], v[1], v[2], v[3]);
+__device__ __forceinline__ void store4(float* d, uint64_t a, uint64_t b) {
+  const float2 x = halves(a), y = halves(b);
+  *reinterpret_cast<float4*>(d) = make_float4(x.x, x.y, y.x, y.y);
 }
-__device__ __forceinline__ void store4(__nv_bfloat16* d, const float (&v)[4]) {
-  const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+__device__ __forceinline__ void store4(__nv_bfloat16* d, uint64_t a, uint64_t b) {
+  const float2 x = halves(a), y = halves(b);
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(y.x, y.y);
   *reinterpret_cast<uint2*>(d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo),
                                             *reinterpret_cast<const uint32_t*>(&hi));
 }
 __device__ __forceinline__ float as_f(float x) { return x; }
 __device__ __forceinline__ float as_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// A unit's pairs from and to one head.  Rotated parts of whole eights move as vectors (p.vec),
-// others element by element.
-template <typename T>
+// A unit's eight elements from and to one head as four pairs, in memory order: v[0], v[1] from oa
+// on, v[2], v[3] from ob on.  Units of whole eights move as vectors (VEC), others element by
+// element, then in pair order (element e of the pair in v[e / 2], its partner in v[2 + e / 2]).
+template <bool VEC, typename T>
 __device__ __forceinline__ void load_unit(const RopeParams& p, const Unit& t, bool on, const T* h,
-                                          float (&a)[4], float (&b)[4]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) a[e] = b[e] = 0.f;
-  if (!on) return;
-  if (p.vec) {
-    load4(h + t.oa, a);
-    load4(h + t.ob, b);
-    if (t.mix) {
-      const float a1 = a[1], a3 = a[3], b0 = b[0], b2 = b[2];
-      a[1] = a[2]; a[2] = b0; a[3] = b2;
-      b[2] = b[1]; b[0] = a1; b[1] = a3;
+                                          uint64_t (&v)[4]) {
+  if (VEC) {
+    if (on) {
+      load4(h + t.oa, v[0], v[1]);
+      load4(h + t.ob, v[2], v[3]);
     }
   } else {
+    float f[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = unit_elem(p, t, 0, e), j = unit_elem(p, t, 1, e);
-      if (i >= 0) a[e] = as_f(h[i]);
-      if (j >= 0) b[e] = as_f(h[j]);
+    for (int e = 0; e < 8; ++e) {
+      const int i = unit_elem(p, t, e >> 2, e & 3);
+      f[e] = on && i >= 0 ? as_f(h[i]) : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = pair(f[2 * e], f[2 * e + 1]);
   }
 }
-template <typename T>
-__device__ __forceinline__ void store_unit(const RopeParams& p, const Unit& t, bool on, T* h,
-                                           const float (&a)[4], const float (&b)[4]) {
-  if (!on) return;
-  if (p.vec) {
-    if (t.mix) {
-      const float lo[4] = {a[0], b[0], a[1], b[1]}, hi[4] = {a[2], b[2], a[3], b[3]};
-      store4(h + t.oa, lo);
-      store4(h + t.ob, hi);
-    } else {
-      store4(h + t.oa, a);
-      store4(h + t.ob, b);
-    }
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_unit(const RopeParams& p, const Unit& t, T* h,
+                                           const uint64_t (&v)[4]) {
+  if (VEC) {
+    store4(h + t.oa, v[0], v[1]);
+    store4(h + t.ob, v[2], v[3]);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int i = unit_elem(p, t, 0, e), j = unit_elem(p, t, 1, e);
-      if (i >= 0) h[i] = to_t<T>(a[e]);
-      if (j >= 0) h[j] = to_t<T>(b[e]);
+      const float2 f = halves(v[e]);
+      const int i = unit_elem(p, t, e >> 1, 2 * (e & 1)), j = unit_elem(p, t, e >> 1, 2 * (e & 1) + 1);
+      if (i >= 0) h[i] = to_t<T>(f.x);
+      if (j >= 0) h[j] = to_t<T>(f.y);
     }
   }
 }
 
-__device__ __forceinline__ void rotate4(float (&a)[4], float (&b)[4], const float (&c)[4],
-                                        const float (&s)[4]) {
+// cos and sin of a lane's four pairs at the current row (sin negated for the transposed turn).
+struct Turns {
+  uint64_t c[2], s[2];
+};
+// Turns a unit's pairs: elements of v[0], v[1] with those of v[2], v[3], or neighbours where the
+// interleaved layout moves as vectors.
+template <bool VEC>
+__device__ __forceinline__ void rotate(const RopeParams& p, uint64_t (&v)[4], const Turns& t) {
+  const uint64_t neg = pair(-1.f, -1.f);
+  if (!VEC || p.half) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float x = a[e], y = b[e];
-    a[e] = x * c[e] - y * s[e];
-    b[e] = y * c[e] + x * s[e];
+    for (int e = 0; e < 2; ++e) {
+      const uint64_t x = v[e], y = v[2 + e];
+      v[e] = fma2(mul2(y, t.s[e]), neg, mul2(x, t.c[e]));
+      v[2 + e] = fma2(y, t.c[e], mul2(x, t.s[e]));
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 x = halves(v[e]), c2 = halves(t.c[e >> 1]), s2 = halves(t.s[e >> 1]);
+      const float c = e & 1 ? c2.y : c2.x, s = e & 1 ? s2.y : s2.x;
+      v[e] = pair(x.x * c - x.y * s, x.y * c + x.x * s);
+    }
   }
 }
 
+__device__ __forceinline__ float sum2(uint64_t a) {
+  const float2 f = halves(a);
+  return f.x + f.y;
+}
 // Sum over the lanes of a head (every lane of the warp takes part).
 __device__ __forceinline__ float head_sum(float v, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
-// The rows and heads of one warp: row by row, or, when there are few rows, parts of a row.
-struct Walk {
-  int64_t item, items, step;
-  int per, iters;
+// ---- a warp's ring ----------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t saddr(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+__device__ __forceinline__ bool try_phase(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "vote.sync.all.pred q, p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// A warp's bounded wait (2 s at 2 GHz).
+__device__ __forceinline__ bool phase_wait(uint32_t bar, uint32_t parity, int* status) {
+  if (try_phase(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!try_phase(bar, parity)) {
+    if (__any_sync(0xffffffffu, clock64() - t0 > 4000000000LL)) {
+      if (status) atomicMax(status, DEV_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
+
+struct RowBuf {
+  const char* base;     // row 0, head 0
+  int64_t ld;           // bytes a row
+  int esize, heads;     // element size, heads that are needed
 };
-__device__ __forceinline__ Walk make_walk(const RopeParams& p) {
-  Walk w;
-  const int hpw = 32 / p.lanes;
-  w.iters = (p.Hq + p.Hkv + p.Hc + hpw - 1) / hpw;
-  w.per = (w.iters + p.chunks - 1) / p.chunks;
-  w.item = static_cast<int64_t>(blockIdx.x) * kRopeWarps + (threadIdx.x >> 5);
-  w.step = static_cast<int64_t>(gridDim.x) * kRopeWarps;
-  w.items = static_cast<int64_t>(seq_total(p.seq)) * p.chunks;
-  return w;
+
+// This warp's parts of rows in order.  A unit of work is a row, or a run of `run` parts of one when
+// there are fewer rows than warps; part c holds heads c hc .. c hc + hc - 1.
+struct Cursor {
+  int64_t left;         // units still to come, this one included
+  int row, first, c;    // row, first part of its run, current part
+};
+__device__ __forceinline__ Cursor first_part(const RopeParams& p, int total) {
+  const int64_t units = static_cast<int64_t>(total) * p.splits;
+  const int64_t g = static_cast<int64_t>(blockIdx.x) * kRopeWarps + (threadIdx.x >> 5);
+  const int64_t all = static_cast<int64_t>(gridDim.x) * kRopeWarps;
+  Cursor k;
+  k.left = units > g ? (units - g + all - 1) / all : 0;
+  k.row = static_cast<int>(g / p.splits);
+  k.first = k.c = static_cast<int>(g % p.splits) * p.run;
+  return k;
+}
+// The next part; true when it is in another unit.
+__device__ __forceinline__ bool next_part(const RopeParams& p, Cursor& k) {
+  if (++k.c < min(k.first + p.run, p.parts)) return false;
+  --k.left;
+  k.row += p.step_row;
+  k.first += p.step_split * p.run;
+  if (k.first >= p.splits * p.run) {
+    k.first -= p.splits * p.run;
+    ++k.row;
+  }
+  k.c = k.first;
+  return true;
 }
 
-// cos and sin (times mscale) of a lane's pairs at a row.
-__device__ __forceinline__ void row_turns(const RopeParams& p, const Unit& t, int row,
-                                          float (&c)[4], float (&s)[4]) {
-  const int pos = p.pos ? p.pos[row] : row - seq_begin(p.seq, row);
+// The warp's ring and what it works with.
+template <int NARR>
+struct Reader {
+  const RopeParams& p;
+  RowBuf buf[NARR];
+  char* ring;            // two stages, then cos and sin tables
+  uint32_t bars;         // two barriers
+  int lane, H, st, got;
+  uint32_t ph;
+  Cursor ahead;          // next part to be copied
+  int issued;
+
+  __device__ __forceinline__ Reader(const RopeParams& p_, char* ring_, uint32_t bars_, int total)
+      : p(p_), ring(ring_), bars(bars_), lane(threadIdx.x & 31), H(p_.Hq + p_.Hkv + p_.Hc), st(0),
+        got(0), ph(0), ahead(first_part(p_, total)), issued(0) {}
+  // Copies the next part into stage s (whose old contents every lane has read).
+  __device__ __forceinline__ void issue(int s) {
+    if (ahead.left <= 0) return;
+    const int h0 = ahead.c * p.hc, h1 = min(h0 + p.hc, H);
+    if (lane == 0) {
+      const uint32_t bar = bars + 8 * s;
+      int n[NARR], bytes = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    c[e] = 1.f;
-    s[e] = 0.f;
-    const int q = 4 * t.u + e;
-    if (t.rot && q < p.R / 2) {
-      turn_cos_sin(pos, p.phase[q], c[e], s[e]);
-      c[e] *= p.mscale;
-      s[e] *= p.mscale;
+      for (int k = 0; k < NARR; ++k) {
+        n[k] = max(min(h1, buf[k].heads) - h0, 0) * p.D * buf[k].esize;
+        bytes += n[k];
+      }
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+                   : "memory");
+      uint32_t at = saddr(ring) + s * p.stage_bytes;
+#pragma unroll
+      for (int k = 0; k < NARR; ++k) {
+        const char* src = buf[k].base + ahead.row * buf[k].ld + static_cast<int64_t>(h0) * p.D * buf[k].esize;
+        if (n[k] > 0)
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(at),
+              "l"(src), "r"(n[k]), "r"(bar)
+              : "memory");
+        at += p.hc * p.D * buf[k].esize;
+      }
+    }
+    __syncwarp();
+    ++issued;
+    next_part(p, ahead);
+  }
+  // Waits for the next stage.
+  __device__ __forceinline__ bool next() { return phase_wait(bars + 8 * st, ph, p.status); }
+  __device__ __forceinline__ const char* stage() const { return ring + st * p.stage_bytes; }
+  // Gives the stage back and copies on.
+  __device__ __forceinline__ void done() {
+    __syncwarp();
+    ++got;
+    issue(st);
+    if (++st == kRopeStages) {
+      st = 0;
+      ph ^= 1;
     }
   }
+  // Given up: what was issued still has to land.
+  __device__ __forceinline__ void drain() {
+    for (; got < issued; ++got) {
+      const long long t0 = clock64();
+      while (!try_phase(bars + 8 * st, ph) && clock64() - t0 < 4000000000LL) {
+      }
+      if (++st == kRopeStages) {
+        st = 0;
+        ph ^= 1;
+      }
+    }
+  }
+};
+
+// Positions of a warp's next 32 units, one a lane.
+struct Positions {
+  int pos, have;
+};
+__device__ __forceinline__ int next_pos(const RopeParams& p, Positions& s, const Cursor& k, int total) {
+  if (s.have == 0) {
+    const int lane = threadIdx.x & 31;
+    const int64_t all = static_cast<int64_t>(gridDim.x) * kRopeWarps;
+    const int64_t unit = static_cast<int64_t>(k.row) * p.splits + k.first / p.run + lane * all;
+    const int row = static_cast<int>(min(unit / p.splits, static_cast<int64_t>(total) - 1));
+    s.pos = p.pos ? p.pos[row] : row - seq_begin(p.seq, row);
+    s.have = 32;
+  }
+  const int r = __shfl_sync(0xffffffffu, s.pos, 32 - s.have);
+  --s.have;
+  return r;
+}
+
+// cos and sin at a position: a pair a lane, handed round through the warp's table.
+__device__ __forceinline__ Turns make_turns(const RopeParams& p, const Unit& t, int pos, float* tab,
+                                            float sign) {
+  const int lane = threadIdx.x & 31, pairs = (p.R / 2 + 3) / 4 * 4;
+  __syncwarp();
+  for (int q = lane; q < pairs; q += 32) {
+    float c = 1.f, s = 0.f;
+    if (q < p.R / 2) {
+      turn_cos_sin(pos, p.phase[q], c, s);
+      c *= p.mscale;
+      s *= p.mscale * sign;
+    }
+    tab[q] = c;
+    tab[64 + q] = s;
+  }
+  __syncwarp();
+  Turns r{};
+  if (t.rot) {
+    load4(tab + 4 * t.u, r.c[0], r.c[1]);
+    load4(tab + 64 + 4 * t.u, r.s[0], r.s[1]);
+  }
+  return r;
+}
+
+// Shared memory of a block: every warp's ring, barriers, and the gains [gq | gk | gq' | gk'][D].
+struct RopeShared {
+  uint64_t bars[kRopeWarps][kRopeStages];
+  float gains[4][128];
+};
+__device__ __forceinline__ void rope_start(const RopeParams& p, RopeShared& sh) {
+  if (threadIdx.x < kRopeWarps * kRopeStages) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(saddr(&sh.bars[0][0]) + 8 * threadIdx.x));
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_entry();
+  if (p.gq)
+    for (int i = threadIdx.x; i < 4 * p.D; i += kRopeThreads) {
+      const int k = i / p.D, e = i % p.D;
+      const float* g = k == 0 ? p.gq : k == 1 ? p.gk : k == 2 ? p.gqd : p.gkd;
+      sh.gains[k][e] = g ? g[e] : 0.f;
+    }
+  __syncthreads();
+}
+__device__ __forceinline__ int warp_bytes(const RopeParams& p) {
+  return kRopeStages * p.stage_bytes + 2 * 64 * static_cast<int>(sizeof(float));
+}
+
+template <typename Tx, typename Ty, bool DUAL, bool NORM, bool VEC>
+__device__ __forceinline__ void fwd_rows(const RopeParams& p, char* ring, RopeShared& sh) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int H = p.Hq + p.Hkv + p.Hc, Hn = p.Hq + p.Hkv, total = seq_total(p.seq);
+  Reader<DUAL ? 2 : 1> rd(p, ring + warp * warp_bytes(p), saddr(sh.bars[warp]), total);
+  rd.buf[0] = {static_cast<const char*>(p.x), p.ldx * static_cast<int>(sizeof(Tx)), sizeof(Tx), H};
+  if constexpr (DUAL) rd.buf[1] = {static_cast<const char*>(p.xd), rd.buf[0].ld, sizeof(Tx), H};
+#pragma unroll
+  for (int s = 0; s < kRopeStages; ++s) rd.issue(s);
+  float* tab = reinterpret_cast<float*>(rd.ring + kRopeStages * p.stage_bytes);
+  const Unit t = make_unit(p, lane);
+  const int sub = lane / p.lanes, hpw = 32 / p.lanes, half = p.hc * p.D;
+  const float invD = 1.f / static_cast<float>(p.D);
+  Positions ps{0, 0};
+  Turns turns{};
+  bool fresh = true;
+  for (Cursor k = first_part(p, total); k.left > 0; fresh = next_part(p, k)) {
+    if (fresh && p.R > 0) turns = make_turns(p, t, next_pos(p, ps, k, total), tab, 1.f);
+    if (!rd.next()) break;
+    const Tx* sx = reinterpret_cast<const Tx*>(rd.stage());
+    const int h0 = k.c * p.hc, n = min(p.hc, H - h0);
+    Ty* y = static_cast<Ty*>(p.y) + k.row * p.ldy + static_cast<int64_t>(h0) * p.D;
+    Ty* yd = DUAL ? static_cast<Ty*>(p.yd) + k.row * p.ldy + static_cast<int64_t>(h0) * p.D : nullptr;
+    for (int hl = sub; hl - sub < n; hl += hpw) {
+      const bool on = t.on && hl < n;
+      const int e0 = hl * p.D, h = h0 + hl;
+      uint64_t v[4] = {}, d[4] = {};
+      load_unit<VEC>(p, t, on, sx + e0, v);
+      if (DUAL) load_unit<VEC>(p, t, on, sx + half + e0, d);
+      if (NORM) {
+        uint64_t q2 = 0, q1 = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          q2 = fma2(v[e], v[e], q2);
+          if (DUAL) q1 = fma2(v[e], d[e], q1);
+        }
+        const float s2 = head_sum(sum2(q2), p.lanes), s1 = DUAL ? head_sum(sum2(q1), p.lanes) : 0.f;
+        if (on && h < Hn) {
+          const float r = rsqrtf(s2 * invD + p.eps);
+          const float rt = DUAL ? -r * r * r * s1 * invD : 0.f;
+          const uint64_t r2 = pair(r, r), rt2 = pair(rt, rt);
+          const int gi = h < p.Hq ? 0 : 1;
+          uint64_t g[4], gd[4];
+          load_unit<VEC>(p, t, true, sh.gains[gi], g);
+          if (DUAL) load_unit<VEC>(p, t, true, sh.gains[2 + gi], gd);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint64_t nv = mul2(v[e], r2);
+            if (DUAL) d[e] = fma2(gd[e], nv, mul2(g[e], fma2(d[e], r2, mul2(v[e], rt2))));
+            v[e] = mul2(g[e], nv);
+          }
+        }
+      }
+      if (on) {
+        if (h < Hn && t.rot) {
+          rotate<VEC>(p, v, turns);
+          if (DUAL) rotate<VEC>(p, d, turns);
+        }
+        store_unit<VEC>(p, t, y + e0, v);
+        if (DUAL) store_unit<VEC>(p, t, yd + e0, d);
+      }
+    }
+    rd.done();
+  }
+  rd.drain();
 }
 
 template <typename Tx, typename Ty, bool DUAL, bool NORM>
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, 2)
     qk_rope_fwd_kernel(const __grid_constant__ RopeParams p) {
-  pdl_entry();
-  const int lane = threadIdx.x & 31;
-  const Unit t = make_unit(p, lane);
-  const int sub = lane / p.lanes, hpw = 32 / p.lanes;
-  const int Hn = p.Hq + p.Hkv, H = Hn + p.Hc;
-  const float invD = 1.f / static_cast<float>(p.D);
-  Walk w = make_walk(p);
-  for (; w.item < w.items; w.item += w.step) {
-    const int row = static_cast<int>(w.item / p.chunks);
-    const int i0 = static_cast<int>(w.item % p.chunks) * w.per;
-    const int i1 = min(w.iters, i0 + w.per);
-    float c[4], s[4];
-    row_turns(p, t, row, c, s);
-    const Tx* x = static_cast<const Tx*>(p.x) + row * p.ldx;
-    const Tx* xd = DUAL ? static_cast<const Tx*>(p.xd) + row * p.ldx : nullptr;
-    Ty* y = static_cast<Ty*>(p.y) + row * p.ldy;
-    Ty* yd = DUAL ? static_cast<Ty*>(p.yd) + row * p.ldy : nullptr;
-    for (int i = i0; i < i1; ++i) {
-      const int h = i * hpw + sub;
-      const bool on = t.on && h < H;
-      float a[4], b[4], ad[4], bd[4];
-      load_unit(p, t, on, x + h * p.D, a, b);
-      if (DUAL) load_unit(p, t, on, xd + h * p.D, ad, bd);
-      if (NORM) {
-        float s2 = 0.f, s1 = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s2 += a[e] * a[e] + b[e] * b[e];
-          if (DUAL) s1 += a[e] * ad[e] + b[e] * bd[e];
-        }
-        s2 = head_sum(s2, p.lanes);
-        if (DUAL) s1 = head_sum(s1, p.lanes);
-        if (h < Hn) {
-          const float r = rsqrtf(s2 * invD + p.eps);
-          const float rd = DUAL ? -r * r * r * s1 * invD : 0.f;
-          float ga[4], gb[4];
-          load_unit(p, t, on, h < p.Hq ? p.gq : p.gk, ga, gb);
-          float da[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f};
-          if (DUAL && p.gqd) load_unit(p, t, on, h < p.Hq ? p.gqd : p.gkd, da, db);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float na = a[e] * r, nb = b[e] * r;
-            if (DUAL) {
-              ad[e] = da[e] * na + ga[e] * (ad[e] * r + a[e] * rd);
-              bd[e] = db[e] * nb + gb[e] * (bd[e] * r + b[e] * rd);
-            }
-            a[e] = ga[e] * na;
-            b[e] = gb[e] * nb;
-          }
-        }
-      }
-      if (h < Hn && t.rot) {
-        rotate4(a, b, c, s);
-        if (DUAL) rotate4(ad, bd, c, s);
-      }
-      store_unit(p, t, on, y + h * p.D, a, b);
-      if (DUAL) store_unit(p, t, on, yd + h * p.D, ad, bd);
-    }
-  }
+  extern __shared__ __align__(128) char ring[];
+  __shared__ __align__(16) RopeShared sh;
+  rope_start(p, sh);
+  if (p.vec) fwd_rows<Tx, Ty, DUAL, NORM, true>(p, ring, sh);
+  else fwd_rows<Tx, Ty, DUAL, NORM, false>(p, ring, sh);
 }
 
-// Accumulators of the gain gradients: dgq, dgk and, with tangents, dgq', dgk'.
-template <typename Tx, typename Ty, bool DUAL, bool NORM>
-__global__ void __launch_bounds__(kRopeThreads)
-    qk_rope_bwd_kernel(const __grid_constant__ RopeParams p) {
-  pdl_entry();
-  constexpr int NA = DUAL ? 4 : 2;
-  __shared__ float sums[NORM ? kRopeWarps : 1][NORM ? NA * 128 : 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// acc: dgq, dgk and, with tangents, dgq', dgk' of this lane's elements.
+template <typename Tx, typename Ty, bool DUAL, bool NORM, bool VEC, int NACC>
+__device__ __forceinline__ void bwd_rows(const RopeParams& p, char* ring, RopeShared& sh,
+                                         uint64_t (&acc)[NACC][4]) {
+  constexpr int NARR = (DUAL ? 2 : 1) * (NORM ? 2 : 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int H = p.Hq + p.Hkv + p.Hc, Hn = p.Hq + p.Hkv, total = seq_total(p.seq);
+  Reader<NARR> rd(p, ring + warp * warp_bytes(p), saddr(sh.bars[warp]), total);
+  const RowBuf dy{static_cast<const char*>(p.dy), p.lddy * static_cast<int>(sizeof(Ty)), sizeof(Ty), H};
+  const RowBuf xb{static_cast<const char*>(p.x), p.ldx * static_cast<int>(sizeof(Tx)), sizeof(Tx), Hn};
+  rd.buf[0] = dy;
+  if constexpr (DUAL) rd.buf[1] = {static_cast<const char*>(p.dyd), dy.ld, sizeof(Ty), H};
+  if constexpr (NORM) rd.buf[DUAL ? 2 : 1] = xb;
+  if constexpr (NORM && DUAL) rd.buf[3] = {static_cast<const char*>(p.xd), xb.ld, sizeof(Tx), Hn};
+#pragma unroll
+  for (int s = 0; s < kRopeStages; ++s) rd.issue(s);
+  float* tab = reinterpret_cast<float*>(rd.ring + kRopeStages * p.stage_bytes);
   const Unit t = make_unit(p, lane);
-  const int sub = lane / p.lanes, hpw = 32 / p.lanes;
-  const int Hn = p.Hq + p.Hkv, H = Hn + p.Hc;
+  const int sub = lane / p.lanes, hpw = 32 / p.lanes, half = p.hc * p.D;
   const float invD = 1.f / static_cast<float>(p.D);
-  float acc[NORM ? NA : 1][8];
-#pragma unroll
-  for (int i = 0; i < (NORM ? NA : 1); ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[i][e] = 0.f;
-  Walk w = make_walk(p);
-  for (; w.item < w.items; w.item += w.step) {
-    const int row = static_cast<int>(w.item / p.chunks);
-    const int i0 = static_cast<int>(w.item % p.chunks) * w.per;
-    const int i1 = min(w.iters, i0 + w.per);
-    float c[4], s[4];
-    row_turns(p, t, row, c, s);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] = -s[e];   // the transposed rotation
-    const Ty* dy = static_cast<const Ty*>(p.dy) + row * p.lddy;
-    const Ty* dyd = DUAL ? static_cast<const Ty*>(p.dyd) + row * p.lddy : nullptr;
-    Ty* dx = static_cast<Ty*>(p.dx) + row * p.lddx;
-    Ty* dxd = DUAL ? static_cast<Ty*>(p.dxd) + row * p.lddx : nullptr;
-    const Tx* x = NORM ? static_cast<const Tx*>(p.x) + row * p.ldx : nullptr;
-    const Tx* xd = NORM && DUAL ? static_cast<const Tx*>(p.xd) + row * p.ldx : nullptr;
-    for (int i = i0; i < i1; ++i) {
-      const int h = i * hpw + sub;
-      const bool on = t.on && h < H, normed = NORM && h < Hn;
-      float a[4], b[4], ad[4], bd[4];
-      load_unit(p, t, on, dy + h * p.D, a, b);
-      if (DUAL) load_unit(p, t, on, dyd + h * p.D, ad, bd);
-      if (h < Hn && t.rot) {
-        rotate4(a, b, c, s);
-        if (DUAL) rotate4(ad, bd, c, s);
+  Positions ps{0, 0};
+  Turns turns{};
+  bool fresh = true;
+  for (Cursor k = first_part(p, total); k.left > 0; fresh = next_part(p, k)) {
+    if (fresh) turns = make_turns(p, t, next_pos(p, ps, k, total), tab, -1.f);   // transposed
+    if (!rd.next()) break;
+    const Ty* sdy = reinterpret_cast<const Ty*>(rd.stage());
+    const Tx* sx = reinterpret_cast<const Tx*>(sdy + (DUAL ? 2 : 1) * half);
+    const int h0 = k.c * p.hc, n = min(p.hc, H - h0);
+    Ty* dx = static_cast<Ty*>(p.dx) + k.row * p.lddx + static_cast<int64_t>(h0) * p.D;
+    Ty* dxd = DUAL ? static_cast<Ty*>(p.dxd) + k.row * p.lddx + static_cast<int64_t>(h0) * p.D : nullptr;
+    for (int hl = sub; hl - sub < n; hl += hpw) {
+      const bool on = t.on && hl < n;
+      const int e0 = hl * p.D, h = h0 + hl;
+      const bool normed = NORM && on && h < Hn;
+      uint64_t v[4] = {}, d[4] = {};
+      load_unit<VEC>(p, t, on, sdy + e0, v);
+      if (DUAL) load_unit<VEC>(p, t, on, sdy + half + e0, d);
+      if (on && h < Hn && t.rot) {
+        rotate<VEC>(p, v, turns);
+        if (DUAL) rotate<VEC>(p, d, turns);
       }
       if (NORM) {
-        float xa[4], xb[4], xad[4], xbd[4];
-        load_unit(p, t, on && normed, x + h * p.D, xa, xb);
-        if (DUAL) load_unit(p, t, on && normed, xd + h * p.D, xad, xbd);
-        float ga[4], gb[4];
-        float da[4] = {0.f, 0.f, 0.f, 0.f}, db[4] = {0.f, 0.f, 0.f, 0.f};
-        load_unit(p, t, on && normed, h < p.Hq ? p.gq : p.gk, ga, gb);
-        if (DUAL && p.gqd) load_unit(p, t, on && normed, h < p.Hq ? p.gqd : p.gkd, da, db);
-        float s2 = 0.f, s1 = 0.f, m = 0.f, md = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float ua = ga[e] * a[e], ub = gb[e] * b[e];
-          s2 += xa[e] * xa[e] + xb[e] * xb[e];
-          m += xa[e] * ua + xb[e] * ub;
-          if (DUAL) {
-            s1 += xa[e] * xad[e] + xb[e] * xbd[e];
-            md += xad[e] * ua + xbd[e] * ub;
-            md += xa[e] * (da[e] * a[e] + ga[e] * ad[e]) + xb[e] * (db[e] * b[e] + gb[e] * bd[e]);
-          }
-        }
-        s2 = head_sum(s2, p.lanes);
-        m = head_sum(m, p.lanes) * invD;
-        if (DUAL) {
-          s1 = head_sum(s1, p.lanes);
-          md = head_sum(md, p.lanes) * invD;
-        }
-        if (normed) {
-          const float r = rsqrtf(s2 * invD + p.eps);
-          const float r3 = r * r * r;
-          const float rd = DUAL ? -r3 * s1 * invD : 0.f;
-          const float k0 = r3 * m, k1 = 3.f * r * r * rd * m + r3 * md;
-          const bool isq = h < p.Hq;
+        uint64_t x[4] = {}, xd[4] = {};
+        load_unit<VEC>(p, t, normed, sx + e0, x);
+        if (DUAL) load_unit<VEC>(p, t, normed, sx + half + e0, xd);
+        const int gi = h < p.Hq ? 0 : 1;
+        uint64_t q2 = 0, q1 = 0, qm = 0, qd = 0;
+        {
+          uint64_t g[4] = {}, gd[4] = {};
+          load_unit<VEC>(p, t, normed, sh.gains[gi], g);
+          if (DUAL) load_unit<VEC>(p, t, normed, sh.gains[2 + gi], gd);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float ca = a[e], cb = b[e], na = xa[e] * r, nb = xb[e] * r;
-            const float wa = ca * na, wb = cb * nb;
-            acc[0][e] += isq ? wa : 0.f;
-            acc[0][4 + e] += isq ? wb : 0.f;
-            acc[NORM ? 1 : 0][e] += isq ? 0.f : wa;
-            acc[NORM ? 1 : 0][4 + e] += isq ? 0.f : wb;
-            a[e] = r * ga[e] * ca - k0 * xa[e];
-            b[e] = r * gb[e] * cb - k0 * xb[e];
+            const uint64_t a = mul2(g[e], v[e]);
+            q2 = fma2(x[e], x[e], q2);
+            qm = fma2(x[e], a, qm);
             if (DUAL) {
-              const float va = ad[e] * na + ca * (xad[e] * r + xa[e] * rd);
-              const float vb = bd[e] * nb + cb * (xbd[e] * r + xb[e] * rd);
-              acc[NORM ? NA - 2 : 0][e] += isq ? va : 0.f;
-              acc[NORM ? NA - 2 : 0][4 + e] += isq ? vb : 0.f;
-              acc[NORM ? NA - 1 : 0][e] += isq ? 0.f : va;
-              acc[NORM ? NA - 1 : 0][4 + e] += isq ? 0.f : vb;
-              ad[e] = rd * ga[e] * ca + r * (da[e] * ca + ga[e] * ad[e]) - k1 * xa[e] - k0 * xad[e];
-              bd[e] = rd * gb[e] * cb + r * (db[e] * cb + gb[e] * bd[e]) - k1 * xb[e] - k0 * xbd[e];
+              q1 = fma2(x[e], xd[e], q1);
+              qd = fma2(xd[e], a, qd);
+              qd = fma2(x[e], fma2(gd[e], v[e], mul2(g[e], d[e])), qd);
+            }
+          }
+        }
+        const float s2 = head_sum(sum2(q2), p.lanes), m = head_sum(sum2(qm), p.lanes) * invD;
+        const float s1 = DUAL ? head_sum(sum2(q1), p.lanes) : 0.f;
+        const float md = DUAL ? head_sum(sum2(qd), p.lanes) * invD : 0.f;
+        if (normed) {
+          const float r = rsqrtf(s2 * invD + p.eps), r3 = r * r * r;
+          const float rt = DUAL ? -r3 * s1 * invD : 0.f;
+          const float k0 = -r3 * m, k1 = -3.f * r * r * rt * m - r3 * md;
+          const uint64_t r2 = pair(r, r), rt2 = pair(rt, rt), k02 = pair(k0, k0), k12 = pair(k1, k1);
+          // the gains are read again rather than kept across the sums: registers
+          asm volatile("" ::: "memory");
+          uint64_t g[4], gd[4];
+          load_unit<VEC>(p, t, true, sh.gains[gi], g);
+          if (DUAL) load_unit<VEC>(p, t, true, sh.gains[2 + gi], gd);
+          // one of the two sums gets the product, the other a zero
+          const float fq = h < p.Hq ? 1.f : 0.f;
+          const uint64_t fq2 = pair(fq, fq), fk2 = pair(1.f - fq, 1.f - fq);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint64_t dyv = v[e], nv = mul2(x[e], r2), gw = mul2(dyv, nv), a = mul2(g[e], dyv);
+            acc[0][e] = fma2(fq2, gw, acc[0][e]);
+            acc[NORM ? 1 : 0][e] = fma2(fk2, gw, acc[NORM ? 1 : 0][e]);
+            v[e] = fma2(r2, a, mul2(k02, x[e]));
+            if (DUAL) {
+              const uint64_t gt = fma2(d[e], nv, mul2(dyv, fma2(xd[e], r2, mul2(x[e], rt2))));
+              acc[NACC - 2 > 0 ? NACC - 2 : 0][e] = fma2(fq2, gt, acc[NACC - 2 > 0 ? NACC - 2 : 0][e]);
+              acc[NACC - 1][e] = fma2(fk2, gt, acc[NACC - 1][e]);
+              const uint64_t b = fma2(gd[e], dyv, mul2(g[e], d[e]));
+              d[e] = fma2(rt2, a, fma2(r2, b, fma2(k12, x[e], mul2(k02, xd[e]))));
             }
           }
         }
       }
-      store_unit(p, t, on, dx + h * p.D, a, b);
-      if (DUAL) store_unit(p, t, on, dxd + h * p.D, ad, bd);
+      if (on) {
+        store_unit<VEC>(p, t, dx + e0, v);
+        if (DUAL) store_unit<VEC>(p, t, dxd + e0, d);
+      }
     }
+    rd.done();
   }
+  rd.drain();
+}
+
+template <typename Tx, typename Ty, bool DUAL, bool NORM>
+__global__ void __launch_bounds__(kRopeThreads, 2)
+    qk_rope_bwd_kernel(const __grid_constant__ RopeParams p) {
+  constexpr int NA = DUAL ? 4 : 2;
+  extern __shared__ __align__(128) char ring[];
+  __shared__ __align__(16) RopeShared sh;
+  rope_start(p, sh);
+  uint64_t acc[NORM ? NA : 1][4] = {};
+  if (p.vec) bwd_rows<Tx, Ty, DUAL, NORM, true>(p, ring, sh, acc);
+  else bwd_rows<Tx, Ty, DUAL, NORM, false>(p, ring, sh, acc);
   if (NORM) {
-    // lanes of the same unit, then the block's warps, in a fixed order
+    // lanes of the same unit, then the block's warps, in a fixed order; the rings are free
+    __syncthreads();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Unit t = make_unit(p, lane);
+    float* sums = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int k = 0; k < NA; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float v = acc[k][e];
+        const float2 f = halves(acc[NORM ? k : 0][e >> 1]);
+        float v = e & 1 ? f.y : f.x;
         for (int o = p.lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        const int i = unit_elem(p, t, e >> 2, e & 3);
-        if (lane < p.lanes && i >= 0) sums[warp][k * p.D + i] = v;
+        // vector units are in memory order, others in pair order
+        const int i = !p.vec ? unit_elem(p, t, e >> 2, e & 3) : t.on ? (e < 4 ? t.oa + e : t.ob + e - 4) : -1;
+        if (lane < p.lanes && i >= 0) sums[(warp * NA + k) * p.D + i] = v;
       }
     __syncthreads();
     float* part = p.part + static_cast<int64_t>(blockIdx.x) * NA * p.D;
     for (int i = threadIdx.x; i < NA * p.D; i += kRopeThreads) {
       float v = 0.f;
-#pragma unroll
-      for (int j = 0; j < kRopeWarps; ++j) v += sums[j][i];
+      for (int j = 0; j < kRopeWarps; ++j) v += sums[j * NA * p.D + i];
       part[i] = v;
     }
   }
 }
 
-// Sum of the blocks' partial gain gradients in a fixed order: 32 columns a block, eight
-// threads a column.
-__global__ void __launch_bounds__(256)
+// Sum of the blocks' partial gain gradients in a fixed order: 32 columns a block, 32 threads a
+// column, their sums by halves.
+__global__ void __launch_bounds__(1024)
     rope_gain_final_kernel(int nblk, int D, int NA, const float* __restrict__ part,
                            float* __restrict__ d0, float* __restrict__ d1, float* __restrict__ d2,
                            float* __restrict__ d3) {
   pdl_entry();
-  __shared__ float s[8][33];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), ty = threadIdx.x >> 5;
+  __shared__ float s[32][33];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int col = blockIdx.x * 32 + tx;
   float v = 0.f;
-  if (col < NA * D)
-    for (int j = ty; j < nblk; j += 8) v += part[static_cast<int64_t>(j) * NA * D + col];
-  s[ty][threadIdx.x & 31] = v;
+  if (col < NA * D) {
+#pragma unroll 4
+    for (int j = ty; j < nblk; j += 32) v += part[static_cast<int64_t>(j) * NA * D + col];
+  }
+  s[ty][tx] = v;
   __syncthreads();
-  if (ty == 0 && col < NA * D) {
-    float sum = 0.f;
+  // warp ty adds up column ty of the block
+  float sum = s[tx][ty];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += s[j][threadIdx.x];
-    const int k = col / D;
-    (k == 0 ? d0 : k == 1 ? d1 : k == 2 ? d2 : d3)[col % D] = sum;
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const int c = blockIdx.x * 32 + ty;
+  if (tx == 0 && c < NA * D) {
+    const int k = c / D;
+    (k == 0 ? d0 : k == 1 ? d1 : k == 2 ? d2 : d3)[c % D] = sum;
   }
 }
 
-template <typename Tx, typename Ty>
-cudaError_t launch_rope(const RopeParams& p, bool bwd, bool dual, bool norm, int grid,
-                        cudaStream_t s) {
-  const dim3 g(grid), b(kRopeThreads);
-  if (bwd) {
-    if (dual) return norm ? launch_k(qk_rope_bwd_kernel<Tx, Ty, true, true>, g, b, 0, s, p)
-                          : launch_k(qk_rope_bwd_kernel<Tx, Ty, true, false>, g, b, 0, s, p);
-    return norm ? launch_k(qk_rope_bwd_kernel<Tx, Ty, false, true>, g, b, 0, s, p)
-                : launch_k(qk_rope_bwd_kernel<Tx, Ty, false, false>, g, b, 0, s, p);
+template <auto kernel>
+cudaError_t launch_ring(const RopeParams& p, int grid, cudaStream_t s) {
+  static PerDeviceOnce once;
+  const cudaError_t e = once.run([](int&) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRopeRing);
+  });
+  if (e != cudaSuccess) return e;
+  return launch_k(kernel, dim3(grid), dim3(kRopeThreads), p.ring_bytes, s, p);
+}
+
+template <typename Tx, typename Ty, bool BWD>
+cudaError_t launch_rope(const RopeParams& p, bool dual, bool norm, int grid, cudaStream_t s) {
+  if constexpr (BWD) {
+    if (dual) return norm ? launch_ring<qk_rope_bwd_kernel<Tx, Ty, true, true>>(p, grid, s)
+                          : launch_ring<qk_rope_bwd_kernel<Tx, Ty, true, false>>(p, grid, s);
+    return norm ? launch_ring<qk_rope_bwd_kernel<Tx, Ty, false, true>>(p, grid, s)
+                : launch_ring<qk_rope_bwd_kernel<Tx, Ty, false, false>>(p, grid, s);
+  } else {
+    if (dual) return norm ? launch_ring<qk_rope_fwd_kernel<Tx, Ty, true, true>>(p, grid, s)
+                          : launch_ring<qk_rope_fwd_kernel<Tx, Ty, true, false>>(p, grid, s);
+    return norm ? launch_ring<qk_rope_fwd_kernel<Tx, Ty, false, true>>(p, grid, s)
+                : launch_ring<qk_rope_fwd_kernel<Tx, Ty, false, false>>(p, grid, s);
   }
-  if (dual) return norm ? launch_k(qk_rope_fwd_kernel<Tx, Ty, true, true>, g, b, 0, s, p)
-                        : launch_k(qk_rope_fwd_kernel<Tx, Ty, true, false>, g, b, 0, s, p);
-  return norm ? launch_k(qk_rope_fwd_kernel<Tx, Ty, false, true>, g, b, 0, s, p)
-              : launch_k(qk_rope_fwd_kernel<Tx, Ty, false, false>, g, b, 0, s, p);
+}
+
+template <bool BWD>
+cudaError_t launch_types(const RopeParams& p, bool x_bf16, bool y_bf16, bool dual, bool norm, int grid,
+                         cudaStream_t s) {
+  return !x_bf16 && !y_bf16 ? launch_rope<float, float, BWD>(p, dual, norm, grid, s)
+         : !x_bf16          ? launch_rope<float, __nv_bfloat16, BWD>(p, dual, norm, grid, s)
+                            : launch_rope<__nv_bfloat16, __nv_bfloat16, BWD>(p, dual, norm, grid, s);
 }
 
 }  // namespace
 
 cudaError_t qk_rope(RopeParams p, bool bwd, bool x_bf16, bool y_bf16, cudaStream_t s) {
   const bool norm = p.gq != nullptr, dual = bwd ? p.dyd != nullptr : p.xd != nullptr;
-  const int units = (p.R / 2 + 3) / 4 + (p.D - p.R + 7) / 8;
+  const int lanes_units = (p.R / 2 + 3) / 4 + (p.D - p.R + 7) / 8;
   p.lanes = 1;
-  while (p.lanes < units) p.lanes *= 2;
+  while (p.lanes < lanes_units) p.lanes *= 2;
   p.vec = p.R % 8 == 0;
-  const int hpw = 32 / p.lanes, iters = (p.Hq + p.Hkv + p.Hc + hpw - 1) / hpw;
-  // a warp a row once the rows fill the GPU's warps; below that, rows are cut into parts of
-  // their heads
+  // heads of a part: what fills a stage, whole warps of them
+  const int two = dual ? 2 : 1, xs = x_bf16 ? 2 : 4, ys = y_bf16 ? 2 : 4;
+  const int head = p.D * two * (bwd ? ys + (norm ? xs : 0) : xs);     // bytes, at most 2 KB
+  const int H = p.Hq + p.Hkv + p.Hc, hpw = 32 / p.lanes;
+  int hc = kRopeStage / head;
+  if (hc > hpw) hc -= hc % hpw;
+  p.hc = hc < H ? hc : H;
+  p.parts = (H + p.hc - 1) / p.hc;
+  p.stage_bytes = (p.hc * head + 127) / 128 * 128;
+  // a warp a row; with fewer than eight rows a warp, runs of a row's parts, so that the last round
+  // of units is a small part of all
   const int64_t warps = static_cast<int64_t>(kRopeMaxBlocks) * kRopeWarps;
-  p.chunks = 1;
-  while (p.chunks < iters && p.seq.rows * static_cast<int64_t>(p.chunks) * 2 <= warps) p.chunks *= 2;
-  const int64_t blocks = (static_cast<int64_t>(p.seq.rows) * p.chunks + kRopeWarps - 1) / kRopeWarps;
+  const int64_t want = (8 * warps + p.seq.rows - 1) / p.seq.rows;
+  p.splits = want < p.parts ? static_cast<int>(want) : p.parts;
+  p.run = (p.parts + p.splits - 1) / p.splits;
+  p.splits = (p.parts + p.run - 1) / p.run;
+  const int64_t blocks = (static_cast<int64_t>(p.seq.rows) * p.splits + kRopeWarps - 1) / kRopeWarps;
   const int grid = static_cast<int>(blocks < kRopeMaxBlocks ? blocks : kRopeMaxBlocks);
-  cudaError_t e =
-      !x_bf16 && !y_bf16 ? launch_rope<float, float>(p, bwd, dual, norm, grid, s)
-      : !x_bf16          ? launch_rope<float, __nv_bfloat16>(p, bwd, dual, norm, grid, s)
-                         : launch_rope<__nv_bfloat16, __nv_bfloat16>(p, bwd, dual, norm, grid, s);
-  if (e != cudaSuccess || !bwd || !norm) return e;
+  p.step_row = grid * kRopeWarps / p.splits;
+  p.step_split = grid * kRopeWarps % p.splits;
   const int NA = dual ? 4 : 2;
-  return launch_k(rope_gain_final_kernel, dim3((NA * p.D + 31) / 32), dim3(256), 0, s, grid, p.D,
+  const int rings = kRopeWarps * (kRopeStages * p.stage_bytes + 2 * 64 * static_cast<int>(sizeof(float)));
+  const int sums = bwd && norm ? kRopeWarps * NA * p.D * static_cast<int>(sizeof(float)) : 0;
+  p.ring_bytes = rings > sums ? rings : sums;
+  const cudaError_t e = bwd ? launch_types<true>(p, x_bf16, y_bf16, dual, norm, grid, s)
+                            : launch_types<false>(p, x_bf16, y_bf16, dual, norm, grid, s);
+  if (e != cudaSuccess || !bwd || !norm) return e;
+  return launch_k(rope_gain_final_kernel, dim3((NA * p.D + 31) / 32), dim3(1024), 0, s, grid, p.D,
                   NA, static_cast<const float*>(p.part), p.dgq, p.dgk, p.dgqd, p.dgkd);
 }
 

@@ -77,7 +77,8 @@ class mf_qk_rope_args(C.Structure):
                 *_ptrs("x xd"), ("ldx", C.c_int64), *_ptrs("y yd"), ("ldy", C.c_int64),
                 *_ptrs("gq gk gqd gkd pos seq_start"), ("n_seq", C.c_int),
                 *_ptrs("dy dyd"), ("lddy", C.c_int64), *_ptrs("dx dxd"), ("lddx", C.c_int64),
-                *_ptrs("dgq dgk dgqd dgkd work"), ("work_bytes", C.c_size_t)]
+                *_ptrs("dgq dgk dgqd dgkd work"), ("work_bytes", C.c_size_t),
+                *_ptrs("status")]
 
 
 class mf_attn_args(C.Structure):
@@ -335,7 +336,7 @@ def _prec(t, name):
 
 
 def _rope_call(first, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
-               pos, seq_start, n_seq):
+               pos, seq_start, n_seq, status):
     import torch
     a = mf_qk_rope_args()
     c = _Call(a, first)
@@ -346,17 +347,18 @@ def _rope_call(first, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk,
         c.vec(name, g, torch.float32, (head_dim,))
     c.vec("pos", pos, torch.int32, (a.n_rows,))
     c.seq(seq_start, n_seq)
+    c.vec("status", status, torch.int32, (1,))
     return c
 
 
 def mf_qk_rope_fwd(x, y, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, xd=None, yd=None,
                    gq=None, gk=None, gqd=None, gkd=None, eps=1e-6, pos=None, seq_start=None,
-                   n_seq=1, stream=None):
+                   n_seq=1, status=None, stream=None):
     """Rows of heads x [N][(n_heads + n_kv_heads + n_copy_heads) head_dim] -> y: RMS norm of the
     query and key heads (with gains gq, gk), rotary positions, the type of y; xd -> yd the
     tangent (see mixflow.h)."""
     c = _rope_call(x, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
-                   pos, seq_start, n_seq)
+                   pos, seq_start, n_seq, status)
     c.a.x_prec, c.a.y_prec = _prec(x, "x"), _prec(y, "y")
     n, cols = x.shape[0], (n_heads + n_kv_heads + n_copy_heads) * head_dim
     c.rows("x", x, x.dtype, n, cols, "ldx")
@@ -369,12 +371,12 @@ def mf_qk_rope_fwd(x, y, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, xd
 def mf_qk_rope_bwd(dy, dx, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, x=None, xd=None,
                    dyd=None, dxd=None, gq=None, gk=None, gqd=None, gkd=None, dgq=None, dgk=None,
                    dgqd=None, dgkd=None, eps=1e-6, pos=None, seq_start=None, n_seq=1, work=None,
-                   stream=None):
+                   status=None, stream=None):
     """Backward of mf_qk_rope_fwd: dy (dyd) -> dx (dxd) and, with gains, dgq, dgk (dgqd, dgkd)
     and x (xd) as the forward had them; work: mf_qk_rope_work_bytes bytes."""
     import torch
     c = _rope_call(dy, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
-                   pos, seq_start, n_seq)
+                   pos, seq_start, n_seq, status)
     c.a.y_prec = _prec(dy, "dy")
     c.a.x_prec = c.a.y_prec if x is None else _prec(x, "x")
     n, cols = dy.shape[0], (n_heads + n_kv_heads + n_copy_heads) * head_dim
