@@ -1741,8 +1741,12 @@ cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
   const __nv_bfloat16* kv[4] = {a.k, a.v, DUAL ? a.kd : nullptr, DUAL ? a.vd : nullptr};
   for (int i = 0; i < 4; ++i) {
     const int64_t lq = i & 1 ? a.lddo : a.ldq, lk = i & 1 ? a.ldv : a.ldk;
-    if (!head_map(&qr[i], qo[i], a.D, N, lq, a.Hq, TR) || !head_map(&qs[i], qo[i], a.D, N, lq, a.Hq, C::BT) ||
-        !head_map(&kr[i], kv[i], a.D, N, lk, a.Hkv, TR) || !head_map(&ks[i], kv[i], a.D, N, lk, a.Hkv, C::BT))
+    if (!head_map(&qr[i], qo[i], a.D, N, lq, a.Hq, TR) || !head_map(&kr[i], kv[i], a.D, N, lk, a.Hkv, TR))
+      return cudaErrorInvalidValue;
+    qs[i] = qr[i];
+    ks[i] = kr[i];
+    if (C::BT != TR && (!head_map(&qs[i], qo[i], a.D, N, lq, a.Hq, C::BT) ||
+                        !head_map(&ks[i], kv[i], a.D, N, lk, a.Hkv, C::BT)))
       return cudaErrorInvalidValue;
   }
   static PerDeviceOnce once;

@@ -263,67 +263,70 @@ class _Call:
     """Argument struct of one operator call, filled tensor by tensor.  The first tensor sets
     the device; every other must live there, have the stated type, and hold the stated rows and
     columns with unit stride along its rows."""
+    __slots__ = ("a", "device")
 
     def __init__(self, args, first):
         if not first.is_cuda:
             raise ValueError(f"expected CUDA tensors, got one on {first.device}")
-        self.a, self.device = args, first.device
+        self.a, self.device = args, first.get_device()
 
     def _base(self, t, name, dtype):
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-        if t.device != self.device:
-            raise ValueError(f"{name}: on {t.device}, expected {self.device}")
+        if t.get_device() != self.device:
+            raise ValueError(f"{name}: on {t.device}, expected cuda:{self.device}")
 
-    def rows(self, name, t, dtype, rows, cols, ld=None):
+    def rows(self, name, t, dtype, rows, cols, ld, step=0):
         """A row buffer [rows][>= cols]; ``ld`` names the struct's leading-dimension field, which
-        a tangent shares with its primal."""
+        a tangent shares with its primal (``step``).  Returns the leading dimension."""
         if t is None:
-            return
+            return step
         self._base(t, name, dtype)
-        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < cols or \
-                (t.shape[1] > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}, expected "
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 2 or shape[0] != rows or shape[1] < cols or (stride[1] != 1 and shape[1] > 1):
+            raise ValueError(f"{name}: shape {tuple(shape)}, strides {stride}, expected "
                              f"[{rows}][{cols} or more] with unit stride along its rows")
         # one row has no stride: any leading dimension that holds it will do
-        step = t.stride(0) if rows > 1 else -(-t.shape[1] // 8) * 8
-        have = getattr(self.a, ld)
-        if have and have != step and rows > 1:
-            raise ValueError(f"{name}: row stride {step}, expected {have} as its primal has")
-        if not have:
-            setattr(self.a, ld, step)
+        have = stride[0] if rows > 1 else -(-shape[1] // 8) * 8
+        if step and have != step and rows > 1:
+            raise ValueError(f"{name}: row stride {have}, expected {step} as its primal has")
+        if not step:
+            setattr(self.a, ld, have)
+            step = have
         setattr(self.a, name, t.data_ptr())
+        return step
 
     def vec(self, name, t, dtype, shape):
         if t is None:
             return
         self._base(t, name, dtype)
-        if tuple(t.shape) != shape or not t.is_contiguous():
+        if t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{name}: shape {tuple(t.shape)}, expected contiguous {shape}")
         setattr(self.a, name, t.data_ptr())
 
-    def seq(self, seq_start, n_seq):
-        import torch
+    def seq(self, seq_start, n_seq, int32):
         if seq_start is not None:
             if seq_start.dim() != 1 or seq_start.shape[0] < 2:
                 raise ValueError(f"seq_start: shape {tuple(seq_start.shape)}, expected [n_seq + 1]")
             n_seq = seq_start.shape[0] - 1
-            self.vec("seq_start", seq_start, torch.int32, (n_seq + 1,))
+            self.vec("seq_start", seq_start, int32, (n_seq + 1,))
         self.a.n_seq = n_seq
 
     def work(self, work):
         if work is None:
             return
-        if work.device != self.device or not work.is_contiguous():
-            raise ValueError(f"work: expected a contiguous tensor on {self.device}")
+        if work.get_device() != self.device or not work.is_contiguous():
+            raise ValueError(f"work: expected a contiguous tensor on cuda:{self.device}")
         self.a.work, self.a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
 
     def run(self, fn, stream):
         import torch
-        if self.device.index != torch.cuda.current_device():
+        if self.device != torch.cuda.current_device():
             with torch.cuda.device(self.device):
                 return self.run(fn, stream)
-        st = getattr(lib(), fn)(C.byref(self.a), _stream(stream))
+        # the current stream's handle without building a Stream object around it (4 us a call)
+        handle = torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+        st = getattr(_lib, fn)(C.byref(self.a), handle)
         if st != 0:
             raise MixflowError(st, fn)
 
@@ -338,6 +341,7 @@ def _prec(t, name):
 def _rope_call(first, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
                pos, seq_start, n_seq, status):
     import torch
+    lib()
     a = mf_qk_rope_args()
     c = _Call(a, first)
     a.n_rows = first.shape[0]
@@ -346,7 +350,7 @@ def _rope_call(first, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk,
     for name, g in (("gq", gq), ("gk", gk), ("gqd", gqd), ("gkd", gkd)):
         c.vec(name, g, torch.float32, (head_dim,))
     c.vec("pos", pos, torch.int32, (a.n_rows,))
-    c.seq(seq_start, n_seq)
+    c.seq(seq_start, n_seq, torch.int32)
     c.vec("status", status, torch.int32, (1,))
     return c
 
@@ -361,10 +365,8 @@ def mf_qk_rope_fwd(x, y, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, xd
                    pos, seq_start, n_seq, status)
     c.a.x_prec, c.a.y_prec = _prec(x, "x"), _prec(y, "y")
     n, cols = x.shape[0], (n_heads + n_kv_heads + n_copy_heads) * head_dim
-    c.rows("x", x, x.dtype, n, cols, "ldx")
-    c.rows("xd", xd, x.dtype, n, cols, "ldx")
-    c.rows("y", y, y.dtype, n, cols, "ldy")
-    c.rows("yd", yd, y.dtype, n, cols, "ldy")
+    c.rows("xd", xd, x.dtype, n, cols, "ldx", c.rows("x", x, x.dtype, n, cols, "ldx"))
+    c.rows("yd", yd, y.dtype, n, cols, "ldy", c.rows("y", y, y.dtype, n, cols, "ldy"))
     c.run("mf_qk_rope_fwd", stream)
 
 
@@ -381,12 +383,10 @@ def mf_qk_rope_bwd(dy, dx, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, 
     c.a.x_prec = c.a.y_prec if x is None else _prec(x, "x")
     n, cols = dy.shape[0], (n_heads + n_kv_heads + n_copy_heads) * head_dim
     qk = (n_heads + n_kv_heads) * head_dim
-    c.rows("dy", dy, dy.dtype, n, cols, "lddy")
-    c.rows("dyd", dyd, dy.dtype, n, cols, "lddy")
-    c.rows("dx", dx, dy.dtype, n, cols, "lddx")
-    c.rows("dxd", dxd, dy.dtype, n, cols, "lddx")
-    c.rows("x", x, None if x is None else x.dtype, n, qk, "ldx")
-    c.rows("xd", xd, None if x is None else x.dtype, n, qk, "ldx")
+    c.rows("dyd", dyd, dy.dtype, n, cols, "lddy", c.rows("dy", dy, dy.dtype, n, cols, "lddy"))
+    c.rows("dxd", dxd, dy.dtype, n, cols, "lddx", c.rows("dx", dx, dy.dtype, n, cols, "lddx"))
+    if x is not None:
+        c.rows("xd", xd, x.dtype, n, qk, "ldx", c.rows("x", x, x.dtype, n, qk, "ldx"))
     for name, g in (("dgq", dgq), ("dgk", dgk), ("dgqd", dgqd), ("dgkd", dgkd)):
         c.vec(name, g, torch.float32, (head_dim,))
     c.work(work)
@@ -421,15 +421,16 @@ def _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, r
                n_seq, scale, status):
     import torch
     bf, f32 = torch.bfloat16, torch.float32
+    lib()
     a = mf_attn_args()
     c = _Call(a, q)
     n, cq, ck = q.shape[0], n_heads * head_dim, n_kv_heads * head_dim
     a.n_rows, a.n_heads, a.n_kv_heads, a.head_dim, a.scale = n, n_heads, n_kv_heads, head_dim, scale
-    c.seq(seq_start, n_seq)
-    for name, t, cols, ld in (("q", q, cq, "ldq"), ("k", k, ck, "ldk"), ("v", v, ck, "ldv"),
-                              ("qd", qd, cq, "ldq"), ("kd", kd, ck, "ldk"), ("vd", vd, ck, "ldv"),
-                              ("o", o, cq, "ldo"), ("od", od, cq, "ldo")):
-        c.rows(name, t, bf, n, cols, ld)
+    c.seq(seq_start, n_seq, torch.int32)
+    c.rows("qd", qd, bf, n, cq, "ldq", c.rows("q", q, bf, n, cq, "ldq"))
+    c.rows("kd", kd, bf, n, ck, "ldk", c.rows("k", k, bf, n, ck, "ldk"))
+    c.rows("vd", vd, bf, n, ck, "ldv", c.rows("v", v, bf, n, ck, "ldv"))
+    c.rows("od", od, bf, n, cq, "ldo", c.rows("o", o, bf, n, cq, "ldo"))
     c.vec("lse", lse, f32, (n_heads, n))
     c.vec("rbar", rbar, f32, (n_heads, n))
     c.vec("status", status, torch.int32, (1,))
@@ -453,11 +454,11 @@ def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim,
     c = _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, rbar, seq_start,
                    n_seq, scale, status)
     n, cq, ck = q.shape[0], n_heads * head_dim, n_kv_heads * head_dim
-    for name, t, cols, ld in (("d_o", d_o, cq, "lddo"), ("d_od", dod, cq, "lddo"),
-                              ("dq", dq, cq, "lddq"), ("dk", dk, ck, "lddk"), ("dv", dv, ck, "lddv"),
-                              ("dqd", dqd, cq, "lddq"), ("dkd", dkd, ck, "lddk"),
-                              ("dvd", dvd, ck, "lddv")):
-        c.rows(name, t, torch.bfloat16, n, cols, ld)
+    bf = torch.bfloat16
+    c.rows("d_od", dod, bf, n, cq, "lddo", c.rows("d_o", d_o, bf, n, cq, "lddo"))
+    c.rows("dqd", dqd, bf, n, cq, "lddq", c.rows("dq", dq, bf, n, cq, "lddq"))
+    c.rows("dkd", dkd, bf, n, ck, "lddk", c.rows("dk", dk, bf, n, ck, "lddk"))
+    c.rows("dvd", dvd, bf, n, ck, "lddv", c.rows("dv", dv, bf, n, ck, "lddv"))
     c.work(work)
     c.run("mf_attn_bwd", stream)
 
