@@ -823,8 +823,7 @@ template <bool DUAL, int HDP, int EW>
 __device__ __forceinline__ void row_dots(const TcParams2& p, int row0, int nvalid, int h, int w,
                                          int lane, float2* out) {
   constexpr int LPR = HDP / 8, STEP = EW * (32 / LPR);
-  auto f8 = [](const __nv_bfloat16* x, bool on, float (&v)[8]) {
-    const uint4 w4 = on ? *reinterpret_cast<const uint4*>(x) : make_uint4(0, 0, 0, 0);
+  auto f8 = [](const uint4& w4, float (&v)[8]) {
     const uint32_t u[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -833,29 +832,45 @@ __device__ __forceinline__ void row_dots(const TcParams2& p, int row0, int nvali
     }
   };
   const int c = 8 * (lane % LPR);
+  constexpr int IT = TR / STEP, NB = DUAL || IT > 4 ? IT / 2 : IT;   // rows read together
 #pragma unroll
-  for (int r = w * (32 / LPR) + lane / LPR; r < TR; r += STEP) {
-    const bool on = r < nvalid && c < p.D;
-    const int64_t oo = (static_cast<int64_t>(row0) + r) * p.ldo + h * p.D + c;
-    const int64_t og = (static_cast<int64_t>(row0) + r) * p.lddo + h * p.D + c;
-    float o[8], g[8], od[8], gd[8], s = 0.f, sd = 0.f;
-    f8(p.o + oo, on, o);
-    f8(p.d_o + og, on, g);
-    if (DUAL) {
-      f8(p.od + oo, on, od);
-      f8(p.d_od + og, on, gd);
+  for (int i0 = 0; i0 < IT; i0 += NB) {
+    uint4 x[NB][DUAL ? 4 : 2];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int r = w * (32 / LPR) + lane / LPR + (i0 + i) * STEP;
+      const bool on = r < nvalid && c < p.D;
+      const int64_t oo = (static_cast<int64_t>(row0) + r) * p.ldo + h * p.D + c;
+      const int64_t og = (static_cast<int64_t>(row0) + r) * p.lddo + h * p.D + c;
+      const uint4 z = make_uint4(0, 0, 0, 0);
+      x[i][0] = on ? *reinterpret_cast<const uint4*>(p.o + oo) : z;
+      x[i][1] = on ? *reinterpret_cast<const uint4*>(p.d_o + og) : z;
+      if (DUAL) {
+        x[i][DUAL ? 2 : 0] = on ? *reinterpret_cast<const uint4*>(p.od + oo) : z;
+        x[i][DUAL ? 3 : 0] = on ? *reinterpret_cast<const uint4*>(p.d_od + og) : z;
+      }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s += o[i] * g[i];
-      if (DUAL) sd += o[i] * gd[i] + od[i] * g[i];
-    }
+    for (int i = 0; i < NB; ++i) {
+      float o[8], g[8], od[8], gd[8], s = 0.f, sd = 0.f;
+      f8(x[i][0], o);
+      f8(x[i][1], g);
+      if (DUAL) {
+        f8(x[i][DUAL ? 2 : 0], od);
+        f8(x[i][DUAL ? 3 : 0], gd);
+      }
 #pragma unroll
-    for (int k = LPR / 2; k > 0; k >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, k);
-      if (DUAL) sd += __shfl_xor_sync(0xffffffffu, sd, k);
+      for (int e = 0; e < 8; ++e) {
+        s += o[e] * g[e];
+        if (DUAL) sd += o[e] * gd[e] + od[e] * g[e];
+      }
+#pragma unroll
+      for (int k = LPR / 2; k > 0; k >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, k);
+        if (DUAL) sd += __shfl_xor_sync(0xffffffffu, sd, k);
+      }
+      if (lane % LPR == 0) out[w * (32 / LPR) + lane / LPR + (i0 + i) * STEP] = make_float2(s, sd);
     }
-    if (lane % LPR == 0) out[r] = make_float2(s, sd);
   }
 }
 
@@ -1701,13 +1716,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 }
 
 // CTAs of a cluster that share the query heads of a group in the key-row kernel: the fewest
-// (dividing the group, at most 8) that fill the GPU's places four times over.
+// (dividing the group, at most 8) that fill the GPU's places three times over.
 int kv_share(int group, int64_t ctas, int per_sm) {
   int best = 1;
   for (int n = 1; n <= 8 && n <= group; ++n) {
     if (group % n) continue;
     best = n;
-    if (ctas * n >= 4ll * 152 * per_sm) break;
+    if (ctas * n >= 3ll * 152 * per_sm) break;
   }
   return best;
 }
