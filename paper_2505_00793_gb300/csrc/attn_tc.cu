@@ -269,10 +269,12 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..5 hold
 // the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).  The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T
 // into S'; P [V | V'] -> [O | T], then (P (*) S') V into T; o' = T / l - rbar o.
-template <bool DUAL, int HDP>
+// TKEYS keys a tile: 64 where the tangents leave no TMEM for more, and where many CTAs are to be
+// had: tiles of 64 let three of them, not two, fill each other's waits on an SM (launch_fwd).
+template <bool DUAL, int HDP, int TKEYS>
 struct FwdCfg {
   static constexpr int NA = HDP / 64;                      // 64-column atoms of a head
-  static constexpr int TK = DUAL ? 64 : 128;               // keys a tile
+  static constexpr int TK = TKEYS;
   static constexpr int NT = DUAL ? 2 : 1;
   static constexpr int Q_B = NT * NA * ATOM128;
   static constexpr int KATOM = TK * 128;
@@ -281,9 +283,10 @@ struct FwdCfg {
   static constexpr int SMEM = Q_B + 2 * STAGES * TILE_B + 1024;
   static constexpr int EW = 4;                             // row warps: a thread a row
   static constexpr int THREADS = 64 + 32 * EW;
-  static constexpr int CTAS = 2;
-  static constexpr uint32_t TMEM_COLS = 256;
-  static constexpr uint32_t C_S = 0, C_SD = 64, C_O = 128, C_T = 192;
+  static constexpr bool SMALL = TK * NT + HDP * NT <= 128;
+  static constexpr int CTAS = SMALL ? 3 : 2;
+  static constexpr uint32_t TMEM_COLS = SMALL ? 128 : 256;
+  static constexpr uint32_t C_S = 0, C_SD = 64, C_O = NT * TK, C_T = 192;
 };
 
 struct TcParams2 {
@@ -326,13 +329,13 @@ __device__ __forceinline__ void stage_out(const uint8_t* buf, int nvalid, int D,
   }
 }
 
-template <bool DUAL, int HDP>
-__global__ void __launch_bounds__(FwdCfg<DUAL, HDP>::THREADS, FwdCfg<DUAL, HDP>::CTAS)
+template <bool DUAL, int HDP, int TKEYS>
+__global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL, HDP, TKEYS>::CTAS)
     attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                        const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQd,
                        const __grid_constant__ CUtensorMap tmKd, const __grid_constant__ CUtensorMap tmVd,
                        const __grid_constant__ TcParams2 p) {
-  using C = FwdCfg<DUAL, HDP>;
+  using C = FwdCfg<DUAL, HDP, TKEYS>;
   constexpr int TK = C::TK, NA = C::NA;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   // barriers, as byte offsets in a set; one set per walk
@@ -722,9 +725,9 @@ TcParams2 tc_params(const AttnParams& a) {
   return p;
 }
 
-template <bool DUAL, int HDP>
+template <bool DUAL, int HDP, int TKEYS>
 cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
-  using C = FwdCfg<DUAL, HDP>;
+  using C = FwdCfg<DUAL, HDP, TKEYS>;
   CUtensorMap q, k, v, qd, kd, vd;
   const int N = a.seq.rows;
   if (!head_map(&q, a.q, a.D, N, a.ldq, a.Hq, TR) || !head_map(&k, a.k, a.D, N, a.ldk, a.Hkv, C::TK) ||
@@ -735,12 +738,12 @@ cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
     return cudaErrorInvalidValue;
   static PerDeviceOnce once;
   cudaError_t e = once.run([](int&) {
-    return cudaFuncSetAttribute(attn_tc_fwd_kernel<DUAL, HDP>,
+    return cudaFuncSetAttribute(attn_tc_fwd_kernel<DUAL, HDP, TKEYS>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   });
   if (e != cudaSuccess) return e;
   const TcParams2 p = tc_params(a);
-  return launch_k(attn_tc_fwd_kernel<DUAL, HDP>, tile_grid(a.Hq, p.tiles), dim3(C::THREADS),
+  return launch_k(attn_tc_fwd_kernel<DUAL, HDP, TKEYS>, tile_grid(a.Hq, p.tiles), dim3(C::THREADS),
                   C::SMEM, s, q, k, v, qd, kd, vd, p);
 }
 
@@ -1791,8 +1794,14 @@ cudaError_t attn_tc_bwd(const AttnParams& a, bool dual, cudaStream_t s) {
 }
 
 cudaError_t attn_tc_fwd(const AttnParams& a, bool dual, cudaStream_t s) {
-  if (dual) return launch_fwd<true, 64>(a, s);
-  return a.D <= 64 ? launch_fwd<false, 64>(a, s) : launch_fwd<false, 128>(a, s);
+  if (dual) return launch_fwd<true, 64, 64>(a, s);
+  if (a.D > 64) return launch_fwd<false, 128, 128>(a, s);
+  // From two rounds of three CTAs an SM on, tiles of 64 keys: 16 heads of 64, six sequences in
+  // 8192 rows 79 us against 90 with tiles of 128 and two CTAs, in 7168 rows (896 CTAs) 76 against
+  // 73, in 4096 rows 39 against 37: with fewer CTAs a walk's own length counts, and it has twice
+  // as many steps.
+  const int64_t ctas = static_cast<int64_t>((a.seq.rows + TR - 1) / TR) * a.Hq;
+  return ctas >= 2 * 3 * 152 ? launch_fwd<false, 64, 64>(a, s) : launch_fwd<false, 64, 128>(a, s);
 }
 
 }  // namespace mf
