@@ -532,6 +532,22 @@ mf_status mf_attn_fwd(const mf_attn_args* args, void* stream);
 mf_status mf_attn_bwd(const mf_attn_args* args, void* stream);
 mf_status mf_attn_work_bytes(const mf_attn_args* args, size_t* bytes);
 
+/* A decoder handle (desc->arch MF_ARCH_DECODER, MF_PREC_BF16, d_model / n_heads <= 64) whose
+ * attention is made of these operators, everything else as with mf_create:
+ *  n_kv_heads  key/value heads, a divisor of n_heads (0 = n_heads): Wqkv is
+ *              [d][(n_heads + 2 n_kv_heads) d_model/n_heads], columns q | k | v;
+ *  qk_norm     1: RMS norm (desc->rms_eps) of every query and key head before the rotation, with
+ *              gains gq, gk [d_model/n_heads] of each block; they lie behind the block's g1 in
+ *              the flat parameter vector (g1, gq, gk, Wqkv, ...).  0: none;
+ *  rope        rotary positions; base 0 = desc->rope_base.
+ * Errors: MF_ERR_INVALID_ARG, MF_ERR_UNSUPPORTED (float32, wider heads), MF_ERR_CUDA. */
+typedef struct {
+  int n_kv_heads, qk_norm;
+  mf_rope_desc rope;
+} mf_decoder_heads;
+
+mf_status mf_create_decoder(const mf_model_desc* desc, const mf_decoder_heads* heads, mf_handle* out);
+
 #ifdef __cplusplus
 }
 #endif

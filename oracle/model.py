@@ -21,6 +21,8 @@ import math
 
 import torch
 
+from oracle import packed
+
 F64 = torch.float64
 
 
@@ -109,6 +111,22 @@ def rope(x, base):
     return x * cos + rot * sin
 
 
+def packed_heads(w, P, l, qkv):
+    """Attention of grouped heads with head norms and rotary variants: qkv [B, S, cols] ->
+    [B, S, d], the batch as packed sequences (oracle/packed.py)."""
+    B, S = qkv.shape[:2]
+    H, Hkv, dh = w.n_heads, w.n_kv_heads or w.n_heads, w.d_model // w.n_heads
+    r = {"layout": "half", "dims": 0, "base": w.rope_base, "scaling": "none", "factor": 1.0,
+         "orig_len": 0, "low_turns": 1.0, "high_turns": 4.0, "mscale": 1.0, **(w.rope or {})}
+    rates = packed.rates(r["dims"] or dh, r["base"], r["scaling"], r["factor"], r["orig_len"],
+                         r["low_turns"], r["high_turns"])
+    gains = (P[f"gq.{l}"], P[f"gk.{l}"]) if w.qk_norm else (None, None)
+    y = packed.qk_rope(qkv.reshape(B * S, -1), *gains, H, Hkv, dh, packed.positions([S] * B),
+                       rates, r["layout"], r["mscale"], w.rms_eps)
+    q, k, v = y.split([H * dh, Hkv * dh, Hkv * dh], 1)
+    return packed.attention(q, k, v, H, Hkv, dh, [S] * B, dh ** -0.5)[0].reshape(B, S, -1)
+
+
 def decoder_logits(w, theta, ids):
     """Decoder-only transformer: token embedding, n_blocks pre-RMSNorm blocks (causal
     multi-head attention with RoPE, GELU MLP, residual connections), final RMSNorm, untied
@@ -121,13 +139,17 @@ def decoder_logits(w, theta, ids):
     mask = torch.triu(torch.ones(S, S, dtype=torch.bool), diagonal=1)
     for l in range(w.n_blocks):
         h = rmsnorm(x, P[f"g1.{l}"], w.rms_eps)
-        qkv = h @ P[f"Wqkv.{l}"].reshape(d, 3 * d)
-        q, k, v = (t.reshape(B, S, H, dh).transpose(1, 2) for t in qkv.split(d, dim=-1))
-        q, k = rope(q, w.rope_base), rope(k, w.rope_base)
-        s = (q @ k.transpose(-1, -2)) / math.sqrt(dh)
-        s = s.masked_fill(mask, float("-inf"))
-        o = torch.softmax(s, dim=-1) @ v                             # [B, H, S, dh]
-        x = x + o.transpose(1, 2).reshape(B, S, d) @ P[f"Wo.{l}"].reshape(d, d)
+        qkv = h @ P[f"Wqkv.{l}"].reshape(d, -1)
+        if w.packed_heads:
+            o = packed_heads(w, P, l, qkv)
+        else:
+            q, k, v = (t.reshape(B, S, H, dh).transpose(1, 2) for t in qkv.split(d, dim=-1))
+            q, k = rope(q, w.rope_base), rope(k, w.rope_base)
+            s = (q @ k.transpose(-1, -2)) / math.sqrt(dh)
+            s = s.masked_fill(mask, float("-inf"))
+            o = torch.softmax(s, dim=-1) @ v                         # [B, H, S, dh]
+            o = o.transpose(1, 2).reshape(B, S, d)
+        x = x + o @ P[f"Wo.{l}"].reshape(d, d)
         h2 = rmsnorm(x, P[f"g2.{l}"], w.rms_eps)
         x = x + act("gelu", h2 @ P[f"W1.{l}"].reshape(d, F)) @ P[f"W2.{l}"].reshape(F, d)
     return rmsnorm(x, P["gf"], w.rms_eps) @ P["Wh"].reshape(d, V)

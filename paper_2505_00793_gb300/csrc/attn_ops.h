@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/mixflow.h"
+
 namespace mf {
 
 // Sequences of a packed batch: rows 0 .. rows-1; start [n+1] on the device, or null for
@@ -43,6 +45,8 @@ struct RopeParams {
   int stage_bytes = 0, ring_bytes = 0;
   uint64_t phase[64];                   // 2^-64 turns a position, per rotated pair
 };
+// Whether r describes rotary positions of heads of D elements.
+bool rope_desc_ok(const mf_rope_desc& r, int D);
 cudaError_t qk_rope(RopeParams p, bool bwd, bool x_bf16, bool y_bf16, cudaStream_t s);
 
 struct AttnParams {

@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/mixflow.h"
+#include "attn_ops.h"
 #include "decoder_layout.h"
 #include "internal.h"
 #include "launch.cuh"
@@ -1728,7 +1729,7 @@ const char* mf_status_string(mf_status s) {
 
 const char* mf_last_error(mf_handle h) { return h ? h->err.c_str() : "NULL handle"; }
 
-mf_status mf_create(const mf_model_desc* d, mf_handle* out) {
+static mf_status create(const mf_model_desc* d, const mf_decoder_heads* heads, mf_handle* out) {
   if (!d || !out) return MF_ERR_INVALID_ARG;
   *out = nullptr;
   if (d->precision != MF_PREC_FP32 && d->precision != MF_PREC_BF16) return MF_ERR_INVALID_ARG;
@@ -1740,7 +1741,16 @@ mf_status mf_create(const mf_model_desc* d, mf_handle* out) {
         d->d_model % 8 != 0 || d->vocab < 2 || d->vocab % 8 != 0 || d->seq_len < 8 ||
         d->seq_len % 8 != 0)
       return MF_ERR_INVALID_ARG;
+    if (heads) {
+      const int dh = d->d_model / d->n_heads;
+      if (heads->n_kv_heads < 0 || (heads->n_kv_heads > 0 && d->n_heads % heads->n_kv_heads != 0) ||
+          (heads->qk_norm != 0 && heads->qk_norm != 1) || !(heads->rope.base >= 0.f) || dh > 128 ||
+          !mf::rope_desc_ok(heads->rope, dh))
+        return MF_ERR_INVALID_ARG;
+      if (d->precision != MF_PREC_BF16 || dh > 64) return MF_ERR_UNSUPPORTED;
+    }
   } else {
+    if (heads) return MF_ERR_INVALID_ARG;
     if (d->arch != MF_ARCH_MLP) return MF_ERR_INVALID_ARG;
     if (d->n_layers < 1 || d->n_layers > MF_MAX_LAYERS) return MF_ERR_INVALID_ARG;
     for (int i = 0; i <= d->n_layers; ++i)
@@ -1757,7 +1767,7 @@ mf_status mf_create(const mf_model_desc* d, mf_handle* out) {
   h->md = *d;
   h->decoder = decoder;
   if (decoder) {
-    h->Ly = dec_layout(*d);
+    h->Ly = dec_layout(*d, heads);
     h->P = dec_param_count(h->Ly);
     h->bf16 = d->precision == MF_PREC_BF16;
     h->dims.assign(1, d->d_model);
@@ -1800,6 +1810,12 @@ mf_status mf_create(const mf_model_desc* d, mf_handle* out) {
   }
   *out = h;
   return MF_OK;
+}
+
+mf_status mf_create(const mf_model_desc* d, mf_handle* out) { return create(d, nullptr, out); }
+
+mf_status mf_create_decoder(const mf_model_desc* d, const mf_decoder_heads* heads, mf_handle* out) {
+  return heads ? create(d, heads, out) : MF_ERR_INVALID_ARG;
 }
 
 mf_status mf_destroy(mf_handle h) {

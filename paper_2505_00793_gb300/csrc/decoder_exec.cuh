@@ -12,8 +12,9 @@
 // otherwise); where those do not apply (float32 decoders, heads other than 64 wide,
 // sequences that are not whole 64-token tiles), the scores, P V and the four backward
 // products run as batched dual GEMMs over batch x heads with the softmax row kernels between
-// them.  RMSNorm, RoPE, the embedding gradient and the loss are row kernels
-// (decoder_kernels.cu).
+// them.  Decoders made with mf_create_decoder (grouped heads, head norms) run mf_qk_rope_* and
+// mf_attn_* instead, the batch being packed sequences of equal length.  RMSNorm, RoPE, the
+// embedding gradient and the loss are row kernels (decoder_kernels.cu).
 
 // A parameter tensor as seen by the fused update/cast kernel: rows x cols at off; the first
 // `cast` rows (0 or all) get bf16 operand copies.
@@ -26,8 +27,8 @@ std::vector<DecTensor> dec_tensors(const DecLayout& Ly) {
   std::vector<DecTensor> t;
   t.push_back({Ly.E, Ly.V, Ly.d, 0});
   for (int l = 0; l < Ly.L; ++l) {
-    t.push_back({Ly.g1[l], 1, Ly.d, 0});
-    t.push_back({Ly.Wqkv[l], Ly.d, 3 * Ly.d, Ly.d});
+    t.push_back({Ly.g1[l], 1, Ly.d + (Ly.norm ? 2 * Ly.dh : 0), 0});   // and gq, gk behind it
+    t.push_back({Ly.Wqkv[l], Ly.d, Ly.W3, Ly.d});
     t.push_back({Ly.Wo[l], Ly.d, Ly.d, Ly.d});
     t.push_back({Ly.g2[l], 1, Ly.d, 0});
     t.push_back({Ly.W1[l], Ly.d, Ly.F, Ly.d});
@@ -68,6 +69,10 @@ struct DecPlan {
   std::vector<size_t> fst;
   size_t fD = 0;
   size_t rope = 0;   // RoPE (cos, sin) table [S][dh/2]
+  // heads of mf_create_decoder: per block the projected rows that the head norms read again
+  // (float32) and the rotated ones (operand type); workspaces, a place for unwanted gradients
+  std::vector<size_t> xh, xhd, yh, yhd;
+  size_t rope_work = 0, rope_work_bytes = 0, gsink = 0;
 };
 
 DecPlan make_dec_plan(const mf_ctx* h, const DecLayout& Ly, int rows, int T, int n_theta_slots,
@@ -109,9 +114,10 @@ DecPlan make_dec_plan(const mf_ctx* h, const DecLayout& Ly, int rows, int T, int
     }
   }
   const size_t Nd4 = N * d * 4, NdT = N * d * es;
-  const size_t head = static_cast<size_t>(BH) * S * Ly.dh * es;
-  p.flash = h->flash && h->bf16 && mf::flash_supported(static_cast<int>(S), Ly.dh);
-  const size_t SS = p.flash ? 0 : static_cast<size_t>(BH) * S * S;
+  const size_t head = Ly.heads ? 0 : static_cast<size_t>(BH) * S * Ly.dh * es;
+  p.flash = !Ly.heads && h->flash && h->bf16 && mf::flash_supported(static_cast<int>(S), Ly.dh);
+  const bool fused = p.flash || Ly.heads;
+  const size_t SS = fused ? 0 : static_cast<size_t>(BH) * S * S;
   const size_t stat = static_cast<size_t>(BH) * S * 4;
   for (int l = 0; l < Ly.L; ++l) {
     p.x1.push_back(take(Nd4)); p.x1d.push_back(take(Nd4));
@@ -124,7 +130,11 @@ DecPlan make_dec_plan(const mf_ctx* h, const DecLayout& Ly, int rows, int T, int
     p.K.push_back(take(head)); p.Kd.push_back(take(head));
     p.Vv.push_back(take(head)); p.Vd.push_back(take(head));
     p.P.push_back(take(SS * es)); p.Pd.push_back(take(SS * es));
-    if (p.flash) p.fst.push_back(take(2 * stat));
+    if (fused) p.fst.push_back(take(2 * stat));
+    if (Ly.heads) {
+      p.yh.push_back(take(N * Ly.W3 * es)); p.yhd.push_back(take(N * Ly.W3 * es));
+      if (Ly.norm) { p.xh.push_back(take(N * Ly.W3 * 4)); p.xhd.push_back(take(N * Ly.W3 * 4)); }
+    }
     p.Om.push_back(take(NdT)); p.Omd.push_back(take(NdT));
     p.z1.push_back(take(N * F * 4)); p.z1d.push_back(take(N * F * 4));
     p.a1.push_back(take(N * F * es)); p.a1d.push_back(take(N * F * es));
@@ -135,26 +145,37 @@ DecPlan make_dec_plan(const mf_ctx* h, const DecLayout& Ly, int rows, int T, int
   p.Fl = take(N * V * 4); p.Fld = take(N * V * 4);
   p.lse = take(N * 4); p.ltok = take(N * 4); p.pf = take(N * 4); p.ldtok = take(N * 4);
   p.dF = take(N * V * es); p.dFd = take(N * V * es);
-  p.qkv = take(N * 3 * d * 4); p.qkvd = take(N * 3 * d * 4);
+  p.qkv = take(N * Ly.W3 * 4); p.qkvd = take(N * Ly.W3 * 4);
   p.Sc = take(SS * 4); p.Scd = take(SS * 4);
   // per-head float32 attention outputs (the fused attention writes them head-merged instead)
-  const size_t osz = p.flash ? 0 : static_cast<size_t>(BH) * S * Ly.dh * 4;
+  const size_t osz = fused ? 0 : static_cast<size_t>(BH) * S * Ly.dh * 4;
   p.O = take(osz); p.Od = take(osz);
   p.y = take(Nd4); p.yd = take(Nd4);
   p.dx = take(Nd4); p.dxd = take(Nd4); p.dh = take(Nd4); p.dhd = take(Nd4);
   p.dy = take(NdT); p.dyd = take(NdT);
-  p.dOh = take(head); p.dOhd = take(head);
+  p.dOh = take(Ly.heads ? NdT : head); p.dOhd = take(Ly.heads ? NdT : head);
   p.dP = take(SS * 4); p.dPd = take(SS * 4);
   p.dS = take(SS * es); p.dSd = take(SS * es);
-  if (p.flash) p.fD = take(2 * stat);
+  if (fused) p.fD = take(2 * stat);
   p.rope = take(static_cast<size_t>(S) * (Ly.dh / 2) * 2 * 4);
-  const size_t head4 = static_cast<size_t>(BH) * S * Ly.dh * 4;
+  const size_t head4 = Ly.heads ? 0 : static_cast<size_t>(BH) * S * Ly.dh * 4;
   p.dQ = take(head4); p.dQd = take(head4); p.dK = take(head4); p.dKd = take(head4);
   p.dV = take(head4); p.dVd = take(head4);
   if (ror)
     for (int l = 0; l < Ly.L; ++l) p.dxs.push_back(take(Nd4));
-  p.dqkv = take(N * 3 * d * es); p.dqkvd = take(N * 3 * d * es);
+  p.dqkv = take(N * Ly.W3 * es); p.dqkvd = take(N * Ly.W3 * es);
   p.dz1 = take(N * F * es); p.dz1d = take(N * F * es);
+  if (Ly.norm) {
+    mf_qk_rope_args ra;
+    memset(&ra, 0, sizeof(ra));
+    ra.n_heads = Ly.H;
+    ra.n_kv_heads = Ly.Hkv;
+    ra.head_dim = Ly.dh;
+    ra.xd = ra.dyd = &ra;   // with tangents
+    mf_qk_rope_work_bytes(&ra, &p.rope_work_bytes);
+    p.rope_work = take(p.rope_work_bytes);
+    p.gsink = take(2 * static_cast<size_t>(Ly.dh) * 4);
+  }
   p.bytes = o;
   return p;
 }
@@ -297,6 +318,115 @@ struct DecExec {
     return fa;
   }
 
+  // ---- heads of mf_create_decoder ------------------------------------------------------------------
+  void op(mf_status r, const char* what, int n) {
+    if (r != MF_OK && st == MF_OK) {
+      st = r;
+      h->err = std::string(what) + ": " + mf_status_string(r);
+    }
+    launched(n);
+  }
+  // the float32 rows [N][W3] of block l's projection
+  float* xrows(int l) const { return at<float>(Ly.norm ? p.xh[l] : p.qkv); }
+  float* xrowsd(int l) const { return at<float>(Ly.norm ? p.xhd[l] : p.qkvd); }
+  mf_qk_rope_args rope_args(int l, int rows, bool dual) const {
+    mf_qk_rope_args a;
+    memset(&a, 0, sizeof(a));
+    a.n_rows = static_cast<int64_t>(rows) * Ly.S;
+    a.n_seq = rows;
+    a.n_heads = Ly.H;
+    a.n_kv_heads = a.n_copy_heads = Ly.Hkv;
+    a.head_dim = Ly.dh;
+    a.x_prec = MF_PREC_FP32;
+    a.y_prec = MF_PREC_BF16;
+    a.eps = Ly.eps;
+    a.rope = Ly.rope;
+    a.x = xrows(l);
+    a.xd = dual ? xrowsd(l) : nullptr;
+    a.ldx = Ly.W3;
+    if (Ly.norm) {
+      a.gq = theta_cur + Ly.gq[l];
+      a.gk = theta_cur + Ly.gk[l];
+      a.gqd = dual ? u_cur + Ly.gq[l] : nullptr;
+      a.gkd = dual ? u_cur + Ly.gk[l] : nullptr;
+    }
+    a.status = h->d_status;
+    return a;
+  }
+  mf_attn_args attn_args(int l, int rows, bool dual) const {
+    mf_attn_args a;
+    memset(&a, 0, sizeof(a));
+    a.n_rows = static_cast<int64_t>(rows) * Ly.S;
+    a.n_seq = rows;
+    a.n_heads = Ly.H;
+    a.n_kv_heads = Ly.Hkv;
+    a.head_dim = Ly.dh;
+    const T* y = at<T>(p.yh[l]);
+    const T* yd = at<T>(p.yhd[l]);
+    const int k = Ly.H * Ly.dh, v = k + Ly.Hkv * Ly.dh;
+    a.q = y; a.k = y + k; a.v = y + v;
+    a.o = at<T>(p.Om[l]);
+    a.lse = at<float>(p.fst[l]);
+    if (dual) {
+      a.qd = yd; a.kd = yd + k; a.vd = yd + v;
+      a.od = at<T>(p.Omd[l]);
+      a.rbar = a.lse + static_cast<int64_t>(Ly.H) * a.n_rows;
+    }
+    a.ldq = a.ldk = a.ldv = Ly.W3;
+    a.ldo = Ly.d;
+    a.status = h->d_status;
+    return a;
+  }
+  void heads_fwd(int l, int rows, bool dual) {
+    mf_qk_rope_args ra = rope_args(l, rows, dual);
+    ra.y = at<T>(p.yh[l]);
+    ra.yd = dual ? at<T>(p.yhd[l]) : nullptr;
+    ra.ldy = Ly.W3;
+    op(mf_qk_rope_fwd(&ra, s), "head norms and rotary positions", 1);
+    const mf_attn_args aa = attn_args(l, rows, dual);
+    op(mf_attn_fwd(&aa, s), "packed attention", 1);
+  }
+  // From dO (float32, in dh) to the rows of dqkv and the gradients of the gains
+  void heads_bwd(int l, int rows, bool dual, float* out_h, float* out_g) {
+    const int N = rows * Ly.S;
+    mf::cast_rows<T>(at<float>(p.dh), N, Ly.d, at<T>(p.dOh), Ly.d, s);
+    launched();
+    if (dual) {
+      mf::cast_rows<T>(at<float>(p.dhd), N, Ly.d, at<T>(p.dOhd), Ly.d, s);
+      launched();
+    }
+    wait_seed_readers(2);    // dqkv's previous readers (the side stream) are done
+    T* dy = at<T>(p.dqkv);
+    T* dyd = at<T>(p.dqkvd);
+    mf_attn_args aa = attn_args(l, rows, dual);
+    const int k = Ly.H * Ly.dh, v = k + Ly.Hkv * Ly.dh;
+    aa.d_o = at<T>(p.dOh);
+    aa.lddo = Ly.d;
+    aa.dq = dy; aa.dk = dy + k; aa.dv = dy + v;
+    if (dual) {
+      aa.d_od = at<T>(p.dOhd);
+      aa.dqd = dyd; aa.dkd = dyd + k; aa.dvd = dyd + v;
+    }
+    aa.lddq = aa.lddk = aa.lddv = Ly.W3;
+    aa.work = at<float>(p.fD);
+    mf_attn_work_bytes(&aa, &aa.work_bytes);
+    op(mf_attn_bwd(&aa, s), "packed attention backward", 2);
+    mf_qk_rope_args ra = rope_args(l, rows, dual);
+    ra.dy = ra.dx = dy;      // in place
+    ra.dyd = ra.dxd = dual ? dyd : nullptr;
+    ra.lddy = ra.lddx = Ly.W3;
+    if (Ly.norm) {
+      float* sink = at<float>(p.gsink);
+      ra.dgq = out_g ? out_g + Ly.gq[l] : sink;
+      ra.dgk = out_g ? out_g + Ly.gk[l] : sink + Ly.dh;
+      ra.dgqd = dual ? out_h + Ly.gq[l] : nullptr;
+      ra.dgkd = dual ? out_h + Ly.gk[l] : nullptr;
+      ra.work = at<char>(p.rope_work);
+      ra.work_bytes = p.rope_work_bytes;
+    }
+    op(mf_qk_rope_bwd(&ra, s), "head norms and rotary positions backward", Ly.norm ? 2 : 1);
+  }
+
   GemmArgs lin(int M, int N, int K, const void* A0, const void* A1, int lda, const void* B0,
                const void* B1, int ldb, bool dual) const {
     GemmArgs g;
@@ -315,6 +445,7 @@ struct DecExec {
   }
 
   void prepare() {
+    if (Ly.heads) return;
     mf::dec_rope_table(Ly.S, Ly.dh, Ly.base, at<float>(p.rope), s);
     launched();
   }
@@ -358,14 +489,17 @@ struct DecExec {
       launched();
       // q k v = h Wqkv   (weights [d][3d] read MN-major)
       {
-        GemmArgs g = lin(N, 3 * d, d, at<T>(p.h1[l]), at<T>(p.h1d[l]), d, W(Ly.Wqkv[l]),
-                         Uw(Ly.Wqkv[l]), ld8(3 * d), dual);
+        GemmArgs g = lin(N, Ly.W3, d, at<T>(p.h1[l]), at<T>(p.h1d[l]), d, W(Ly.Wqkv[l]),
+                         Uw(Ly.Wqkv[l]), ld8(Ly.W3), dual);
         g.b_mn = true;
-        g.C0 = at<float>(p.qkv); g.ldc0 = 3 * d;
-        g.C1 = at<float>(p.qkvd); g.ldc1 = 3 * d;
+        g.C0 = xrows(l); g.ldc0 = Ly.W3;
+        g.C1 = xrowsd(l); g.ldc1 = Ly.W3;
         if (!dual) g.terms = mf::T_C0_A0B0;
         gemm(g);
       }
+      if (Ly.heads) {
+        heads_fwd(l, rows, dual);
+      } else {
       const float qscale = 1.f / sqrtf(static_cast<float>(dh));
       mf::RopeSplit<T> rs{at<float>(p.qkv), at<T>(p.Q[l]), at<T>(p.K[l]), at<T>(p.Vv[l])}, rsd;
       if (dual) rsd = {at<float>(p.qkvd), at<T>(p.Qd[l]), at<T>(p.Kd[l]), at<T>(p.Vd[l])};
@@ -410,6 +544,7 @@ struct DecExec {
       if (dual) {
         mf::dec_head_merge<T>(N, S, H, dh, at<float>(p.Od), at<T>(p.Omd[l]), d, s);
         launched();
+      }
       }
       }
       // y = O Wo
@@ -675,6 +810,9 @@ struct DecExec {
         g.C1 = at<float>(p.dhd); g.ldc1 = d;
         gemm(g);
       }
+      if (Ly.heads) {
+        heads_bwd(l, rows, dual, out_h, out_g);
+      } else {
       if (!p.flash) {
         mf::dec_head_split<T>(N, S, H, dh, at<float>(p.dh), at<T>(p.dOh), s);
         launched();
@@ -766,11 +904,12 @@ struct DecExec {
           launched();
         }
       }
-      wprod(d, 3 * d, at<T>(p.h1[l]), at<T>(p.h1d[l]), at<T>(p.dqkv), at<T>(p.dqkvd), dual,
+      }
+      wprod(d, Ly.W3, at<T>(p.h1[l]), at<T>(p.h1d[l]), at<T>(p.dqkv), at<T>(p.dqkvd), dual,
             G(Ly.Wqkv[l]), Hh(Ly.Wqkv[l]), WS_QKV);
       {
-        GemmArgs g = lin(N, d, 3 * d, at<T>(p.dqkv), at<T>(p.dqkvd), 3 * d, W(Ly.Wqkv[l]),
-                         Uw(Ly.Wqkv[l]), ld8(3 * d), dual);
+        GemmArgs g = lin(N, d, Ly.W3, at<T>(p.dqkv), at<T>(p.dqkvd), Ly.W3, W(Ly.Wqkv[l]),
+                         Uw(Ly.Wqkv[l]), ld8(Ly.W3), dual);
         g.C0 = at<float>(p.dh); g.ldc0 = d;
         g.C1 = at<float>(p.dhd); g.ldc1 = d;
         gemm(g);

@@ -181,6 +181,11 @@ mf_status attn_params(const mf_attn_args& a, bool bwd, AttnParams* p) {
 
 }  // namespace
 
+bool mf::rope_desc_ok(const mf_rope_desc& r, int D) {
+  RopeParams p;
+  return make_rope(r, D, &p);
+}
+
 extern "C" {
 
 mf_status mf_qk_rope_work_bytes(const mf_qk_rope_args* args, size_t* bytes) {

@@ -38,7 +38,7 @@ EXPORTS = ["mf_create", "mf_destroy", "mf_set_allocator", "mf_param_count",
            "mf_set_kernel_timing", "mf_kernel_time", "mf_inject_fault", "mf_dual_gemm_bf16",
            "mf_hvp_noalloc", "mf_set_option", "mf_replay_gemms", "mf_checkpoint_plan",
            "mf_qk_rope_fwd", "mf_qk_rope_bwd", "mf_qk_rope_work_bytes", "mf_attn_fwd",
-           "mf_attn_bwd", "mf_attn_work_bytes"]
+           "mf_attn_bwd", "mf_attn_work_bytes", "mf_create_decoder"]
 
 
 class mf_model_desc(C.Structure):
@@ -64,6 +64,10 @@ class mf_rope_desc(C.Structure):
     _fields_ = [("layout", C.c_int), ("dims", C.c_int), ("base", C.c_float),
                 ("scaling", C.c_int), ("factor", C.c_float), ("orig_len", C.c_int),
                 ("low_turns", C.c_float), ("high_turns", C.c_float), ("mscale", C.c_float)]
+
+
+class mf_decoder_heads(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int), ("qk_norm", C.c_int), ("rope", mf_rope_desc)]
 
 
 def _ptrs(names):
@@ -107,6 +111,8 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     H = C.c_void_p
     sig = {
         "mf_create": ([C.POINTER(mf_model_desc), C.POINTER(H)], C.c_int),
+        "mf_create_decoder": ([C.POINTER(mf_model_desc), C.POINTER(mf_decoder_heads), C.POINTER(H)],
+                              C.c_int),
         "mf_destroy": ([H], C.c_int),
         "mf_set_allocator": ([H, vp, vp, vp], C.c_int),
         "mf_param_count": ([H, C.POINTER(mf_loop_desc), i64p, i64p], C.c_int),
@@ -204,6 +210,15 @@ def model_desc_for(w) -> mf_model_desc:
     d.precision = PRECISIONS[w.precision]
     d.chain_steps = int(w.extra.get("chain_steps", 0))
     return d
+
+
+def decoder_heads_for(w) -> mf_decoder_heads | None:
+    """mf_decoder_heads of a ``synth.Workload`` whose decoder has grouped heads, head norms or
+    rotary positions of its own (None: mf_create does)."""
+    if getattr(w, "arch", "mlp") != "decoder" or not w.packed_heads:
+        return None
+    rope = {"base": w.rope_base, **(w.rope or {})}
+    return mf_decoder_heads(w.n_kv_heads, int(w.qk_norm), rope_desc(**rope))
 
 
 def checkpoint_plan(T: int, ckpt_every: int = 1, ckpt_slots: int = 0):
@@ -466,19 +481,22 @@ def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim,
 class MixFlow:
     """One library handle for one inner-model architecture."""
 
-    def __init__(self, desc: mf_model_desc):
+    def __init__(self, desc: mf_model_desc, heads: mf_decoder_heads | None = None):
         self._lib = lib()
         self.desc = desc
         h = C.c_void_p()
-        st = self._lib.mf_create(C.byref(desc), C.byref(h))
+        if heads is None:
+            st = self._lib.mf_create(C.byref(desc), C.byref(h))
+        else:
+            st = self._lib.mf_create_decoder(C.byref(desc), C.byref(heads), C.byref(h))
         if st != 0:
-            raise MixflowError(st, "mf_create")
+            raise MixflowError(st, "mf_create" if heads is None else "mf_create_decoder")
         self.h = h
         self.x_dtype, self.y_dtype = io_dtypes(desc)
 
     @classmethod
     def for_workload(cls, w):
-        return cls(model_desc_for(w))
+        return cls(model_desc_for(w), decoder_heads_for(w))
 
     def close(self):
         if getattr(self, "h", None):

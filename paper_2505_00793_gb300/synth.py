@@ -101,6 +101,16 @@ class Workload:
     init_std: float = 0.02
     rope_base: float = 10000.0
     rms_eps: float = 1e-6
+    # grouped heads, head norms and rotary variants (mf_create_decoder): key/value heads (0 =
+    # n_heads), norms of query and key heads, arguments of native.rope_desc
+    n_kv_heads: int = 0
+    qk_norm: bool = False
+    rope: dict | None = None
+
+    @property
+    def packed_heads(self) -> bool:
+        """Whether the decoder needs mf_create_decoder."""
+        return bool(self.n_kv_heads or self.qk_norm or self.rope is not None)
 
     @property
     def n_layers(self) -> int:
@@ -116,12 +126,18 @@ class Workload:
     def decoder_layout(self):
         """(name, size) of each decoder tensor in flat-parameter order: embedding E [V][d];
         per block g1 [d], Wqkv [d][3d], Wo [d][d], g2 [d], W1 [d][dff], W2 [dff][d]; final gain
-        gf [d]; head Wh [d][V]."""
+        gf [d]; head Wh [d][V].  With grouped heads Wqkv has (n_heads + 2 n_kv_heads) d/n_heads
+        columns; with head norms gq, gk [d/n_heads] follow g1."""
         d, V, F = self.d_model, self.vocab, self.d_ff
+        dh = d // self.n_heads
+        cols = (self.n_heads + 2 * (self.n_kv_heads or self.n_heads)) * dh
         out = [("E", V * d)]
         for l in range(self.n_blocks):
-            out += [(f"g1.{l}", d), (f"Wqkv.{l}", d * 3 * d), (f"Wo.{l}", d * d),
-                    (f"g2.{l}", d), (f"W1.{l}", d * F), (f"W2.{l}", F * d)]
+            out += [(f"g1.{l}", d)]
+            if self.qk_norm:
+                out += [(f"gq.{l}", dh), (f"gk.{l}", dh)]
+            out += [(f"Wqkv.{l}", d * cols), (f"Wo.{l}", d * d), (f"g2.{l}", d),
+                    (f"W1.{l}", d * F), (f"W2.{l}", F * d)]
         out += [("gf", d), ("Wh", d * V)]
         return out
 
