@@ -533,19 +533,19 @@ __device__ __forceinline__ void bwd_rows(const RopeParams& p, char* ring, RopeSh
           uint64_t g[4], gd[4];
           load_unit<VEC>(p, t, true, sh.gains[gi], g);
           if (DUAL) load_unit<VEC>(p, t, true, sh.gains[2 + gi], gd);
-          // one of the two sums gets the product, the other a zero
-          const float fq = h < p.Hq ? 1.f : 0.f;
-          const uint64_t fq2 = pair(fq, fq), fk2 = pair(1.f - fq, 1.f - fq);
+          // query and key heads' sums apart: a NaN of the one does not reach the other
+          const bool query = h < p.Hq;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint64_t dyv = v[e], nv = mul2(x[e], r2), gw = mul2(dyv, nv), a = mul2(g[e], dyv);
-            acc[0][e] = fma2(fq2, gw, acc[0][e]);
-            acc[NORM ? 1 : 0][e] = fma2(fk2, gw, acc[NORM ? 1 : 0][e]);
+            acc[0][e] = add2(query ? gw : 0, acc[0][e]);
+            acc[NORM ? 1 : 0][e] = add2(query ? 0 : gw, acc[NORM ? 1 : 0][e]);
             v[e] = fma2(r2, a, mul2(k02, x[e]));
             if (DUAL) {
               const uint64_t gt = fma2(d[e], nv, mul2(dyv, fma2(xd[e], r2, mul2(x[e], rt2))));
-              acc[NACC - 2 > 0 ? NACC - 2 : 0][e] = fma2(fq2, gt, acc[NACC - 2 > 0 ? NACC - 2 : 0][e]);
-              acc[NACC - 1][e] = fma2(fk2, gt, acc[NACC - 1][e]);
+              constexpr int iq = NACC - 2 > 0 ? NACC - 2 : 0;
+              acc[iq][e] = add2(query ? gt : 0, acc[iq][e]);
+              acc[NACC - 1][e] = add2(query ? 0 : gt, acc[NACC - 1][e]);
               const uint64_t b = fma2(gd[e], dyv, mul2(g[e], d[e]));
               d[e] = fma2(rt2, a, fma2(r2, b, fma2(k12, x[e], mul2(k02, xd[e]))));
             }

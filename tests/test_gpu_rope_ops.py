@@ -222,3 +222,44 @@ def test_rope_no_rows():
     for t in d + dz:
         assert (t == 0).all()
     assert (y == 2.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dual", [False, True])
+def test_rope_not_finite_stays_in_its_head(dual):
+    """A NaN or an infinity in one head reaches that head's own outputs and gains alone: not the
+    other kind of heads' gains, nor any other head or row."""
+    torch, native = need_gpu()
+    N, Hq, Hkv, D = 9, 3, 2, 40
+    g = torch.Generator().manual_seed(4)
+    rnd = lambda *s: torch.randn(*s, generator=g).cuda()
+    W = (Hq + 2 * Hkv) * D
+    base = {k: rnd(N, W) for k in ("x", "dy") + (("xd", "dyd") if dual else ())}
+    gains = dict(gq=rnd(D), gk=rnd(D), **(dict(gqd=rnd(D), gkd=rnd(D)) if dual else {}))
+    names = ["dgq", "dgk"] + ["dgqd", "dgkd"] * dual
+    work = torch.empty(native.mf_qk_rope_work_bytes(N, Hq, Hkv, D, dual), dtype=torch.uint8, device="cuda")
+
+    def run(v):
+        kw = dict(n_heads=Hq, n_kv_heads=Hkv, head_dim=D, rope=native.rope_desc(), n_copy_heads=Hkv, **gains)
+        o = {k: torch.empty(N, W, device="cuda") for k in ("y", "dx") + (("yd", "dxd") if dual else ())}
+        dg = {k: torch.empty(D, device="cuda") for k in names}
+        native.mf_qk_rope_fwd(v["x"], o["y"], xd=v.get("xd"), yd=o.get("yd"), **kw)
+        native.mf_qk_rope_bwd(v["dy"], o["dx"], x=v["x"], xd=v.get("xd"), dyd=v.get("dyd"),
+                              dxd=o.get("dxd"), work=work, **dg, **kw)
+        return o, dg
+
+    ref, dref = run(base)
+    for head, val in ((1, float("nan")), (Hq, float("inf")), (Hq + Hkv, float("nan"))):
+        for name in base:
+            v = {k: t.clone() for k, t in base.items()}
+            v[name][4, head * D + 7] = val
+            o, dg = run(v)
+            for k in o:
+                other = torch.ones(N, W, dtype=torch.bool, device="cuda")
+                other[4, head * D:(head + 1) * D] = False
+                assert torch.equal(o[k][other], ref[k][other]), (head, name, k)
+            for k in names:
+                kind = 0 if k.startswith("dgq") else 1
+                mine = 0 if head < Hq else 1 if head < Hq + Hkv else 2
+                if kind != mine:
+                    assert torch.equal(dg[k], dref[k]), (head, name, k)
