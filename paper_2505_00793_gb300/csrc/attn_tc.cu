@@ -267,8 +267,14 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // ---- forward ------------------------------------------------------------------------------------
 // One CTA per (query head, 128 rows): warp 0 loads (Q once, then key tiles into a ring of K and a
 // ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..5 hold
-// the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).  The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T
-// into S'; P [V | V'] -> [O | T], then (P (*) S') V into T; o' = T / l - rbar o.
+// the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).
+// The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T into S';
+// P [V | V'] -> [O | T], then (P (*) S') V into T; o' = T / l - rbar o.
+// What bounds it: at 128 columns the products (one head of 16384 rows: 0.70 us a tile pair of 128
+// by 128 and SM, 0.53 at the tensor cores' clocked rate); at 64 the chain scores - maximum -
+// exponentials - product of each CTA, which two or three CTAs an SM fill by turns.  Taking the
+// exponentials against the last tile's maximum, so that they need not wait for this one's, cost
+// registers and was 0 to 15 % slower.
 // TKEYS keys a tile: 64 where the tangents leave no TMEM for more, and where many CTAs are to be
 // had: tiles of 64 let three of them, not two, fill each other's waits on an SM (launch_fwd).
 template <bool DUAL, int HDP, int TKEYS>
@@ -318,15 +324,19 @@ __device__ __forceinline__ void stage16(uint8_t* buf, int r, int c0, const float
         make_uint4(pack_bf16x2(v[8 * h], v[8 * h + 1]), pack_bf16x2(v[8 * h + 2], v[8 * h + 3]),
                    pack_bf16x2(v[8 * h + 4], v[8 * h + 5]), pack_bf16x2(v[8 * h + 6], v[8 * h + 7]));
 }
-template <int W>
+// By THREADS threads, each a chunk of every RS-th row.
+template <int W, int THREADS>
 __device__ __forceinline__ void stage_out(const uint8_t* buf, int nvalid, int D, __nv_bfloat16* dst,
-                                          int64_t ld, int t, int threads) {
-  for (int i = t; i < TR * (W / 8); i += threads) {
-    const int r = i / (W / 8), c = i % (W / 8);
-    if (r < nvalid && 8 * c < D)
-      *reinterpret_cast<uint4*>(dst + r * ld + 8 * c) =
-          *reinterpret_cast<const uint4*>(buf + r * (2 * W) + ((c ^ (r & 7)) << 4));
-  }
+                                          int64_t ld, int t) {
+  constexpr int RS = THREADS / (W / 8);
+  static_assert(RS % 8 == 0 && TR % RS == 0, "a thread's chunk has one place in all its rows");
+  const int c = t % (W / 8), r0 = t / (W / 8);
+  if (8 * c >= D) return;
+  const uint8_t* from = buf + r0 * (2 * W) + ((c ^ (r0 & 7)) << 4);
+  dst += r0 * ld + 8 * c;
+#pragma unroll 1
+  for (int r = r0; r < nvalid; r += RS, from += RS * 2 * W, dst += RS * ld)
+    *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(from);
 }
 
 template <bool DUAL, int HDP, int TKEYS>
@@ -674,9 +684,9 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
     asm volatile("bar.sync 5, %0;" ::"n"(C::EW * 32) : "memory");
     if (ok) {
       const int64_t at = static_cast<int64_t>(row0) * p.ldo + h * p.D;
-      stage_out<HDP>(smem, nvalid, p.D, p.ow + at, p.ldo, threadIdx.x - 64, C::EW * 32);
+      stage_out<HDP, C::EW * 32>(smem, nvalid, p.D, p.ow + at, p.ldo, threadIdx.x - 64);
       if (DUAL)
-        stage_out<HDP>(smem + TR * HDP * 2, nvalid, p.D, p.owd + at, p.ldo, threadIdx.x - 64, C::EW * 32);
+        stage_out<HDP, C::EW * 32>(smem + TR * HDP * 2, nvalid, p.D, p.owd + at, p.ldo, threadIdx.x - 64);
     }
     tc_fence_before();
     fence_async_smem();
@@ -887,7 +897,6 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   using C = BwdCfg<DUAL, HDP>;
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  // barriers, as byte offsets in a set; one set per walk
   // barriers, as byte offsets in a set; one set per walk
   constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_DP_FULL = 16, B_P_FULL = 24, B_DS_FULL = 32,
                      B_DRAIN = 40, B_CLEAN = 48, B_READ = 64;
@@ -1309,44 +1318,50 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   tc_fence_after();
   if (careful || !redo_flag || *abort) break;
   }
-  // the cluster's sums, rank by rank in order, each CTA its part of the rows; the second barrier
-  // keeps a CTA's shared memory until the others have read it
+  // The cluster's sums, rank by rank in order, each CTA its part of the rows; the second barrier
+  // keeps a CTA's shared memory until the others have read it.  Short code counts here: it runs once
+  // a CTA, and unrolled eight ranks wide it took 4.5 us of a CTA's 45 (16 heads of 64 over 4, two
+  // CTAs a cluster, tangents), as much as the reads themselves.
   cluster_sync_all();
   if (warp >= 3 && !*abort) {
     const int rows = (TR + p.share - 1) / p.share;
     const int r0 = rank * rows, nr = min(min(r0 + rows, TR), nvalid) - r0;
-    constexpr int CH = HDP / 8;
-    // eight columns of one sum at a time; all the ranks' reads in flight together
-    for (int i = static_cast<int>(threadIdx.x) - 96; i < nr * (2 * C::NT * CH); i += 32 * C::EW) {
-      const int c = i % CH, k = i / CH % (2 * C::NT), r = r0 + i / (2 * C::NT * CH);
-      if (8 * c >= p.D) continue;
-      const uint32_t at = (k * TR + r) * (4 * HDP);
-      const uint32_t o0 = at + (((2 * c) ^ (r & 7)) << 4), o1 = at + (((2 * c + 1) ^ (r & 7)) << 4);
-      float4 x = *reinterpret_cast<const float4*>(smem + o0), y = *reinterpret_cast<const float4*>(smem + o1);
-      if (p.share > 1) {
-        float4 xs[8], ys[8];
+    // A lane has four columns of one sum, so that a warp reads whole rows, and every RS-th row,
+    // NI of them together.
+    constexpr int CH = HDP / 4, RS = 32 * C::EW / (2 * C::NT * CH), NI = 2;
+    static_assert(RS * 2 * C::NT * CH == 32 * C::EW, "every thread its columns");
+    const int t = static_cast<int>(threadIdx.x) - 96, c = t % CH, k = t / CH % (2 * C::NT);
+    const int end = r0 + nr;
+    // dV (dV') as they are, dK (dK') with the scale of the scores
+    const bool isv = k < C::NT;
+    const float f = isv ? 1.f : p.scale;
+    const int64_t ld = isv ? p.lddv : p.lddk;
+    __nv_bfloat16* dst = (k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd) +
+                         row0 * ld + hk * p.D + 4 * c;
+    const uint32_t own = smem_u32(smem) + k * TR * (4 * HDP);
+#pragma unroll 1
+    for (int r = r0 + t / (2 * C::NT * CH); r < end; r += NI * RS) {
+      float4 x[NI];
+#pragma unroll 1
+      for (int j = 0; j < p.share; ++j) {
+        const uint32_t from = j == rank ? own : dsmem_addr(own, j);
+        float4 v[NI];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < p.share) {
-            xs[j] = ld_cluster4(dsmem_addr(smem_u32(smem + o0), j));
-            ys[j] = ld_cluster4(dsmem_addr(smem_u32(smem + o1), j));
-          }
-        x = xs[0];
-        y = ys[0];
+        for (int u = 0; u < NI; ++u) {
+          const int q = (r + u * RS) & (TR - 1);
+          v[u] = ld_cluster4(from + q * (4 * HDP) + ((c ^ (q & 7)) << 4));
+        }
 #pragma unroll
-        for (int j = 1; j < 8; ++j)
-          if (j < p.share) {
-            x.x += xs[j].x; x.y += xs[j].y; x.z += xs[j].z; x.w += xs[j].w;
-            y.x += ys[j].x; y.y += ys[j].y; y.z += ys[j].z; y.w += ys[j].w;
-          }
+        for (int u = 0; u < NI; ++u)
+          x[u] = j == 0 ? v[u] : make_float4(x[u].x + v[u].x, x[u].y + v[u].y, x[u].z + v[u].z, x[u].w + v[u].w);
       }
-      // dV (dV') as they are, dK (dK') with the scale of the scores
-      const bool isv = k < C::NT;
-      const float f = isv ? 1.f : p.scale;
-      __nv_bfloat16* dst = k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd;
-      *reinterpret_cast<uint4*>(dst + (row0 + r) * (isv ? p.lddv : p.lddk) + hk * p.D + 8 * c) =
-          make_uint4(pack_bf16x2(x.x * f, x.y * f), pack_bf16x2(x.z * f, x.w * f),
-                     pack_bf16x2(y.x * f, y.y * f), pack_bf16x2(y.z * f, y.w * f));
+      if (4 * c < p.D) {
+#pragma unroll
+        for (int u = 0; u < NI; ++u)
+          if (r + u * RS < end)
+            *reinterpret_cast<uint2*>(dst + (r + u * RS) * ld) =
+                make_uint2(pack_bf16x2(x[u].x * f, x[u].y * f), pack_bf16x2(x[u].z * f, x[u].w * f));
+      }
     }
   }
   cluster_leave();
@@ -1366,7 +1381,6 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   using C = BwdCfg<DUAL, HDP>;
   constexpr int NA = C::NA, BT = C::BT, CW = C::CW;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  // barriers, as byte offsets in a set; one set per walk
   // barriers, as byte offsets in a set; one set per walk
   constexpr uint32_t B_RES_FULL = 0, B_S_FULL = 8, B_S_FREE = 16, B_DRAIN = 24;
   // one for each buffer of dP: the next tile's phase may be complete before somebody has come to
@@ -1701,9 +1715,9 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     row_bar<C::EW>();
     if (ok) {
       const int64_t at = static_cast<int64_t>(row0) * p.lddq + h * p.D;
-      stage_out<HDP>(smem, nvalid, p.D, p.dq + at, p.lddq, threadIdx.x - 96, C::EW * 32);
+      stage_out<HDP, C::EW * 32>(smem, nvalid, p.D, p.dq + at, p.lddq, threadIdx.x - 96);
       if (DUAL)
-        stage_out<HDP>(smem + TR * HDP * 2, nvalid, p.D, p.dqd + at, p.lddq, threadIdx.x - 96, C::EW * 32);
+        stage_out<HDP, C::EW * 32>(smem + TR * HDP * 2, nvalid, p.D, p.dqd + at, p.lddq, threadIdx.x - 96);
     }
     tc_fence_before();
     fence_async_smem();
