@@ -31,7 +31,8 @@
  *    connections, final RMSNorm, untied head; per-sequence next-token cross-entropy (mean
  *    over the seq_len predicted positions).  No biases.  Flat parameter order: E [vocab][d];
  *    per block g1 [d], Wqkv [d][3d] (q | k | v columns, heads contiguous), Wo [d][d],
- *    g2 [d], W1 [d][d_ff], W2 [d_ff][d]; then gf [d], Wh [d][vocab].
+ *    g2 [d], W1 [d][d_ff], W2 [d_ff][d]; then gf [d], Wh [d][vocab].  Grouped heads, head
+ *    norms and rotary variants: mf_create_decoder.
  *
  * Conventions for every call:
  *  - Tensor arguments are device pointers owned by the caller (e.g. torch CUDA tensors),
@@ -405,7 +406,8 @@ mf_status mf_dual_gemm_bf16(int M, int N, int K, const void* A0, int lda0, const
  *
  * Row buffers are row-major with a leading dimension in elements: a multiple of 8, and at
  * least the columns used; their first element lies on a 16-byte boundary.  So q, k and v may
- * be column ranges of one buffer.  head_dim is a multiple of 8, at most 128. */
+ * be column ranges of one buffer.  Outputs overlap neither inputs nor one another, but where
+ * stated.  head_dim is a multiple of 8, at most 128. */
 enum { MF_ROPE_HALF = 0, MF_ROPE_INTERLEAVED = 1 };
 enum { MF_ROPE_SCALE_NONE = 0, MF_ROPE_SCALE_LINEAR = 1, MF_ROPE_SCALE_BASE = 2,
        MF_ROPE_SCALE_BANDS = 3 };
@@ -448,7 +450,8 @@ typedef struct {
  *  seq_start, n_seq  as above; with pos given, both may be 0: every row is taken.
  * The backward pass takes the forward's x, xd (with gains only), gains, positions and
  *  dy, dyd  gradients of y and y' (type y_prec, lddy), and writes
- *  dx, dxd  gradients of x and their tangents (type y_prec, lddx; dx may be dy);
+ *  dx, dxd  gradients of x and their tangents (type y_prec, lddx; dx may be dy, and dxd dyd, or
+ *           x and xd, where types and leading dimensions agree);
  *  dgq, dgk, dgqd, dgkd  gradients of the gains [head_dim] float32, summed over rows and heads
  *           in a fixed order (nullable only without gains, the tangents without xd):
  *   dy_ = R(p)^T dy,  dg = sum dy_ x r,  dx = r a - r^3 x mean(x a) with a = g dy_.
@@ -503,9 +506,9 @@ mf_status mf_qk_rope_work_bytes(const mf_qk_rope_args* args, size_t* bytes);
  *           Calls that overlap in time need one each.
  * No value outside a row's own keys reaches it, not finite or not: what a masked place or a
  * row behind the last sequence holds does not matter.  A row that does attend to a key row
- * with a NaN or an infinity gets NaN or infinity itself.
- *  status   device int32 (nullable): raised to MF_ERR_TIMEOUT when a bounded wait of a kernel
- *           ran out; outputs are then undefined.
+ * with a NaN or an infinity may get NaN or an infinity itself.
+ *  status   device int32 (nullable), never lowered: raised to MF_ERR_TIMEOUT when a bounded wait
+ *           of a kernel ran out, or above where a kernel could not run; outputs are then undefined.
  * Errors: MF_ERR_INVALID_ARG, MF_ERR_UNSUPPORTED (tangents of heads wider than 64),
  * MF_ERR_CUDA. */
 typedef struct {
@@ -540,6 +543,7 @@ mf_status mf_attn_work_bytes(const mf_attn_args* args, size_t* bytes);
  *              gains gq, gk [d_model/n_heads] of each block; they lie behind the block's g1 in
  *              the flat parameter vector (g1, gq, gk, Wqkv, ...).  0: none;
  *  rope        rotary positions; base 0 = desc->rope_base.
+ * MF_OPT_FLASH_ATTN has no part in such a handle.
  * Errors: MF_ERR_INVALID_ARG, MF_ERR_UNSUPPORTED (float32, wider heads), MF_ERR_CUDA. */
 typedef struct {
   int n_kv_heads, qk_norm;

@@ -14,6 +14,11 @@
 // memory is moved for it, and the products of one CTA, issued by one thread in order, need no
 // barrier between reading P and overwriting it with the next scores.
 //
+// Rounded to bf16 are the outputs and, as operands of the tensor cores next to bf16 rows, P, P',
+// dS and dS', each by 2^-8 of its value at most; scores, maxima, sums, lse, rbar, D and every
+// accumulator are float32.  Against 64 bits an output is off by 0.0024 to 0.0026 in relative L2,
+// of which its own rounding is 0.0017.
+//
 // Values of masked places: a product with a zero of P still meets them (0 * inf = NaN).  So a
 // CTA whose results are all finite is done; one that finds a NaN or an infinity in them walks its
 // tiles a second time, carefully: in mixed tiles the rows that P or dS will multiply are looked
@@ -270,11 +275,12 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).
 // The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T into S';
 // P [V | V'] -> [O | T], then (P (*) S') V into T; o' = T / l - rbar o.
-// What bounds it: at 128 columns the products (one head of 16384 rows: 0.70 us a tile pair of 128
-// by 128 and SM, 0.53 at the tensor cores' clocked rate); at 64 the chain scores - maximum -
-// exponentials - product of each CTA, which two or three CTAs an SM fill by turns.  Taking the
+// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 362 us, 1.45 PF/s of
+// causal work, the tensor pipe busy 67 % of the cycles); at 64 the chain scores - maximum -
+// exponentials - product of each CTA, which two or three CTAs an SM fill by turns (16 heads, 16384
+// rows: 0.95 PF/s; 16 heads with tangents, eight sequences of 1024: 80 us, pipe 36 %).  Taking the
 // exponentials against the last tile's maximum, so that they need not wait for this one's, cost
-// registers and was 0 to 15 % slower.
+// registers and was up to 17 % slower.
 // TKEYS keys a tile: 64 where the tangents leave no TMEM for more, and where many CTAs are to be
 // had: tiles of 64 let three of them, not two, fill each other's waits on an SM (launch_fwd).
 template <bool DUAL, int HDP, int TKEYS>
@@ -772,6 +778,12 @@ cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
 // The products run in the order  dV(i) S(i+1) | dK(i) dP(i+1):  while the row warps turn dP(i)
 // into dS(i), the tensor cores work on dV(i) and S(i+1); while they turn S(i+1) into P(i+1), on
 // dK(i) and dP(i+1).
+// What bounds them (per SM): at 128 columns the seven products of a tile pair (query rows 1.04 us
+// a pair of 128 by 128, key rows 1.43, 0.80 and 1.07 at the tensor cores' clocked rate); with
+// tangents 0.98 and 1.32 us a pair of 128 by 64 (0.60, 0.80); at 64 columns without, the row
+// warps' arithmetic and issue.  A CTA adds 6 us that nothing hides where one has the SM: its first
+// loads 1.1, first scores 2 to 4, results 1.2 (query rows); 1.2, 1.5, 3 to 5 (key rows).  A
+// single pass would need five products but add dQ up by atomics, in an order of the moment.
 // Query-row kernel, per key tile:  dS as above, untransposed, over dP;  dQ += dS K,
 // dQ' += dS' K + dS K'.  dP has two buffers, so that S(j+1) and dP(j+1) run while the row warps
 // work on tile j.

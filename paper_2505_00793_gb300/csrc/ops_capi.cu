@@ -3,6 +3,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "../../include/mixflow.h"
 #include "attn_ops.h"
 
@@ -130,6 +132,19 @@ bool in_place_ok(const void* in, int64_t ldin, const void* out, int64_t ldout, b
   return in != out || (ldin == ldout && same_type);
 }
 
+// Whether no output begins where another buffer of the call does.  (More cannot be told from
+// addresses: column ranges of one buffer of rows interleave.)
+bool outputs_apart(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* const* q = outs.begin(); q != o; ++q)
+      if (*q == *o) return false;
+    for (const void* i : ins)
+      if (i == *o) return false;
+  }
+  return true;
+}
+
 mf_status attn_params(const mf_attn_args& a, bool bwd, AttnParams* p) {
   if (!heads_ok(a.n_heads, a.n_kv_heads, 0, a.head_dim) || a.n_heads % a.n_kv_heads)
     return MF_ERR_INVALID_ARG;
@@ -158,6 +173,10 @@ mf_status attn_params(const mf_attn_args& a, bool bwd, AttnParams* p) {
   }
   if (!ok) return MF_ERR_INVALID_ARG;
   if (dual && a.head_dim > 64) return MF_ERR_UNSUPPORTED;
+  if (bwd ? !outputs_apart({a.dq, a.dk, a.dv, a.dqd, a.dkd, a.dvd, a.work},
+                           {a.q, a.k, a.v, a.qd, a.kd, a.vd, a.o, a.od, a.d_o, a.d_od, a.lse, a.rbar})
+          : !outputs_apart({a.o, a.od, a.lse, a.rbar}, {a.q, a.k, a.v, a.qd, a.kd, a.vd}))
+    return MF_ERR_INVALID_ARG;
   auto cb = [](const void* x) { return static_cast<const __nv_bfloat16*>(x); };
   auto mb = [](void* x) { return static_cast<__nv_bfloat16*>(x); };
   p->Hq = a.n_heads; p->Hkv = a.n_kv_heads; p->D = a.head_dim;
@@ -208,6 +227,8 @@ mf_status mf_qk_rope_fwd(const mf_qk_rope_args* args, void* stream) {
       !aligned(a.yd) || !in_place_ok(a.x, a.ldx, a.y, a.ldy, a.x_prec == a.y_prec) ||
       (a.xd && !in_place_ok(a.xd, a.ldx, a.yd, a.ldy, a.x_prec == a.y_prec)))
     return MF_ERR_INVALID_ARG;
+  if (!outputs_apart({a.y, a.yd}, {a.y == a.x ? nullptr : a.x, a.yd == a.xd ? nullptr : a.xd}))
+    return MF_ERR_INVALID_ARG;
   p.y = a.y; p.yd = a.yd; p.ldy = a.ldy;
   return done(mf::qk_rope(p, false, a.x_prec == MF_PREC_BF16, a.y_prec == MF_PREC_BF16,
                           static_cast<cudaStream_t>(stream)));
@@ -238,6 +259,15 @@ mf_status mf_qk_rope_bwd(const mf_qk_rope_args* args, void* stream) {
       !aligned(a.dyd) || !aligned(a.dxd) || !in_place_ok(a.dy, a.lddy, a.dx, a.lddx, true) ||
       (dual && !in_place_ok(a.dyd, a.lddy, a.dxd, a.lddx, true)) ||
       (norm && (!rows_ok(a.x, a.ldx, qk, a.n_rows) || (dual && !aligned(a.xd)))))
+    return MF_ERR_INVALID_ARG;
+  // a warp has read all of its part of a row before it writes any: dx may be x too
+  const bool over_x = in_place_ok(a.x, a.ldx, a.dx, a.lddx, a.x_prec == a.y_prec) &&
+                      (!dual || in_place_ok(a.xd, a.ldx, a.dxd, a.lddx, a.x_prec == a.y_prec));
+  if ((norm && !over_x) ||
+      !outputs_apart({a.dx, a.dxd, a.dgq, a.dgk, a.dgqd, a.dgkd, norm ? a.work : nullptr},
+                     {a.dx == a.dy ? nullptr : a.dy, a.dxd == a.dyd ? nullptr : a.dyd,
+                      !norm || a.dx == a.x ? nullptr : a.x, !norm || a.dxd == a.xd ? nullptr : a.xd, a.gq,
+                      a.gk, a.gqd, a.gkd}))
     return MF_ERR_INVALID_ARG;
   p.dy = a.dy; p.dyd = a.dyd; p.lddy = a.lddy;
   p.dx = a.dx; p.dxd = a.dxd; p.lddx = a.lddx;

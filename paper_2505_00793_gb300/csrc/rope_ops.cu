@@ -13,12 +13,18 @@
 // half and their four partners, else eight neighbours.  A head takes the next power of two of
 // lanes, and sums over a head are shuffles.
 //
-// What bounds it is memory.  Every warp reads ahead of its arithmetic by itself: it copies parts of
-// rows into a ring of its own in shared memory (bulk copies, two stages), so that what is in flight
-// does not depend on registers, and meets no other warp.  Plain loads left the memory idle two
-// thirds of the time; a ring for a whole block cost more in barriers than the heads in arithmetic.
-// The cos and sin of a row's position are computed a pair a lane and kept in registers for all its
-// heads.
+// What bounds the forward pass is memory.  Every warp reads ahead of its arithmetic by itself: it
+// copies parts of rows into a ring of its own in shared memory (bulk copies, two stages), so that
+// what is in flight does not depend on registers, and meets no other warp.  Plain loads left the
+// memory idle two thirds of the time; a ring for a whole block cost more in barriers than the heads
+// in arithmetic.  The cos and sin of a row's position are computed a pair a lane and kept in
+// registers for all its heads.  Measured: 16 + 16 + 16 heads of 64 with tangents, 8192 rows,
+// float32 to bf16, 302 MB in 56 us (5.4 TB/s, 80 % of a plain copy); 8 + 2 + 2 heads of 128,
+// 40001 rows of bf16, 246 MB in 42 us (5.8 TB/s).
+// What bounds the backward pass with norms is arithmetic whose latency 16 warps an SM do not cover
+// (issue slots 57 % busy): 16 + 4 + 4 heads of 64 with tangents, 8192 rows, 185 MB in 53 us; 12 +
+// 3 + 3 heads of 80 (10 of 16 lanes in use), 5003 rows of float32, 82 MB in 31 us.  A third block
+// an SM spilled: 34 us for the last, 45 for the second.
 #include "attn_ops.h"
 #include "device_math.cuh"
 #include "launch.cuh"

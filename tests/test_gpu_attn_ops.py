@@ -22,6 +22,15 @@ CASES = {
     "odd_width": ([200, 77], 0, 3, 3, 40),
     "many_short": ([3, 5, 1, 7, 2, 9, 4, 4, 8, 6, 1, 1, 30, 17, 2, 90, 12], 2, 2, 2, 16),
     "long": ([700], 0, 2, 1, 64),
+    # groups that one cluster shares whole: eight, six, seven and ten heads
+    "group_8": ([260, 40], 0, 8, 1, 32),
+    "group_6": ([131, 5], 3, 6, 1, 64),
+    "group_7_of_2": ([90, 60], 0, 14, 2, 64),
+    "group_10": ([140], 0, 10, 1, 24),
+    # so many CTAs that tiles of 64 keys are taken
+    "many_heads": ([300, 1, 128, 211, 0, 400, 353, 400], 2, 64, 8, 64),
+    # more sequences than a block reads at once
+    "many_sequences": ([0, 1, 2, 0, 1, 3] * 380, 1, 2, 1, 16),
 }
 WIDE = {
     "wide_one": ([1], 0, 2, 1, 128),
@@ -93,6 +102,86 @@ def test_attention_masked_places_do_not_matter(D, dual, poison):
         assert (got[k][n:] == au.MARK).all(), k
         if not k.startswith("dq"):
             assert not torch.isfinite(got[k][115:215]).all(1).any(), k
+
+
+@pytest.mark.gpu
+def test_attention_masked_places_do_not_matter_many_heads():
+    """The same where there are so many CTAs that tiles of 64 keys are taken."""
+    torch, native = need_gpu()
+    lens, tail, Hq, Hkv, D = [70, 45, 100, 20], 33, 320, 1, 24
+    n = sum(lens)
+    clean = au.data(lens, tail, Hq, Hkv, D, False, seed=6)
+    want = {k: t.clone() for k, t in au.run(native, au.wide(clean), lens, Hq, Hkv, D).items()}
+    dirty = {k: t.clone() for k, t in clean.items()}
+    bad = list(range(70, 115)) + list(range(n, n + tail))
+    for t in dirty.values():
+        t[bad] = math.nan
+    got = au.run(native, au.wide(dirty), lens, Hq, Hkv, D)
+    torch.cuda.synchronize()
+    rest = torch.tensor([r for r in range(n) if r not in bad]).cuda()
+    for k in ("o", "dq", "dk", "dv"):
+        assert torch.equal(got[k][rest], want[k][rest]), k
+    assert torch.equal(got["lse"][:, rest], want["lse"][:, rest])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,dual", [(64, True), (128, False)])
+def test_attention_two_calls_at_once(D, dual):
+    """Calls that overlap on two streams, each with its own workspace, do not meet."""
+    torch, native = need_gpu()
+    jobs = []
+    for seed, lens in ((1, [700, 90]), (2, [64, 400, 333])):
+        v = au.wide(au.data(lens, 0, 4, 2, D, dual, seed=seed))
+        jobs.append((v, lens, {k: t.clone() for k, t in au.run(native, v, lens, 4, 2, D).items()}))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(20):
+        outs = []
+        for (v, lens, _), s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                outs.append(au.run(native, v, lens, 4, 2, D))
+        torch.cuda.synchronize()
+        for (v, lens, want), got in zip(jobs, outs):
+            for k in au.names(dual):
+                assert torch.equal(got[k], want[k]), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dual", [False, True])
+def test_rows_far_apart(dual):
+    """Elements behind the 2^31st of a buffer: the same bits as from rows close together."""
+    torch, native = need_gpu()
+    N, Hq, Hkv, D = 9000, 2, 1, 32
+    lens = [4000, 1, 4999]
+    W = (Hq + 2 * Hkv) * D
+    far = torch.empty(N, 245760, dtype=torch.bfloat16, device="cuda")      # 2.2e9 elements
+    v = {k: t.cuda() for k, t in au.data(lens, 0, Hq, Hkv, D, dual).items()}
+    want = au.run(native, v, lens, Hq, Hkv, D)
+    at = 245760 - 8
+    def put(cols):
+        nonlocal at
+        at -= cols
+        return far[:, at:at + cols]
+    apart = {}
+    for k, t in v.items():
+        apart[k] = put(t.shape[1])
+        apart[k].copy_(t)
+    out = {k: (put(t.shape[1]) if t.dtype is torch.bfloat16 and t.shape[0] == N else t.clone())
+           for k, t in want.items()}
+    got = au.run(native, apart, lens, Hq, Hkv, D, out=out)
+    for k in au.names(dual):
+        assert torch.equal(got[k], want[k]), k
+    # the head norms between rows as far apart
+    x = torch.cat([v["q"], v["k"], v["v"]], 1)
+    kw = dict(n_heads=Hq, n_kv_heads=Hkv, head_dim=D, rope=native.rope_desc(), n_copy_heads=Hkv,
+              gq=torch.ones(D, device="cuda"), gk=torch.ones(D, device="cuda"),
+              seq_start=au.starts_of(lens).cuda())
+    y = torch.empty_like(x)
+    native.mf_qk_rope_fwd(x, y, **kw)
+    xf, yf = put(W), put(W)
+    xf.copy_(x)
+    native.mf_qk_rope_fwd(xf, yf, **kw)
+    assert torch.equal(yf, y)
 
 
 @pytest.mark.gpu

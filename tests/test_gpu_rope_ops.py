@@ -156,7 +156,7 @@ def test_rope_far_and_negative_positions(layout):
 
 @pytest.mark.gpu
 def test_rope_in_place_and_equal_sequences():
-    """y = x, dx = dy, and equal sequences given by their number."""
+    """y = x, dx = dy, dx = x, and equal sequences given by their number."""
     torch, native = need_gpu()
     D, Hq, Hkv, B, S = 64, 4, 2, 3, 33
     g = torch.Generator().manual_seed(2)
@@ -172,12 +172,12 @@ def test_rope_in_place_and_equal_sequences():
     assert torch.equal(y, z)
     work = torch.empty(native.mf_qk_rope_work_bytes(B * S, Hq, Hkv, D), dtype=torch.uint8, device="cuda")
     out = []
-    for dx, dy in ((torch.empty_like(y), y), (z, z)):
+    for dx, dy in ((torch.empty_like(y), y), (z, z), (x.clone(), y)):
         a, b = torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
-        native.mf_qk_rope_bwd(dy, dx, x=x, dgq=a, dgk=b, work=work, n_seq=B, **kw)
+        native.mf_qk_rope_bwd(dy, dx, x=dx if torch.equal(dx, x) else x, dgq=a, dgk=b, work=work, n_seq=B, **kw)
         out.append((dx, a, b))
-    for s, t in zip(*out):
-        assert torch.equal(s, t)
+    for s, t, u in zip(*out):
+        assert torch.equal(s, t) and torch.equal(s, u)
 
 
 @pytest.mark.gpu
@@ -263,3 +263,41 @@ def test_rope_not_finite_stays_in_its_head(dual):
                 mine = 0 if head < Hq else 1 if head < Hq + Hkv else 2
                 if kind != mine:
                     assert torch.equal(dg[k], dref[k]), (head, name, k)
+
+
+@pytest.mark.gpu
+def test_rope_captured_with_other_lengths():
+    """Both passes in one graph, replayed after the starts have changed on the device."""
+    torch, native = need_gpu()
+    N, Hq, Hkv, D = 300, 4, 2, 64
+    g = torch.Generator().manual_seed(8)
+    x, dy = (torch.randn(N, (Hq + 2 * Hkv) * D, generator=g).cuda() for _ in range(2))
+    gains = dict(gq=torch.rand(D, generator=g).cuda() + 0.5, gk=torch.rand(D, generator=g).cuda() + 0.5)
+    starts = torch.tensor([0, 100, 300], dtype=torch.int32, device="cuda")
+    work = torch.empty(native.mf_qk_rope_work_bytes(N, Hq, Hkv, D), dtype=torch.uint8, device="cuda")
+
+    def run(o):
+        kw = dict(n_heads=Hq, n_kv_heads=Hkv, head_dim=D, rope=native.rope_desc(), n_copy_heads=Hkv,
+                  seq_start=starts, **gains)
+        native.mf_qk_rope_fwd(x, o["y"], **kw)
+        native.mf_qk_rope_bwd(dy, o["dx"], x=x, dgq=o["dgq"], dgk=o["dgk"], work=work, **kw)
+
+    def outs():
+        o = {k: torch.zeros_like(x) for k in ("y", "dx")}
+        return {**o, **{k: torch.zeros(D, device="cuda") for k in ("dgq", "dgk")}}
+
+    run(outs())
+    torch.cuda.synchronize()
+    o, graph = outs(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(o)
+    for s in ([0, 100, 300], [0, 7, 260], [0, 0, 1]):
+        starts.copy_(torch.tensor(s, dtype=torch.int32))
+        for t in o.values():
+            t.zero_()
+        graph.replay()
+        want = outs()
+        run(want)
+        torch.cuda.synchronize()
+        for k in o:
+            assert torch.equal(o[k], want[k]), (s, k)

@@ -28,9 +28,8 @@ def _rope(native, **kw):
     a.x_prec = a.y_prec = 1
     a.eps, a.n_seq = 1e-6, 1
     a.rope = native.rope_desc()
-    for k in ("x", "y", "dy", "dx", "gq", "gk", "dgq", "dgk", "work"):
-        setattr(a, k, P)
-    a.y, a.dx = 2 * P, 2 * P
+    for i, k in enumerate(("x", "y", "dy", "dx", "gq", "gk", "dgq", "dgk", "work")):
+        setattr(a, k, P * (1 + i))
     a.ldx = a.ldy = a.lddy = a.lddx = 256
     a.work_bytes = 1 << 30
     for k, v in kw.items():
@@ -93,8 +92,8 @@ def test_rope_refuses_per_pass(native):
 def _attn(native, **kw):
     a = native.mf_attn_args()
     a.n_rows, a.n_heads, a.n_kv_heads, a.head_dim, a.n_seq = 8, 4, 2, 64, 1
-    for k in ("q", "k", "v", "o", "lse", "d_o", "dq", "dk", "dv", "work"):
-        setattr(a, k, P)
+    for i, k in enumerate(("q", "k", "v", "o", "lse", "d_o", "dq", "dk", "dv", "work")):
+        setattr(a, k, P * (1 + i))
     for k in ("ldq", "ldk", "ldv", "ldo", "lddo", "lddq", "lddk", "lddv"):
         setattr(a, k, 256)
     a.work_bytes = 1 << 30
@@ -103,19 +102,19 @@ def _attn(native, **kw):
     return a
 
 
-DUAL = {k: P for k in ("qd", "kd", "vd", "od", "rbar", "d_od", "dqd", "dkd", "dvd")}
+DUAL = {k: P * (20 + i) for i, k in enumerate(("qd", "kd", "vd", "od", "rbar", "d_od", "dqd", "dkd", "dvd"))}
 ATTN_BAD = [
     dict(n_rows=-1), dict(n_rows=2 ** 31), dict(n_heads=0), dict(n_heads=3), dict(n_kv_heads=0),
     dict(head_dim=0), dict(head_dim=60), dict(head_dim=136), dict(scale=-1.0), dict(scale=math.inf),
     dict(scale=math.nan), dict(n_seq=0), dict(n_seq=3), dict(q=None), dict(k=None), dict(v=None),
     dict(o=None), dict(lse=None), dict(q=P + 8), dict(ldq=248), dict(ldk=120), dict(ldv=260),
     dict(ldo=0), dict(ldq=-256), dict(ldk=1 << 40),
-] + [dict({k: None}, **{j: P for j in DUAL if j != k}) for k in ("qd", "kd", "vd", "od", "rbar")] \
+] + [dict({k: None}, **{j: DUAL[j] for j in DUAL if j != k}) for k in ("qd", "kd", "vd", "od", "rbar")] \
   + [dict(DUAL, kd=P + 2)]
 ATTN_BWD_BAD = [dict(d_o=None), dict(dq=None), dict(dk=P + 4), dict(dv=None), dict(work=None),
                 dict(work=P + 8), dict(work_bytes=127), dict(lddo=8), dict(lddq=248), dict(lddk=4),
                 dict(lddv=130), dict(DUAL, d_od=None), dict(DUAL, dqd=None), dict(DUAL, work_bytes=255),
-                dict(dkd=P)]
+                dict(dkd=DUAL["dkd"])]
 
 
 @pytest.mark.parametrize("kw", ATTN_BAD, ids=str)
@@ -127,6 +126,34 @@ def test_attention_refuses(native, kw):
 @pytest.mark.parametrize("kw", ATTN_BWD_BAD, ids=str)
 def test_attention_backward_refuses(native, kw):
     assert native.lib().mf_attn_bwd(C.byref(_attn(native, **kw)), None) == INVALID
+
+
+@pytest.mark.parametrize("out,other", [("o", "q"), ("o", "v"), ("od", "o"), ("od", "kd"), ("o", "lse")])
+def test_attention_refuses_outputs_over_others(native, out, other):
+    kw = dict(DUAL)
+    base = _attn(native, **kw)
+    a = _attn(native, **{**kw, out: getattr(base, other)})
+    assert native.lib().mf_attn_fwd(C.byref(a), None) == INVALID
+
+
+@pytest.mark.parametrize("out,other", [("dq", "q"), ("dk", "dv"), ("dv", "d_o"), ("dqd", "dq"), ("dkd", "k"),
+                                       ("work", "o"), ("dq", "o"), ("dvd", "od")])
+def test_attention_backward_refuses_outputs_over_others(native, out, other):
+    base = _attn(native, **DUAL)
+    a = _attn(native, **{**DUAL, out: getattr(base, other)})
+    assert native.lib().mf_attn_bwd(C.byref(a), None) == INVALID
+
+
+def test_rope_refuses_outputs_over_others(native):
+    """In place is y = x, yd = xd, dx = dy or x, dxd = dyd or xd; nothing else."""
+    L, t = native.lib(), dict(xd=P * 30, yd=P * 31, dyd=P * 32, dxd=P * 33, dgqd=P * 34, dgkd=P * 35)
+    base = _rope(native, **t)
+    for out, other in (("yd", "y"), ("y", "xd"), ("yd", "x")):
+        assert L.mf_qk_rope_fwd(C.byref(_rope(native, **{**t, out: getattr(base, other)})), None) == INVALID
+    for out, other in (("dxd", "dx"), ("dx", "xd"), ("dxd", "dy"), ("dgq", "dgk"), ("dgqd", "gq"), ("work", "dx")):
+        assert L.mf_qk_rope_bwd(C.byref(_rope(native, **{**t, out: getattr(base, other)})), None) == INVALID
+    assert L.mf_qk_rope_bwd(C.byref(_rope(native, dx=base.x, lddx=264)), None) == INVALID
+    assert L.mf_qk_rope_bwd(C.byref(_rope(native, dx=base.x, x_prec=0)), None) == INVALID
 
 
 def test_attention_refuses_wide_tangents(native):
