@@ -14,17 +14,17 @@
 // lanes, and sums over a head are shuffles.
 //
 // What bounds the forward pass is memory.  Every warp reads ahead of its arithmetic by itself: it
-// copies parts of rows into a ring of its own in shared memory (bulk copies, two stages), so that
+// copies parts of rows into a ring of its own in shared memory (bulk copies), so that
 // what is in flight does not depend on registers, and meets no other warp.  Plain loads left the
 // memory idle two thirds of the time; a ring for a whole block cost more in barriers than the heads
 // in arithmetic.  The cos and sin of a row's position are computed a pair a lane and kept in
 // registers for all its heads.  Measured: 16 + 16 + 16 heads of 64 with tangents, 8192 rows,
-// float32 to bf16, 302 MB in 56 us (5.4 TB/s, 80 % of a plain copy); 8 + 2 + 2 heads of 128,
-// 40001 rows of bf16, 246 MB in 42 us (5.8 TB/s).
+// float32 to bf16, 302 MB in 50 us (6.1 TB/s, 89 % of a plain copy); 8 + 2 + 2 heads of 128,
+// 40001 rows of bf16, 246 MB in 41 us (6.0 TB/s).
 // What bounds the backward pass with norms is arithmetic whose latency 16 warps an SM do not cover
 // (issue slots 57 % busy): 16 + 4 + 4 heads of 64 with tangents, 8192 rows, 185 MB in 53 us; 12 +
 // 3 + 3 heads of 80 (10 of 16 lanes in use), 5003 rows of float32, 82 MB in 31 us.  A third block
-// an SM spilled: 34 us for the last, 45 for the second.
+// an SM spilled: 34 us for the last.
 #include "attn_ops.h"
 #include "device_math.cuh"
 #include "launch.cuh"
@@ -36,9 +36,13 @@ namespace {
 
 constexpr int kRopeWarps = 8;
 constexpr int kRopeThreads = 32 * kRopeWarps;
-constexpr int kRopeStages = 2;
-constexpr int kRopeStage = 6 * 1024;                   // bytes of a stage (at most), two a warp
-constexpr int kRopeRing = kRopeWarps * (kRopeStages * kRopeStage + 512);   // of a block, two an SM
+// A warp's ring: stages, and bytes of one at most.  Heads of 64 with tangents, 8192 rows: forward
+// 49.8 us with three stages of 4 KB (eight heads), 55.9 with two of 6 KB, 55.1 with four of 3 KB;
+// backward 53.5 with two of 6 KB (eight heads), 56.9 and 58.9 with two and three of 4 KB.
+constexpr int kFwdStages = 3, kFwdStage = 4 * 1024;
+constexpr int kBwdStages = 2, kBwdStage = 6 * 1024;
+constexpr int kRopeRing = kRopeWarps * (12 * 1024 + 512);          // of a block, two an SM
+static_assert(kFwdStages * kFwdStage == 12 * 1024 && kBwdStages * kBwdStage == 12 * 1024);
 
 // cos and sin of pos * phase, phase in units of 2^-64 turns: the product modulo 2^64 is the
 // angle modulo a turn, exactly, so a far position loses nothing.  The nearest quarter turn is
@@ -249,12 +253,12 @@ __device__ __forceinline__ bool next_part(const RopeParams& p, Cursor& k) {
 }
 
 // The warp's ring and what it works with.
-template <int NARR>
+template <int NARR, int STAGES>
 struct Reader {
   const RopeParams& p;
   RowBuf buf[NARR];
-  char* ring;            // two stages, then cos and sin tables
-  uint32_t bars;         // two barriers
+  char* ring;            // its stages, then cos and sin tables
+  uint32_t bars;         // a barrier a stage
   int lane, H, st, got;
   uint32_t ph;
   Cursor ahead;          // next part to be copied
@@ -301,7 +305,7 @@ struct Reader {
     __syncwarp();
     ++got;
     issue(st);
-    if (++st == kRopeStages) {
+    if (++st == STAGES) {
       st = 0;
       ph ^= 1;
     }
@@ -312,7 +316,7 @@ struct Reader {
       const long long t0 = clock64();
       while (!try_phase(bars + 8 * st, ph) && clock64() - t0 < 4000000000LL) {
       }
-      if (++st == kRopeStages) {
+      if (++st == STAGES) {
         st = 0;
         ph ^= 1;
       }
@@ -364,11 +368,11 @@ __device__ __forceinline__ Turns make_turns(const RopeParams& p, const Unit& t, 
 
 // Shared memory of a block: every warp's ring, barriers, and the gains [gq | gk | gq' | gk'][D].
 struct RopeShared {
-  uint64_t bars[kRopeWarps][kRopeStages];
+  uint64_t bars[kRopeWarps][kFwdStages];
   float gains[4][128];
 };
 __device__ __forceinline__ void rope_start(const RopeParams& p, RopeShared& sh) {
-  if (threadIdx.x < kRopeWarps * kRopeStages) {
+  if (threadIdx.x < kRopeWarps * kFwdStages) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(saddr(&sh.bars[0][0]) + 8 * threadIdx.x));
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -381,20 +385,22 @@ __device__ __forceinline__ void rope_start(const RopeParams& p, RopeShared& sh) 
     }
   __syncthreads();
 }
-__device__ __forceinline__ int warp_bytes(const RopeParams& p) {
-  return kRopeStages * p.stage_bytes + 2 * 64 * static_cast<int>(sizeof(float));
+constexpr int kTurnBytes = 2 * 64 * static_cast<int>(sizeof(float));
+__device__ __forceinline__ int warp_bytes(const RopeParams& p, int stages) {
+  return stages * p.stage_bytes + kTurnBytes;
 }
 
 template <typename Tx, typename Ty, bool DUAL, bool NORM, bool VEC>
 __device__ __forceinline__ void fwd_rows(const RopeParams& p, char* ring, RopeShared& sh) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int H = p.Hq + p.Hkv + p.Hc, Hn = p.Hq + p.Hkv, total = seq_total(p.seq);
-  Reader<DUAL ? 2 : 1> rd(p, ring + warp * warp_bytes(p), saddr(sh.bars[warp]), total);
+  constexpr int STAGES = kFwdStages;
+  Reader<DUAL ? 2 : 1, STAGES> rd(p, ring + warp * warp_bytes(p, STAGES), saddr(sh.bars[warp]), total);
   rd.buf[0] = {static_cast<const char*>(p.x), p.ldx * static_cast<int>(sizeof(Tx)), sizeof(Tx), H};
   if constexpr (DUAL) rd.buf[1] = {static_cast<const char*>(p.xd), rd.buf[0].ld, sizeof(Tx), H};
 #pragma unroll
-  for (int s = 0; s < kRopeStages; ++s) rd.issue(s);
-  float* tab = reinterpret_cast<float*>(rd.ring + kRopeStages * p.stage_bytes);
+  for (int s = 0; s < STAGES; ++s) rd.issue(s);
+  float* tab = reinterpret_cast<float*>(rd.ring + STAGES * p.stage_bytes);
   const Unit t = make_unit(p, lane);
   const int sub = lane / p.lanes, hpw = 32 / p.lanes, half = p.hc * p.D;
   const float invD = 1.f / static_cast<float>(p.D);
@@ -469,7 +475,8 @@ __device__ __forceinline__ void bwd_rows(const RopeParams& p, char* ring, RopeSh
   constexpr int NARR = (DUAL ? 2 : 1) * (NORM ? 2 : 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int H = p.Hq + p.Hkv + p.Hc, Hn = p.Hq + p.Hkv, total = seq_total(p.seq);
-  Reader<NARR> rd(p, ring + warp * warp_bytes(p), saddr(sh.bars[warp]), total);
+  constexpr int STAGES = kBwdStages;
+  Reader<NARR, STAGES> rd(p, ring + warp * warp_bytes(p, STAGES), saddr(sh.bars[warp]), total);
   const RowBuf dy{static_cast<const char*>(p.dy), p.lddy * static_cast<int>(sizeof(Ty)), sizeof(Ty), H};
   const RowBuf xb{static_cast<const char*>(p.x), p.ldx * static_cast<int>(sizeof(Tx)), sizeof(Tx), Hn};
   rd.buf[0] = dy;
@@ -477,8 +484,8 @@ __device__ __forceinline__ void bwd_rows(const RopeParams& p, char* ring, RopeSh
   if constexpr (NORM) rd.buf[DUAL ? 2 : 1] = xb;
   if constexpr (NORM && DUAL) rd.buf[3] = {static_cast<const char*>(p.xd), xb.ld, sizeof(Tx), Hn};
 #pragma unroll
-  for (int s = 0; s < kRopeStages; ++s) rd.issue(s);
-  float* tab = reinterpret_cast<float*>(rd.ring + kRopeStages * p.stage_bytes);
+  for (int s = 0; s < STAGES; ++s) rd.issue(s);
+  float* tab = reinterpret_cast<float*>(rd.ring + STAGES * p.stage_bytes);
   const Unit t = make_unit(p, lane);
   const int sub = lane / p.lanes, hpw = 32 / p.lanes, half = p.hc * p.D;
   const float invD = 1.f / static_cast<float>(p.D);
@@ -678,7 +685,7 @@ cudaError_t qk_rope(RopeParams p, bool bwd, bool x_bf16, bool y_bf16, cudaStream
   const int two = dual ? 2 : 1, xs = x_bf16 ? 2 : 4, ys = y_bf16 ? 2 : 4;
   const int head = p.D * two * (bwd ? ys + (norm ? xs : 0) : xs);     // bytes, at most 2 KB
   const int H = p.Hq + p.Hkv + p.Hc, hpw = 32 / p.lanes;
-  int hc = kRopeStage / head;
+  int hc = (bwd ? kBwdStage : kFwdStage) / head;
   if (hc > hpw) hc -= hc % hpw;
   p.hc = hc < H ? hc : H;
   p.parts = (H + p.hc - 1) / p.hc;
@@ -695,7 +702,7 @@ cudaError_t qk_rope(RopeParams p, bool bwd, bool x_bf16, bool y_bf16, cudaStream
   p.step_row = grid * kRopeWarps / p.splits;
   p.step_split = grid * kRopeWarps % p.splits;
   const int NA = dual ? 4 : 2;
-  const int rings = kRopeWarps * (kRopeStages * p.stage_bytes + 2 * 64 * static_cast<int>(sizeof(float)));
+  const int rings = kRopeWarps * ((bwd ? kBwdStages : kFwdStages) * p.stage_bytes + kTurnBytes);
   const int sums = bwd && norm ? kRopeWarps * NA * p.D * static_cast<int>(sizeof(float)) : 0;
   p.ring_bytes = rings > sums ? rings : sums;
   const cudaError_t e = bwd ? launch_types<true>(p, x_bf16, y_bf16, dual, norm, grid, s)
