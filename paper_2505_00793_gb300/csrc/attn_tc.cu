@@ -27,6 +27,8 @@
 // for a check of its results.
 //
 // Every wait is bounded (2 s), as in flash_tc.cu.
+#include <limits.h>
+
 #include "attn_ops.h"
 #include "attn_tc_util.cuh"
 #include "packed_rows.cuh"
@@ -1165,7 +1167,9 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     const int r = q4 * 32 + lane;
     const int part = (warp - 3) >> 2, cb = part * CW;
     const uint32_t lane_base = tb + (static_cast<uint32_t>(q4 * 32) << 16) + cb;
-    const int hi = tile_hi(st_rows, row0, r);
+    // the row behind its sequence's last; the sign bit marks a sequence's first row, which attends
+    // to one key, itself
+    const int hi = tile_hi(st_rows, row0, r) | (tile_lo(st_rows, row0, r) == row0 + r ? INT_MIN : 0);
     const uint64_t c2p = pair(p.c2, p.c2), sc = pair(p.scale, p.scale);
     bool ok = true;
     int t = 0;
@@ -1173,7 +1177,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       const int sl = i & 1;
       const bool mx = mixed(t);
       // columns a .. b - 1 (of the tile) attend to this key
-      const int a = r - t * BT, b = hi - (row0 + t * BT);
+      const int a = r - t * BT, b = (hi & INT_MAX) - (row0 + t * BT);
       if (++t == nqt) t = 0;
       // the statistics
       if (!rwait(bb + B_CLEAN + 8 * sl, (i >> 1) & 1, p.status, abort)) { ok = false; break; }
@@ -1294,8 +1298,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           if (DUAL) tmem_st8(lane_base + C::C_DPD + c0 / 2, sdk);
         }
       };
-      if (mx) scores(std::true_type{});
-      else scores(std::false_type{});
+      if (mx) {
+        // a row with one key has P = 1 and dS = dS' = 0, of which dP - D, two sums of the same
+        // terms, would leave their rounding
+#pragma unroll
+        for (int w = 0; w < C::OWN; ++w)
+          if (hi < 0) own[w] &= ~col_bits(a - cb - 32 * w, a - cb - 32 * w);
+        scores(std::true_type{});
+      } else {
+        scores(std::false_type{});
+      }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -1592,6 +1604,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     const int part = (warp - 3) >> 2, cb = part * CW;
     const uint32_t lane_base = tb + (static_cast<uint32_t>(q4 * 32) << 16) + cb;
     const int lo = tile_lo(st_rows, row0, r);
+    const bool lone = lo == row0 + r;     // attends to one key, itself
     const int64_t row = row0 + r, si = static_cast<int64_t>(h) * p.seq.rows + row;
     const bool on = r < nvalid;
     // D of the rows, a row's chunks of 16 bytes in neighbouring lanes
@@ -1696,8 +1709,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           if (DUAL) tmem_st8(aP + BT + c0 / 2, sdk);
         }
       };
-      if (mx) scores(std::true_type{});
-      else scores(std::false_type{});
+      if (mx) {
+#pragma unroll
+        for (int w = 0; w < C::OWN; ++w) own[w] = lone ? 0u : own[w];    // dS = 0, as above
+        scores(std::true_type{});
+      } else {
+        scores(std::false_type{});
+      }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
