@@ -276,7 +276,12 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..5 hold
 // the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).
 // The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T into S';
-// P [V | V'] -> [O | T], then (P (*) S') V into T; o' = T / l - rbar o.
+// P [V | V'] -> [O | T], then (P (*) (S' - c)) V into T; o' = T / l - (rbar - c) o.  c is a mean of the
+// row's S' so far: what all of a row's S' have in common (keys or their tangents with a common
+// part) cancels in o', and rounded to bf16 as part of P (*) S' it would leave 2^-9 of itself.  With
+// keys of 10 of a unit vector in common o' was off by 0.012 in relative L2, with 30 by 0.035;
+// now 0.0022.  The mean costs a second look at a row's first tile (4 %: 16 heads with tangents,
+// eight sequences of 1024, 78.7 to 81.9 us).
 // What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 362 us, 1.45 PF/s of
 // causal work, the tensor pipe busy 67 % of the cycles); at 64 the chain scores - maximum -
 // exponentials - product of each CTA, which two or three CTAs an SM fill by turns (16 heads, 16384
@@ -534,7 +539,10 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
     const uint32_t aS = lanes + C::C_S, aSd = lanes + C::C_SD;
     const int lo = tile_lo(st_rows, row0, r);
     const uint64_t c2p = pair(p.c2, p.c2), scp = pair(p.scale, p.scale);
-    float m2 = -INFINITY, l = 0.f, rs = 0.f;
+    float m2 = -INFINITY, l = 0.f, rs = 0.f;    // rs: sum P (S' - cen)
+    float cen = 0.f;
+    // a row's first whole tile, where its first one holds the end of another sequence
+    const int j1 = (lo - k0) % TK ? (lo - k0) / TK + 1 : -1;
     bool ok = true;
     for (int j = 0; j < nkt; ++j) {
       const int st = j % C::STAGES;
@@ -579,26 +587,60 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       else find_max(std::false_type{});
       const float t2 = mx * p.c2;
       float f = 1.f;
-      if (t2 > m2 + TAU) {
+      bool again = DUAL && j == j1;
+      // with tangents earlier: a key that outweighs what c is the mean of takes part in it
+      if (t2 > m2 + (DUAL ? TAU / 2 : TAU)) {
         f = ex2(m2 - t2);
         m2 = t2;
+        again = true;
       }
       l *= f;
       rs *= f;
-      if (j > 0 && __any_sync(0xffffffffu, f != 1.f)) {
-        // scores j were issued behind the products of tile j - 1, which are done
+      const float base = m2 == -INFINITY ? 0.f : m2;     // no key of the row so far: P = 0
+      if (__any_sync(0xffffffffu, again)) {
+        float dc = 0.f;
+        if (DUAL) {
+          // c becomes the mean over all keys so far
+          float wl = 0.f, ws = 0.f;
 #pragma unroll 1
-        for (int c0 = 0; c0 < HDP * C::NT; c0 += 16) {
-          float v[16];
-          const uint32_t at = lanes + C::C_O + c0;
-          tmem_ld16(at, v);
+          for (int c0 = 0; c0 < TK; c0 += 16) {
+            float x[16], y[16];
+            tmem_ld16_nowait(aS + c0, x);
+            tmem_ld16_nowait(aSd + c0, y);
+            tmem_wait_ld();
+            const uint32_t w = mx_tile ? (c0 < 32 ? own[0] : own[TK / 32 - 1]) >> (c0 & 16) : 0xffffu;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] *= f;
-          tmem_st16(at, v);
+            for (int i = 0; i < 16; ++i) {
+              const float pe = w >> i & 1 ? ex2(fmaf(x[i], p.c2, -base)) : 0.f;
+              wl += pe;
+              ws = fmaf(pe, w >> i & 1 ? y[i] : 0.f, ws);
+            }
+          }
+          if (again) {
+            dc = __fdividef(fmaf(cen, wl, -p.scale * ws) - rs, l + wl);
+            rs = fmaf(dc, l, rs);
+            cen -= dc;
+          }
+        }
+        if (j > 0) {
+          // scores j were issued behind the products of tile j - 1, which are done
+#pragma unroll 1
+          for (int c0 = 0; c0 < HDP; c0 += 16) {
+            float v[16], t[16];
+            tmem_ld16_nowait(lanes + C::C_O + c0, v);
+            if (DUAL) tmem_ld16_nowait(lanes + C::C_T + c0, t);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              v[i] *= f;
+              if (DUAL) t[i] = fmaf(dc, v[i], t[i] * f);
+            }
+            tmem_st16(lanes + C::C_O + c0, v);
+            if (DUAL) tmem_st16(lanes + C::C_T + c0, t);
+          }
         }
       }
-      const float base = m2 == -INFINITY ? 0.f : m2;     // no key of the row so far: P = 0
-      const uint64_t nm = pair(-base, -base);
+      const uint64_t nm = pair(-base, -base), nc = pair(-cen, -cen);
       uint64_t l2 = 0, r2 = 0;
       auto probs = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
@@ -624,7 +666,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
               l2 = add2(l2, pp);
               pk[i / 2] = pack_bf16x2(p0, p1);
               if (DUAL) {
-                const uint64_t ps = mul2(mul2(pp, scp), pair(sd[i], sd[i + 1]));
+                const uint64_t ps = mul2(pp, fma2(pair(sd[i], sd[i + 1]), scp, nc));
                 r2 = add2(r2, ps);
                 psk[i / 2] = pack2(ps);
               }
@@ -657,7 +699,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
     if (ok && rwait(bb + B_DRAIN, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const float inv = 1.f / l;
-      const float rb = DUAL ? rs * inv : 0.f;
+      const float rc = DUAL ? rs * inv : 0.f;     // rbar - cen
       float z = 0.f;
 #pragma unroll
       for (int c = 0; c < HDP; c += 16) {
@@ -668,7 +710,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           o[i] *= inv;
-          if (DUAL) t[i] = t[i] * inv - rb * o[i];
+          if (DUAL) t[i] = t[i] * inv - rc * o[i];
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -682,7 +724,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       if (r < nvalid) {
         const int64_t si = static_cast<int64_t>(h) * p.seq.rows + row0 + r;
         p.lse[si] = (m2 + log2f(l)) * LN2;
-        if (DUAL) p.rbar[si] = rb;
+        if (DUAL) p.rbar[si] = cen + rc;
       }
     } else {
       ok = false;
