@@ -506,7 +506,8 @@ mf_status mf_qk_rope_work_bytes(const mf_qk_rope_args* args, size_t* bytes);
  *           Calls that overlap in time need one each.
  * No value outside a row's own keys reaches it, not finite or not: what a masked place or a
  * row behind the last sequence holds does not matter.  A row that does attend to a key row
- * with a NaN or an infinity may get NaN or an infinity itself.
+ * with a NaN or an infinity may get NaN or an infinity itself.  Primal outputs do not depend on
+ * tangents: what is not finite in those alone reaches od, rbar, dqd, dkd and dvd alone.
  *  status   device int32 (nullable), never lowered: raised to MF_ERR_TIMEOUT when a bounded wait
  *           of a kernel ran out, or above where a kernel could not run; outputs are then undefined.
  * Errors: MF_ERR_INVALID_ARG, MF_ERR_UNSUPPORTED (tangents of heads wider than 64),

@@ -23,8 +23,8 @@
 // CTA whose results are all finite is done; one that finds a NaN or an infinity in them walks its
 // tiles a second time, carefully: in mixed tiles the rows that P or dS will multiply are looked
 // over first, what is not finite in them becomes zero, and rows that do attend to such a row get
-// NaN.  Others come out as if it was not there, bit for bit, and a call without such values pays
-// for a check of its results.
+// NaN, in their tangents alone where only tangents were not finite.  Others come out as if it was
+// not there, bit for bit, and a call without such values pays for a check of its results.
 //
 // Every wait is bounded (2 s), as in flash_tc.cu.
 #include <limits.h>
@@ -233,9 +233,9 @@ __device__ __forceinline__ uint32_t nan_pair(uint32_t w) {
 
 // ---- non-finite values of a mixed tile --------------------------------------------------------
 // A warp looks over `atoms` blocks of `rows` 128-byte rows of bf16, zeroes what is not finite
-// and sets the bit of its row in bad[].  0 * x is zero for every finite x and NaN otherwise, so
+// and sets the bit of its row in bad[].  With tangents these lie behind, and have bits of their own.  0 * x is zero for every finite x and NaN otherwise, so
 // one multiply-add a pair tells whether there is anything to do.
-__device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32_t* bad, int lane) {
+__device__ __forceinline__ void scrub_part(uint8_t* base, int rows, int atoms, uint32_t* bad, int lane) {
   const __nv_bfloat162 z = __float2bfloat162_rn(0.f);
   __nv_bfloat162 acc = z;
   const uint4* p = reinterpret_cast<const uint4*>(base);
@@ -269,6 +269,12 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
     fence_async_smem();
   }
   __syncwarp();
+}
+
+template <bool DUAL>
+__device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32_t (*bad)[4], int lane) {
+  scrub_part(base, rows, atoms, bad[0], lane);
+  if (DUAL) scrub_part(base + rows * atoms * 128, rows, atoms, bad[1], lane);
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -368,7 +374,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       B_V_CLEAN = 32 + 32 * C::STAGES;
   constexpr int NBARS = 4 + 5 * C::STAGES;
   __shared__ __align__(8) uint64_t bars[2][NBARS];
-  __shared__ uint32_t bad[C::STAGES][4];
+  __shared__ uint32_t bad[C::STAGES][2][4];    // rows of V, of V'
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, redo_flag;
@@ -499,9 +505,9 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       const uint32_t ph = (j / C::STAGES) & 1;
       if (careful) {
         if (!rwait(bb + B_V_FULL + 8 * st, ph, p.status, abort)) break;
-        if (lane < 4) bad[st][lane] = 0;
+        if (lane < 8) bad[st][lane >> 2][lane & 3] = 0;
         __syncwarp();
-        if (mixed(j)) scrub(sV + st * C::TILE_B, TK, C::NT * NA, bad[st], lane);
+        if (mixed(j)) scrub<DUAL>(sV + st * C::TILE_B, TK, NA, bad[st], lane);
         if (lane == 0) bar_arrive(bb + B_V_CLEAN + 8 * st);
         __syncwarp();
       }
@@ -543,7 +549,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
     float cen = 0.f;
     // a row's first whole tile, where its first one holds the end of another sequence
     const int j1 = (lo - k0) % TK ? (lo - k0) / TK + 1 : -1;
-    bool ok = true;
+    bool ok = true, hit = false, hitd = false;   // the row attends to a noted row of V, of V'
     for (int j = 0; j < nkt; ++j) {
       const int st = j % C::STAGES;
       const bool mx_tile = mixed(j);
@@ -556,7 +562,13 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
         }
         const int kb = k0 + j * TK;
 #pragma unroll
-        for (int c = 0; c < TK / 32; ++c) own[c] = col_bits(lo - kb - 32 * c, row0 + r - kb - 32 * c);
+        for (int c = 0; c < TK / 32; ++c) {
+          own[c] = col_bits(lo - kb - 32 * c, row0 + r - kb - 32 * c);
+          if (careful) {
+            hit |= (own[c] & bad[st][0][c]) != 0;
+            hitd |= DUAL && (own[c] & bad[st][1][c]) != 0;
+          }
+        }
       }
       tc_fence_after();
       // mixed tiles have code of their own: selects in the common one would be issued for every
@@ -671,16 +683,6 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
                 psk[i / 2] = pack2(ps);
               }
             }
-            if (MASK && careful) {
-              const uint32_t w = (own[c] & bad[st][c]) >> (16 * g);
-              if (w & 0xffffu) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                  pk[i] |= nan_pair(w >> (2 * i));
-                  if (DUAL) psk[i] |= nan_pair(w >> (2 * i));
-                }
-              }
-            }
             tmem_st8(aS + 32 * c + 8 * g, pk);
             if (DUAL) tmem_st8(aSd + 32 * c + 8 * g, psk);
           }
@@ -698,8 +700,8 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
     }
     if (ok && rwait(bb + B_DRAIN, 0, p.status, abort) && !*abort) {
       tc_fence_after();
-      const float inv = 1.f / l;
-      const float rc = DUAL ? rs * inv : 0.f;     // rbar - cen
+      const float inv = hit ? NAN : 1.f / l, invd = hitd ? NAN : inv;
+      const float rc = DUAL ? rs / l : 0.f;     // rbar - cen
       float z = 0.f;
 #pragma unroll
       for (int c = 0; c < HDP; c += 16) {
@@ -710,7 +712,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           o[i] *= inv;
-          if (DUAL) t[i] = t[i] * inv - rc * o[i];
+          if (DUAL) t[i] = t[i] * invd - rc * o[i];
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -960,7 +962,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
                      B_Y_EMPTY = B_Y_FULL + 8 * C::YS;
   constexpr int NBARS = 10 + 2 * C::XS + 2 * C::YS;
   __shared__ __align__(8) uint64_t bars[2][NBARS];
-  __shared__ uint32_t bad[2][4];
+  __shared__ uint32_t bad[2][2][4];            // rows of Q and dO, of Q' and dO'
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, redo_flag;
@@ -1108,10 +1110,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
         if (!rwait(bb + B_X_FULL + 8 * x.st, x.ph, p.status, abort)) break;
         if (!rwait(bb + B_Y_FULL + 8 * y.st, y.ph, p.status, abort)) break;
         if (mx) {
-          if (lane < 4) bad[sl][lane] = 0;
+          if (lane < 8) bad[sl][lane >> 2][lane & 3] = 0;
           __syncwarp();
-          scrub(sX + x.st * C::TILE_B, BT, C::NT * NA, bad[sl], lane);
-          scrub(sY + y.st * C::TILE_B, BT, C::NT * NA, bad[sl], lane);
+          scrub<DUAL>(sX + x.st * C::TILE_B, BT, NA, bad[sl], lane);
+          scrub<DUAL>(sY + y.st * C::TILE_B, BT, NA, bad[sl], lane);
         }
         x.next();
         y.next();
@@ -1223,12 +1225,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       if (++t == nqt) t = 0;
       // the statistics
       if (!rwait(bb + B_CLEAN + 8 * sl, (i >> 1) & 1, p.status, abort)) { ok = false; break; }
-      uint32_t own[C::OWN], bads[C::OWN] = {};   // the row's own columns, the noted ones of them
+      // the row's own columns, the noted ones of them, those noted in the tangents too
+      uint32_t own[C::OWN], bads[C::OWN] = {}, badd[C::OWN] = {};
       if (mx) {
 #pragma unroll
         for (int w = 0; w < C::OWN; ++w) {
           own[w] = col_bits(a - cb - 32 * w, b - 1 - cb - 32 * w);
-          if (careful) bads[w] = own[w] & (bad[sl][(cb >> 5) + w] >> (cb & 31));
+          if (careful) {
+            bads[w] = own[w] & (bad[sl][0][(cb >> 5) + w] >> (cb & 31));
+            badd[w] = bads[w] | (DUAL ? own[w] & (bad[sl][1][(cb >> 5) + w] >> (cb & 31)) : 0u);
+          }
         }
       }
       const float4* stat = reinterpret_cast<const float4*>(sStat + sl * C::STAT_F + cb);
@@ -1274,11 +1280,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               }
             }
           }
-          if (MASK && bads[c0 >> 5]) {
+          if (MASK && badd[c0 >> 5]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               pk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
-              if (DUAL) pdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) pdk[k] |= nan_pair(badd[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_S + c0 / 2, pk);
@@ -1329,11 +1335,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               }
             }
           }
-          if (MASK && bads[c0 >> 5]) {
+          if (MASK && badd[c0 >> 5]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
-              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(badd[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(lane_base + C::C_DP + c0 / 2, sk);
@@ -1456,7 +1462,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
                      B_Y_FULL = B_CLEAN + 8 * C::XS, B_Y_EMPTY = B_Y_FULL + 8 * C::YS;
   constexpr int NBARS = 8 + 3 * C::XS + 2 * C::YS;
   __shared__ __align__(8) uint64_t bars[2][NBARS];
-  __shared__ uint32_t bad[C::XS][4];
+  __shared__ uint32_t bad[C::XS][2][4];        // rows of K, of K'
   __shared__ float2 sD[TR];
   __shared__ SeqTile st_rows;
   __shared__ uint32_t tmem_slot;
@@ -1565,9 +1571,9 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     Ring<C::XS> x;
     for (int j = 0; careful && j < nkt; ++j) {
       if (!rwait(bb + B_X_FULL + 8 * x.st, x.ph, p.status, abort)) break;
-      if (lane < 4) bad[x.st][lane] = 0;
+      if (lane < 8) bad[x.st][lane >> 2][lane & 3] = 0;
       __syncwarp();
-      if (mixed(j)) scrub(sX + x.st * C::TILE_B, BT, C::NT * NA, bad[x.st], lane);
+      if (mixed(j)) scrub<DUAL>(sX + x.st * C::TILE_B, BT, NA, bad[x.st], lane);
       if (lane == 0) bar_arrive(bb + B_CLEAN + 8 * x.st);
       x.next();
     }
@@ -1665,7 +1671,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     for (int j = 0; j < nkt; ++j, x.next()) {
       const bool mx = mixed(j);
       const int a = lo - (k0 + j * BT), b = row0 + r - (k0 + j * BT);
-      uint32_t own[C::OWN], bads[C::OWN] = {};   // the row's own columns, the noted ones of them
+      uint32_t own[C::OWN], bads[C::OWN] = {}, badd[C::OWN] = {};   // as in the key-row kernel
       if (mx) {
         if (careful && !rwait(bb + B_CLEAN + 8 * x.st, x.ph, p.status, abort)) {
           ok = false;
@@ -1674,7 +1680,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 #pragma unroll
         for (int w = 0; w < C::OWN; ++w) {
           own[w] = col_bits(a - cb - 32 * w, b - cb - 32 * w);
-          if (careful) bads[w] = own[w] & (bad[x.st][(cb >> 5) + w] >> (cb & 31));
+          if (careful) {
+            bads[w] = own[w] & (bad[x.st][0][(cb >> 5) + w] >> (cb & 31));
+            badd[w] = bads[w] | (DUAL ? own[w] & (bad[x.st][1][(cb >> 5) + w] >> (cb & 31)) : 0u);
+          }
         }
       }
       if (!rwait(bb + B_S_FULL, j & 1, p.status, abort)) { ok = false; break; }
@@ -1740,11 +1749,11 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
               sdk[f / 2] = pack_bf16x2(z.x, z.y);
             }
           }
-          if (MASK && bads[c0 >> 5]) {
+          if (MASK && badd[c0 >> 5]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               sk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
-              if (DUAL) sdk[k] |= nan_pair(bads[c0 >> 5] >> ((c0 & 31) + 2 * k));
+              if (DUAL) sdk[k] |= nan_pair(badd[c0 >> 5] >> ((c0 & 31) + 2 * k));
             }
           }
           tmem_st8(aP + c0 / 2, sk);
