@@ -145,7 +145,9 @@ DecPlan make_dec_plan(const mf_ctx* h, const DecLayout& Ly, int rows, int T, int
   p.Fl = take(N * V * 4); p.Fld = take(N * V * 4);
   p.lse = take(N * 4); p.ltok = take(N * 4); p.pf = take(N * 4); p.ldtok = take(N * 4);
   p.dF = take(N * V * es); p.dFd = take(N * V * es);
-  p.qkv = take(N * Ly.W3 * 4); p.qkvd = take(N * Ly.W3 * 4);
+  // with head norms every block keeps its own (xh, xhd)
+  const size_t qkv4 = Ly.norm ? 0 : N * Ly.W3 * 4;
+  p.qkv = take(qkv4); p.qkvd = take(qkv4);
   p.Sc = take(SS * 4); p.Scd = take(SS * 4);
   // per-head float32 attention outputs (the fused attention writes them head-merged instead)
   const size_t osz = fused ? 0 : static_cast<size_t>(BH) * S * Ly.dh * 4;
@@ -157,7 +159,7 @@ DecPlan make_dec_plan(const mf_ctx* h, const DecLayout& Ly, int rows, int T, int
   p.dP = take(SS * 4); p.dPd = take(SS * 4);
   p.dS = take(SS * es); p.dSd = take(SS * es);
   if (fused) p.fD = take(2 * stat);
-  p.rope = take(static_cast<size_t>(S) * (Ly.dh / 2) * 2 * 4);
+  p.rope = take(Ly.heads ? 0 : static_cast<size_t>(S) * (Ly.dh / 2) * 2 * 4);
   const size_t head4 = Ly.heads ? 0 : static_cast<size_t>(BH) * S * Ly.dh * 4;
   p.dQ = take(head4); p.dQd = take(head4); p.dK = take(head4); p.dKd = take(head4);
   p.dV = take(head4); p.dVd = take(head4);
