@@ -99,8 +99,9 @@ mf_status done(cudaError_t e) {
   return MF_ERR_CUDA;
 }
 
-size_t rope_work(const mf_qk_rope_args& a) {
-  return static_cast<size_t>(mf::kRopeMaxBlocks) * (a.dyd || a.xd ? 4 : 2) * a.head_dim * sizeof(float);
+// Partial sums of two gains' gradients, and with tangents of theirs.
+size_t rope_work(const mf_qk_rope_args& a, bool dual) {
+  return static_cast<size_t>(mf::kRopeMaxBlocks) * (dual ? 4 : 2) * a.head_dim * sizeof(float);
 }
 
 // Checks what the two passes share and fills the kernels' parameters.
@@ -210,7 +211,7 @@ extern "C" {
 mf_status mf_qk_rope_work_bytes(const mf_qk_rope_args* args, size_t* bytes) {
   if (!args || !bytes || !heads_ok(args->n_heads, args->n_kv_heads, args->n_copy_heads, args->head_dim))
     return MF_ERR_INVALID_ARG;
-  *bytes = rope_work(*args);
+  *bytes = rope_work(*args, args->dyd || args->xd);   // xd: asked with the forward's arguments
   return MF_OK;
 }
 
@@ -243,7 +244,7 @@ mf_status mf_qk_rope_bwd(const mf_qk_rope_args* args, void* stream) {
   const bool dual = a.dyd != nullptr, norm = a.gq != nullptr;
   if (!both(a.dyd, a.dxd) || (a.gqd && !dual)) return MF_ERR_INVALID_ARG;
   if (norm && (!a.dgq || !a.dgk || (dual && (!a.dgqd || !a.dgkd || !a.xd)) || !a.work ||
-               !aligned(a.work) || a.work_bytes < rope_work(a)))
+               !aligned(a.work) || a.work_bytes < rope_work(a, dual)))
     return MF_ERR_INVALID_ARG;
   if (a.n_rows == 0) {   // sums over no rows
     cudaError_t e = cudaSuccess;

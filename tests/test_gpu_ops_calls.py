@@ -30,6 +30,27 @@ def test_equal_sequences_by_their_number(D, dual, n, length):
 
 
 @pytest.mark.gpu
+def test_rope_primal_backward_beside_a_tangent():
+    """xd given, no tangent of dy: the gradients of the primal pass, in its workspace."""
+    torch, native = need_gpu()
+    N, Hq, Hkv, D = 70, 3, 1, 64
+    g = torch.Generator().manual_seed(52)
+    rnd = lambda *s: torch.randn(*s, generator=g).cuda()
+    W = (Hq + Hkv) * D
+    x, xd, dy, gq, gk = rnd(N, W), rnd(N, W), rnd(N, W), rnd(D), rnd(D)
+    kw = dict(n_heads=Hq, n_kv_heads=Hkv, head_dim=D, rope=native.rope_desc(), gq=gq, gk=gk)
+    work = torch.empty(native.mf_qk_rope_work_bytes(N, Hq, Hkv, D), dtype=torch.uint8, device="cuda")
+    got = []
+    for tangent in (None, xd):
+        o = [torch.full_like(x, 3.0), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")]
+        native.mf_qk_rope_bwd(dy, o[0], x=x, xd=tangent, dgq=o[1], dgk=o[2], work=work, **kw)
+        got.append(o)
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
 def test_norms_reserve_what_they_use():
     """Head norms keep each block's projected rows and their tangents, in place of the one pair of
     buffers that all blocks share without norms."""
