@@ -1743,9 +1743,11 @@ static mf_status create(const mf_model_desc* d, const mf_decoder_heads* heads, m
       return MF_ERR_INVALID_ARG;
     if (heads) {
       const int dh = d->d_model / d->n_heads;
+      mf_rope_desc rope = heads->rope;      // as dec_layout resolves it
+      if (rope.base == 0.f && d->rope_base > 0.f) rope.base = d->rope_base;
       if (heads->n_kv_heads < 0 || (heads->n_kv_heads > 0 && d->n_heads % heads->n_kv_heads != 0) ||
-          (heads->qk_norm != 0 && heads->qk_norm != 1) || !(heads->rope.base >= 0.f) || dh > 128 ||
-          !mf::rope_desc_ok(heads->rope, dh))
+          (heads->qk_norm != 0 && heads->qk_norm != 1) || !(rope.base >= 0.f) || dh > 128 ||
+          !mf::rope_desc_ok(rope, dh) || (heads->qk_norm && std::isinf(d->rms_eps)))
         return MF_ERR_INVALID_ARG;
       if (d->precision != MF_PREC_BF16 || dh > 64) return MF_ERR_UNSUPPORTED;
     }
