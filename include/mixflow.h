@@ -445,7 +445,7 @@ typedef struct {
  *  x, xd    rows and their tangent (nullable: no tangent), leading dimension ldx.
  *  y, yd    outputs, ldy.  y may be x (and yd xd) where types and leading dimensions agree.
  *  gq, gk   [head_dim] float32 gains of query and key heads (both or neither); gqd, gkd their
- *           tangents (nullable: zero).
+ *           tangents (nullable: zero).  Each begins on a 16-byte boundary, as the row buffers do.
  *  pos      [n_rows] int32 positions, any sign (nullable: the row's place in its sequence).
  *  seq_start, n_seq  as above; with pos given, both may be 0: every row is taken.
  * The backward pass takes the forward's x, xd (with gains only), gains, positions and

@@ -374,8 +374,8 @@ def mf_qk_rope_fwd(x, y, n_heads, n_kv_heads, head_dim, rope, n_copy_heads=0, xd
                    gq=None, gk=None, gqd=None, gkd=None, eps=1e-6, pos=None, seq_start=None,
                    n_seq=1, status=None, stream=None):
     """Rows of heads x [N][(n_heads + n_kv_heads + n_copy_heads) head_dim] -> y: RMS norm of the
-    query and key heads (with gains gq, gk), rotary positions, the type of y; xd -> yd the
-    tangent (see mixflow.h)."""
+    query and key heads (with gains gq, gk, each on a 16-byte boundary), rotary positions, the
+    type of y; xd -> yd the tangent (see mixflow.h)."""
     c = _rope_call(x, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
                    pos, seq_start, n_seq, status)
     c.a.x_prec, c.a.y_prec = _prec(x, "x"), _prec(y, "y")
