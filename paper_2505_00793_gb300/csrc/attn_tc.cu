@@ -316,7 +316,7 @@ struct FwdCfg {
 
 struct TcParams2 {
   SeqRows seq;
-  int Hq, Hkv, D, tiles;
+  int D, tiles;
   int G;                          // query heads of a group
   int share, Gs;                  // key-row kernel: CTAs that share a group, query heads of each
   float c2, scale;                // scale log2 e, scale
@@ -773,7 +773,7 @@ TcParams2 tc_params(const AttnParams& a) {
   TcParams2 p;
   memset(&p, 0, sizeof(p));
   p.seq = a.seq;
-  p.Hq = a.Hq; p.Hkv = a.Hkv; p.D = a.D;
+  p.D = a.D;
   p.tiles = (a.seq.rows + TR - 1) / TR;
   p.G = a.Hq / a.Hkv;
   p.scale = a.scale;

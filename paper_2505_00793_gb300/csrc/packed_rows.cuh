@@ -23,14 +23,10 @@ __device__ __forceinline__ int seq_find(const SeqRows& s, int row) {
   return lo;
 }
 
-// First row of row's sequence, and the row behind its last one.
+// First row of row's sequence.
 __device__ __forceinline__ int seq_begin(const SeqRows& s, int row) {
   if (!s.start) return row - row % s.len;
   return min(max(s.start[seq_find(s, row)], 0), row);
-}
-__device__ __forceinline__ int seq_end(const SeqRows& s, int row) {
-  if (!s.start) return row - row % s.len + s.len;
-  return min(max(s.start[seq_find(s, row) + 1], row + 1), s.rows);
 }
 
 }  // namespace mf

@@ -408,7 +408,7 @@ __device__ __forceinline__ void fwd_rows(const RopeParams& p, char* ring, RopeSh
   Turns turns{};
   bool fresh = true;
   for (Cursor k = first_part(p, total); k.left > 0; fresh = next_part(p, k)) {
-    if (fresh && p.R > 0) turns = make_turns(p, t, next_pos(p, ps, k, total), tab, 1.f);
+    if (fresh) turns = make_turns(p, t, next_pos(p, ps, k, total), tab, 1.f);
     if (!rd.next()) break;
     const Tx* sx = reinterpret_cast<const Tx*>(rd.stage());
     const int h0 = k.c * p.hc, n = min(p.hc, H - h0);
