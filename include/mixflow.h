@@ -424,7 +424,8 @@ enum { MF_ROPE_SCALE_NONE = 0, MF_ROPE_SCALE_LINEAR = 1, MF_ROPE_SCALE_BASE = 2,
  *           fewer than low_turns get w_j / factor, and between the two (0 <= low < high) the
  *           weight of w_j rises linearly with the turns.
  * Angles are reduced modulo a turn in 64-bit fixed point, so that far positions cost no
- * accuracy (about 1e-7 in cos and sin, as at position 0). */
+ * accuracy but that of the rates themselves, which are 64-bit floats: about 1e-7 in cos and sin,
+ * as at position 0, up to 10^8 positions, 5e-7 at 2^31. */
 typedef struct {
   int layout, dims;
   float base;

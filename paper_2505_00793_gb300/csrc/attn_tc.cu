@@ -14,10 +14,17 @@
 // memory is moved for it, and the products of one CTA, issued by one thread in order, need no
 // barrier between reading P and overwriting it with the next scores.
 //
-// Rounded to bf16 are the outputs and, as operands of the tensor cores next to bf16 rows, P, P',
-// dS and dS', each by 2^-8 of its value at most; scores, maxima, sums, lse, rbar, D and every
-// accumulator are float32.  Against 64 bits an output is off by 0.0024 to 0.0026 in relative L2,
-// of which its own rounding is 0.0017.
+// Rounded to bf16 are the outputs and, as operands of the tensor cores next to bf16 rows, P,
+// P (*) (S' - c), P', dS and dS', each by 2^-8 of its value at most: the tensor cores take both operands
+// of a product in one 16-bit type, and the rows are bf16.  Scores, maxima, sums, lse, rbar, D and
+// every accumulator are float32; D comes from the rounded o, D' from o and o'.  Off from 64 bits, in
+// relative L2 (an output's own rounding alone is 0.0017; independent rows of unit variance):
+//   1024 tokens             o 0.0020, o' 0.0022, dv, dv' 0.0023, dq, dk, dq', dk' 0.0025
+//   2 tokens                dq, dk 0.0038, dq', dk' 0.0042 (8 tokens 0.0031): dP - D is a difference of
+//                           near values, and D carries o's rounding
+//   scores of std 3, 8      o' 0.0027, 0.0040, dq .. dk' up to 0.0034, 0.0058
+//   keys with 3, 10 of a unit vector in common    dq, dq' 0.0088, 0.029, all else as above: the roundings
+//                           of dS and D leave sum dS = 0 off by 2^-9 of its terms, times what the keys share
 //
 // Values of masked places: a product with a zero of P still meets them (0 * inf = NaN).  So a
 // CTA whose results are all finite is done; one that finds a NaN or an infinity in them walks its
@@ -287,11 +294,12 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // part) cancels in o', and rounded to bf16 as part of P (*) S' it would leave 2^-9 of itself.  With
 // keys of 10 of a unit vector in common o' was off by 0.012 in relative L2, with 30 by 0.035;
 // now 0.0022.  The mean costs a second look at a row's first tile (4 %: 16 heads with tangents,
-// eight sequences of 1024, 78.7 to 81.9 us).
-// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 362 us, 1.45 PF/s of
-// causal work, the tensor pipe busy 67 % of the cycles); at 64 the chain scores - maximum -
+// eight sequences of 1024, 78.7 to 81.9 us; 81 with the marks of noted rows kept apart).
+// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 387 us, 1.42 PF/s of
+// causal work, and 360 us, 1.53 PF/s, over the same rows again and again; the tensor pipe busy 67 % of
+// the cycles); at 64 the chain scores - maximum -
 // exponentials - product of each CTA, which two or three CTAs an SM fill by turns (16 heads, 16384
-// rows: 0.95 PF/s; 16 heads with tangents, eight sequences of 1024: 80 us, pipe 36 %).  Taking the
+// rows: 0.94 PF/s; 16 heads with tangents, eight sequences of 1024: 81 us, pipe 35 %).  Taking the
 // exponentials against the last tile's maximum, so that they need not wait for this one's, cost
 // registers and was up to 17 % slower.
 // TKEYS keys a tile: 64 where the tangents leave no TMEM for more, and where many CTAs are to be
@@ -1814,7 +1822,10 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 }
 
 // CTAs of a cluster that share the query heads of a group in the key-row kernel: the fewest
-// (dividing the group, at most 8) that fill the GPU's places three times over.
+// (dividing the group, at most 8) that fill the GPU's places three times over.  A backward pass with
+// one CTA a group, these, and as many as divide it: 8 heads of 64 over one, 512 rows 78, 28 and 28 us;
+// 16 over 4 with tangents, 8192 rows 252, 236 and 264; 32 over 8, 16384 rows in sequences of 256 212,
+// 212 and 292; 16 of 128 over 4, 12289 rows 669, 569 and 635.
 int kv_share(int group, int64_t ctas, int per_sm) {
   int best = 1;
   for (int n = 1; n <= 8 && n <= group; ++n) {
@@ -1891,10 +1902,12 @@ cudaError_t attn_tc_bwd(const AttnParams& a, bool dual, cudaStream_t s) {
 cudaError_t attn_tc_fwd(const AttnParams& a, bool dual, cudaStream_t s) {
   if (dual) return launch_fwd<true, 64, 64>(a, s);
   if (a.D > 64) return launch_fwd<false, 128, 128>(a, s);
-  // From two rounds of three CTAs an SM on, tiles of 64 keys: 16 heads of 64, six sequences in
-  // 8192 rows 79 us against 90 with tiles of 128 and two CTAs, in 7168 rows (896 CTAs) 76 against
-  // 73, in 4096 rows 39 against 37: with fewer CTAs a walk's own length counts, and it has twice
-  // as many steps.
+  // From two rounds of three CTAs an SM on, tiles of 64 keys, whatever the sequences' lengths and the
+  // heads' width: 16 heads of 64, 8192 rows in sequences of 16, 128, 1024 and 4096 take 20, 19, 40 and
+  // 90 us against 24, 23, 43 and 99 with tiles of 128 and two CTAs; heads of 32 the same; 32 heads in
+  // 16384 rows 70, 64, 128 and 332 against 89, 82, 148 and 352.  With fewer CTAs a walk's own
+  // length counts, and it has twice as many steps: 4096 rows (512 CTAs) in sequences of 128, 1024 and
+  // 4096 take 13, 24 and 60 us against 13, 26 and 56.
   const int64_t ctas = static_cast<int64_t>((a.seq.rows + TR - 1) / TR) * a.Hq;
   return ctas >= 2 * 3 * 152 ? launch_fwd<false, 64, 64>(a, s) : launch_fwd<false, 64, 128>(a, s);
 }
