@@ -240,7 +240,7 @@ __device__ __forceinline__ uint32_t nan_pair(uint32_t w) {
 
 // ---- non-finite values of a mixed tile --------------------------------------------------------
 // A warp looks over `atoms` blocks of `rows` 128-byte rows of bf16, zeroes what is not finite
-// and sets the bit of its row in bad[].  With tangents these lie behind, and have bits of their own.  0 * x is zero for every finite x and NaN otherwise, so
+// and sets the bit of its row in bad[].  0 * x is zero for every finite x and NaN otherwise, so
 // one multiply-add a pair tells whether there is anything to do.
 __device__ __forceinline__ void scrub_part(uint8_t* base, int rows, int atoms, uint32_t* bad, int lane) {
   const __nv_bfloat162 z = __float2bfloat162_rn(0.f);
@@ -278,6 +278,7 @@ __device__ __forceinline__ void scrub_part(uint8_t* base, int rows, int atoms, u
   __syncwarp();
 }
 
+// An operand's rows, and behind them its tangent's, which have bits of their own.
 template <bool DUAL>
 __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32_t (*bad)[4], int lane) {
   scrub_part(base, rows, atoms, bad[0], lane);
@@ -289,17 +290,20 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // ring of V), warp 1 owns TMEM, looks over mixed V tiles and issues the products, warps 2..5 hold
 // the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).
 // The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T into S';
-// P [V | V'] -> [O | T], then (P (*) (S' - c)) V into T; o' = T / l - (rbar - c) o.  c is a mean of the
-// row's S' so far: what all of a row's S' have in common (keys or their tangents with a common
-// part) cancels in o', and rounded to bf16 as part of P (*) S' it would leave 2^-9 of itself.  With
-// keys of 10 of a unit vector in common o' was off by 0.012 in relative L2, with 30 by 0.035;
-// now 0.0022.  The mean costs a second look at a row's first tile (4 %: 16 heads with tangents,
-// eight sequences of 1024, 78.7 to 81.9 us; 81 with the marks of noted rows kept apart).
+// P [V | V'] -> [O | T], then (P (*) (S' - c)) V into T; o' = T / l - (rbar - c) o.  c is a mean of
+// the row's S', over its first tiles and over keys that outweigh those: what all of a row's S' have
+// in common (keys or their tangents with a common part) cancels in o', and rounded to bf16 as part
+// of P (*) S' it would leave 2^-9 of itself.  With keys of 10 of a unit vector in common o' was off by
+// 0.012 in relative L2, with 30 by 0.035; now 0.0022.  The mean costs nothing where scores spread like a
+// unit normal (16 heads with tangents, eight sequences of 1024: 79 us either way); where maxima move
+// on many tiles it costs a look more at each: scores of std 3 and 8 82 to 92 us and 89 to 118, o' off
+// by 0.0030 and 0.0045 where it was by 0.0032 and 0.0052.  The plain mean of the first tile alone took 82
+// and 90 us, but left rows of one heavy key further off than P (*) S' did.
 // What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 387 us, 1.42 PF/s of
 // causal work, and 360 us, 1.53 PF/s, over the same rows again and again; the tensor pipe busy 67 % of
 // the cycles); at 64 the chain scores - maximum -
 // exponentials - product of each CTA, which two or three CTAs an SM fill by turns (16 heads, 16384
-// rows: 0.94 PF/s; 16 heads with tangents, eight sequences of 1024: 81 us, pipe 35 %).  Taking the
+// rows: 0.94 PF/s; 16 heads with tangents, eight sequences of 1024: 79 us, pipe 36 %).  Taking the
 // exponentials against the last tile's maximum, so that they need not wait for this one's, cost
 // registers and was up to 17 % slower.
 // TKEYS keys a tile: 64 where the tangents leave no TMEM for more, and where many CTAs are to be
@@ -607,9 +611,9 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       else find_max(std::false_type{});
       const float t2 = mx * p.c2;
       float f = 1.f;
-      bool again = DUAL && j == j1;
-      // with tangents earlier: a key that outweighs what c is the mean of takes part in it
-      if (t2 > m2 + (DUAL ? TAU / 2 : TAU)) {
+      bool again = DUAL && j == j1, heavy = mx_tile;
+      if (t2 > m2 + TAU) {
+        heavy |= m2 != -INFINITY;
         f = ex2(m2 - t2);
         m2 = t2;
         again = true;
@@ -620,24 +624,43 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       if (__any_sync(0xffffffffu, again)) {
         float dc = 0.f;
         if (DUAL) {
-          // c becomes the mean over all keys so far
+          // Over a row's first whole tile the plain mean.  In a mixed one, where the row may have few
+          // keys and this be its last, and where its maximum has moved, that with the weights P over all
+          // keys so far: rbar itself, if no more come or none that weigh.
           float wl = 0.f, ws = 0.f;
+          auto mean = [&](auto weighted) {
+            constexpr bool W = decltype(weighted)::value;
 #pragma unroll 1
-          for (int c0 = 0; c0 < TK; c0 += 16) {
-            float x[16], y[16];
-            tmem_ld16_nowait(aS + c0, x);
-            tmem_ld16_nowait(aSd + c0, y);
-            tmem_wait_ld();
-            const uint32_t w = mx_tile ? (c0 < 32 ? own[0] : own[TK / 32 - 1]) >> (c0 & 16) : 0xffffu;
+            for (int c0 = 0; c0 < TK; c0 += 16) {
+              float x[16], y[16];
+              if (W) tmem_ld16_nowait(aS + c0, x);
+              tmem_ld16_nowait(aSd + c0, y);
+              tmem_wait_ld();
+              if constexpr (W) {
+                const uint32_t w = mx_tile ? (c0 < 32 ? own[0] : own[TK / 32 - 1]) >> (c0 & 16) : 0xffffu;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float pe = w >> i & 1 ? ex2(fmaf(x[i], p.c2, -base)) : 0.f;
-              wl += pe;
-              ws = fmaf(pe, w >> i & 1 ? y[i] : 0.f, ws);
+                for (int i = 0; i < 16; ++i) {
+                  x[i] = heavy ? ex2(fmaf(x[i], p.c2, -base)) : 1.f;
+                  x[i] = w >> i & 1 ? x[i] : 0.f;
+                  y[i] = w >> i & 1 ? x[i] * y[i] : 0.f;
+                }
+              }
+#pragma unroll
+              for (int k = 8; k > 0; k >>= 1)
+#pragma unroll
+                for (int i = 0; i < k; ++i) {
+                  if (W) x[i] += x[i + k];
+                  y[i] += y[i + k];
+                }
+              if (W) wl += x[0];
+              ws += y[0];
             }
-          }
-          if (again) {
-            dc = __fdividef(fmaf(cen, wl, -p.scale * ws) - rs, l + wl);
+          };
+          if (__any_sync(0xffffffffu, again && heavy)) mean(std::true_type{});
+          else mean(std::false_type{});
+          if (again && m2 != -INFINITY) {
+            dc = heavy ? __fdividef(fmaf(cen, wl, -p.scale * ws) - rs, l + wl)
+                       : fmaf(-p.scale / TK, ws, cen);
             rs = fmaf(dc, l, rs);
             cen -= dc;
           }

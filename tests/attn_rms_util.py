@@ -166,7 +166,7 @@ def emulate(v, lens, Hq, Hkv, D, scale=None, centre=True, drop=()):
         Sd = scale * (Qd @ K.mT + Q @ Kd.mT) * low
         rb = (p * Sd).sum(-1, keepdim=True) / l
         out["rbar"][:, s] = rb.squeeze(-1)
-        c = (p * Sd)[..., :64].sum(-1, keepdim=True) / p[..., :64].sum(-1, keepdim=True) if centre else 0 * rb
+        c = Sd[..., :64].sum(-1, keepdim=True) / low[:, :64].sum(-1, keepdim=True) if centre else 0 * rb
         od = (r16(p * (Sd - c)) @ V + r16(p) @ Vd * ("od" not in drop)) / l - (rb - c) * acc
         put("od", od)
         Od = r16(od)
