@@ -22,7 +22,7 @@
 //   1024 tokens             o 0.0020, o' 0.0022, dv, dv' 0.0023, dq, dk, dq', dk' 0.0025
 //   2 tokens                dq, dk 0.0038, dq', dk' 0.0042 (8 tokens 0.0031): dP - D is a difference of
 //                           near values, and D carries o's rounding
-//   scores of std 3, 8      o' 0.0027, 0.0040, dq .. dk' up to 0.0034, 0.0058
+//   scores of std 3, 8      o' 0.0030, 0.0045, dq .. dk' up to 0.0035, 0.0075
 //   keys with 3, 10 of a unit vector in common    dq, dq' 0.0088, 0.029, all else as above: the roundings
 //                           of dS and D leave sum dS = 0 off by 2^-9 of its terms, times what the keys share
 //
@@ -299,7 +299,7 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // on many tiles it costs a look more at each: scores of std 3 and 8 82 to 92 us and 89 to 118, o' off
 // by 0.0030 and 0.0045 where it was by 0.0032 and 0.0052.  The plain mean of the first tile alone took 82
 // and 90 us, but left rows of one heavy key further off than P (*) S' did.
-// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 387 us, 1.42 PF/s of
+// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 381 to 387 us, 1.43 PF/s of
 // causal work, and 360 us, 1.53 PF/s, over the same rows again and again; the tensor pipe busy 67 % of
 // the cycles); at 64 the chain scores - maximum -
 // exponentials - product of each CTA, which two or three CTAs an SM fill by turns (16 heads, 16384
