@@ -65,3 +65,60 @@ def test_norms_reserve_what_they_use():
     pair = 2 * 16 * 128 * (4 + 2 * 2) * 32 * 4
     # the gains themselves, their copies and the workspace of their sums are below a quarter of it
     assert size[True] - size[False] <= (w.n_blocks - 1) * pair + pair // 4
+
+
+@pytest.mark.gpu
+def test_more_row_tiles_than_a_grid_is_high():
+    """Tiles behind the 65535th: the same bits as those rows by themselves."""
+    torch, native = need_gpu()
+    D, L, n = 8, 64, 65535 * 128 + 384
+    g = torch.Generator(device="cuda").manual_seed(53)
+    v = {k: torch.randn(n, D, generator=g, device="cuda").bfloat16()
+         for k in ("q", "k", "v", "do", "qd", "kd", "vd", "dod")}
+    outs = []
+    for rows in (n, 512):
+        w = {k: t[n - rows:] for k, t in v.items()}
+        starts = torch.arange(0, rows + 1, L, dtype=torch.int32, device="cuda")
+        outs.append(au.run(native, w, None, 1, 1, D, starts=starts))
+    torch.cuda.synchronize()
+    assert int(outs[0]["status"].item()) == 0
+    for k in au.names(True):
+        a, b = outs[0][k], outs[1][k]
+        a = a[:, n - 512:] if k in ("lse", "rbar") else a[n - 512:]
+        assert torch.equal(a, b) and torch.isfinite(b).all(), k
+        assert not (outs[0][k] == au.MARK).all(), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dual", [False, True])
+def test_many_heads_of_few_rows(dual):
+    """Two thousand query heads over one key head of eight columns."""
+    torch, native = need_gpu()
+    lens, Hq, Hkv, D = [3, 0, 5, 1], 2048, 1, 8
+    v = au.data(lens, 2, Hq, Hkv, D, dual, seed=54)
+    ref, bound = au.reference(v, lens, Hq, Hkv, D)
+    out = au.run(native, au.wide(v), lens, Hq, Hkv, D)
+    torch.cuda.synchronize()
+    au.check(out, ref, bound, sum(lens), dual)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,dual", [(64, False), (64, True), (128, False)])
+def test_sequences_do_not_feel_one_another(D, dual):
+    """A sequence's bits do not depend on what shares its tiles: other sequences' maxima that move,
+    tangents of other sizes, values near the largest."""
+    torch, native = need_gpu()
+    lens, Hq, Hkv = [40, 77, 200, 3, 130, 60], 4, 2
+    v = au.data(lens, 9, Hq, Hkv, D, dual, seed=55)
+    want = {k: t.clone() for k, t in au.run(native, au.wide(v), lens, Hq, Hkv, D).items()}
+    others = [r for r in range(sum(lens) + 9) if not (117 <= r < 317 or 320 <= r < 450)]
+    mine = [r for r in range(sum(lens)) if r not in others]
+    for scale in (30.0, 1e-3, 1e18):
+        w = {k: t.clone() for k, t in v.items()}
+        for t in w.values():
+            t[others] = (t[others].float() * scale).bfloat16()
+        got = au.run(native, au.wide(w), lens, Hq, Hkv, D)
+        torch.cuda.synchronize()
+        for k in au.names(dual):
+            a, b = (got[k].t(), want[k].t()) if k in ("lse", "rbar") else (got[k], want[k])
+            assert torch.equal(a[mine], b[mine]), (scale, k)
