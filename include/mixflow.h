@@ -537,6 +537,21 @@ mf_status mf_attn_fwd(const mf_attn_args* args, void* stream);
 mf_status mf_attn_bwd(const mf_attn_args* args, void* stream);
 mf_status mf_attn_work_bytes(const mf_attn_args* args, size_t* bytes);
 
+/* The same attention with a sliding window: a row attends to itself, to the window - 1 rows before
+ * it and to the first n_sink rows of its sequence (those up to itself), so never to no row.
+ *  args     as for mf_attn_fwd and mf_attn_bwd, tangents and gradients included; `work` of the
+ *           backward pass holds mf_attn_window_work_bytes() bytes, for the call's own args
+ *           (n_rows, heads, head_dim, whether there are tangents), window and n_sink.
+ *  window   >= 1; with window >= n_rows every row of a sequence up to its own is attended to, and
+ *           the results are mf_attn_*'s, bit for bit.
+ *  n_sink   0 .. 128.  The backward pass must be given the forward's window and n_sink.
+ * Sums over rows, a sink's over all rows of its sequence, are taken in a fixed order in float32.
+ * Errors: as for mf_attn_*; MF_ERR_INVALID_ARG (window < 1, n_sink < 0), MF_ERR_UNSUPPORTED
+ * (n_sink > 128). */
+mf_status mf_attn_window_fwd(const mf_attn_args* args, int64_t window, int n_sink, void* stream);
+mf_status mf_attn_window_bwd(const mf_attn_args* args, int64_t window, int n_sink, void* stream);
+mf_status mf_attn_window_work_bytes(const mf_attn_args* args, int64_t window, int n_sink, size_t* bytes);
+
 /* A decoder handle (desc->arch MF_ARCH_DECODER, MF_PREC_BF16, d_model / n_heads <= 64) whose
  * attention is made of these operators, everything else as with mf_create:
  *  n_kv_heads  key/value heads, a divisor of n_heads (0 = n_heads): Wqkv is

@@ -76,6 +76,25 @@ def attention(q, k, v, Hq, Hkv, D, lens, scale):
     return torch.cat(os), torch.cat(ls, 1)
 
 
+def window_pairs(lens, window, sinks, device="cpu"):
+    """Which rows attend to which, [N][N]: a row of a sequence to itself, the window - 1 rows before
+    it and the first sinks rows of the sequence up to itself."""
+    n = torch.tensor(lens, dtype=torch.long, device=device)
+    seq = torch.repeat_interleave(torch.arange(len(lens), device=device), n)
+    place = torch.arange(len(seq), device=device) - (torch.cumsum(n, 0) - n)[seq]
+    i, j = place[:, None], place[None, :]
+    return (seq[:, None] == seq[None, :]) & (j <= i) & ((i - j < window) | (j < sinks))
+
+
+def masked_attention(q, k, v, Hq, Hkv, D, pairs, scale):
+    """(o [N][Hq D], lse [Hq][N]) of rows that attend where pairs [N][N] says so."""
+    heads = lambda t, H: t.unflatten(1, (H, D)).transpose(0, 1)
+    K, V = (heads(t, Hkv).repeat_interleave(Hq // Hkv, 0) for t in (k, v))
+    S = (scale * heads(q, Hq) @ K.mT).masked_fill(~pairs, -math.inf)
+    lse = torch.logsumexp(S, -1)
+    return (torch.exp(S - lse[..., None]) @ V).transpose(0, 1).flatten(1), lse
+
+
 def grads(f, prim, cot):
     """Gradients of <f(prim), cot>."""
     return torch.func.vjp(f, *prim)[1](cot)

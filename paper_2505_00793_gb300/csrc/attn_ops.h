@@ -1,5 +1,5 @@
-// Operators on packed token rows (the entry points mf_qk_rope_* and mf_attn_* of ops_capi.cu,
-// which checks the arguments; kernels in rope_ops.cu and attn_tc.cu).
+// Operators on packed token rows (the entry points mf_qk_rope_*, mf_attn_* and mf_attn_window_* of
+// ops_capi.cu, which checks the arguments; kernels in rope_ops.cu and attn_tc_impl.cuh).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -63,9 +63,24 @@ struct AttnParams {
   float *lse = nullptr, *rbar = nullptr;     // [Hq][rows]
   float *Dr = nullptr, *Drd = nullptr;       // backward: D = rowsum(dO O) and its tangent
   int* status = nullptr;
+  // attn_window_*: rows of a window (fewer than seq.rows), first rows of a sequence that stay
+  // visible, sums of those rows' gradients
+  int window = 0, sinks = 0;
+  float* part = nullptr;
 };
 // Both passes (attn_tc.cu): heads of up to 128 columns, 64 with tangents.
 cudaError_t attn_tc_fwd(const AttnParams& p, bool dual, cudaStream_t s);
 cudaError_t attn_tc_bwd(const AttnParams& p, bool dual, cudaStream_t s);
+// The same with a window (attn_tc_window.cu).
+cudaError_t attn_window_fwd(const AttnParams& p, bool dual, cudaStream_t s);
+cudaError_t attn_window_bwd(const AttnParams& p, bool dual, cudaStream_t s);
+constexpr int kMaxSinks = 128;               // a tile of key rows
+// Query rows of a chunk that one CTA of the backward pass takes for a sequence's sinks.
+inline int window_chunk(int window) { return window > 512 ? 1024 : 512; }
+// Floats of AttnParams::part.
+inline int64_t window_part(int64_t rows, int Hkv, int D, int window, int sinks, bool dual) {
+  const int64_t chunk = window_chunk(window), chunks = (rows + chunk - 1) / chunk;
+  return sinks > 0 && chunks > 1 ? 2 * chunks * Hkv * (dual ? 4 : 2) * sinks * (D > 64 ? 128 : 64) : 0;
+}
 
 }  // namespace mf

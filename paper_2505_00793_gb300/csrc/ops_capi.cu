@@ -146,7 +146,18 @@ bool outputs_apart(std::initializer_list<const void*> outs, std::initializer_lis
   return true;
 }
 
-mf_status attn_params(const mf_attn_args& a, bool bwd, AttnParams* p) {
+size_t attn_work(const mf_attn_args& a) {
+  return static_cast<size_t>(a.n_rows) * a.n_heads * sizeof(float) * (a.qd ? 2 : 1);
+}
+// Behind that, on a 16-byte boundary, the sums of sinks.
+size_t window_work(const mf_attn_args& a, int64_t window, int sinks) {
+  const size_t rows = (attn_work(a) + 15) / 16 * 16;
+  const bool all = window >= a.n_rows;           // plain attention
+  return rows + (all ? 0 : sizeof(float) * mf::window_part(a.n_rows, a.n_kv_heads, a.head_dim,
+                                                           static_cast<int>(window), sinks, a.qd != nullptr));
+}
+
+mf_status attn_params(const mf_attn_args& a, bool bwd, AttnParams* p, size_t work) {
   if (!heads_ok(a.n_heads, a.n_kv_heads, 0, a.head_dim) || a.n_heads % a.n_kv_heads)
     return MF_ERR_INVALID_ARG;
   if (!make_seq(a.n_rows, a.seq_start, a.n_seq, false, &p->seq)) return MF_ERR_INVALID_ARG;
@@ -169,8 +180,7 @@ mf_status attn_params(const mf_attn_args& a, bool bwd, AttnParams* p) {
     ok = ok && rows_ok(a.d_o, a.lddo, cq, N) && rows_ok(a.dq, a.lddq, cq, N) &&
          rows_ok(a.dk, a.lddk, ck, N) && rows_ok(a.dv, a.lddv, ck, N) && a.work && aligned(a.work);
     if (dual) ok = ok && aligned(a.d_od) && aligned(a.dqd) && aligned(a.dkd) && aligned(a.dvd);
-    size_t need = 0;
-    ok = ok && mf_attn_work_bytes(&a, &need) == MF_OK && a.work_bytes >= need;
+    ok = ok && a.work_bytes >= work;
   }
   if (!ok) return MF_ERR_INVALID_ARG;
   if (dual && a.head_dim > 64) return MF_ERR_UNSUPPORTED;
@@ -197,6 +207,27 @@ mf_status attn_params(const mf_attn_args& a, bool bwd, AttnParams* p) {
     p->Drd = dual ? p->Dr + static_cast<int64_t>(a.n_heads) * N : nullptr;
   }
   return MF_OK;
+}
+
+mf_status attn_window(const mf_attn_args* args, int64_t window, int n_sink, bool bwd, void* stream) {
+  if (!args || window < 1 || n_sink < 0) return MF_ERR_INVALID_ARG;
+  const mf_attn_args& a = *args;
+  AttnParams p;
+  const bool sized = n_sink <= mf::kMaxSinks && a.n_rows >= 0 && a.n_rows <= INT32_MAX - 256 &&
+                     heads_ok(a.n_heads, a.n_kv_heads, 0, a.head_dim);    // else refused below
+  const size_t work = sized ? window_work(a, window, n_sink) : 0;
+  const mf_status st = attn_params(a, bwd, &p, work);
+  if (st != MF_OK) return st;
+  if (n_sink > mf::kMaxSinks) return MF_ERR_UNSUPPORTED;
+  if (a.n_rows == 0) return MF_OK;
+  const bool dual = a.qd != nullptr;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // a window that holds every row is no window: the kernels without one
+  if (window >= a.n_rows) return done(bwd ? mf::attn_tc_bwd(p, dual, s) : mf::attn_tc_fwd(p, dual, s));
+  p.window = static_cast<int>(window);
+  p.sinks = n_sink;
+  if (bwd) p.part = reinterpret_cast<float*>(static_cast<char*>(a.work) + (attn_work(a) + 15) / 16 * 16);
+  return done(bwd ? mf::attn_window_bwd(p, dual, s) : mf::attn_window_fwd(p, dual, s));
 }
 
 }  // namespace
@@ -282,14 +313,14 @@ mf_status mf_attn_work_bytes(const mf_attn_args* args, size_t* bytes) {
   if (!args || !bytes || args->n_rows < 0 || args->n_rows > INT32_MAX - 256 || args->n_heads < 1 ||
       args->n_heads > 65536)
     return MF_ERR_INVALID_ARG;
-  *bytes = static_cast<size_t>(args->n_rows) * args->n_heads * sizeof(float) * (args->qd ? 2 : 1);
+  *bytes = attn_work(*args);
   return MF_OK;
 }
 
 mf_status mf_attn_fwd(const mf_attn_args* args, void* stream) {
   if (!args) return MF_ERR_INVALID_ARG;
   AttnParams p;
-  const mf_status st = attn_params(*args, false, &p);
+  const mf_status st = attn_params(*args, false, &p, 0);
   if (st != MF_OK || args->n_rows == 0) return st;
   return done(mf::attn_tc_fwd(p, args->qd != nullptr, static_cast<cudaStream_t>(stream)));
 }
@@ -297,9 +328,26 @@ mf_status mf_attn_fwd(const mf_attn_args* args, void* stream) {
 mf_status mf_attn_bwd(const mf_attn_args* args, void* stream) {
   if (!args) return MF_ERR_INVALID_ARG;
   AttnParams p;
-  const mf_status st = attn_params(*args, true, &p);
+  const mf_status st = attn_params(*args, true, &p, attn_work(*args));
   if (st != MF_OK || args->n_rows == 0) return st;
   return done(mf::attn_tc_bwd(p, args->qd != nullptr, static_cast<cudaStream_t>(stream)));
+}
+
+mf_status mf_attn_window_work_bytes(const mf_attn_args* args, int64_t window, int n_sink, size_t* bytes) {
+  if (!args || !bytes || args->n_rows < 0 || args->n_rows > INT32_MAX - 256 ||
+      !heads_ok(args->n_heads, args->n_kv_heads, 0, args->head_dim) || window < 1 || n_sink < 0)
+    return MF_ERR_INVALID_ARG;
+  if (n_sink > mf::kMaxSinks) return MF_ERR_UNSUPPORTED;
+  *bytes = window_work(*args, window, n_sink);
+  return MF_OK;
+}
+
+mf_status mf_attn_window_fwd(const mf_attn_args* args, int64_t window, int n_sink, void* stream) {
+  return attn_window(args, window, n_sink, false, stream);
+}
+
+mf_status mf_attn_window_bwd(const mf_attn_args* args, int64_t window, int n_sink, void* stream) {
+  return attn_window(args, window, n_sink, true, stream);
 }
 
 }  // extern "C"

@@ -38,7 +38,8 @@ EXPORTS = ["mf_create", "mf_destroy", "mf_set_allocator", "mf_param_count",
            "mf_set_kernel_timing", "mf_kernel_time", "mf_inject_fault", "mf_dual_gemm_bf16",
            "mf_hvp_noalloc", "mf_set_option", "mf_replay_gemms", "mf_checkpoint_plan",
            "mf_qk_rope_fwd", "mf_qk_rope_bwd", "mf_qk_rope_work_bytes", "mf_attn_fwd",
-           "mf_attn_bwd", "mf_attn_work_bytes", "mf_create_decoder"]
+           "mf_attn_bwd", "mf_attn_work_bytes", "mf_create_decoder", "mf_attn_window_fwd",
+           "mf_attn_window_bwd", "mf_attn_window_work_bytes"]
 
 
 class mf_model_desc(C.Structure):
@@ -136,6 +137,8 @@ def load(path: str = LIB_PATH) -> C.CDLL:
         "mf_dual_gemm_bf16": ([C.c_int, C.c_int, C.c_int, vp, C.c_int, vp, C.c_int, vp, C.c_int, vp,
                                C.c_int, vp, C.c_int, vp, vp, C.c_int, vp, C.c_uint, vp], C.c_int),
     }
+    for name in ("mf_attn_window_fwd", "mf_attn_window_bwd", "mf_attn_window_work_bytes"):
+        sig[name] = ([vp, C.c_int64, C.c_int, vp], C.c_int)
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
         f.argtypes = args
@@ -334,14 +337,14 @@ class _Call:
             raise ValueError(f"work: expected a contiguous tensor on cuda:{self.device}")
         self.a.work, self.a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
 
-    def run(self, fn, stream):
+    def run(self, fn, stream, *more):
         import torch
         if self.device != torch.cuda.current_device():
             with torch.cuda.device(self.device):
-                return self.run(fn, stream)
+                return self.run(fn, stream, *more)
         # the current stream's handle without building a Stream object around it (4 us a call)
         handle = torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
-        st = getattr(_lib, fn)(C.byref(self.a), handle)
+        st = getattr(_lib, fn)(C.byref(self.a), *more, handle)
         if st != 0:
             raise MixflowError(st, fn)
 
@@ -424,9 +427,9 @@ def mf_attn_work_bytes(n_rows, n_heads, dual=False):
     return _bytes_of("mf_attn_work_bytes", a)
 
 
-def _bytes_of(fn, a):
+def _bytes_of(fn, a, *more):
     b = C.c_size_t()
-    st = getattr(lib(), fn)(C.byref(a), C.byref(b))
+    st = getattr(lib(), fn)(C.byref(a), *more, C.byref(b))
     if st != 0:
         raise MixflowError(st, fn)
     return b.value
@@ -460,11 +463,8 @@ def mf_attn_fwd(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd=None, kd=None
                n_seq, scale, status).run("mf_attn_fwd", stream)
 
 
-def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd=None,
-                kd=None, vd=None, od=None, rbar=None, dod=None, dqd=None, dkd=None, dvd=None,
-                seq_start=None, n_seq=1, scale=0.0, status=None, stream=None):
-    """Backward of mf_attn_fwd from its inputs and outputs and d_o (dod) -> dq, dk, dv (dqd, dkd,
-    dvd); work: mf_attn_work_bytes bytes."""
+def _attn_bwd_call(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd, kd,
+                   vd, od, rbar, dod, dqd, dkd, dvd, seq_start, n_seq, scale, status):
     import torch
     c = _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, rbar, seq_start,
                    n_seq, scale, status)
@@ -475,7 +475,45 @@ def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim,
     c.rows("dkd", dkd, bf, n, ck, "lddk", c.rows("dk", dk, bf, n, ck, "lddk"))
     c.rows("dvd", dvd, bf, n, ck, "lddv", c.rows("dv", dv, bf, n, ck, "lddv"))
     c.work(work)
-    c.run("mf_attn_bwd", stream)
+    return c
+
+
+def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd=None,
+                kd=None, vd=None, od=None, rbar=None, dod=None, dqd=None, dkd=None, dvd=None,
+                seq_start=None, n_seq=1, scale=0.0, status=None, stream=None):
+    """Backward of mf_attn_fwd from its inputs and outputs and d_o (dod) -> dq, dk, dv (dqd, dkd,
+    dvd); work: mf_attn_work_bytes bytes."""
+    _attn_bwd_call(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd, kd,
+                   vd, od, rbar, dod, dqd, dkd, dvd, seq_start, n_seq, scale,
+                   status).run("mf_attn_bwd", stream)
+
+
+def mf_attn_window_work_bytes(n_rows, n_heads, n_kv_heads, head_dim, window, n_sink=0, dual=False):
+    """Bytes of `work` that mf_attn_window_bwd takes."""
+    a = mf_attn_args()
+    a.n_rows, a.n_heads, a.n_kv_heads, a.head_dim = n_rows, n_heads, n_kv_heads, head_dim
+    a.qd = 16 if dual else None
+    return _bytes_of("mf_attn_window_work_bytes", a, window, n_sink)
+
+
+def mf_attn_window_fwd(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, window, n_sink=0, qd=None,
+                       kd=None, vd=None, od=None, rbar=None, seq_start=None, n_seq=1, scale=0.0,
+                       status=None, stream=None):
+    """mf_attn_fwd where a row attends to itself, the window - 1 rows before it and the first
+    n_sink rows of its sequence (see mixflow.h)."""
+    _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, rbar, seq_start,
+               n_seq, scale, status).run("mf_attn_window_fwd", stream, window, n_sink)
+
+
+def mf_attn_window_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, window,
+                       work, n_sink=0, qd=None, kd=None, vd=None, od=None, rbar=None, dod=None,
+                       dqd=None, dkd=None, dvd=None, seq_start=None, n_seq=1, scale=0.0,
+                       status=None, stream=None):
+    """Backward of mf_attn_window_fwd, as mf_attn_bwd is of mf_attn_fwd; work:
+    mf_attn_window_work_bytes bytes."""
+    _attn_bwd_call(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd, kd,
+                   vd, od, rbar, dod, dqd, dkd, dvd, seq_start, n_seq, scale,
+                   status).run("mf_attn_window_bwd", stream, window, n_sink)
 
 
 class MixFlow:
