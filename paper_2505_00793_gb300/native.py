@@ -139,6 +139,9 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     }
     for name in ("mf_attn_window_fwd", "mf_attn_window_bwd", "mf_attn_window_work_bytes"):
         sig[name] = ([vp, C.c_int64, C.c_int, vp], C.c_int)
+    for op in ("mf_qk_rope", "mf_attn"):
+        for call in ("fwd", "bwd", "work_bytes"):
+            sig[f"{op}_{call}"] = ([vp, vp], C.c_int)
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
         f.argtypes = args
