@@ -552,6 +552,50 @@ mf_status mf_attn_window_fwd(const mf_attn_args* args, int64_t window, int n_sin
 mf_status mf_attn_window_bwd(const mf_attn_args* args, int64_t window, int n_sink, void* stream);
 mf_status mf_attn_window_work_bytes(const mf_attn_args* args, int64_t window, int n_sink, size_t* bytes);
 
+/* Embedding lookup with scaling, and the gradient of the table:
+ *   y_r = scale E[id_r],   tangent: y'_r = scale E'[id_r]
+ *   dE_v = scale sum_{r: id_r = v} dy_r,   dE'_v = scale sum_{r: id_r = v} dy'_r
+ * A row whose id is no row of the table (below 0, or vocab and above) is padding: its y is zero and
+ * it has no part in dE.
+ *  n_rows   rows of ids, y and dy; 0 is a lookup that does nothing, and a gradient of zeros.
+ *  vocab, dim   rows and columns of the table, >= 1; dim at most 2^20, of any size.
+ *  ids      [n_rows] int32.
+ *  E, Ed    the table and its tangent (nullable: no tangent), type e_prec, ldE.
+ *  y, yd    outputs, type y_prec, ldy (yd with Ed).
+ *  scale    finite; multiplied in float32, results are rounded once.
+ *  seq_start, n_seq  as above; both may be 0: every row is taken.
+ * The backward pass takes ids, scale and
+ *  dy, dyd  gradients of y and y' (type y_prec, lddy; dyd nullable), and writes
+ *  dE, dEd  float32, lddE (dEd with dyd): all of it, zeros where no row has the id.  Sums are
+ *           float32 in an order that depends on ids and sizes alone.
+ *  work     mf_embed_work_bytes() bytes (from n_rows, vocab, dim and whether dyd is given) on a
+ *           16-byte boundary; its contents need not be kept.  Calls that overlap in time need one
+ *           each.
+ * Types are MF_PREC_FP32 or MF_PREC_BF16, in any combination.
+ * Errors: MF_ERR_INVALID_ARG, MF_ERR_CUDA. */
+typedef struct {
+  int64_t n_rows, vocab, dim;
+  int e_prec, y_prec;
+  float scale;
+  const int32_t* ids;
+  const void *E, *Ed;
+  int64_t ldE;
+  void *y, *yd;
+  int64_t ldy;
+  const int32_t* seq_start;
+  int n_seq;
+  const void *dy, *dyd;
+  int64_t lddy;
+  float *dE, *dEd;
+  int64_t lddE;
+  void* work;
+  size_t work_bytes;
+} mf_embed_args;
+
+mf_status mf_embed_fwd(const mf_embed_args* args, void* stream);
+mf_status mf_embed_bwd(const mf_embed_args* args, void* stream);
+mf_status mf_embed_work_bytes(const mf_embed_args* args, size_t* bytes);
+
 /* A decoder handle (desc->arch MF_ARCH_DECODER, MF_PREC_BF16, d_model / n_heads <= 64) whose
  * attention is made of these operators, everything else as with mf_create:
  *  n_kv_heads  key/value heads, a divisor of n_heads (0 = n_heads): Wqkv is

@@ -1,5 +1,6 @@
-// Operators on packed token rows (the entry points mf_qk_rope_*, mf_attn_* and mf_attn_window_* of
-// ops_capi.cu, which checks the arguments; kernels in rope_ops.cu and attn_tc_impl.cuh).
+// Operators on packed token rows (the entry points mf_qk_rope_*, mf_attn_*, mf_attn_window_* and
+// mf_embed_* of ops_capi.cu, which checks the arguments; kernels in rope_ops.cu, attn_tc_impl.cuh
+// and embed_ops.cu).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -82,5 +83,28 @@ inline int64_t window_part(int64_t rows, int Hkv, int D, int window, int sinks, 
   const int64_t chunk = window_chunk(window), chunks = (rows + chunk - 1) / chunk;
   return sinks > 0 && chunks > 1 ? 2 * chunks * Hkv * (dual ? 4 : 2) * sinks * (D > 64 ? 128 : 64) : 0;
 }
+
+
+struct EmbedParams {
+  SeqRows seq;                               // rows of tokens: those before the last sequence's end
+  int vocab = 0, dim = 0;
+  float scale = 1.f;
+  const int* ids = nullptr;
+  const void *E = nullptr, *Ed = nullptr;
+  void *y = nullptr, *yd = nullptr;
+  const void *dy = nullptr, *dyd = nullptr;
+  float *dE = nullptr, *dEd = nullptr;
+  int64_t ldE = 0, ldy = 0, lddy = 0, lddE = 0;
+};
+// How the gradient of a table is summed (embed_ops.cu).
+struct EmbedPlan {
+  int bits = 0, passes = 0;                  // of a digit; of the sort
+  int tile = 0, tiles = 0;                   // tokens of a block of the sort, blocks
+  int slabs = 0, per = 0, ranges = 0;        // of 128 columns; units of work of a range, ranges
+  int64_t list = 0, hist = 0, flags = 0, part = 0, bytes = 0;   // offsets into the workspace
+};
+EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual);
+cudaError_t embed_fwd(const EmbedParams& p, bool e_bf16, bool y_bf16, cudaStream_t s);
+cudaError_t embed_bwd(const EmbedParams& p, bool y_bf16, void* work, cudaStream_t s);
 
 }  // namespace mf

@@ -11,6 +11,7 @@
 namespace {
 
 using mf::AttnParams;
+using mf::EmbedParams;
 using mf::RopeParams;
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -230,6 +231,23 @@ mf_status attn_window(const mf_attn_args* args, int64_t window, int n_sink, bool
   return done(bwd ? mf::attn_window_bwd(p, dual, s) : mf::attn_window_fwd(p, dual, s));
 }
 
+bool embed_sizes_ok(const mf_embed_args& a) {
+  return a.n_rows >= 0 && a.n_rows <= INT32_MAX - 256 && a.vocab >= 1 && a.vocab <= INT32_MAX - 256 &&
+         a.dim >= 1 && a.dim <= (1 << 20);
+}
+bool prec_ok(int p) { return p == MF_PREC_FP32 || p == MF_PREC_BF16; }
+
+mf_status embed_params(const mf_embed_args& a, EmbedParams* p) {
+  if (!embed_sizes_ok(a) || !prec_ok(a.y_prec) || !finite(a.scale)) return MF_ERR_INVALID_ARG;
+  if (!make_seq(a.n_rows, a.seq_start, a.n_seq, true, &p->seq)) return MF_ERR_INVALID_ARG;
+  if (a.n_rows > 0 && !a.ids) return MF_ERR_INVALID_ARG;
+  p->vocab = static_cast<int>(a.vocab);
+  p->dim = static_cast<int>(a.dim);
+  p->scale = a.scale;
+  p->ids = a.ids;
+  return MF_OK;
+}
+
 }  // namespace
 
 bool mf::rope_desc_ok(const mf_rope_desc& r, int D) {
@@ -348,6 +366,45 @@ mf_status mf_attn_window_fwd(const mf_attn_args* args, int64_t window, int n_sin
 
 mf_status mf_attn_window_bwd(const mf_attn_args* args, int64_t window, int n_sink, void* stream) {
   return attn_window(args, window, n_sink, true, stream);
+}
+
+mf_status mf_embed_work_bytes(const mf_embed_args* args, size_t* bytes) {
+  if (!args || !bytes || !embed_sizes_ok(*args)) return MF_ERR_INVALID_ARG;
+  *bytes = static_cast<size_t>(mf::embed_plan(args->n_rows, args->vocab, args->dim, args->dyd != nullptr).bytes);
+  return MF_OK;
+}
+
+mf_status mf_embed_fwd(const mf_embed_args* args, void* stream) {
+  if (!args) return MF_ERR_INVALID_ARG;
+  const mf_embed_args& a = *args;
+  EmbedParams p;
+  const mf_status st = embed_params(a, &p);
+  if (st != MF_OK) return st;
+  if (!prec_ok(a.e_prec)) return MF_ERR_INVALID_ARG;
+  if (a.n_rows == 0) return MF_OK;
+  if (!both(a.Ed, a.yd) || !rows_ok(a.E, a.ldE, a.dim, a.vocab) || !rows_ok(a.y, a.ldy, a.dim, a.n_rows) || !aligned(a.Ed) ||
+      !aligned(a.yd) || !outputs_apart({a.y, a.yd}, {a.E, a.Ed, a.ids}))
+    return MF_ERR_INVALID_ARG;
+  p.E = a.E; p.Ed = a.Ed; p.ldE = a.ldE;
+  p.y = a.y; p.yd = a.yd; p.ldy = a.ldy;
+  return done(mf::embed_fwd(p, a.e_prec == MF_PREC_BF16, a.y_prec == MF_PREC_BF16, static_cast<cudaStream_t>(stream)));
+}
+
+mf_status mf_embed_bwd(const mf_embed_args* args, void* stream) {
+  if (!args) return MF_ERR_INVALID_ARG;
+  const mf_embed_args& a = *args;
+  EmbedParams p;
+  const mf_status st = embed_params(a, &p);
+  if (st != MF_OK) return st;
+  const bool dual = a.dEd != nullptr;       // without rows dyd may be null
+  if ((a.n_rows > 0 && !both(a.dyd, a.dEd)) || !rows_ok(a.dE, a.lddE, a.dim, a.vocab) || !aligned(a.dEd) ||
+      (a.n_rows > 0 && (!rows_ok(a.dy, a.lddy, a.dim, a.n_rows) || !aligned(a.dyd))) || !a.work || !aligned(a.work) ||
+      a.work_bytes < static_cast<size_t>(mf::embed_plan(a.n_rows, a.vocab, a.dim, dual).bytes) ||
+      !outputs_apart({a.dE, a.dEd, a.work}, {a.dy, a.dyd, a.ids}))
+    return MF_ERR_INVALID_ARG;
+  p.dy = a.dy; p.dyd = a.dyd; p.lddy = a.lddy;
+  p.dE = a.dE; p.dEd = a.dEd; p.lddE = a.lddE;
+  return done(mf::embed_bwd(p, a.y_prec == MF_PREC_BF16, a.work, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

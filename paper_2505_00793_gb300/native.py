@@ -39,7 +39,8 @@ EXPORTS = ["mf_create", "mf_destroy", "mf_set_allocator", "mf_param_count",
            "mf_hvp_noalloc", "mf_set_option", "mf_replay_gemms", "mf_checkpoint_plan",
            "mf_qk_rope_fwd", "mf_qk_rope_bwd", "mf_qk_rope_work_bytes", "mf_attn_fwd",
            "mf_attn_bwd", "mf_attn_work_bytes", "mf_create_decoder", "mf_attn_window_fwd",
-           "mf_attn_window_bwd", "mf_attn_window_work_bytes"]
+           "mf_attn_window_bwd", "mf_attn_window_work_bytes", "mf_embed_fwd", "mf_embed_bwd",
+           "mf_embed_work_bytes"]
 
 
 class mf_model_desc(C.Structure):
@@ -97,6 +98,14 @@ class mf_attn_args(C.Structure):
                 *_ptrs("status")]
 
 
+class mf_embed_args(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("vocab", C.c_int64), ("dim", C.c_int64), ("e_prec", C.c_int),
+                ("y_prec", C.c_int), ("scale", C.c_float), *_ptrs("ids E Ed"), ("ldE", C.c_int64),
+                *_ptrs("y yd"), ("ldy", C.c_int64), *_ptrs("seq_start"), ("n_seq", C.c_int),
+                *_ptrs("dy dyd"), ("lddy", C.c_int64), *_ptrs("dE dEd"), ("lddE", C.c_int64),
+                *_ptrs("work"), ("work_bytes", C.c_size_t)]
+
+
 class MixflowError(RuntimeError):
     def __init__(self, status, msg=""):
         super().__init__(f"{STATUS.get(status, status)}: {msg}")
@@ -139,7 +148,7 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     }
     for name in ("mf_attn_window_fwd", "mf_attn_window_bwd", "mf_attn_window_work_bytes"):
         sig[name] = ([vp, C.c_int64, C.c_int, vp], C.c_int)
-    for op in ("mf_qk_rope", "mf_attn"):
+    for op in ("mf_qk_rope", "mf_attn", "mf_embed"):
         for call in ("fwd", "bwd", "work_bytes"):
             sig[f"{op}_{call}"] = ([vp, vp], C.c_int)
     for name, (args, res) in sig.items():
@@ -517,6 +526,52 @@ def mf_attn_window_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, he
     _attn_bwd_call(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd, kd,
                    vd, od, rbar, dod, dqd, dkd, dvd, seq_start, n_seq, scale,
                    status).run("mf_attn_window_bwd", stream, window, n_sink)
+
+
+def _embed_call(ids, table, rows, scale, seq_start):
+    import torch
+    lib()
+    a = mf_embed_args()
+    c = _Call(a, ids)
+    if ids.dim() != 1 or table.dim() != 2:
+        raise ValueError(f"ids, table: shapes {tuple(ids.shape)}, {tuple(table.shape)}, expected [n_rows] and "
+                         "[vocab][dim]")
+    a.n_rows, (a.vocab, a.dim), a.scale = ids.shape[0], table.shape, scale
+    a.y_prec = _prec(rows, "y")
+    c.vec("ids", ids, torch.int32, (a.n_rows,))
+    c.seq(seq_start, 0, torch.int32)
+    return c
+
+
+def mf_embed_fwd(ids, E, y, scale=1.0, Ed=None, yd=None, seq_start=None, stream=None):
+    """y [N][dim] = scale E[ids] (rows of zeros where an id is no row of E [vocab][dim]); Ed -> yd
+    the tangent (see mixflow.h)."""
+    c = _embed_call(ids, E, y, scale, seq_start)
+    a = c.a
+    a.e_prec = _prec(E, "E")
+    c.rows("Ed", Ed, E.dtype, a.vocab, a.dim, "ldE", c.rows("E", E, E.dtype, a.vocab, a.dim, "ldE"))
+    c.rows("yd", yd, y.dtype, a.n_rows, a.dim, "ldy", c.rows("y", y, y.dtype, a.n_rows, a.dim, "ldy"))
+    c.run("mf_embed_fwd", stream)
+
+
+def mf_embed_bwd(ids, dy, dE, work, scale=1.0, dyd=None, dEd=None, seq_start=None, stream=None):
+    """Gradient of mf_embed_fwd's table: dE [vocab][dim] float32 from dy [N][dim] (dEd from dyd);
+    work: mf_embed_work_bytes bytes."""
+    import torch
+    c = _embed_call(ids, dE, dy, scale, seq_start)
+    a, f32 = c.a, torch.float32
+    c.rows("dyd", dyd, dy.dtype, a.n_rows, a.dim, "lddy", c.rows("dy", dy, dy.dtype, a.n_rows, a.dim, "lddy"))
+    c.rows("dEd", dEd, f32, a.vocab, a.dim, "lddE", c.rows("dE", dE, f32, a.vocab, a.dim, "lddE"))
+    c.work(work)
+    c.run("mf_embed_bwd", stream)
+
+
+def mf_embed_work_bytes(n_rows, vocab, dim, dual=False):
+    """Bytes of `work` that mf_embed_bwd takes."""
+    a = mf_embed_args()
+    a.n_rows, a.vocab, a.dim = n_rows, vocab, dim
+    a.dyd = 16 if dual else None
+    return _bytes_of("mf_embed_work_bytes", a)
 
 
 class MixFlow:

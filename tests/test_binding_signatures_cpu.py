@@ -9,6 +9,6 @@ def test_every_call_declares_its_arguments():
     L = native.load()
     for name in native.EXPORTS:
         assert getattr(L, name).argtypes is not None, name
-    for op in ("mf_qk_rope", "mf_attn", "mf_attn_window"):
+    for op in ("mf_qk_rope", "mf_attn", "mf_attn_window", "mf_embed"):
         for call in ("fwd", "bwd", "work_bytes"):
             assert getattr(L, f"{op}_{call}").argtypes[-1] is C.c_void_p
