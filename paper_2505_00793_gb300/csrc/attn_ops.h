@@ -100,8 +100,10 @@ struct EmbedParams {
 struct EmbedPlan {
   int bits = 0, passes = 0;                  // of a digit; of the sort
   int tile = 0, tiles = 0;                   // tokens of a block of the sort, blocks
-  int slabs = 0, per = 0, ranges = 0;        // of 128 columns; units of work of a range, ranges
-  int64_t list = 0, hist = 0, flags = 0, part = 0, bytes = 0;   // offsets into the workspace
+  bool cluster = false;                      // the sort is one cluster's
+  int slabs = 0, parts = 0;                  // of 128 columns; warps of a range
+  int per = 0, groups = 0;                   // steps of a range, a warp's; blocks along the ranges
+  int64_t list = 0, hist = 0, ends = 0, part = 0, bytes = 0;   // offsets into the workspace
 };
 EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual);
 cudaError_t embed_fwd(const EmbedParams& p, bool e_bf16, bool y_bf16, cudaStream_t s);

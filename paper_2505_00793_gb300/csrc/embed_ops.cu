@@ -10,6 +10,7 @@
 // into one path of "add a token's row" and "write a table's row", cut into ranges of equal length:
 // however the ids are spread, every warp moves the same bytes.
 #include "attn_ops.h"
+#include "internal.h"
 #include "launch.cuh"
 #include "packed_rows.cuh"
 
@@ -20,20 +21,37 @@ namespace {
 
 constexpr unsigned ALL = 0xffffffffu;
 
-// Four columns of a row, n of them there (n >= 4: all).
-__device__ __forceinline__ float4 load4(const float* p, int n) {
-  if (n >= 4) return *reinterpret_cast<const float4*>(p);
-  return make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, 0.f);
-}
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p, int n) {
-  if (n >= 4) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
-                       __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+// Four columns of a row as they lie in memory, n of them there (n >= 4: all), and their values.
+// Apart, so that several loads are in flight before the first value is needed.
+template <typename T>
+struct Four;
+template <>
+struct Four<float> {
+  float4 w;
+  __device__ __forceinline__ void zero() { w = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load(const float* p, int n) {
+    if (n >= 4) w = *reinterpret_cast<const float4*>(p);
+    else w = make_float4(p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, 0.f);
   }
-  return make_float4(__bfloat162float(p[0]), n > 1 ? __bfloat162float(p[1]) : 0.f,
-                     n > 2 ? __bfloat162float(p[2]) : 0.f, 0.f);
-}
+  __device__ __forceinline__ float4 get() const { return w; }
+};
+template <>
+struct Four<__nv_bfloat16> {
+  uint2 w;
+  __device__ __forceinline__ void zero() { w = make_uint2(0, 0); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
+    if (n >= 4) {
+      w = *reinterpret_cast<const uint2*>(p);
+    } else {
+      const uint16_t* u = reinterpret_cast<const uint16_t*>(p);
+      w = make_uint2(u[0] | (n > 1 ? static_cast<uint32_t>(u[1]) << 16 : 0u), n > 2 ? u[2] : 0u);
+    }
+  }
+  __device__ __forceinline__ float4 get() const {
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xffff0000u));
+  }
+};
 __device__ __forceinline__ void store4(float* p, int n, const float4& v) {
   if (n >= 4) {
     *reinterpret_cast<float4*>(p) = v;
@@ -78,7 +96,7 @@ __global__ void __launch_bounds__(LOOK_THREADS)
   const TE* E = static_cast<const TE*>(tangent ? p.Ed : p.E);
   TY* y = static_cast<TY*>(tangent ? p.yd : p.y);
   for (int i0 = threadIdx.x; i0 < n; i0 += LOOK_ITEMS * LOOK_THREADS) {
-    float4 x[LOOK_ITEMS];
+    Four<TE> x[LOOK_ITEMS];
     int row[LOOK_ITEMS], col[LOOK_ITEMS];
 #pragma unroll
     for (int k = 0; k < LOOK_ITEMS; ++k) {
@@ -86,56 +104,37 @@ __global__ void __launch_bounds__(LOOK_THREADS)
       row[k] = i / units;
       col[k] = 4 * (i - row[k] * units);
       row[k] += r0;
-      x[k] = zero4();
+      x[k].zero();
       if (i < n) {
         const int id = p.ids[row[k]];
-        if (id >= 0 && id < p.vocab) x[k] = load4(E + id * p.ldE + col[k], p.dim - col[k]);
+        if (id >= 0 && id < p.vocab) x[k].load(E + id * p.ldE + col[k], p.dim - col[k]);
       }
     }
 #pragma unroll
     for (int k = 0; k < LOOK_ITEMS; ++k)
       if (i0 + k * LOOK_THREADS < n)
-        store4(y + row[k] * p.ldy + col[k], p.dim - col[k], times4(x[k], p.scale));
+        store4(y + row[k] * p.ldy + col[k], p.dim - col[k], times4(x[k].get(), p.scale));
   }
 }
 
 // ---- tokens sorted by id --------------------------------------------------------------------------
-// Least significant digit first, digits of up to nine bits, each pass stable.  A block takes a tile
-// of tokens; hist[pass][tile][digit] says how many of a tile's tokens have a digit.  The first
-// pass's table comes from the ids, each later one's from the pass before it, which knows where its
-// tokens go.
-constexpr int DIGITS = 512, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32;
-constexpr int SORT_ROUNDS = 4, SORT_SUB = SORT_THREADS * SORT_ROUNDS;
-constexpr int MAX_TILES = 64;
+// Least significant digit first, digits of up to nine bits, each pass stable.  A block takes a tile of
+// tokens, a warp neighbours of it.  A token goes behind all tokens of smaller digits, those of its digit
+// in the tiles before, those in its tile's warps before, and those in its warp before.
+constexpr int DIGITS = 512, SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32;
+constexpr int SORT_ROUNDS = 8, SORT_SUB = SORT_ROUNDS * SORT_THREADS;    // tokens of a thread, of a block at a time
+constexpr int CLUSTER_TILES = 8, MAX_TILES = 64;
+static_assert(SORT_THREADS == DIGITS, "a thread a digit");
+
+struct SortShared {
+  uint16_t cnt[SORT_WARPS][DIGITS];   // tokens of a warp with a digit; those of the warps before
+  int base[DIGITS], wtot[SORT_WARPS];
+};
 
 // A token's key: its id, behind all of the table where it has none.
 __device__ __forceinline__ int token_key(const EmbedParams& p, int row, int total) {
-  if (row >= total) return p.vocab;
-  const int id = p.ids[row];
-  return id >= 0 && id < p.vocab ? id : p.vocab;
-}
-
-__global__ void __launch_bounds__(SORT_THREADS)
-    token_hist_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, int* hist) {
-  __shared__ int cnt[DIGITS];
-  pdl_entry();
-  const int t = threadIdx.x, tile = blockIdx.x, lane = t & 31;
-  const int total = seq_total(p.seq);
-  if (t < DIGITS) {
-    cnt[t] = 0;
-    for (int k = 1; k < m.passes; ++k) hist[(k * m.tiles + tile) * DIGITS + t] = 0;
-  }
-  __syncthreads();
-  const int64_t a = static_cast<int64_t>(tile) * m.tile;
-  const int n = static_cast<int>(min(static_cast<int64_t>(m.tile), p.seq.rows - a));
-  for (int i0 = 0; i0 < n; i0 += SORT_THREADS) {
-    const int i = i0 + t;
-    const int d = i < n ? token_key(p, static_cast<int>(a) + i, total) & ((1 << m.bits) - 1) : -1;
-    const unsigned peers = __match_any_sync(ALL, d);
-    if (d >= 0 && lane == __ffs(peers) - 1) atomicAdd(&cnt[d], __popc(peers));
-  }
-  __syncthreads();
-  if (t < DIGITS) hist[tile * DIGITS + t] = cnt[t];
+  const int id = p.ids[row];          // before it is known whether it counts: one wait less
+  return row < total && id >= 0 && id < p.vocab ? id : p.vocab;
 }
 
 // Inclusive sum over a warp.
@@ -148,108 +147,240 @@ __device__ __forceinline__ int warp_sum_scan(int v, int lane) {
   return v;
 }
 
-template <bool FIRST>
+// Lanes of the warp whose d agrees in its lowest `bits`, nine at most.  (match.any takes longer the more values there
+// are: 1500 cycles more a round of 32 warps.)
+__device__ __forceinline__ unsigned peers_of(int d, int bits) {
+  unsigned peers = ALL;
+#pragma unroll
+  for (int b = 0; b < 9; ++b) {
+    const bool one = d >> b & 1;
+    const unsigned set = __ballot_sync(ALL, one);
+    peers &= b >= bits ? ALL : one ? set : ~set;
+  }
+  return peers;
+}
+
+// Ranks of a thread's tokens (x negative: none) among those of their digit in their warp, and in cnt those
+// of the warps before; returns the tile's tokens of digit threadIdx.x.
+__device__ __forceinline__ int rank_tokens(const int2 (&x)[SORT_ROUNDS], int (&rank)[SORT_ROUNDS], int rounds, int shift,
+                                           int bits, SortShared& sh) {
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5, mask = (1 << bits) - 1;
+  for (int i = t; i < SORT_WARPS * DIGITS / 8; i += SORT_THREADS)
+    reinterpret_cast<uint4*>(&sh.cnt[0][0])[i] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < SORT_ROUNDS; ++k) {
+    if (k >= rounds) break;
+    const bool in = x[k].x >= 0;
+    const int d = (x[k].x >> shift) & mask;
+    const unsigned peers = peers_of(d, bits) & __ballot_sync(ALL, in);
+    const int old = in ? sh.cnt[w][d] : 0;
+    __syncwarp();
+    if (in && lane == __ffs(peers) - 1) sh.cnt[w][d] = static_cast<uint16_t>(old + __popc(peers));
+    __syncwarp();
+    rank[k] = old + __popc(peers & ((1u << lane) - 1));
+  }
+  __syncthreads();
+  int run = 0;
+#pragma unroll
+  for (int k = 0; k < SORT_WARPS; ++k) {
+    const int c = sh.cnt[k][t];
+    sh.cnt[k][t] = static_cast<uint16_t>(run);
+    run += c;
+  }
+  return run;
+}
+
+// Tokens of digits smaller than threadIdx.x, from those of each.
+__device__ __forceinline__ int smaller_digits(int tokens, SortShared& sh) {
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5;
+  const int inc = warp_sum_scan(tokens, lane);
+  if (lane == 31) sh.wtot[w] = inc;
+  __syncthreads();
+  int ahead = inc - tokens;
+#pragma unroll
+  for (int k = 0; k < SORT_WARPS; ++k) ahead += k < w ? sh.wtot[k] : 0;
+  return ahead;
+}
+
+// Up to 32768 tokens: one cluster, whose CTAs keep their tiles in shared memory and store tokens into one
+// another's.
+struct ClusterShared {
+  SortShared s;
+  int hist[2][DIGITS];                // of the tile, by pass
+  int2 token[2][SORT_SUB];
+};
+
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
+               "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// This address in the shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t in_cta(const void* at, int rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;"
+      : "=r"(a)
+      : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(at))), "r"(rank));
+  return a;
+}
+
+__global__ void __launch_bounds__(SORT_THREADS)
+    token_cluster_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, int2* list) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  ClusterShared& sh = *reinterpret_cast<ClusterShared*>(raw);
+  pdl_entry();
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5, tile = blockIdx.x;
+  const int total = seq_total(p.seq), first = tile * m.tile, n = min(m.tile, p.seq.rows - first);
+  const int rounds = m.tile / SORT_THREADS, mask = (1 << m.bits) - 1;
+  int2 x[SORT_ROUNDS];
+  int rank[SORT_ROUNDS];
+#pragma unroll
+  for (int k = 0; k < SORT_ROUNDS; ++k) {
+    const int i = (w * rounds + k) * 32 + lane;
+    x[k] = k < rounds && i < n ? make_int2(token_key(p, first + i, total), first + i) : make_int2(-1, 0);
+  }
+  for (int pass = 0; pass < m.passes; ++pass) {
+    const int shift = pass * m.bits;
+    const bool last = pass + 1 == m.passes;
+    if (pass > 0) {
+#pragma unroll
+      for (int k = 0; k < SORT_ROUNDS; ++k) {
+        const int i = (w * rounds + k) * 32 + lane;
+        if (k < rounds && i < n) x[k] = sh.token[pass & 1][i];
+      }
+    }
+    sh.hist[pass & 1][t] = rank_tokens(x, rank, rounds, shift, m.bits, sh.s);
+    cluster_barrier();
+    int before = 0, all = 0, c[CLUSTER_TILES];
+#pragma unroll
+    for (int k = 0; k < CLUSTER_TILES; ++k)
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[k]) : "r"(in_cta(&sh.hist[pass & 1][t], min(k, m.tiles - 1))));
+#pragma unroll
+    for (int k = 0; k < CLUSTER_TILES; ++k) {
+      all += k < m.tiles ? c[k] : 0;
+      before += k < tile ? c[k] : 0;
+    }
+    sh.s.base[t] = before + smaller_digits(all, sh.s);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SORT_ROUNDS; ++k) {
+      if (k >= rounds) break;
+      if (x[k].x < 0) continue;
+      const int d = (x[k].x >> shift) & mask, at = sh.s.base[d] + sh.s.cnt[w][d] + rank[k];
+      if (last) {
+        list[at] = x[k];
+      } else {
+        const int cta = at / m.tile;
+        asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(
+                         in_cta(&sh.token[(pass + 1) & 1][at - cta * m.tile], cta)),
+                     "r"(x[k].x), "r"(x[k].y)
+                     : "memory");
+      }
+    }
+    // tokens have arrived, and a histogram has been read before its buffer is written again or its CTA ends
+    cluster_barrier();
+  }
+}
+
+// More tokens: a launch for the first digit's table hist[tile][digit], and one a pass, which fills the next
+// digit's table.
+__global__ void __launch_bounds__(SORT_THREADS)
+    token_hist_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, int* hist) {
+  __shared__ int cnt[DIGITS];
+  pdl_entry();
+  const int t = threadIdx.x, lane = t & 31, tile = blockIdx.x, total = seq_total(p.seq);
+  cnt[t] = 0;
+  for (int k = 1; k < m.passes; ++k) hist[(k * m.tiles + tile) * DIGITS + t] = 0;
+  __syncthreads();
+  const int64_t a = static_cast<int64_t>(tile) * m.tile;
+  const int end = static_cast<int>(min(static_cast<int64_t>(p.seq.rows), a + m.tile));
+  for (int i0 = static_cast<int>(a); i0 < end; i0 += SORT_SUB) {
+    int d[SORT_ROUNDS];
+#pragma unroll
+    for (int k = 0; k < SORT_ROUNDS; ++k) {
+      const int i = i0 + k * SORT_THREADS + t;
+      d[k] = i < end ? token_key(p, i, total) & ((1 << m.bits) - 1) : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < SORT_ROUNDS; ++k) {
+      if (i0 + k * SORT_THREADS >= end) break;
+      const unsigned peers = peers_of(d[k], m.bits) & __ballot_sync(ALL, d[k] >= 0);
+      if (d[k] >= 0 && lane == __ffs(peers) - 1) atomicAdd(&cnt[d[k]], __popc(peers));
+    }
+  }
+  __syncthreads();
+  hist[tile * DIGITS + t] = cnt[t];
+}
+
 __global__ void __launch_bounds__(SORT_THREADS)
     token_sort_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, int pass,
                       const int2* from, int2* to, int* hist) {
-  __shared__ __align__(16) uint16_t cnt[SORT_WARPS][DIGITS];   // tokens of a warp with a digit; those before them
-  __shared__ int base[DIGITS], half[2][DIGITS], wtot[DIGITS / 32];
+  __shared__ __align__(16) SortShared sh;
   pdl_entry();
-  const int t = threadIdx.x, tile = blockIdx.x, lane = t & 31, w = t >> 5;
-  const int total = seq_total(p.seq), N = p.seq.rows;
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5, tile = blockIdx.x, total = seq_total(p.seq);
   const int shift = pass * m.bits, mask = (1 << m.bits) - 1;
-  const int* h = hist + pass * m.tiles * DIGITS;
+  const int* h = hist + pass * m.tiles * DIGITS + t;
   int* next = pass + 1 < m.passes ? hist + (pass + 1) * m.tiles * DIGITS : nullptr;
-
-  // where this tile's tokens of a digit begin: behind all smaller digits and the tiles before
-  {
-    const int d = t % DIGITS, part = t / DIGITS;
-    int before = 0, all = 0;
-#pragma unroll 16
-    for (int k = part; k < m.tiles; k += 2) {
-      const int c = h[k * DIGITS + d];
-      all += c;
-      before += k < tile ? c : 0;
-    }
-    half[part][d] = all;
-    if (part == 1) base[d] = before;
-    __syncthreads();
-    int sum = 0, inc = 0;
-    if (t < DIGITS) {
-      sum = half[0][d] + half[1][d];
-      inc = warp_sum_scan(sum, lane);
-      if (lane == 31) wtot[w] = inc;
-    }
-    __syncthreads();
-    if (t < DIGITS) {
-      int ahead = 0;
-      for (int k = 0; k < w; ++k) ahead += wtot[k];
-      base[d] += before + ahead + inc - sum;
-    }
-  }
   const int64_t a = static_cast<int64_t>(tile) * m.tile;
-  const int end = static_cast<int>(min(static_cast<int64_t>(N), a + m.tile));
-  for (int s0 = static_cast<int>(a); s0 < end; s0 += SORT_SUB) {
-    for (int i = t; i < SORT_WARPS * DIGITS / 8; i += SORT_THREADS)
-      reinterpret_cast<uint4*>(&cnt[0][0])[i] = make_uint4(0, 0, 0, 0);
-    int2 x[SORT_ROUNDS];
-    int rank[SORT_ROUNDS];
+  const int end = static_cast<int>(min(static_cast<int64_t>(p.seq.rows), a + m.tile));
+  const int rounds = min(m.tile / SORT_THREADS, SORT_ROUNDS);
+  int tile_bits = 0;
+  while ((m.tiles - 1) >> tile_bits) ++tile_bits;
+  int2 x[SORT_ROUNDS];
+  int rank[SORT_ROUNDS];
+  auto load = [&](int s0) {
 #pragma unroll
     for (int k = 0; k < SORT_ROUNDS; ++k) {
-      const int i = s0 + (w * SORT_ROUNDS + k) * 32 + lane;     // a warp's tokens are neighbours
-      x[k] = make_int2(-1, i);
-      if (i < end) x[k] = FIRST ? make_int2(token_key(p, i, total), i) : from[i];
+      const int i = s0 + (w * rounds + k) * 32 + lane;
+      x[k] = make_int2(-1, 0);
+      if (k < rounds && i < end) x[k] = pass == 0 ? make_int2(token_key(p, i, total), i) : from[i];
     }
+  };
+  load(static_cast<int>(a));
+  int before = 0, all = 0;
+#pragma unroll 16
+  for (int k = 0; k < m.tiles; ++k) {
+    const int c = h[k * DIGITS];
+    all += c;
+    before += k < tile ? c : 0;
+  }
+  int base = before + smaller_digits(all, sh);
+  for (int s0 = static_cast<int>(a); s0 < end; s0 += rounds * SORT_THREADS) {
+    if (s0 > a) load(s0);
+    const int mine = rank_tokens(x, rank, rounds, shift, m.bits, sh);
+    sh.base[t] = base;
+    base += mine;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < SORT_ROUNDS; ++k) {
+      if (k >= rounds) break;
       const bool in = x[k].x >= 0;
-      const int d = in ? (x[k].x >> shift) & mask : -1;
-      const unsigned peers = __match_any_sync(ALL, d);
-      const int old = in ? cnt[w][d] : 0;
-      __syncwarp();
-      if (in && lane == __ffs(peers) - 1) cnt[w][d] = static_cast<uint16_t>(old + __popc(peers));
-      __syncwarp();
-      rank[k] = old + __popc(peers & ((1u << lane) - 1));
-    }
-    __syncthreads();
-    int run = 0;
-    if (t < DIGITS)
-#pragma unroll 8
-      for (int k = 0; k < SORT_WARPS; ++k) {
-        const int c = cnt[k][t];
-        cnt[k][t] = static_cast<uint16_t>(run);
-        run += c;
-      }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < SORT_ROUNDS; ++k) {
-      const bool in = x[k].x >= 0;
-      int at = 0, slot = -1;
+      int to_tile = 0, d = 0;
       if (in) {
-        const int d = (x[k].x >> shift) & mask;
-        at = base[d] + cnt[w][d] + rank[k];
+        d = (x[k].x >> shift) & mask;
+        const int at = sh.base[d] + sh.cnt[w][d] + rank[k];
         to[at] = x[k];
-        if (next) slot = at / m.tile * DIGITS + ((x[k].x >> (shift + m.bits)) & mask);
+        to_tile = at / m.tile;
       }
       if (next) {
-        const unsigned peers = __match_any_sync(ALL, slot);
-        if (in && lane == __ffs(peers) - 1) atomicAdd(&next[slot], __popc(peers));
+        d = (x[k].x >> (shift + m.bits)) & mask;
+        const unsigned peers = peers_of(d, m.bits) & peers_of(to_tile, tile_bits) & __ballot_sync(ALL, in);
+        if (in && lane == __ffs(peers) - 1) atomicAdd(&next[to_tile * DIGITS + d], __popc(peers));
       }
     }
-    __syncthreads();
-    if (t < DIGITS) base[t] += run;
-    // base and cnt are written again behind the next barrier only
+    __syncthreads();                  // base and cnt are written again
   }
 }
 
 // ---- sums ---------------------------------------------------------------------------------------
 // The path: step by step the next token of the list, if it belongs to table row v, is added to v's
 // sum, else row v is written and v + 1 is next.  Token i of key k is taken at step i + k, so the
-// state at a step is found by a search.  A warp takes 128 columns of a range of `per` steps.  A
-// border of two ranges that cuts an id's tokens moves ahead of them, if there are fewer than 32
-// of them before it; else both sides' sums go to the workspace, and embed_join_kernel adds them up.
-constexpr int SUM_WARPS = 8, SLAB = 128, AHEAD = 8;
+// state at a step is found by a search.  A warp takes NV slabs of 128 columns of a range of `per`
+// steps.  A border of two ranges that cuts an id's tokens moves ahead of them, if there are fewer than 32
+// of them before it; else both sides' sums are added up at the end: those of a block's eight ranges by
+// the block, and where a block's own border cuts, through the workspace by embed_join_kernel.
+constexpr int SUM_WARPS = 8, SLAB = 128;
+constexpr int64_t SUM_HELD = 152 * 24;             // warps that the GPU holds
 
 struct PathState {
   int i, v;              // tokens taken, rows written
@@ -284,125 +415,213 @@ __device__ __forceinline__ PathState path_state(const int2* list, int64_t d, int
   return s;
 }
 
-template <typename TY>
+// Bytes of a row that are asked for together count: 256 bytes at a time of rows in any order come at
+// 4.4 TB/s.  So a lane has four columns of NV neighbouring slabs.
+template <typename TY, int NV>
 __global__ void __launch_bounds__(32 * SUM_WARPS)
-    embed_sum_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, int parts,
-                     const int2* list, int* headv, int* tailv, float* part) {
+    embed_sum_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, const int2* list,
+                     int* headv, int* tailv, float* part) {
+  __shared__ float4 heads[SUM_WARPS][NV][32], tails[SUM_WARPS][NV][32];
+  __shared__ int head_row[SUM_WARPS], tail_row[1 + SUM_WARPS];  // -1: none; the first, of the block's own start
+  constexpr int FLIGHT = 32 / sizeof(TY);      // loads in flight: 128 bytes a lane
+  constexpr int AHEAD = FLIGHT / NV;
   pdl_entry();
   const int lane = threadIdx.x & 31;
-  const int64_t g = static_cast<int64_t>(blockIdx.x) * SUM_WARPS + (threadIdx.x >> 5);
-  const int64_t range = g / parts;
-  if (range >= m.ranges) return;
-  const int slab = static_cast<int>(g - range * parts);          // tangents' behind the primal ones
-  const bool tangent = slab >= m.slabs;
-  const int col = (tangent ? slab - m.slabs : slab) * SLAB + 4 * lane, cols = p.dim - col;
+  // a block's warps take neighbouring ranges of the same columns
+  const int w = threadIdx.x >> 5;
+  const int64_t group = blockIdx.x / m.parts, range = group * SUM_WARPS + w;
+  const int part_of = static_cast<int>(blockIdx.x - group * m.parts);   // tangents' behind the primal ones
+  const int half = m.parts / (p.dEd ? 2 : 1);
+  const bool tangent = part_of >= half;
+  const int slab = (tangent ? part_of - half : part_of) * NV;    // first of NV
+  const int col = slab * SLAB + 4 * lane, cols = p.dim - col;
   const TY* dy = static_cast<const TY*>(tangent ? p.dyd : p.dy) + col;
   float* dE = (tangent ? p.dEd : p.dE) + col;
   const int V = p.vocab, N = p.seq.rows;
-  const int64_t d0 = range * m.per, d1 = min(d0 + m.per, static_cast<int64_t>(N) + V);
+  // ranges behind the last are empty
+  const int64_t steps = static_cast<int64_t>(N) + V, d0 = min(range * m.per, steps), d1 = min(d0 + m.per, steps);
   const int at = path_search(list, N, lane < 16 ? d0 : d1, lane);
   const PathState a = path_state(list, d0, __shfl_sync(ALL, at, 0), V, lane);
   const PathState b = path_state(list, d1, __shfl_sync(ALL, at, 16), V, lane);
-  float* mine = part + ((2 * range) * parts + slab) * SLAB + 4 * lane;    // head, and behind it tail
-  const int64_t step = static_cast<int64_t>(parts) * SLAB;
-  if (slab == 0 && lane == 0) {
-    headv[range] = a.cut && b.v > a.v ? a.v : -1;
-    tailv[range] = b.cut ? b.v : -1;
-  }
-  float4 acc = zero4();
+  float4 acc[NV];
+  auto zero = [&]() {
+#pragma unroll
+    for (int q = 0; q < NV; ++q) acc[q] = zero4();
+  };
+  zero();
   int v = a.v;
   bool head = a.cut;
+  auto row_sum = [&](float f) {
+    float* row = dE + v * p.lddE;
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+      if (cols > q * SLAB) store4(row + q * SLAB, cols - q * SLAB, times4(acc[q], f));
+  };
   auto write_to = [&](int to) {
     if (v >= to) return;
-    if (head) *reinterpret_cast<float4*>(mine) = acc;
-    else if (cols > 0) store4(dE + v * p.lddE, cols, times4(acc, p.scale));
+    if (head) {
+#pragma unroll
+      for (int q = 0; q < NV; ++q) heads[w][q][lane] = acc[q];
+    } else {
+      row_sum(p.scale);
+    }
     head = false;
-    acc = zero4();
+    zero();
     ++v;
-#pragma unroll 4
-    for (; v < to; ++v)
-      if (cols > 0) store4(dE + v * p.lddE, cols, acc);
+#pragma unroll 2
+    for (; v < to; ++v) row_sum(0.f);
   };
+  auto entry = [&](int j) { return j + lane < b.i ? list[j + lane] : make_int2(V, 0); };
+  int2 next = entry(a.i);
   for (int j = a.i; j < b.i; j += 32) {
-    int2 kp = make_int2(V, 0);
-    if (j + lane < b.i) kp = list[j + lane];
+    const int2 kp = next;
+    next = entry(j + 32);
+#pragma unroll 1
     for (int u0 = 0; u0 < 32 && j + u0 < b.i; u0 += AHEAD) {
-      float4 x[AHEAD];
+      Four<TY> x[AHEAD][NV];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int key = __shfl_sync(ALL, kp.x, u0 + u), row = __shfl_sync(ALL, kp.y, u0 + u);
-        x[u] = key < V && cols > 0 ? load4(dy + row * p.lddy, cols) : zero4();
+        const TY* from = dy + row * p.lddy;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+          x[u][q].zero();
+          if (key < V && cols > q * SLAB) x[u][q].load(from + q * SLAB, cols - q * SLAB);
+        }
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int key = __shfl_sync(ALL, kp.x, u0 + u);
         if (key < V) {         // those without a table row come last
           write_to(key);
-          add4(acc, x[u]);
+#pragma unroll
+          for (int q = 0; q < NV; ++q) add4(acc[q], x[u][q].get());
         }
       }
     }
   }
   write_to(b.v);
-  if (b.cut) *reinterpret_cast<float4*>(mine + step) = acc;
+#pragma unroll
+  for (int q = 0; q < NV; ++q) tails[w][q][lane] = acc[q];       // of the row that the end cuts
+  if (lane == 0) {
+    head_row[w] = a.cut && b.v > a.v ? a.v : -1;
+    tail_row[1 + w] = b.cut ? b.v : -1;
+    if (w == 0) tail_row[0] = a.cut ? a.v : -1;
+  }
+  __syncthreads();
+  // Range by range, a slab a warp: `open` is the sum of the row that the last end has cut.  It began before
+  // the block as long as no range has written a row.
+  if (w >= NV || slab + w >= m.slabs) return;
+  const int64_t step = static_cast<int64_t>(m.slabs) * (p.dEd ? 2 : 1) * SLAB;
+  // the block's own ends: head, and behind it tail, of all slabs, the tangents' behind
+  float* mine = part + 2 * group * step + static_cast<int64_t>((tangent ? m.slabs : 0) + slab + w) * SLAB + 4 * lane;
+  int before = -1;
+  bool ours = false;                  // the open row's tokens begin in the block
+  float4 open = zero4();
+#pragma unroll 1
+  for (int k = 0; k < SUM_WARPS; ++k) {
+    const int hr = head_row[k], tr = tail_row[1 + k];
+    if (hr >= 0) {
+      add4(open, heads[k][w][lane]);
+      if (ours) {
+        if (cols > w * SLAB) store4(dE + hr * p.lddE + w * SLAB, cols - w * SLAB, times4(open, p.scale));
+      } else {
+        *reinterpret_cast<float4*>(mine) = open;
+        before = hr;
+      }
+    }
+    if (tr < 0) continue;
+    if (hr >= 0 || tail_row[k] != tr) {       // else the range lies inside the row
+      open = zero4();
+      ours = true;
+    }
+    add4(open, tails[k][w][lane]);
+  }
+  const int last = tail_row[SUM_WARPS];
+  if (last >= 0) *reinterpret_cast<float4*>(mine + step) = open;
+  if (part_of == 0 && w == 0 && lane == 0) {
+    headv[group] = before;
+    tailv[group] = last;
+  }
 }
 
-// Rows whose tokens lie in several ranges: the sums at the ends of the ranges before the one that
-// writes the row, and that one's own, in their order: eight groups of threads add neighbours.
-constexpr int JOIN_GROUPS = 8;
+// Rows whose tokens lie in several blocks' ranges: the sums at the ends of the blocks before the one that
+// writes the row, and that one's own, in their order.  A warp adds up to 31 such sums; more, the
+// block's warps, neighbours each.
+constexpr int JOIN_WARPS = 16;
 
-__global__ void __launch_bounds__(32 * JOIN_GROUPS)
-    embed_join_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, int parts,
-                      const int* headv, const int* tailv, const float* part) {
-  __shared__ int2 found[32 * JOIN_GROUPS];
-  __shared__ int count[JOIN_GROUPS];
-  __shared__ float4 sums[JOIN_GROUPS][32];
+__global__ void __launch_bounds__(32 * JOIN_WARPS)
+    embed_join_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m, const int* headv, const int* tailv,
+                      const float* part) {
+  __shared__ int2 found[32 * JOIN_WARPS];
+  __shared__ int count[JOIN_WARPS];
+  __shared__ bool longer[32 * JOIN_WARPS];
+  __shared__ float4 sums[JOIN_WARPS][32];
   pdl_entry();
   const int t = threadIdx.x, lane = t & 31, w = t >> 5;
   const int slab = blockIdx.y;
   const bool tangent = slab >= m.slabs;
   const int col = (tangent ? slab - m.slabs : slab) * SLAB + 4 * lane, cols = p.dim - col;
   float* dE = (tangent ? p.dEd : p.dE) + col;
-  const int64_t step = static_cast<int64_t>(parts) * SLAB;
-  const float* sum = part + static_cast<int64_t>(slab) * SLAB + 4 * lane;   // of range r: + 2 r step, its tail + step
-  for (int64_t r0 = blockIdx.x; r0 < m.ranges; r0 += static_cast<int64_t>(32 * JOIN_GROUPS) * gridDim.x) {
+  const int64_t step = static_cast<int64_t>(gridDim.y) * SLAB;
+  const float* sum = part + static_cast<int64_t>(slab) * SLAB + 4 * lane;   // of group r: + 2 r step, its tail + step
+  auto tail_sums = [&](int a, int b) {
+    float4 acc = zero4();
+#pragma unroll 16
+    for (int k = a; k < b; ++k) add4(acc, *reinterpret_cast<const float4*>(sum + (2 * static_cast<int64_t>(k) + 1) * step));
+    return acc;
+  };
+  auto write = [&](int group, int row, float4 acc) {
+    add4(acc, *reinterpret_cast<const float4*>(sum + 2 * static_cast<int64_t>(group) * step));
+    if (cols > 0) store4(dE + row * p.lddE, cols, times4(acc, p.scale));
+  };
+  for (int64_t r0 = blockIdx.x; r0 < m.groups; r0 += static_cast<int64_t>(32 * JOIN_WARPS) * gridDim.x) {
     const int64_t r = r0 + static_cast<int64_t>(t) * gridDim.x;
-    const int v = r < m.ranges ? headv[r] : -1;
+    const int v = r < m.groups ? headv[r] : -1;
     const unsigned hits = __ballot_sync(ALL, v >= 0);
-    __syncthreads();                      // the last batch has been read
     if (lane == 0) count[w] = __popc(hits);
     __syncthreads();
     int n = 0, at = 0;
-    for (int k = 0; k < JOIN_GROUPS; ++k) {
+    for (int k = 0; k < JOIN_WARPS; ++k) {
       at += k < w ? count[k] : 0;
       n += count[k];
     }
     if (v >= 0) found[at + __popc(hits & ((1u << lane) - 1))] = make_int2(static_cast<int>(r), v);
     __syncthreads();
+    for (int e = w; e < n; e += JOIN_WARPS) {
+      const int group = found[e].x, row = found[e].y, q = group - 1 - lane;
+      const unsigned same = __ballot_sync(ALL, q >= 0 && tailv[max(q, 0)] == row);
+      if (lane == 0) longer[e] = same == ALL;
+      if (same != ALL) write(group, row, tail_sums(group - __ffs(~same) + 1, group));
+    }
+    __syncthreads();
     for (int e = 0; e < n; ++e) {
-      const int range = found[e].x, row = found[e].y;
+      if (!longer[e]) continue;
+      const int group = found[e].x, row = found[e].y;
       int tails = 0;
       for (;;) {
-        const int q = range - 1 - tails - lane;
-        const unsigned same = __ballot_sync(ALL, q >= 0 && tailv[q] == row);
-        tails += same == ALL ? 32 : __ffs(~same) - 1;
-        if (same != ALL) break;
+        const int q = group - 1 - tails - t;
+        const unsigned same = __ballot_sync(ALL, q >= 0 && tailv[max(q, 0)] == row);
+        if (lane == 0) count[w] = same == ALL ? 32 : __ffs(~same) - 1;
+        __syncthreads();
+        int more = 0;
+        for (int k = 0; k < JOIN_WARPS && more == 32 * k; ++k) more += count[k];
+        __syncthreads();
+        tails += more;
+        if (more < 32 * JOIN_WARPS) break;
       }
-      const int a = static_cast<int>(static_cast<int64_t>(tails) * w / JOIN_GROUPS);
-      const int b = static_cast<int>(static_cast<int64_t>(tails) * (w + 1) / JOIN_GROUPS);
-      const float* from = sum + (2 * static_cast<int64_t>(range - tails) + 1) * step;
-      float4 acc = zero4();
-#pragma unroll 8
-      for (int k = a; k < b; ++k) add4(acc, *reinterpret_cast<const float4*>(from + 2 * k * step));
+      const int first = group - tails;
+      float4 acc = tail_sums(first + static_cast<int>(static_cast<int64_t>(tails) * w / JOIN_WARPS),
+                             first + static_cast<int>(static_cast<int64_t>(tails) * (w + 1) / JOIN_WARPS));
       sums[w][lane] = acc;
       __syncthreads();
       if (w == 0) {
-        for (int k = 1; k < JOIN_GROUPS; ++k) add4(acc, sums[k][lane]);
-        add4(acc, *reinterpret_cast<const float4*>(sum + 2 * static_cast<int64_t>(range) * step));
-        if (cols > 0) store4(dE + row * p.lddE, cols, times4(acc, p.scale));
+        for (int k = 1; k < JOIN_WARPS; ++k) add4(acc, sums[k][lane]);
+        write(group, row, acc);
       }
       __syncthreads();
     }
+    __syncthreads();                      // found and count are written again
   }
 }
 
@@ -416,20 +635,25 @@ EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual) {
   while (key < 31 && (vocab >> key) > 0) ++key;          // keys 0 .. vocab
   m.passes = (key + 8) / 9;
   m.bits = (key + m.passes - 1) / m.passes;
-  m.tile = static_cast<int>(up((rows + MAX_TILES - 1) / MAX_TILES, SORT_SUB));
-  m.tiles = m.tile ? static_cast<int>((rows + m.tile - 1) / m.tile) : 0;
+  m.cluster = rows <= CLUSTER_TILES * SORT_SUB;
+  const int64_t most = m.cluster ? CLUSTER_TILES : MAX_TILES;
+  int64_t tile = up((rows + most - 1) / most, SORT_THREADS);
+  if (tile > SORT_SUB) tile = up(tile, SORT_SUB);
+  m.tile = static_cast<int>(tile);
+  m.tiles = rows > 0 ? static_cast<int>((rows + tile - 1) / tile) : 0;
   m.slabs = static_cast<int>((dim + SLAB - 1) / SLAB);
-  const int64_t parts = static_cast<int64_t>(m.slabs) * (dual ? 2 : 1), steps = rows + vocab;
-  // two ranges for every warp that the GPU holds, of 32 to 512 steps
-  int64_t per = (steps * parts + 2 * 152 * 32 - 1) / (2 * 152 * 32);
-  per = per < 32 ? 32 : per > 512 ? 512 : per;
-  m.per = static_cast<int>(per);
-  m.ranges = static_cast<int>((steps + per - 1) / per);
+  const int64_t slabs = static_cast<int64_t>(m.slabs) * (dual ? 2 : 1), steps = rows + vocab;
+  // Short ranges leave warps for all of the GPU and spread what is slow, but each costs a search.  64 steps
+  // against 32, 96 and 128: 8192 tokens, 32768 ids, two tables of 1024 columns 75 us against 77, 81 and 85;
+  // 131071 tokens, 50001 ids, 768 columns 99 against 107, 99 and 105.  4096 tokens, 8192 ids, 512
+  // columns: 30 us with 32 steps, 32 with 64.
+  m.per = steps * slabs >= 2 * 64 * SUM_HELD ? 64 : 32;
+  m.groups = static_cast<int>((steps + m.per * SUM_WARPS - 1) / (m.per * SUM_WARPS));
   m.list = 0;
   m.hist = up(2 * rows * static_cast<int64_t>(sizeof(int2)), 16);
-  m.flags = m.hist + static_cast<int64_t>(m.passes) * m.tiles * DIGITS * sizeof(int);
-  m.part = m.flags + up(2 * static_cast<int64_t>(m.ranges) * sizeof(int), 16);
-  m.bytes = m.part + 2 * static_cast<int64_t>(m.ranges) * parts * SLAB * sizeof(float);
+  m.ends = m.hist + static_cast<int64_t>(m.passes) * m.tiles * DIGITS * sizeof(int);
+  m.part = m.ends + up(2 * static_cast<int64_t>(m.groups) * sizeof(int), 16);
+  m.bytes = m.part + 2 * static_cast<int64_t>(m.groups) * slabs * SLAB * sizeof(float);
   return m;
 }
 
@@ -445,37 +669,49 @@ cudaError_t embed_fwd(const EmbedParams& p, bool e_bf16, bool y_bf16, cudaStream
 
 cudaError_t embed_bwd(const EmbedParams& p, bool y_bf16, void* work, cudaStream_t s) {
   const bool dual = p.dEd != nullptr;
-  const EmbedPlan m = embed_plan(p.seq.rows, p.vocab, p.dim, dual);
+  EmbedPlan m = embed_plan(p.seq.rows, p.vocab, p.dim, dual);
   char* base = static_cast<char*>(work);
   int2* lists[2] = {reinterpret_cast<int2*>(base + m.list), reinterpret_cast<int2*>(base + m.list) + p.seq.rows};
   int* hist = reinterpret_cast<int*>(base + m.hist);
-  int* headv = reinterpret_cast<int*>(base + m.flags);
-  int* tailv = headv + m.ranges;
+  int* headv = reinterpret_cast<int*>(base + m.ends);
+  int* tailv = headv + m.groups;
   float* part = reinterpret_cast<float*>(base + m.part);
-  const int parts = m.slabs * (dual ? 2 : 1);
-  const unsigned tiles = static_cast<unsigned>(m.tiles);
   cudaError_t e = cudaSuccess;
-  if (tiles) e = launch_k(token_hist_kernel, dim3(tiles), dim3(SORT_THREADS), 0, s, p, m, hist);
-  for (int k = 0; tiles && k < m.passes && e == cudaSuccess; ++k) {
-    const int2* from = lists[(k + 1) & 1];
-    e = k == 0 ? launch_k(token_sort_kernel<true>, dim3(tiles), dim3(SORT_THREADS), 0, s, p, m, k, from, lists[0], hist)
-               : launch_k(token_sort_kernel<false>, dim3(tiles), dim3(SORT_THREADS), 0, s, p, m, k, from,
-                          lists[k & 1], hist);
+  if (m.tiles && m.cluster) {
+    static PerDeviceOnce once;
+    e = once.run([](int&) {
+      return cudaFuncSetAttribute(token_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(ClusterShared));
+    });
+    if (e == cudaSuccess)
+      e = launch_cluster(token_cluster_kernel, dim3(m.tiles), m.tiles, SORT_THREADS, sizeof(ClusterShared), s, p, m,
+                         lists[(m.passes - 1) & 1]);
+  } else if (m.tiles) {
+    e = launch_k(token_hist_kernel, dim3(m.tiles), dim3(SORT_THREADS), 0, s, p, m, hist);
+    for (int k = 0; k < m.passes && e == cudaSuccess; ++k)
+      e = launch_k(token_sort_kernel, dim3(m.tiles), dim3(SORT_THREADS), 0, s, p, m, k,
+                   static_cast<const int2*>(lists[(k + 1) & 1]), lists[k & 1], hist);
   }
   if (e != cudaSuccess) return e;
   const int2* list = lists[(m.passes - 1) & 1];
-  const int64_t blocks = (static_cast<int64_t>(m.ranges) * parts + SUM_WARPS - 1) / SUM_WARPS;
+  // Two slabs a warp for rows of bf16, where that leaves two rounds of warps: 131071 tokens, 50001 ids, 768
+  // columns 99 us against 112; float32 rows gain nothing (75 us against 83 in the case of 1024 columns).
+  const int slabs = m.slabs * (dual ? 2 : 1);
+  const int64_t warps = (static_cast<int64_t>(p.seq.rows) + p.vocab) / m.per * slabs;
+  const int wide = y_bf16 && m.slabs > 1 && warps >= 4 * SUM_HELD ? 2 : 1;
+  m.parts = (m.slabs + wide - 1) / wide * (dual ? 2 : 1);
+  const int64_t blocks = static_cast<int64_t>(m.groups) * m.parts;
   if (blocks > INT_MAX) return cudaErrorInvalidValue;
   auto sum = [&](auto kernel) {
-    return launch_k(kernel, dim3(static_cast<unsigned>(blocks)), dim3(32 * SUM_WARPS), 0, s, p, m, parts, list, headv,
-                    tailv, part);
+    return launch_k(kernel, dim3(static_cast<unsigned>(blocks)), dim3(32 * SUM_WARPS), 0, s, p, m, list, headv, tailv,
+                    part);
   };
-  e = y_bf16 ? sum(embed_sum_kernel<__nv_bfloat16>) : sum(embed_sum_kernel<float>);
-  if (e != cudaSuccess || p.seq.rows < 32) return e;       // no border has 32 tokens of a row before it
-  const int wide = 4 * 152 / parts;
-  const int x = wide < 1 ? 1 : wide < m.ranges ? wide : m.ranges;
-  return launch_k(embed_join_kernel, dim3(static_cast<unsigned>(x), static_cast<unsigned>(parts)),
-                  dim3(32 * JOIN_GROUPS), 0, s, p, m, parts, headv, tailv, part);
+  e = !y_bf16 ? sum(embed_sum_kernel<float, 1>)
+      : wide == 2 ? sum(embed_sum_kernel<__nv_bfloat16, 2>) : sum(embed_sum_kernel<__nv_bfloat16, 1>);
+  if (e != cudaSuccess || m.groups < 2 || p.seq.rows < 32) return e;   // no border has 32 tokens of a row before it
+  const int most = 2 * 152 / slabs;
+  const int x = most < 1 ? 1 : most < m.groups ? most : m.groups;
+  return launch_k(embed_join_kernel, dim3(static_cast<unsigned>(x), static_cast<unsigned>(slabs)),
+                  dim3(32 * JOIN_WARPS), 0, s, p, m, headv, tailv, part);
 }
 
 }  // namespace mf
