@@ -641,26 +641,30 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       tc_fence_after();
       // mixed tiles have code of their own: selects in the common one would be issued for every
       // element, taken or not
-      float sv[32], mx = -INFINITY;
-      auto load_scores = [&](int c, auto masked) {
-        tmem_ld32_nowait(aS + 32 * c, sv);
-        tmem_wait_ld();
-        if constexpr (decltype(masked)::value) {
+      // Scores come in groups of 16 columns, the next one while one is looked at.
+      constexpr int GROUPS = TK / 16;
+      float sv[2][16], mx = -INFINITY;
+      auto load_group = [&](int g) { tmem_ld16_nowait(aS + 16 * g, sv[g & 1]); };
+      auto mask_group = [&](int g) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) sv[i] = own[c] >> i & 1 ? sv[i] : -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i) sv[g & 1][i] = own[g >> 1] >> (16 * (g & 1) + i) & 1 ? sv[g & 1][i] : -INFINITY;
       };
       auto find_max = [&](auto masked) {
+        load_group(0);
+        tmem_wait_ld();
 #pragma unroll
-        for (int c = 0; c < TK / 32; ++c) {
-          load_scores(c, masked);
-          float y0 = mx, y1 = sv[0];
+        for (int g = 0; g < GROUPS; ++g) {
+          if (g + 1 < GROUPS) load_group(g + 1);
+          if constexpr (decltype(masked)::value) mask_group(g);
+          const float* v = sv[g & 1];
+          float y0 = mx, y1 = v[0];
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            y0 = fmaxf(fmaxf(y0, sv[i]), sv[i + 1]);
-            y1 = fmaxf(fmaxf(y1, sv[i + 2]), sv[i + 3]);
+          for (int i = 0; i < 16; i += 4) {
+            y0 = fmaxf(fmaxf(y0, v[i]), v[i + 1]);
+            y1 = fmaxf(fmaxf(y1, v[i + 2]), v[i + 3]);
           }
           mx = fmaxf(y0, y1);
+          if (g + 1 < GROUPS) tmem_wait_ld();
         }
       };
       if (mx_tile) find_max(std::true_type{});
@@ -743,36 +747,40 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL
       uint64_t l2 = 0, r2 = 0;
       auto probs = [&](auto masked) {
         constexpr bool MASK = decltype(masked)::value;
+        // from the last 32 columns on, whose scores are still here (masked, too)
+        auto group = [](int k) { return 2 * (TK / 32 - 1 - k / 2) + (k & 1); };
+        float sd[2][16];
+        if (DUAL) tmem_ld16(aSd + 16 * group(0), sd[0]);
 #pragma unroll
-        for (int c = TK / 32 - 1; c >= 0; --c) {
-          if (c != TK / 32 - 1) load_scores(c, masked);    // the last ones are still here
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            float sd[16];
-            if (DUAL) {
-              tmem_ld16(aSd + 32 * c + 16 * g, sd);
-              if (MASK) {   // the tangent of a masked score may be anything
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sd[i] = own[c] >> (16 * g + i) & 1 ? sd[i] : 0.f;
-              }
-            }
-            uint32_t pk[8], psk[8];
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              const float2 x = halves(fma2(pair(sv[16 * g + i], sv[16 * g + i + 1]), c2p, nm));
-              const float p0 = ex2(x.x), p1 = ex2(x.y);
-              const uint64_t pp = pair(p0, p1);
-              l2 = add2(l2, pp);
-              pk[i / 2] = pack_bf16x2(p0, p1);
-              if (DUAL) {
-                const uint64_t ps = mul2(pp, fma2(pair(sd[i], sd[i + 1]), scp, nc));
-                r2 = add2(r2, ps);
-                psk[i / 2] = pack2(ps);
-              }
-            }
-            tmem_st8(aS + 32 * c + 8 * g, pk);
-            if (DUAL) tmem_st8(aSd + 32 * c + 8 * g, psk);
+        for (int k = 0; k < GROUPS; ++k) {
+          const int g = group(k), b = g & 1;
+          if (k + 1 < GROUPS) {
+            if (k > 0) load_group(group(k + 1));
+            if (DUAL) tmem_ld16_nowait(aSd + 16 * group(k + 1), sd[b ^ 1]);
           }
+          if (MASK && k > 1) mask_group(g);
+          if (DUAL && MASK) {   // the tangent of a masked score may be anything
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sd[b][i] = own[g >> 1] >> (16 * b + i) & 1 ? sd[b][i] : 0.f;
+          }
+          uint32_t pk[8], psk[8];
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float2 x = halves(fma2(pair(sv[b][i], sv[b][i + 1]), c2p, nm));
+            const float p0 = ex2(x.x), p1 = ex2(x.y);
+            const uint64_t pp = pair(p0, p1);
+            l2 = add2(l2, pp);
+            pk[i / 2] = pack_bf16x2(p0, p1);
+            if (DUAL) {
+              const uint64_t ps = mul2(pp, fma2(pair(sd[b][i], sd[b][i + 1]), scp, nc));
+              r2 = add2(r2, ps);
+              psk[i / 2] = pack2(ps);
+            }
+          }
+          if (k + 1 < GROUPS && (DUAL || k > 0)) tmem_wait_ld();
+          // each 32 keys' P begins where their scores did
+          tmem_st8(aS + 32 * (g >> 1) + 8 * b, pk);
+          if (DUAL) tmem_st8(aSd + 32 * (g >> 1) + 8 * b, psk);
         }
       };
       if (mx_tile) probs(std::true_type{});
@@ -996,12 +1004,13 @@ __device__ __forceinline__ int64_t part_at(const TcParams2& p, int sums, int hdp
 }
 
 // dK, dV (and tangents) of the sinks of the sequence that begins in chunk y and reaches behind it:
-// one CTA a key/value head, a thread four columns of a sink's sum.
+// CTAs of a key/value head, a thread four columns of a sink's sum.
+constexpr int SINK_THREADS = 128;
 template <bool DUAL, int HDP>
-__global__ void __launch_bounds__(256) sink_sum_kernel(const __grid_constant__ TcParams2 p) {
+__global__ void __launch_bounds__(SINK_THREADS) sink_sum_kernel(const __grid_constant__ TcParams2 p) {
   constexpr int SUMS = DUAL ? 4 : 2, CH = HDP / 4;
   pdl_entry();
-  const int hk = static_cast<int>(blockIdx.x), c0 = tile_index();
+  const int hk = static_cast<int>(blockIdx.x) % p.Hkv, c0 = tile_index();
   if (c0 >= p.chunks - 1) return;
   const int row = (c0 + 1) * p.chunk;            // below seq.rows: there is a chunk behind c0
   if (row >= seq_total(p.seq)) return;
@@ -1009,21 +1018,20 @@ __global__ void __launch_bounds__(256) sink_sum_kernel(const __grid_constant__ T
   if (start / p.chunk != c0 || !has_far(p, start, end)) return;
   // start + window < end, so neither overflows
   const int first = max(c0 + 1, (start + p.window) / p.chunk), last = (end - 1) / p.chunk;
-  for (int i = static_cast<int>(threadIdx.x); i < SUMS * p.sinks * CH; i += 256) {
-    const int c = i % CH, place = i / CH % p.sinks, k = i / CH / p.sinks;
-    if (4 * c >= p.D || place >= end - start) continue;
-    float4 x = *reinterpret_cast<const float4*>(p.part + part_at(p, SUMS, HDP, c0, hk, k, place) + 4 * c);
-#pragma unroll 4
-    for (int j = first; j <= last; ++j) {
-      const float4 v = *reinterpret_cast<const float4*>(p.part + part_at(p, SUMS, HDP, p.chunks + j, hk, k, place) + 4 * c);
-      x = make_float4(x.x + v.x, x.y + v.y, x.z + v.z, x.w + v.w);
-    }
-    const bool isv = k < SUMS / 2;
-    const float f = isv ? 1.f : p.scale;
-    __nv_bfloat16* dst = k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd;
-    *reinterpret_cast<uint2*>(dst + (static_cast<int64_t>(start) + place) * (isv ? p.lddv : p.lddk) + hk * p.D + 4 * c) =
-        make_uint2(pack_bf16x2(x.x * f, x.y * f), pack_bf16x2(x.z * f, x.w * f));
+  const int i = static_cast<int>(blockIdx.x) / p.Hkv * SINK_THREADS + static_cast<int>(threadIdx.x);
+  const int c = i % CH, place = i / CH % p.sinks, k = i / CH / p.sinks;
+  if (k >= SUMS || 4 * c >= p.D || place >= end - start) return;
+  float4 x = *reinterpret_cast<const float4*>(p.part + part_at(p, SUMS, HDP, c0, hk, k, place) + 4 * c);
+#pragma unroll 8
+  for (int j = first; j <= last; ++j) {
+    const float4 v = *reinterpret_cast<const float4*>(p.part + part_at(p, SUMS, HDP, p.chunks + j, hk, k, place) + 4 * c);
+    x = make_float4(x.x + v.x, x.y + v.y, x.z + v.z, x.w + v.w);
   }
+  const bool isv = k < SUMS / 2;
+  const float f = isv ? 1.f : p.scale;
+  __nv_bfloat16* dst = k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd;
+  *reinterpret_cast<uint2*>(dst + (static_cast<int64_t>(start) + place) * (isv ? p.lddv : p.lddk) + hk * p.D + 4 * c) =
+      make_uint2(pack_bf16x2(x.x * f, x.y * f), pack_bf16x2(x.z * f, x.w * f));
 }
 
 // The row warps' barrier.
@@ -1126,12 +1134,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   int rank, hk;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%clusterid.x;" : "=r"(hk));
-  int tile = tile_index();
-  // with sinks the first CTAs take a chunk of query rows each, all others a tile of key rows
+  const int tile = tile_index();
+  // with sinks the last CTAs take a chunk of query rows each, all others a tile of key rows (first, the
+  // shorter chunks filled less of the last round: 325 us a training step against 316, 16 heads over 4,
+  // 16384 rows, window 512; 973 against 966 with 16 heads of 128 over 2, 24577 rows, window 1000)
   const int nfar = WIN && p.sinks > 0 ? p.chunks - 1 : 0;
-  const int far = WIN && tile < nfar ? tile + 1 : 0;
-  tile -= nfar;
-  if (tile >= p.tiles) return;
+  const int far = WIN && tile >= p.tiles ? tile - p.tiles + 1 : 0;
+  if (WIN ? far > nfar : tile >= p.tiles) return;
   const int trow0 = WIN && far ? far * p.chunk : tile * TR;   // the tile whose sequences are looked up
   const int G = p.Gs, h0 = (hk * p.share + rank) * G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -2027,12 +2036,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 // one CTA a group, these, and as many as divide it: 8 heads of 64 over one, 512 rows 78, 28 and 28 us;
 // 16 over 4 with tangents, 8192 rows 252, 236 and 264; 32 over 8, 16384 rows in sequences of 256 212,
 // 212 and 292; 16 of 128 over 4, 12289 rows 669, 569 and 635.
-int kv_share(int group, int64_t ctas, int per_sm) {
+// With a window all walks are as long, and the fewest that fill the places once do: 16 heads over 4, 8192
+// rows, window 257 with tangents 300 us a training step against 314 with three times, 16384 rows, window 512
+// 316 against 319, 16 heads of 128 over 2, 24577 rows, window 1000 966 against 976; four CTAs a group 362,
+// 357 and 1054.
+int kv_share(int group, int64_t ctas, int per_sm, int fill) {
   int best = 1;
   for (int n = 1; n <= 8 && n <= group; ++n) {
     if (group % n) continue;
     best = n;
-    if (ctas * n >= 3ll * 152 * per_sm) break;
+    if (ctas * n >= static_cast<int64_t>(fill) * 152 * per_sm) break;
   }
   return best;
 }
@@ -2065,7 +2078,7 @@ cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
   });
   if (e != cudaSuccess) return e;
   TcParams2 p = tc_params(a);
-  p.share = kv_share(p.G, static_cast<int64_t>(p.tiles) * a.Hkv, C::CTAS);
+  p.share = kv_share(p.G, static_cast<int64_t>(p.tiles) * a.Hkv, C::CTAS, WIN ? 1 : 3);
   p.Gs = p.G / p.share;
   e = launch_k(attn_tc_bwd_q_kernel<DUAL, HDP, WIN>, tile_grid(a.Hq, p.tiles), dim3(C::THREADS),
                C::SMEM_Q, s, qr[0], qr[1], qr[2], qr[3], ks[0], ks[1], ks[2], ks[3], p);
@@ -2081,7 +2094,9 @@ cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
                      C::THREADS, C::SMEM_KV, s, kr[0], kr[1], kr[2], kr[3], qs[0], qs[1], qs[2], qs[3], p);
   if constexpr (WIN) {
     if (e == cudaSuccess && nfar > 0)
-      e = launch_k(sink_sum_kernel<DUAL, HDP>, tile_grid(a.Hkv, nfar), dim3(256), 0, s, p);
+      e = launch_k(sink_sum_kernel<DUAL, HDP>,
+                   tile_grid(a.Hkv * (((DUAL ? 4 : 2) * a.sinks * (HDP / 4) + SINK_THREADS - 1) / SINK_THREADS), nfar),
+                   dim3(SINK_THREADS), 0, s, p);
   }
   return e;
 }
