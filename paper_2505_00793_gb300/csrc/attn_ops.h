@@ -98,6 +98,8 @@ struct EmbedParams {
 };
 // How the gradient of a table is summed (embed_ops.cu).
 struct EmbedPlan {
+  int blocks = 0, shared = 0;                // one launch of so many blocks a part, their shared memory
+  uint32_t by = 0;                           // (2^32 / blocks, rounded up); or:
   int bits = 0, passes = 0;                  // of a digit; of the sort
   int tile = 0, tiles = 0;                   // tokens of a block of the sort, blocks
   bool cluster = false;                      // the sort is one cluster's

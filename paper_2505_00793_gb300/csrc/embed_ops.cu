@@ -13,9 +13,9 @@
 // Measured (of 6.75 TB/s, a plain copy): 8192 tokens, 32768 ids, two tables of 1024 columns, float32: lookup
 // 94 MB in 18 us (78 %), gradient 335 MB in 70 us (71 %), of which the sort takes 10, the sums 57 (87 %)
 // and the rows that blocks share 4; 131071 tokens, 50001 ids, 768 columns of bf16 355 MB in 103 us (51 %):
-// 23, 72 and 8; 4096 tokens, 8192 ids, 512 columns 21 MB in 24 us, launches and latencies.  Zeros written
-// by blocks beside the sort, and sums of the ids that occur alone, took longer (87 us in the first): writes
-// by themselves come at 4.5 TB/s, among reads at 6.
+// 23, 72 and 8.  4096 tokens, 8192 ids, 512 columns take one launch, 21 MB in 12 us, latencies.  Zeros
+// written by blocks beside the sort, and sums of the ids that occur alone, took longer (87 us in the
+// first): writes by themselves come at 4.5 TB/s, among reads at 6.
 #include "attn_ops.h"
 #include "internal.h"
 #include "launch.cuh"
@@ -394,14 +394,15 @@ struct PathState {
   bool cut;              // inside a row's tokens
 };
 
-// Both ends of a range, by the halves of a warp: tokens taken before step d of this half.
-__device__ __forceinline__ int path_search(const int2* list, int N, int64_t d, int lane) {
+// Both ends of a range, by the halves of a warp: tokens taken before step d of this half.  key(i) is token i's.
+template <typename Key>
+__device__ __forceinline__ int path_search(const Key& key, int N, int64_t d, int lane) {
   int lo = 0, hi = N;
   const int l = lane & 15, sh = lane & 16;
   while (__any_sync(ALL, lo < hi)) {
     const int step = (hi - lo + 17) / 17;
     const int64_t x = lo + static_cast<int64_t>(l + 1) * step - 1;
-    const bool ahead = x < hi && x + list[x].x < d;
+    const bool ahead = x < hi && x + key(x) < d;
     const int c = __popc((__ballot_sync(ALL, ahead) >> sh) & 0xffffu);
     const int64_t top = lo + static_cast<int64_t>(c + 1) * step - 1;
     hi = static_cast<int>(min(static_cast<int64_t>(hi), top));
@@ -409,14 +410,15 @@ __device__ __forceinline__ int path_search(const int2* list, int N, int64_t d, i
   }
   return lo;
 }
-__device__ __forceinline__ PathState path_state(const int2* list, int64_t d, int i, int V, int lane) {
+template <typename Key>
+__device__ __forceinline__ PathState path_state(const Key& key, int64_t d, int i, int V, int lane) {
   PathState s{i, static_cast<int>(d - i), false};
   if (s.v >= V) {
     s.v = V;
     return s;
   }
   const int j = i - 1 - lane;
-  const unsigned mine = __ballot_sync(ALL, j >= 0 && list[j].x == s.v);
+  const unsigned mine = __ballot_sync(ALL, j >= 0 && key(j) == s.v);
   s.cut = mine == ALL;
   if (!s.cut) s.i -= __ffs(~mine) - 1;
   return s;
@@ -447,9 +449,10 @@ __global__ void __launch_bounds__(32 * SUM_WARPS)
   const int V = p.vocab, N = p.seq.rows;
   // ranges behind the last are empty
   const int64_t steps = static_cast<int64_t>(N) + V, d0 = min(range * m.per, steps), d1 = min(d0 + m.per, steps);
-  const int at = path_search(list, N, lane < 16 ? d0 : d1, lane);
-  const PathState a = path_state(list, d0, __shfl_sync(ALL, at, 0), V, lane);
-  const PathState b = path_state(list, d1, __shfl_sync(ALL, at, 16), V, lane);
+  auto key_of = [&](int64_t i) { return list[i].x; };
+  const int at = path_search(key_of, N, lane < 16 ? d0 : d1, lane);
+  const PathState a = path_state(key_of, d0, __shfl_sync(ALL, at, 0), V, lane);
+  const PathState b = path_state(key_of, d1, __shfl_sync(ALL, at, 16), V, lane);
   float4 acc[NV];
   auto zero = [&]() {
 #pragma unroll
@@ -552,6 +555,165 @@ __global__ void __launch_bounds__(32 * SUM_WARPS)
   }
 }
 
+// Few tokens: one launch.  Block b of n owns the table's rows b, b + n, b + 2n, ... (the smallest ids are the
+// most frequent) in 128 columns.  It looks all ids over for its rows, sorts what it finds in shared
+// memory, and walks the path of its own tokens and rows, a range a warp.
+constexpr int NEAR_WARPS = 16, NEAR_THREADS = 32 * NEAR_WARPS;
+constexpr int NEAR_TOKENS = 6144, NEAR_OWN = 8192;             // and rows of a block, at most
+constexpr int NEAR_BITS = 13, NEAR_IDS = NEAR_TOKENS / NEAR_THREADS;
+// Tokens of a warp's part of the ids.
+__host__ __device__ constexpr int near_part(int rows) { return (rows + NEAR_THREADS - 1) / NEAR_THREADS * 32; }
+
+constexpr int NEAR_SHARED = (2 * NEAR_TOKENS + NEAR_OWN) * 4;  // bytes, at most
+
+template <typename TY>
+__global__ void __launch_bounds__(NEAR_THREADS, 2)
+    embed_near_kernel(const __grid_constant__ EmbedParams p, const __grid_constant__ EmbedPlan m) {
+  constexpr int AHEAD = 8;
+  constexpr uint32_t AT = (1u << NEAR_BITS) - 1;        // a token: its row's place in the block, and its own place
+  extern __shared__ uint32_t near_raw[];
+  __shared__ float4 heads[NEAR_WARPS][32], tails[NEAR_WARPS][32];
+  __shared__ int head_row[NEAR_WARPS], tail_row[1 + NEAR_WARPS], wtot[NEAR_WARPS], found[NEAR_WARPS];
+  pdl_entry();
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5, total = seq_total(p.seq);
+  const int b = blockIdx.x / m.parts, n = m.blocks, slab = blockIdx.x - b * m.parts;
+  const bool tangent = slab >= m.slabs;
+  const int col = (tangent ? slab - m.slabs : slab) * SLAB + 4 * lane, cols = p.dim - col;
+  const TY* dy = static_cast<const TY*>(tangent ? p.dyd : p.dy) + col;
+  float* dE = (tangent ? p.dEd : p.dE) + b * p.lddE + col;
+  const int64_t ld = n * p.lddE;                // from one row of the block to the next
+  const int R = (p.vocab - b + n - 1) / n, S = near_part(p.seq.rows);
+  uint32_t* raw = near_raw;                     // as they are found, by warps
+  uint32_t* list = raw + NEAR_WARPS * S;        // side by side
+  int* start = reinterpret_cast<int*>(list + NEAR_WARPS * S);    // tokens of a row; where they begin
+  int id[NEAR_IDS];
+#pragma unroll
+  for (int k = 0; k < NEAR_IDS; ++k) {
+    const int i = w * S + 32 * k + lane;
+    id[k] = 32 * k < S && i < total ? p.ids[i] : -1;
+  }
+  for (int i = t; i < R; i += NEAR_THREADS) start[i] = 0;
+  __syncthreads();
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < NEAR_IDS; ++k) {
+    const int r = m.by ? __umulhi(id[k], m.by) : id[k];      // id / n
+    const bool hit = id[k] >= 0 && id[k] < p.vocab && id[k] - r * n == b;
+    const unsigned hits = __ballot_sync(ALL, hit);
+    if (hit) {
+      raw[w * S + mine + __popc(hits & ((1u << lane) - 1))] = static_cast<uint32_t>(r) << NEAR_BITS | (w * S + 32 * k + lane);
+      atomicAdd(&start[r], 1);
+    }
+    mine += __popc(hits);
+  }
+  if (lane == 0) found[w] = mine;
+  __syncthreads();
+  // where rows' tokens begin: a thread sums neighbouring rows
+  const int chunk = (R + NEAR_THREADS - 1) / NEAR_THREADS, c0 = min(t * chunk, R), c1 = min(c0 + chunk, R);
+  int sum = 0;
+  for (int i = c0; i < c1; ++i) sum += start[i];
+  const int inc = warp_sum_scan(sum, lane);
+  if (lane == 31) wtot[w] = inc;
+  __syncthreads();
+  int at = inc - sum, T = 0;
+  for (int k = 0; k < NEAR_WARPS; ++k) {
+    at += k < w ? wtot[k] : 0;
+    T += found[k];
+  }
+  for (int i = c0; i < c1; ++i) {
+    const int c = start[i];
+    start[i] = at;
+    at += c;
+  }
+  __syncthreads();
+  // found tokens side by side, in their order, which one warp keeps as it sorts them
+  int ahead = 0;
+  for (int k = 0; k < w; ++k) ahead += found[k];
+  for (int i = lane; i < mine; i += 32) list[ahead + i] = raw[w * S + i];
+  __syncthreads();
+  uint32_t* sorted = raw;
+  if (w == 0)
+    for (int j = 0; j < T; j += 32) {
+      const bool in = j + lane < T;
+      const uint32_t e = in ? list[j + lane] : ALL;
+      const unsigned peers = __match_any_sync(ALL, e >> NEAR_BITS);
+      const int old = in ? start[e >> NEAR_BITS] : 0, before = __popc(peers & ((1u << lane) - 1));
+      __syncwarp();
+      if (in && before == 0) start[e >> NEAR_BITS] = old + __popc(peers);
+      if (in) sorted[old + before] = e;
+      __syncwarp();
+    }
+  __syncthreads();
+
+  const int steps = T + R, per = (steps + NEAR_WARPS - 1) / NEAR_WARPS;
+  const int d0 = min(w * per, steps), d1 = min(d0 + per, steps);
+  auto key_of = [&](int64_t i) { return static_cast<int>(sorted[i] >> NEAR_BITS); };
+  const int ends = path_search(key_of, T, lane < 16 ? d0 : d1, lane);
+  // all cuts stay where they are: the block joins them, and ranges are short
+  auto state = [&](int d, int i) {
+    PathState s{i, min(d - i, R), false};
+    s.cut = s.v < R && i > 0 && key_of(i - 1) == s.v;
+    return s;
+  };
+  const PathState a = state(d0, __shfl_sync(ALL, ends, 0)), z = state(d1, __shfl_sync(ALL, ends, 16));
+  float4 acc = zero4();
+  int v = a.v;
+  bool head = a.cut;
+  auto write_to = [&](int to) {
+    if (v >= to) return;
+    if (head) heads[w][lane] = acc;
+    else if (cols > 0) store4(dE + v * ld, cols, times4(acc, p.scale));
+    head = false;
+    acc = zero4();
+    ++v;
+#pragma unroll 4
+    for (; v < to; ++v)
+      if (cols > 0) store4(dE + v * ld, cols, acc);
+  };
+  for (int j = a.i; j < z.i; j += 32) {
+    const uint32_t kp = j + lane < z.i ? sorted[j + lane] : 0u;
+#pragma unroll 1
+    for (int u0 = 0; u0 < 32 && j + u0 < z.i; u0 += AHEAD) {
+      Four<TY> x[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const uint32_t e = __shfl_sync(ALL, kp, u0 + u);
+        x[u].zero();
+        if (j + u0 + u < z.i && cols > 0) x[u].load(dy + static_cast<int64_t>(e & AT) * p.lddy, cols);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const uint32_t e = __shfl_sync(ALL, kp, u0 + u);
+        if (j + u0 + u < z.i) {
+          write_to(static_cast<int>(e >> NEAR_BITS));
+          add4(acc, x[u].get());
+        }
+      }
+    }
+  }
+  write_to(z.v);
+  tails[w][lane] = acc;
+  if (lane == 0) {
+    head_row[w] = a.cut && z.v > a.v ? a.v : -1;
+    tail_row[1 + w] = z.cut ? z.v : -1;
+    if (w == 0) tail_row[0] = -1;
+  }
+  __syncthreads();
+  if (w > 0) return;
+  float4 open = zero4();                        // as in embed_sum_kernel, of rows that all begin here
+#pragma unroll 1
+  for (int k = 0; k < NEAR_WARPS; ++k) {
+    const int hr = head_row[k], tr = tail_row[1 + k];
+    if (hr >= 0) {
+      add4(open, heads[k][lane]);
+      if (cols > 0) store4(dE + hr * ld, cols, times4(open, p.scale));
+    }
+    if (tr < 0) continue;
+    if (hr >= 0 || tail_row[k] != tr) open = zero4();
+    add4(open, tails[k][lane]);
+  }
+}
+
 // Rows whose tokens lie in several blocks' ranges: the sums at the ends of the blocks before the one that
 // writes the row, and that one's own, in their order.  A warp adds up to 31 such sums; more, the
 // block's warps, neighbours each.
@@ -638,6 +800,24 @@ int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual) {
   EmbedPlan m;
+  m.slabs = static_cast<int>((dim + SLAB - 1) / SLAB);
+  m.parts = m.slabs * (dual ? 2 : 1);
+  // Up to 6144 tokens one launch of two blocks an SM, of 64 steps at least, if a block's rows fit: 4096 of 8192
+  // ids, 512 columns of bf16 12 us against 25 (8192 tokens 18 against 25), 1000 of them 12 against 21.
+  // Where one id has many tokens its block takes longer, 4096 tokens of 50001 ids, a third of them one,
+  // 30 against 29, 8192 47 against 35; so do tables of 128 MB and more (two of 32768 by 1024, 4096 tokens
+  // 67 against 64).
+  const int64_t held = 2 * 152 / m.parts, some = (rows + vocab + 63) / 64;
+  const int64_t blocks = held < 1 ? 1 : held < some ? held : some, own = (vocab + blocks - 1) / blocks;
+  if (rows <= NEAR_TOKENS && own <= NEAR_OWN) {
+    m.blocks = static_cast<int>(blocks);
+    // id / blocks as the upper half of a product: exact below 2^32 / blocks, and there are 304 blocks of 8192
+    // ids at most
+    m.by = blocks > 1 ? static_cast<uint32_t>(((int64_t{1} << 32) + blocks - 1) / blocks) : 0;
+    m.shared = static_cast<int>((2 * NEAR_WARPS * near_part(static_cast<int>(rows)) + own) * sizeof(uint32_t));
+    m.bytes = 16;                                       // no workspace
+    return m;
+  }
   int key = 1;
   while (key < 31 && (vocab >> key) > 0) ++key;          // keys 0 .. vocab
   m.passes = (key + 8) / 9;
@@ -648,7 +828,6 @@ EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual) {
   if (tile > SORT_SUB) tile = up(tile, SORT_SUB);
   m.tile = static_cast<int>(tile);
   m.tiles = rows > 0 ? static_cast<int>((rows + tile - 1) / tile) : 0;
-  m.slabs = static_cast<int>((dim + SLAB - 1) / SLAB);
   const int64_t slabs = static_cast<int64_t>(m.slabs) * (dual ? 2 : 1), steps = rows + vocab;
   // Short ranges leave warps for all of the GPU and spread what is slow, but each costs a search.  64 steps
   // against 32, 96 and 128: 8192 tokens, 32768 ids, two tables of 1024 columns 75 us against 77, 81 and 85;
@@ -677,6 +856,17 @@ cudaError_t embed_fwd(const EmbedParams& p, bool e_bf16, bool y_bf16, cudaStream
 cudaError_t embed_bwd(const EmbedParams& p, bool y_bf16, void* work, cudaStream_t s) {
   const bool dual = p.dEd != nullptr;
   EmbedPlan m = embed_plan(p.seq.rows, p.vocab, p.dim, dual);
+  if (m.blocks) {
+    auto near = [&](auto kernel, PerDeviceOnce& once) {
+      const cudaError_t r = once.run([&](int&) {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NEAR_SHARED);
+      });
+      if (r != cudaSuccess) return r;
+      return launch_k(kernel, dim3(static_cast<unsigned>(m.blocks * m.parts)), dim3(NEAR_THREADS), m.shared, s, p, m);
+    };
+    static PerDeviceOnce once[2];
+    return y_bf16 ? near(embed_near_kernel<__nv_bfloat16>, once[1]) : near(embed_near_kernel<float>, once[0]);
+  }
   char* base = static_cast<char*>(work);
   int2* lists[2] = {reinterpret_cast<int2*>(base + m.list), reinterpret_cast<int2*>(base + m.list) + p.seq.rows};
   int* hist = reinterpret_cast<int*>(base + m.hist);

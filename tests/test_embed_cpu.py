@@ -38,7 +38,7 @@ FWD = [dict(e_prec=-1), dict(E=None), dict(y=None), dict(E=P + 8), dict(y=3 * P 
        dict(y=P), dict(Ed=P * 9, yd=3 * P), dict(Ed=P * 9, yd=P * 9)]
 BWD = [dict(dy=None), dict(dE=None), dict(dy=4 * P + 8), dict(dE=5 * P + 4), dict(lddy=16), dict(lddE=20),
        dict(lddE=1 << 40), dict(dyd=P * 9), dict(dEd=P * 9), dict(work=None), dict(work=6 * P + 4),
-       dict(work_bytes=1000), dict(dE=4 * P), dict(dE=P), dict(work=4 * P), dict(dyd=P * 9, dEd=P * 5),
+       dict(work_bytes=15), dict(dE=4 * P), dict(dE=P), dict(work=4 * P), dict(dyd=P * 9, dEd=P * 5),
        dict(dyd=P * 9, dEd=P * 9)]
 
 

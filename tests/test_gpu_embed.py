@@ -5,8 +5,8 @@ finite, streams, graphs.
 
 Bounds.  A lookup is one float32 product (2^-24 of it, and as much again for the scale's own rounding)
 rounded to its type.  A gradient passes through at most 512 + 32 additions of a range, then those of a
-group of ranges and of the eight groups: below 1100 in all for up to 2^18 tokens, and never more than
-its tokens and eight; each is off by 2^-24 of the magnitudes summed."""
+block's ranges and of the blocks that share the row: below 1100 in all for up to 2^18 tokens, and never
+more than its tokens and eight; each is off by 2^-24 of the magnitudes summed."""
 import math
 
 import pytest
@@ -38,6 +38,22 @@ CASES = {
     "border": (32, 0, 40, 8, "f32", "f32", "all", 0),
     "heavy": (20000, 0, 5000, 200, "f32", "bf16", "heavy", 0.1),
     "last_id": (500, 0, 900, 20, "f32", "f32", "last", 0),
+    # the most tokens and the most rows of one launch, and one more
+    "one_launch_tokens": (6144, 0, 3000, 24, "f32", "bf16", "heavy", 0.1),
+    "more_tokens": (6145, 0, 3000, 24, "f32", "bf16", "heavy", 0.1),
+    "one_launch_rows": (40, 0, 304 * 8192, 3, "f32", "f32", "uniform", 0),
+    "more_rows": (40, 0, 304 * 8192 + 1, 3, "f32", "f32", "uniform", 0),
+    "one_block": (700, 3, 9, 7, "f32", "bf16", "zipf", 0.1),
+    "one_block_a_part": (500, 0, 8192, 40000, "bf16", "bf16", "heavy", 0),
+    "all_one_id_long": (9000, 0, 700, 130, "f32", "f32", "all", 0),
+    "border_long": (32, 0, 304 * 8192 + 1, 8, "f32", "f32", "all", 0),
+    # sorts of one, two and three digits, by one cluster and by launches
+    "cluster_one_digit": (7000, 7, 510, 40, "f32", "f32", "zipf", 0),
+    "cluster_two_digits": (8192, 0, 511, 40, "f32", "bf16", "uniform", 0),
+    "cluster_three_digits": (9001, 0, 2 ** 18, 8, "f32", "f32", "zipf", 0.05),
+    "cluster_most": (32768, 0, 3000, 12, "f32", "f32", "zipf", 0.1),
+    "launches_one_digit": (32769, 0, 200, 12, "f32", "f32", "uniform", 0.1),
+    "launches_three_digits": (33000, 9, 300000, 4, "f32", "bf16", "zipf", 0.1),
     "padding_only": (400, 5, 100, 64, "f32", "f32", "zipf", 1),
 }
 
@@ -147,7 +163,9 @@ def test_embed_types(te, ty):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("name", ["two_digits", "many_tiles", "all_one_id", "heavy", "long_tiles"])
+@pytest.mark.parametrize("name", ["two_digits", "many_tiles", "all_one_id", "heavy", "long_tiles", "more_tokens", "one_launch_tokens",
+                                  "all_one_id_long", "cluster_one_digit", "cluster_most", "launches_one_digit",
+                                  "launches_three_digits"])
 def test_embed_whole_numbers_are_exact(name):
     """Small whole numbers sum exactly in any order: every token once, in its own row."""
     torch, native = need_gpu()
@@ -185,17 +203,18 @@ def test_embed_all_rows_without_sequences():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("value", [math.nan, math.inf])
-def test_embed_values_that_are_not_finite(value):
+@pytest.mark.parametrize("tokens", [600, 8000])
+def test_embed_values_that_are_not_finite(value, tokens):
     """A table row reaches the rows of its id alone, a row's gradient its id's row alone; padding and
     rows behind the last sequence reach nothing."""
     torch, native = need_gpu()
-    case = (6000, 30, 800, 72, "f32", "f32", "heavy", 0.1)
+    case = (tokens, 30, 800, 72, "f32", "f32", "heavy", 0.1)
     s = make(torch, case, 86, False)
     want = {k: t.clone() for k, t in run(torch, native, s, 2.0, False).items()}
-    ids = s["ids"][:6000].long()
+    ids = s["ids"][:tokens].long()
     pads = torch.nonzero((ids < 0) | (ids >= 800)).squeeze(1)
     s["dy"][pads] = value
-    s["dy"][6000:] = value
+    s["dy"][tokens:] = value
     row = torch.nonzero((ids >= 0) & (ids < 800))[17].item()
     s["dy"][row, 3] = value
     s["E"][5] = value
@@ -205,14 +224,14 @@ def test_embed_values_that_are_not_finite(value):
     keep[ids[row], 3] = False
     assert torch.equal(o["dE"][keep], want["dE"][keep]) and not torch.isfinite(o["dE"][ids[row], 3])
     keep = s["ids"] != 5
-    assert torch.equal(o["y"][keep], want["y"][keep]) and not torch.isfinite(o["y"][:6000][ids == 5]).any()
+    assert torch.equal(o["y"][keep], want["y"][keep]) and not torch.isfinite(o["y"][:tokens][ids == 5]).any()
 
 
 @pytest.mark.gpu
 def test_embed_same_bits_again_and_at_once():
     torch, native = need_gpu()
     jobs = []
-    for seed, name in ((1, "many_tiles"), (2, "heavy"), (3, "slab")):
+    for seed, name in ((1, "many_tiles"), (2, "heavy"), (3, "slab"), (4, "one_launch_tokens")):
         s = make(torch, CASES[name], seed, True)
         jobs.append((s, {k: t.clone() for k, t in run(torch, native, s, 3.0, True).items()}))
     torch.cuda.synchronize()
@@ -230,17 +249,18 @@ def test_embed_same_bits_again_and_at_once():
 
 
 @pytest.mark.gpu
-def test_embed_captured_with_other_tokens():
+@pytest.mark.parametrize("rows", [6000, 9000, 40000])
+def test_embed_captured_with_other_tokens(rows):
     """A captured call replayed after ids, lengths and gradients have changed on the device."""
     torch, native = need_gpu()
-    N, V, D = 9000, 2000, 48
+    N, V, D = rows, 2000, 48
     s = make(torch, (N, 0, V, D, "f32", "f32", "zipf", 0.1), 87, True)
     o = run(torch, native, s, 1.5, True)
     torch.cuda.synchronize()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         run(torch, native, s, 1.5, True, out=o)
-    for seed, kind, n in ((1, "all", N), (2, "uniform", 5000), (3, "heavy", 31), (4, "zipf", 0), (5, "zipf", N)):
+    for seed, kind, n in ((1, "all", N), (2, "uniform", N // 2 + 3), (3, "heavy", 31), (4, "zipf", 0), (5, "zipf", N)):
         new = make(torch, (n, N - n, V, D, "f32", "f32", kind, 0.2), seed, True)
         for k in s:
             s[k].copy_(new[k])
