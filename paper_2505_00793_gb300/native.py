@@ -311,7 +311,8 @@ class _Call:
         a tangent shares with its primal (``step``).  Returns the leading dimension."""
         if t is None:
             return step
-        self._base(t, name, dtype)
+        if t.dtype is not dtype or t.get_device() != self.device:
+            self._base(t, name, dtype)
         shape, stride = t.shape, t.stride()
         if len(shape) != 2 or shape[0] != rows or shape[1] < cols or (stride[1] != 1 and shape[1] > 1):
             raise ValueError(f"{name}: shape {tuple(shape)}, strides {stride}, expected "
@@ -329,17 +330,19 @@ class _Call:
     def vec(self, name, t, dtype, shape):
         if t is None:
             return
-        self._base(t, name, dtype)
+        if t.dtype is not dtype or t.get_device() != self.device:
+            self._base(t, name, dtype)
         if t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{name}: shape {tuple(t.shape)}, expected contiguous {shape}")
         setattr(self.a, name, t.data_ptr())
 
     def seq(self, seq_start, n_seq, int32):
         if seq_start is not None:
-            if seq_start.dim() != 1 or seq_start.shape[0] < 2:
-                raise ValueError(f"seq_start: shape {tuple(seq_start.shape)}, expected [n_seq + 1]")
-            n_seq = seq_start.shape[0] - 1
-            self.vec("seq_start", seq_start, int32, (n_seq + 1,))
+            shape = seq_start.shape
+            if len(shape) != 1 or shape[0] < 2:
+                raise ValueError(f"seq_start: shape {tuple(shape)}, expected [n_seq + 1]")
+            n_seq = shape[0] - 1
+            self.vec("seq_start", seq_start, int32, shape)
         self.a.n_seq = n_seq
 
     def work(self, work):
@@ -351,7 +354,7 @@ class _Call:
 
     def run(self, fn, stream, *more):
         import torch
-        if self.device != torch.cuda.current_device():
+        if self.device != torch._C._cuda_getDevice():
             with torch.cuda.device(self.device):
                 return self.run(fn, stream, *more)
         # the current stream's handle without building a Stream object around it (4 us a call)
@@ -363,9 +366,12 @@ class _Call:
 
 def _prec(t, name):
     import torch
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"{name}: dtype {t.dtype}, expected torch.float32 or torch.bfloat16")
-    return PRECISIONS["bf16" if t.dtype == torch.bfloat16 else "fp32"]
+    d = t.dtype
+    if d is torch.bfloat16:
+        return PRECISIONS["bf16"]
+    if d is torch.float32:
+        return PRECISIONS["fp32"]
+    raise ValueError(f"{name}: dtype {d}, expected torch.float32 or torch.bfloat16")
 
 
 def _rope_call(first, n_heads, n_kv_heads, head_dim, rope, n_copy_heads, gq, gk, gqd, gkd, eps,
@@ -533,24 +539,24 @@ def _embed_call(ids, table, rows, scale, seq_start):
     lib()
     a = mf_embed_args()
     c = _Call(a, ids)
-    if ids.dim() != 1 or table.dim() != 2:
-        raise ValueError(f"ids, table: shapes {tuple(ids.shape)}, {tuple(table.shape)}, expected [n_rows] and "
-                         "[vocab][dim]")
-    a.n_rows, (a.vocab, a.dim), a.scale = ids.shape[0], table.shape, scale
+    n, shape = ids.shape, table.shape
+    if len(n) != 1 or len(shape) != 2:
+        raise ValueError(f"ids, table: shapes {tuple(n)}, {tuple(shape)}, expected [n_rows] and [vocab][dim]")
+    a.n_rows, a.vocab, a.dim, a.scale = n[0], *shape, scale
     a.y_prec = _prec(rows, "y")
-    c.vec("ids", ids, torch.int32, (a.n_rows,))
-    c.seq(seq_start, 0, torch.int32)
-    return c
+    c.vec("ids", ids, torch.int32, n)
+    if seq_start is not None:
+        c.seq(seq_start, 0, torch.int32)
+    return c, n[0], *shape
 
 
 def mf_embed_fwd(ids, E, y, scale=1.0, Ed=None, yd=None, seq_start=None, stream=None):
     """y [N][dim] = scale E[ids] (rows of zeros where an id is no row of E [vocab][dim]); Ed -> yd
     the tangent (see mixflow.h)."""
-    c = _embed_call(ids, E, y, scale, seq_start)
-    a = c.a
-    a.e_prec = _prec(E, "E")
-    c.rows("Ed", Ed, E.dtype, a.vocab, a.dim, "ldE", c.rows("E", E, E.dtype, a.vocab, a.dim, "ldE"))
-    c.rows("yd", yd, y.dtype, a.n_rows, a.dim, "ldy", c.rows("y", y, y.dtype, a.n_rows, a.dim, "ldy"))
+    c, n, vocab, dim = _embed_call(ids, E, y, scale, seq_start)
+    c.a.e_prec = _prec(E, "E")
+    c.rows("Ed", Ed, E.dtype, vocab, dim, "ldE", c.rows("E", E, E.dtype, vocab, dim, "ldE"))
+    c.rows("yd", yd, y.dtype, n, dim, "ldy", c.rows("y", y, y.dtype, n, dim, "ldy"))
     c.run("mf_embed_fwd", stream)
 
 
@@ -558,10 +564,10 @@ def mf_embed_bwd(ids, dy, dE, work, scale=1.0, dyd=None, dEd=None, seq_start=Non
     """Gradient of mf_embed_fwd's table: dE [vocab][dim] float32 from dy [N][dim] (dEd from dyd);
     work: mf_embed_work_bytes bytes."""
     import torch
-    c = _embed_call(ids, dE, dy, scale, seq_start)
-    a, f32 = c.a, torch.float32
-    c.rows("dyd", dyd, dy.dtype, a.n_rows, a.dim, "lddy", c.rows("dy", dy, dy.dtype, a.n_rows, a.dim, "lddy"))
-    c.rows("dEd", dEd, f32, a.vocab, a.dim, "lddE", c.rows("dE", dE, f32, a.vocab, a.dim, "lddE"))
+    c, n, vocab, dim = _embed_call(ids, dE, dy, scale, seq_start)
+    f32 = torch.float32
+    c.rows("dyd", dyd, dy.dtype, n, dim, "lddy", c.rows("dy", dy, dy.dtype, n, dim, "lddy"))
+    c.rows("dEd", dEd, f32, vocab, dim, "lddE", c.rows("dE", dE, f32, vocab, dim, "lddE"))
     c.work(work)
     c.run("mf_embed_bwd", stream)
 
