@@ -317,7 +317,11 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // registers and was up to 17 % slower.
 // TKEYS keys a tile: 64 where the tangents leave no TMEM for more, and where many CTAs are to be
 // had: tiles of 64 let three of them, not two, fill each other's waits on an SM (launch_fwd).
-template <bool DUAL, int HDP, int TKEYS>
+// With a window, whose walks are short and all as long, four CTAs of 64 keys a tile hide one another's ends
+// better, for fewer registers: 16 heads over 4, 32768 rows, window 1024 208 us against 227, 16 heads over 8,
+// 16384 rows, window 128 50 against 53; without one 16 heads over 4, 8192 rows 191 (a training step)
+// against 181.
+template <bool DUAL, int HDP, int TKEYS, bool WIN>
 struct FwdCfg {
   static constexpr int NA = HDP / 64;                      // 64-column atoms of a head
   static constexpr int TK = TKEYS;
@@ -330,7 +334,7 @@ struct FwdCfg {
   static constexpr int EW = 4;                             // row warps: a thread a row
   static constexpr int THREADS = 64 + 32 * EW;
   static constexpr bool SMALL = TK * NT + HDP * NT <= 128;
-  static constexpr int CTAS = SMALL ? 3 : 2;
+  static constexpr int CTAS = SMALL ? (WIN ? 4 : 3) : 2;
   static constexpr uint32_t TMEM_COLS = SMALL ? 128 : 256;
   static constexpr uint32_t C_S = 0, C_SD = 64, C_O = NT * TK, C_T = 192;
 };
@@ -426,12 +430,12 @@ struct KeyWalk {
 };
 
 template <bool DUAL, int HDP, int TKEYS, bool WIN>
-__global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS>::THREADS, FwdCfg<DUAL, HDP, TKEYS>::CTAS)
+__global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg<DUAL, HDP, TKEYS, WIN>::CTAS)
     attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                        const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQd,
                        const __grid_constant__ CUtensorMap tmKd, const __grid_constant__ CUtensorMap tmVd,
                        const __grid_constant__ TcParams2 p) {
-  using C = FwdCfg<DUAL, HDP, TKEYS>;
+  using C = FwdCfg<DUAL, HDP, TKEYS, WIN>;
   constexpr int TK = C::TK, NA = C::NA;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   // barriers, as byte offsets in a set; one set per walk
@@ -887,7 +891,7 @@ TcParams2 tc_params(const AttnParams& a) {
 
 template <bool DUAL, int HDP, int TKEYS, bool WIN>
 cudaError_t launch_fwd(const AttnParams& a, cudaStream_t s) {
-  using C = FwdCfg<DUAL, HDP, TKEYS>;
+  using C = FwdCfg<DUAL, HDP, TKEYS, WIN>;
   CUtensorMap q, k, v, qd, kd, vd;
   const int N = a.seq.rows;
   if (!head_map(&q, a.q, a.D, N, a.ldq, a.Hq, TR) || !head_map(&k, a.k, a.D, N, a.ldk, a.Hkv, C::TK) ||
