@@ -175,8 +175,8 @@ struct SeqTile {
   uint32_t bits[4];
 };
 
-// The table is filled by all threads of the block: each reads its first start (SeqLoad) before
-// the block's first barrier, so that the reads of the prologue are in flight together.
+// The table is filled by the first `threads` of the block: each reads its first start (SeqLoad) before
+// their first barrier, so that the reads of the prologue are in flight together.
 struct SeqLoad {
   int first, v;
 };
@@ -197,8 +197,8 @@ __device__ __forceinline__ void seq_tile_init(const SeqRows& s, int row0, SeqTil
 __device__ __forceinline__ void seq_tile_fill(const SeqRows& s, int row0, SeqTile& t, int threads,
                                               const SeqLoad& l) {
   if (!s.start) {
-    const int p = threadIdx.x;
-    if (p > 0 && p < TR && (row0 + p) % s.len == 0) atomicOr(&t.bits[p >> 5], 1u << (p & 31));
+    for (int p = threadIdx.x; p < TR; p += threads)
+      if (p > 0 && (row0 + p) % s.len == 0) atomicOr(&t.bits[p >> 5], 1u << (p & 31));
     return;
   }
   int v = l.v;
@@ -1593,6 +1593,24 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   tc_fence_after();
   if (careful || !redo_flag || *abort) break;
   }
+  // Rows whose sums leave as float32, for sink_sum_kernel: sinks that other CTAs have sums of too, as slot
+  // and place, behind the accumulators.  (Looked up for each sum, with divisions, it took 7 us of a CTA's
+  // 68, heads of 128.)
+  int* sink_of = reinterpret_cast<int*>(smem + 2 * C::NT * TR * 4 * HDP);
+  static_assert(2 * C::NT * TR * 4 * HDP + TR * 4 <= C::OPND_B, "behind the accumulators");
+  if constexpr (WIN) {
+    const int q = static_cast<int>(threadIdx.x) - 96;
+    if (p.sinks > 0 && q >= 0 && q < TR && !*abort) {
+      int at = -1;
+      if (far) {
+        at = (p.chunks + far) << 7 | q;
+      } else if (q < nvalid) {
+        const int start = tile_lo(st_rows, row0, q), place = row0 + q - start;
+        if (place < p.sinks && has_far(p, start, tile_hi(st_rows, row0, q))) at = start / p.chunk << 7 | place;
+      }
+      sink_of[q] = at;
+    }
+  }
   // The cluster's sums, rank by rank in order, each CTA its part of the rows; the second barrier
   // keeps a CTA's shared memory until the others have read it.  Short code counts here: it runs once
   // a CTA, and unrolled eight ranks wide it took 4.5 us of a CTA's 45 (16 heads of 64 over 4, two
@@ -1603,7 +1621,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     const int r0 = rank * rows, nr = min(min(r0 + rows, TR), nvalid) - r0;
     // A lane has four columns of one sum, so that a warp reads whole rows, and every RS-th row,
     // NI of them together.
-    constexpr int CH = HDP / 4, RS = 32 * C::EW / (2 * C::NT * CH), NI = 2;
+    constexpr int CH = HDP / 4, RS = 32 * C::EW / (2 * C::NT * CH), NI = WIN ? (C::CTAS == 1 ? 8 : 4) : 2;
     static_assert(RS * 2 * C::NT * CH == 32 * C::EW, "every thread its columns");
     const int t = static_cast<int>(threadIdx.x) - 96, c = t % CH, k = t / CH % (2 * C::NT);
     const int end = r0 + nr;
@@ -1631,20 +1649,12 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           x[u] = j == 0 ? v[u] : make_float4(x[u].x + v[u].x, x[u].y + v[u].y, x[u].z + v[u].z, x[u].w + v[u].w);
       }
       uint32_t rows_left = (1u << NI) - 1;
-      if constexpr (WIN) {
-        // sinks that other CTAs have sums of too leave as float32, for sink_sum_kernel
+      if (WIN && p.sinks > 0) {
 #pragma unroll
         for (int u = 0; u < NI; ++u) {
-          const int q = r + u * RS;
-          if (p.sinks == 0 || q >= end) continue;
-          int place = q, slot = p.chunks + far;
-          if (!far) {
-            const int start = tile_lo(st_rows, row0, q);
-            place = row0 + q - start;
-            slot = start / p.chunk;
-            if (place >= p.sinks || !has_far(p, start, tile_hi(st_rows, row0, q))) continue;
-          }
-          *reinterpret_cast<float4*>(p.part + part_at(p, 2 * C::NT, HDP, slot, hk, k, place) + 4 * c) = x[u];
+          const int at = r + u * RS < end ? sink_of[(r + u * RS) & (TR - 1)] : -1;
+          if (at < 0) continue;
+          *reinterpret_cast<float4*>(p.part + part_at(p, 2 * C::NT, HDP, at >> 7, hk, k, at & 127) + 4 * c) = x[u];
           rows_left &= ~(1u << u);
         }
       }
@@ -1717,30 +1727,46 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   };
 
   pdl_entry();
-  const SeqLoad sl = seq_tile_load(p.seq, row0);
   const int nvalid = min(seq_total(p.seq) - row0, TR);
   if (nvalid <= 0) return;
-  seq_tile_init(p.seq, row0, st_rows);
-  // a barrier a thread; the first thread's own is the one that its loads complete
-  if (threadIdx.x < 2 * NBARS) {
-    const uint32_t b = threadIdx.x % NBARS;
-    bar_init(smem_u32(&bars[0][0]) + 8 * threadIdx.x, 8 * b == B_S_FREE || (8 * b & ~8u) == B_DS_FULL ? C::EW : 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  // The first three warps set up and look the sequences up, while the row warps sum D of the rows and read
+  // their statistics: behind one another these took 4 us of a CTA's 17 (heads of 128, window 1000).
+  float lse = 0.f, rbar = 0.f;
+  if (warp < 3) {
+    const SeqLoad sl = seq_tile_load(p.seq, row0);
+    seq_tile_init(p.seq, row0, st_rows);
+    // a barrier a thread; the first thread's own is the one that its loads complete
+    static_assert(2 * NBARS <= 96, "a thread a barrier");
+    if (threadIdx.x < 2 * NBARS) {
+      const uint32_t b = threadIdx.x % NBARS;
+      bar_init(smem_u32(&bars[0][0]) + 8 * threadIdx.x, 8 * b == B_S_FREE || (8 * b & ~8u) == B_DS_FULL ? C::EW : 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+      abort_flag = redo_flag = 0;
+      load_rows(smem_u32(&bars[0][0]) + B_RES_FULL);   // the rows' own operands need nothing of the sequences
+    }
+    if (warp == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                       smem_u32(&tmem_slot)),
+                   "r"(C::COLS));
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("bar.sync 2, 96;" ::: "memory");
+    seq_tile_fill(p.seq, row0, st_rows, 96, sl);
+    tc_fence_before();
+    asm volatile("bar.sync 2, 96;" ::: "memory");
+    asm volatile("bar.arrive 3, %0;" ::"n"(C::THREADS) : "memory");
+  } else {
+    const int64_t r = (warp & 3) * 32 + lane, si = static_cast<int64_t>(h) * p.seq.rows + row0 + r;
+    if (r < nvalid) {
+      lse = p.lse[si];
+      if (DUAL) rbar = p.rbar[si];
+    }
+    // D of the rows, a row's chunks of 16 bytes in neighbouring lanes
+    row_dots<DUAL, HDP, C::EW>(p, row0, nvalid, h, warp - 3, lane, sD);
+    asm volatile("bar.sync 3, %0;" ::"n"(C::THREADS) : "memory");
   }
-  if (threadIdx.x == 0) {
-    abort_flag = redo_flag = 0;
-    load_rows(smem_u32(&bars[0][0]) + B_RES_FULL);   // the rows' own operands need nothing of the sequences
-  }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                     smem_u32(&tmem_slot)),
-                 "r"(C::COLS));
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-  }
-  __syncthreads();
-  seq_tile_fill(p.seq, row0, st_rows, C::THREADS, sl);
-  tc_fence_before();
-  __syncthreads();
   tc_fence_after();
   const uint32_t tb = tmem_slot;
   volatile int* abort = &abort_flag;
@@ -1878,15 +1904,12 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
     const bool lone = lo == row0 + r || (WIN && p.window == 1 && p.sinks == 0);
     const int64_t row = row0 + r, si = static_cast<int64_t>(h) * p.seq.rows + row;
     const bool on = r < nvalid;
-    // D of the rows, a row's chunks of 16 bytes in neighbouring lanes
-    if (!careful) row_dots<DUAL, HDP, C::EW>(p, row0, nvalid, h, warp - 3, lane, sD);
-    row_bar<C::EW>();
     const float Dv = sD[r].x, Dd = sD[r].y;
     if (on && part == 0) {
       p.Dr[si] = Dv;
       if (DUAL) p.Drd[si] = Dd;
     }
-    const float lse2 = on ? p.lse[si] * LOG2E : 0.f, rb = DUAL && on ? p.rbar[si] : 0.f;
+    const float lse2 = lse * LOG2E, rb = rbar;
     const uint64_t c2p = pair(p.c2, p.c2), nl = pair(-lse2, -lse2), nD = pair(-Dv, -Dv);
     const uint64_t nr = pair(-rb, -rb), nDd = pair(-Dd, -Dd), sc = pair(p.scale, p.scale);
     bool ok = true;
