@@ -1045,8 +1045,9 @@ __device__ __forceinline__ void row_bar() {
 }
 
 // D = rowsum(dO (*) O) of the tile's rows, and its tangent rowsum(dO' (*) O + dO (*) O'), by the
-// row warps: the lanes of a row read its 16-byte chunks side by side.
-template <bool DUAL, int HDP, int EW>
+// row warps: the lanes of a row read its 16-byte chunks side by side.  ALL: every row's reads in flight
+// together.
+template <bool DUAL, int HDP, int EW, bool ALL>
 __device__ __forceinline__ void row_dots(const TcParams2& p, int row0, int nvalid, int h, int w,
                                          int lane, float2* out) {
   constexpr int LPR = HDP / 8, STEP = EW * (32 / LPR);
@@ -1059,7 +1060,7 @@ __device__ __forceinline__ void row_dots(const TcParams2& p, int row0, int nvali
     }
   };
   const int c = 8 * (lane % LPR);
-  constexpr int IT = TR / STEP, NB = DUAL || IT > 4 ? IT / 2 : IT;   // rows read together
+  constexpr int IT = TR / STEP, NB = ALL ? IT : DUAL || IT > 4 ? IT / 2 : IT;   // rows read together
 #pragma unroll
   for (int i0 = 0; i0 < IT; i0 += NB) {
     uint4 x[NB][DUAL ? 4 : 2];
@@ -1764,7 +1765,7 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       if (DUAL) rbar = p.rbar[si];
     }
     // D of the rows, a row's chunks of 16 bytes in neighbouring lanes
-    row_dots<DUAL, HDP, C::EW>(p, row0, nvalid, h, warp - 3, lane, sD);
+    row_dots<DUAL, HDP, C::EW, C::CTAS == 1>(p, row0, nvalid, h, warp - 3, lane, sD);
     asm volatile("bar.sync 3, %0;" ::"n"(C::THREADS) : "memory");
   }
   tc_fence_after();
