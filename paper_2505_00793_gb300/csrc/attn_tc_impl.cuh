@@ -308,9 +308,9 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // on many tiles it costs a look more at each: scores of std 3 and 8 82 to 92 us and 89 to 118, o' off
 // by 0.0030 and 0.0045 where it was by 0.0032 and 0.0052.  The plain mean of the first tile alone took 82
 // and 90 us, but left rows of one heavy key further off than P (*) S' did.
-// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 381 to 387 us, 1.43 PF/s of
-// causal work, and 360 us, 1.53 PF/s, over the same rows again and again; the tensor pipe busy 67 % of
-// the cycles); at 64 the chain scores - maximum -
+// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 344 to 350 us, 1.58 PF/s of
+// causal work; 358 with scores read 32 columns at a time, the tensor pipe busy 67 % of the cycles); at 64
+// the chain scores - maximum -
 // exponentials - product of each CTA, which two or three CTAs an SM fill by turns (16 heads, 16384
 // rows: 0.94 PF/s; 16 heads with tangents, eight sequences of 1024: 79 us, pipe 36 %).  Taking the
 // exponentials against the last tile's maximum, so that they need not wait for this one's, cost
@@ -386,6 +386,17 @@ __device__ __forceinline__ void stage_out(const uint8_t* buf, int nvalid, int D,
     *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(from);
 }
 
+// With a window (WIN) row i of a sequence that begins at lo attends to the rows j of it with j <= i and
+// i - j < window or j - lo < sinks: the same sums over fewer pairs.  A tile of 128 rows walks window + 127
+// keys, and 128 at most of sinks before them, so that its ends, some 6000 cycles of a forward CTA (set-up and
+// first scores 4000, results 2200) beside 1900 a tile, weigh more than without one.  Of the products
+// that the pairs need, at 1888 TF/s: 16 heads of 64 over 4, 32768 rows, window 1024 203 us forward (72: 669
+// TF/s); window 512, 16384 rows 301 us forward and backward (45); 16 heads of 128 over 2, 24577 rows,
+// window 1000 942 us (305).  Issue slots are half used, the tensor pipe 30 %: the chain of a tile
+// bounds it, and four CTAs an SM fill what three left.  Tried, and no faster: products and exponentials of
+// no more sinks than there are, columns that no row of a warp attends to left out of masked tiles, two
+// buffers of scores, the next CTA's rows fetched into L2.
+//
 // The key tiles that a tile of query rows walks: from the first row's sequence on (k0), or, with
 // a window, from the first row's window on, ahead of them the sinks of its sequence where they lie
 // before that window.  (Other sequences of the tile begin inside it, and so do their sinks.)
@@ -645,20 +656,29 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
       tc_fence_after();
       // mixed tiles have code of their own: selects in the common one would be issued for every
       // element, taken or not
-      // Scores come in groups of 16 columns, the next one while one is looked at.
+      // Scores come in groups of 16 columns, the next one while one is looked at; with tangents two
+      // together, between whose parts there is enough to do (81 us for 79 otherwise, 16 heads, eight
+      // sequences of 1024).
       constexpr int GROUPS = TK / 16;
       float sv[2][16], mx = -INFINITY;
       auto load_group = [&](int g) { tmem_ld16_nowait(aS + 16 * g, sv[g & 1]); };
+      auto load_pair = [&](int g) {
+        tmem_ld32_nowait(aS + 16 * g, sv[0]);
+        tmem_wait_ld();
+      };
       auto mask_group = [&](int g) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) sv[g & 1][i] = own[g >> 1] >> (16 * (g & 1) + i) & 1 ? sv[g & 1][i] : -INFINITY;
       };
       auto find_max = [&](auto masked) {
-        load_group(0);
-        tmem_wait_ld();
+        if (!DUAL) {
+          load_group(0);
+          tmem_wait_ld();
+        }
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-          if (g + 1 < GROUPS) load_group(g + 1);
+          if (DUAL && g % 2 == 0) load_pair(g);
+          if (!DUAL && g + 1 < GROUPS) load_group(g + 1);
           if constexpr (decltype(masked)::value) mask_group(g);
           const float* v = sv[g & 1];
           float y0 = mx, y1 = v[0];
@@ -668,7 +688,7 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
             y1 = fmaxf(fmaxf(y1, v[i + 2]), v[i + 3]);
           }
           mx = fmaxf(y0, y1);
-          if (g + 1 < GROUPS) tmem_wait_ld();
+          if (!DUAL && g + 1 < GROUPS) tmem_wait_ld();
         }
       };
       if (mx_tile) find_max(std::true_type{});
@@ -753,19 +773,17 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
         constexpr bool MASK = decltype(masked)::value;
         // from the last 32 columns on, whose scores are still here (masked, too)
         auto group = [](int k) { return 2 * (TK / 32 - 1 - k / 2) + (k & 1); };
-        float sd[2][16];
-        if (DUAL) tmem_ld16(aSd + 16 * group(0), sd[0]);
 #pragma unroll
         for (int k = 0; k < GROUPS; ++k) {
           const int g = group(k), b = g & 1;
-          if (k + 1 < GROUPS) {
-            if (k > 0) load_group(group(k + 1));
-            if (DUAL) tmem_ld16_nowait(aSd + 16 * group(k + 1), sd[b ^ 1]);
-          }
+          float sd[16];
+          if (DUAL && k > 1 && b == 0) load_pair(g);
+          if (!DUAL && k > 0 && k + 1 < GROUPS) load_group(group(k + 1));
+          if (DUAL) tmem_ld16(aSd + 16 * g, sd);
           if (MASK && k > 1) mask_group(g);
           if (DUAL && MASK) {   // the tangent of a masked score may be anything
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sd[b][i] = own[g >> 1] >> (16 * b + i) & 1 ? sd[b][i] : 0.f;
+            for (int i = 0; i < 16; ++i) sd[i] = own[g >> 1] >> (16 * b + i) & 1 ? sd[i] : 0.f;
           }
           uint32_t pk[8], psk[8];
 #pragma unroll
@@ -776,12 +794,12 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
             l2 = add2(l2, pp);
             pk[i / 2] = pack_bf16x2(p0, p1);
             if (DUAL) {
-              const uint64_t ps = mul2(pp, fma2(pair(sd[b][i], sd[b][i + 1]), scp, nc));
+              const uint64_t ps = mul2(pp, fma2(pair(sd[i], sd[i + 1]), scp, nc));
               r2 = add2(r2, ps);
               psk[i / 2] = pack2(ps);
             }
           }
-          if (k + 1 < GROUPS && (DUAL || k > 0)) tmem_wait_ld();
+          if (!DUAL && k > 0 && k + 1 < GROUPS) tmem_wait_ld();
           // each 32 keys' P begins where their scores did
           tmem_st8(aS + 32 * (g >> 1) + 8 * b, pk);
           if (DUAL) tmem_st8(aSd + 32 * (g >> 1) + 8 * b, psk);
