@@ -69,7 +69,7 @@ struct AttnParams {
   int window = 0, sinks = 0;
   float* part = nullptr;
 };
-// Both passes (attn_tc.cu): heads of up to 128 columns, 64 with tangents.
+// Both passes (attn_tc.cu, kernels in attn_tc_impl.cuh): heads of up to 128 columns, 64 with tangents.
 cudaError_t attn_tc_fwd(const AttnParams& p, bool dual, cudaStream_t s);
 cudaError_t attn_tc_bwd(const AttnParams& p, bool dual, cudaStream_t s);
 // The same with a window (attn_tc_window.cu).

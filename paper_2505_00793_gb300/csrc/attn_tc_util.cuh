@@ -1,4 +1,4 @@
-// Device helpers of the tcgen05 attention kernels (flash_tc.cu, attn_tc.cu): TMEM access by
+// Device helpers of the tcgen05 attention kernels (flash_tc.cu, attn_tc_impl.cuh): TMEM access by
 // rows, arithmetic on pairs of float32, bounded waits.
 #pragma once
 
