@@ -12,8 +12,8 @@
 //
 // Measured (of 6.75 TB/s, a plain copy): 8192 tokens, 32768 ids, two tables of 1024 columns, float32: lookup
 // 94 MB in 18 us (78 %), gradient 335 MB in 70 us (71 %), of which the sort takes 10, the sums 57 (87 %)
-// and the rows that blocks share 4; 131071 tokens, 50001 ids, 768 columns of bf16 355 MB in 103 us (51 %):
-// 23, 72 and 8.  4096 tokens, 8192 ids, 512 columns take one launch, 21 MB in 12 us, latencies.  Zeros
+// and the rows that blocks share 4; 131071 tokens, 50001 ids, 768 columns of bf16 355 MB in 96 us (55 %):
+// 23, 65 and 8.  4096 tokens, 8192 ids, 512 columns take one launch, 21 MB in 12 us, latencies.  Zeros
 // written by blocks beside the sort, and sums of the ids that occur alone, took longer (87 us in the
 // first): writes by themselves come at 4.5 TB/s, among reads at 6.
 #include "attn_ops.h"
@@ -384,9 +384,10 @@ __global__ void __launch_bounds__(SORT_THREADS)
 // sum, else row v is written and v + 1 is next.  Token i of key k is taken at step i + k, so the
 // state at a step is found by a search.  A warp takes NV slabs of 128 columns of a range of `per`
 // steps.  A border of two ranges that cuts an id's tokens moves ahead of them, if there are fewer than 32
-// of them before it; else both sides' sums are added up at the end: those of a block's eight ranges by
-// the block, and where a block's own border cuts, through the workspace by embed_join_kernel.
-constexpr int SUM_WARPS = 8, SLAB = 128;
+// of them before it; else both sides' sums are added up at the end: those of a block's ranges by the
+// block, and where a block's own border cuts, through the workspace by embed_join_kernel.
+// Four warps a block: 131071 tokens, 50001 ids, 768 columns of bf16 96 us; eight 104, two 98, sixteen 105.
+constexpr int SUM_WARPS = 4, SLAB = 128;
 constexpr int64_t SUM_HELD = 152 * 24;             // warps that the GPU holds
 
 struct PathState {
@@ -830,9 +831,8 @@ EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual) {
   m.tiles = rows > 0 ? static_cast<int>((rows + tile - 1) / tile) : 0;
   const int64_t slabs = static_cast<int64_t>(m.slabs) * (dual ? 2 : 1), steps = rows + vocab;
   // Short ranges leave warps for all of the GPU and spread what is slow, but each costs a search.  64 steps
-  // against 32, 96 and 128: 8192 tokens, 32768 ids, two tables of 1024 columns 75 us against 77, 81 and 85;
-  // 131071 tokens, 50001 ids, 768 columns 99 against 107, 99 and 105.  4096 tokens, 8192 ids, 512
-  // columns: 30 us with 32 steps, 32 with 64.
+  // against 48, 96 and 128: 8192 tokens, 32768 ids, two tables of 1024 columns 72 us against 71, 78 and 85;
+  // 131071 tokens, 50001 ids, 768 columns 96 against 101, 112 and 109.
   m.per = steps * slabs >= 2 * 64 * SUM_HELD ? 64 : 32;
   m.groups = static_cast<int>((steps + m.per * SUM_WARPS - 1) / (m.per * SUM_WARPS));
   m.list = 0;
@@ -891,7 +891,7 @@ cudaError_t embed_bwd(const EmbedParams& p, bool y_bf16, void* work, cudaStream_
   if (e != cudaSuccess) return e;
   const int2* list = lists[(m.passes - 1) & 1];
   // Two slabs a warp for rows of bf16, where that leaves two rounds of warps: 131071 tokens, 50001 ids, 768
-  // columns 99 us against 112; float32 rows gain nothing (75 us against 83 in the case of 1024 columns).
+  // columns 96 us against 115, three 99; float32 rows gain nothing (83 us against 75 in the case of 1024).
   const int slabs = m.slabs * (dual ? 2 : 1);
   const int64_t warps = (static_cast<int64_t>(p.seq.rows) + p.vocab) / m.per * slabs;
   const int wide = y_bf16 && m.slabs > 1 && warps >= 4 * SUM_HELD ? 2 : 1;
