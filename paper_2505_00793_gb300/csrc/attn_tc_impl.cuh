@@ -1236,6 +1236,16 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       qb = row0 + min(p.window, hi0 - row0);
     }
   }
+  const bool alone = p.share == 1;
+  // Whether row q's sums leave as float32, for sink_sum_kernel: sinks that other CTAs have sums of too, as
+  // slot and place (-1: no).  Looked up once a row: for each sum, with divisions, it took 7 us of a CTA's 68
+  // (heads of 128).
+  auto sink_slot = [&](int q) {
+    if (!WIN || p.sinks == 0 || q >= nvalid) return -1;
+    if (far) return (p.chunks + far) << 7 | q;
+    const int start = tile_lo(st_rows, row0, q), place = row0 + q - start;
+    return place < p.sinks && has_far(p, start, tile_hi(st_rows, row0, q)) ? start / p.chunk << 7 | place : -1;
+  };
   const int nqt = (q1 - q0 + BT - 1) / BT;          // query tiles of a head
   const int ntile = nqt * G;
   // whether some key row is not attended to by the whole of query tile t
@@ -1583,11 +1593,14 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
       __syncwarp();
       if (lane == 0) bar_arrive(bb + B_DS_FULL);
     }
-    // accumulators to shared memory, over the operands, which every product has read: a tile of
-    // float32 rows each, 16-byte chunk c of row r at place c ^ (r & 7)
+    // Accumulators to shared memory, over the operands, which every product has read: the results' rows where
+    // this CTA has all of their sums, else a tile of float32 rows each, 16-byte chunk c of row r at place
+    // c ^ (r & 7).  (Always float32, the way out took 9 to 12 thousand cycles of a CTA's 21 to 120, results
+    // four.)
     if (ok && rwait(bb + B_DRAIN, 0, p.status, abort) && !*abort) {
       tc_fence_after();
       const uint32_t acc = tb + (static_cast<uint32_t>(q4 * 32) << 16) + part * C::OW;
+      const int at = WIN && alone ? sink_slot(r) : -1;
       float z = 0.f;
       // rolled up where two CTAs share the SM: code that runs once a CTA is not in the instruction cache when it
       // is wanted (16 heads over 4, 16384 rows, window 512 301 us a training step against 292; heads of 128 894
@@ -1600,10 +1613,23 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
           tmem_ld16(acc + C::C_A + k * HDP + c0, v);
 #pragma unroll
           for (int e = 0; e < 16; ++e) add_check(z, v[e]);
+          float* to = reinterpret_cast<float*>(smem + (k * TR + r) * (4 * HDP));
+          int sw = r & 7;
+          if (alone) {
+            if (at < 0) {
+              // dV (dV') as they are, dK (dK') with the scale of the scores
+              const float f = k < C::NT ? 1.f : p.scale;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] *= f;
+              stage16<HDP>(smem + k * TR * HDP * 2, r, part * C::OW + c0, v);
+              continue;
+            }
+            to = p.part + part_at(p, 2 * C::NT, HDP, at >> 7, hk, k, at & 127);
+            sw = 0;
+          }
 #pragma unroll
           for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<float4*>(smem + (k * TR + r) * (4 * HDP) +
-                                       ((((part * C::OW + c0 + e) / 4) ^ (r & 7)) << 4)) =
+            *reinterpret_cast<float4*>(to + 4 * (((part * C::OW + c0 + e) / 4) ^ sw)) =
                 make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
       if (r < nvalid && z != 0.f) redo_flag = 1;
@@ -1615,23 +1641,28 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
   tc_fence_after();
   if (careful || !redo_flag || *abort) break;
   }
-  // Rows whose sums leave as float32, for sink_sum_kernel: sinks that other CTAs have sums of too, as slot
-  // and place, behind the accumulators.  (Looked up for each sum, with divisions, it took 7 us of a CTA's
-  // 68, heads of 128.)
+  if (alone) {
+    // rows whose sums have left as float32 are written again by sink_sum_kernel
+    if (warp >= 3 && !*abort && !(WIN && far)) {
+#pragma unroll 1
+      for (int k = 0; k < 2 * C::NT; ++k) {
+        const int64_t ld = k < C::NT ? p.lddv : p.lddk;
+        __nv_bfloat16* dst = k == 0 ? p.dv : !DUAL ? p.dk : k == 1 ? p.dvd : k == 2 ? p.dk : p.dkd;
+        stage_out<HDP, C::EW * 32>(smem + k * TR * HDP * 2, nvalid, p.D, dst + row0 * ld + hk * p.D, ld,
+                                   static_cast<int>(threadIdx.x) - 96);
+      }
+    }
+    if (warp == 1) {
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tb),
+                   "r"(C::COLS));
+    }
+    return;
+  }
   int* sink_of = reinterpret_cast<int*>(smem + 2 * C::NT * TR * 4 * HDP);
   static_assert(2 * C::NT * TR * 4 * HDP + TR * 4 <= C::OPND_B, "behind the accumulators");
   if constexpr (WIN) {
     const int q = static_cast<int>(threadIdx.x) - 96;
-    if (p.sinks > 0 && q >= 0 && q < TR && !*abort) {
-      int at = -1;
-      if (far) {
-        at = (p.chunks + far) << 7 | q;
-      } else if (q < nvalid) {
-        const int start = tile_lo(st_rows, row0, q), place = row0 + q - start;
-        if (place < p.sinks && has_far(p, start, tile_hi(st_rows, row0, q))) at = start / p.chunk << 7 | place;
-      }
-      sink_of[q] = at;
-    }
+    if (p.sinks > 0 && q >= 0 && q < TR && !*abort) sink_of[q] = sink_slot(q);
   }
   // The cluster's sums, rank by rank in order, each CTA its part of the rows; the second barrier
   // keeps a CTA's shared memory until the others have read it.  Short code counts here: it runs once
