@@ -391,8 +391,8 @@ __device__ __forceinline__ void stage_out(const uint8_t* buf, int nvalid, int D,
 // keys, and 128 at most of sinks before them, so that its ends, some 6000 cycles of a forward CTA (set-up and
 // first scores 4000, results 2200) beside 1900 a tile, weigh more than without one.  Of the products
 // that the pairs need, at 1888 TF/s: 16 heads of 64 over 4, 32768 rows, window 1024 203 us forward (72: 669
-// TF/s); window 512, 16384 rows 293 us forward and backward (45); 16 heads of 128 over 2, 24577 rows,
-// window 1000 945 us (305).  Issue slots are half used, the tensor pipe 30 %: the chain of a tile
+// TF/s); window 512, 16384 rows 292 us forward and backward (45); 16 heads of 128 over 2, 24577 rows,
+// window 1000 938 us (305).  Issue slots are half used, the tensor pipe 30 %: the chain of a tile
 // bounds it, and four CTAs an SM fill what three left.  Tried, and no faster: products and exponentials of
 // no more sinks than there are, columns that no row of a warp attends to left out of masked tiles, two
 // buffers of scores, the next CTA's rows fetched into L2.
