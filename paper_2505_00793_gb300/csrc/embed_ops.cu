@@ -851,7 +851,7 @@ EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual) {
 cudaError_t embed_fwd(const EmbedParams& p, bool e_bf16, bool y_bf16, cudaStream_t s) {
   const int units = (p.dim + 3) / 4;
   const int rows = units >= LOOK_THREADS * LOOK_ITEMS ? 1 : LOOK_THREADS * LOOK_ITEMS / units;
-  const dim3 grid(static_cast<unsigned>((p.seq.rows + rows - 1) / rows), p.Ed ? 2 : 1);
+  const dim3 grid(static_cast<unsigned>((p.seq.rows - 1) / rows + 1), p.Ed ? 2 : 1);
   auto run = [&](auto kernel) { return launch_k(kernel, grid, dim3(LOOK_THREADS), 0, s, p, rows, units); };
   if (e_bf16)
     return y_bf16 ? run(embed_fwd_kernel<__nv_bfloat16, __nv_bfloat16>) : run(embed_fwd_kernel<__nv_bfloat16, float>);
