@@ -2166,7 +2166,7 @@ cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
   int nfar = 0;
   if constexpr (WIN) {
     p.chunk = window_chunk(a.window);
-    p.chunks = (N + p.chunk - 1) / p.chunk;
+    p.chunks = (N - 1) / p.chunk + 1;              // N + chunk may pass 2^31 - 1
     p.part = a.part;
     nfar = a.sinks > 0 ? p.chunks - 1 : 0;
   }
