@@ -566,9 +566,9 @@ mf_status mf_attn_window_work_bytes(const mf_attn_args* args, int64_t window, in
  *  seq_start, n_seq  as above; both may be 0: every row is taken.
  * The backward pass takes ids, scale and
  *  dy, dyd  gradients of y and y' (type y_prec, lddy; dyd nullable), and writes
- *  dE, dEd  float32, lddE (dEd with dyd): all of it, zeros where no row has the id.  Sums are
- *           float32 in an order that depends on ids and sizes alone.
- *  work     mf_embed_work_bytes() bytes (from n_rows, vocab, dim and whether dyd is given) on a
+ *  dE, dEd  float32, lddE (dEd with dyd; without rows dyd may be null): all of it, zeros where no row
+ *           has the id.  Sums are float32 in an order that depends on ids and sizes alone.
+ *  work     mf_embed_work_bytes() bytes (from n_rows, vocab, dim and whether dyd or dEd is given) on a
  *           16-byte boundary; its contents need not be kept.  Calls that overlap in time need one
  *           each.
  * Types are MF_PREC_FP32 or MF_PREC_BF16, in any combination.

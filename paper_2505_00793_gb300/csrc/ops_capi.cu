@@ -235,6 +235,10 @@ bool embed_sizes_ok(const mf_embed_args& a) {
   return a.n_rows >= 0 && a.n_rows <= INT32_MAX - 256 && a.vocab >= 1 && a.vocab <= INT32_MAX - 256 &&
          a.dim >= 1 && a.dim <= (1 << 20);
 }
+// Without rows dyd may be null where dEd is given.
+size_t embed_work(const mf_embed_args& a) {
+  return static_cast<size_t>(mf::embed_plan(a.n_rows, a.vocab, a.dim, a.dyd || a.dEd).bytes);
+}
 bool prec_ok(int p) { return p == MF_PREC_FP32 || p == MF_PREC_BF16; }
 
 mf_status embed_params(const mf_embed_args& a, EmbedParams* p) {
@@ -370,7 +374,7 @@ mf_status mf_attn_window_bwd(const mf_attn_args* args, int64_t window, int n_sin
 
 mf_status mf_embed_work_bytes(const mf_embed_args* args, size_t* bytes) {
   if (!args || !bytes || !embed_sizes_ok(*args)) return MF_ERR_INVALID_ARG;
-  *bytes = static_cast<size_t>(mf::embed_plan(args->n_rows, args->vocab, args->dim, args->dyd != nullptr).bytes);
+  *bytes = embed_work(*args);
   return MF_OK;
 }
 
@@ -396,10 +400,9 @@ mf_status mf_embed_bwd(const mf_embed_args* args, void* stream) {
   EmbedParams p;
   const mf_status st = embed_params(a, &p);
   if (st != MF_OK) return st;
-  const bool dual = a.dEd != nullptr;       // without rows dyd may be null
   if ((a.n_rows > 0 && !both(a.dyd, a.dEd)) || !rows_ok(a.dE, a.lddE, a.dim, a.vocab) || !aligned(a.dEd) ||
       (a.n_rows > 0 && (!rows_ok(a.dy, a.lddy, a.dim, a.n_rows) || !aligned(a.dyd))) || !a.work || !aligned(a.work) ||
-      a.work_bytes < static_cast<size_t>(mf::embed_plan(a.n_rows, a.vocab, a.dim, dual).bytes) ||
+      a.work_bytes < embed_work(a) ||
       !outputs_apart({a.dE, a.dEd, a.work}, {a.dy, a.dyd, a.ids}))
     return MF_ERR_INVALID_ARG;
   p.dy = a.dy; p.dyd = a.dyd; p.lddy = a.lddy;
