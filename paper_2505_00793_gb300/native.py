@@ -506,12 +506,18 @@ def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim,
                    status).run("mf_attn_bwd", stream)
 
 
+def _window_ints(window, n_sink):
+    """window and n_sink within the C types: ctypes would cut the upper bits off, and 2^32 + 1 sinks
+    be one.  The ends mean the same (every row; more sinks than there may be; less than none)."""
+    return min(max(window, -1), 2 ** 63 - 1), min(max(n_sink, -1), 2 ** 31 - 1)
+
+
 def mf_attn_window_work_bytes(n_rows, n_heads, n_kv_heads, head_dim, window, n_sink=0, dual=False):
     """Bytes of `work` that mf_attn_window_bwd takes."""
     a = mf_attn_args()
     a.n_rows, a.n_heads, a.n_kv_heads, a.head_dim = n_rows, n_heads, n_kv_heads, head_dim
     a.qd = 16 if dual else None
-    return _bytes_of("mf_attn_window_work_bytes", a, window, n_sink)
+    return _bytes_of("mf_attn_window_work_bytes", a, *_window_ints(window, n_sink))
 
 
 def mf_attn_window_fwd(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, window, n_sink=0, qd=None,
@@ -520,7 +526,7 @@ def mf_attn_window_fwd(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, window, n
     """mf_attn_fwd where a row attends to itself, the window - 1 rows before it and the first
     n_sink rows of its sequence (see mixflow.h)."""
     _attn_call(q, k, v, o, lse, n_heads, n_kv_heads, head_dim, qd, kd, vd, od, rbar, seq_start,
-               n_seq, scale, status).run("mf_attn_window_fwd", stream, window, n_sink)
+               n_seq, scale, status).run("mf_attn_window_fwd", stream, *_window_ints(window, n_sink))
 
 
 def mf_attn_window_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, window,
@@ -531,7 +537,7 @@ def mf_attn_window_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, he
     mf_attn_window_work_bytes bytes."""
     _attn_bwd_call(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim, work, qd, kd,
                    vd, od, rbar, dod, dqd, dkd, dvd, seq_start, n_seq, scale,
-                   status).run("mf_attn_window_bwd", stream, window, n_sink)
+                   status).run("mf_attn_window_bwd", stream, *_window_ints(window, n_sink))
 
 
 def _embed_call(ids, table, rows, scale, seq_start):
