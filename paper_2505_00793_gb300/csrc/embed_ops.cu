@@ -566,6 +566,7 @@ __global__ void __launch_bounds__(32 * SUM_WARPS)
 // memory, and walks the path of its own tokens and rows, a range a warp.
 constexpr int NEAR_WARPS = 16, NEAR_THREADS = 32 * NEAR_WARPS;
 constexpr int NEAR_TOKENS = 6144, NEAR_OWN = 8192;             // and rows of a block, at most
+constexpr int NEAR_EACH = 1024;                                // tokens a row of the table, at most
 constexpr int NEAR_BITS = 13, NEAR_IDS = NEAR_TOKENS / NEAR_THREADS;
 // Tokens of a warp's part of the ids.
 __host__ __device__ constexpr int near_part(int rows) { return (rows + NEAR_THREADS - 1) / NEAR_THREADS * 32; }
@@ -809,13 +810,18 @@ EmbedPlan embed_plan(int64_t rows, int64_t vocab, int64_t dim, bool dual) {
   m.slabs = static_cast<int>((dim + SLAB - 1) / SLAB);
   m.parts = m.slabs * (dual ? 2 : 1);
   // Up to 6144 tokens one launch of two blocks an SM, of 64 steps at least, if a block's rows fit: 4096 of 8192
-  // ids, 512 columns of bf16 12 us against 25 (8192 tokens 18 against 25), 1000 of them 12 against 21.
-  // Where one id has many tokens its block takes longer, 4096 tokens of 50001 ids, a third of them one,
-  // 30 against 29, 8192 47 against 35; so do tables of 128 MB and more (two of 32768 by 1024, 4096 tokens
-  // 67 against 64).
+  // ids, 512 columns of bf16 16 us against 28 (6144 tokens 18 against 30), 1000 of them 12 against 24;
+  // of 600000 ids, 128 columns 57 to 66 against 71 to 73; two tables of 32768 by 1024 59 to 70 against 67 to
+  // 73.  It takes longer, and the sort is taken, where a row has many tokens, as a block takes them all:
+  // 1000 tokens of one id 20 us against 20, 2000 33 against 22, 6144 82 to 90 against 22 to 30, and of four
+  // ids 41 against 30 (4096 31 against 30); and where slabs leave a part fewer than four blocks, which fill
+  // the places badly: 4096 tokens of 8000 ids, 8192 columns (four) 76 to 86 against 77 to 79, with tangents
+  // (two) 141 to 162 against 123, 20000 columns (one) 203 to 272 against 145.  (What the ids are is not known
+  // here: 4096 of 50001, a third of them one, take 30 against 29.)
   const int64_t held = 2 * 152 / m.parts, some = (rows + vocab + 63) / 64;
-  const int64_t blocks = held < 1 ? 1 : held < some ? held : some, own = (vocab + blocks - 1) / blocks;
-  if (rows <= NEAR_TOKENS && own <= NEAR_OWN) {
+  const int64_t blocks = held < some ? held : some;
+  if (held >= 4 && rows <= NEAR_TOKENS && rows <= NEAR_EACH * vocab && (vocab + blocks - 1) / blocks <= NEAR_OWN) {
+    const int64_t own = (vocab + blocks - 1) / blocks;
     m.blocks = static_cast<int>(blocks);
     // id / blocks as the upper half of a product: exact below 2^32 / blocks, and there are 304 blocks of 8192
     // ids at most
