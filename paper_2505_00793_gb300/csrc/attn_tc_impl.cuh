@@ -317,10 +317,11 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // registers and was up to 17 % slower.
 // TKEYS keys a tile: 64 where the tangents leave no TMEM for more, and where many CTAs are to be
 // had: tiles of 64 let three of them, not two, fill each other's waits on an SM (launch_fwd).
-// With a window, whose walks are short and all as long, four CTAs of 64 keys a tile hide one another's ends
-// better, for fewer registers: 16 heads over 4, 32768 rows, window 1024 208 us against 227, 16 heads over 8,
-// 16384 rows, window 128 50 against 53; without one 16 heads over 4, 8192 rows 191 (a training step)
-// against 181.
+// With a window, whose walks are all as long, four CTAs of 64 keys a tile hide one another's ends better, for
+// fewer registers: 16 heads over 4, 32768 rows, windows of 32, 1024, 4096, 8192 and 24000 84, 207, 539, 932 and
+// 1885 us against 90, 225, 592, 1026 and 2076 with three; 8192 rows, windows of 128, 1024, 3000 and 8191 33, 59,
+// 115 and 158 against 35, 66, 111 and 162; without one 16 heads over 4, 8192 rows 191 (a training step)
+// against 181.  (Few CTAs and a long window: attn_window_fwd.)
 template <bool DUAL, int HDP, int TKEYS, bool WIN>
 struct FwdCfg {
   static constexpr int NA = HDP / 64;                      // 64-column atoms of a head
@@ -2116,10 +2117,13 @@ __global__ void __launch_bounds__(BwdCfg<DUAL, HDP>::THREADS, BwdCfg<DUAL, HDP>:
 // one CTA a group, these, and as many as divide it: 8 heads of 64 over one, 512 rows 78, 28 and 28 us;
 // 16 over 4 with tangents, 8192 rows 252, 236 and 264; 32 over 8, 16384 rows in sequences of 256 212,
 // 212 and 292; 16 of 128 over 4, 12289 rows 669, 569 and 635.
-// With a window all walks are as long, and the fewest that fill the places once do: 16 heads over 4, 8192
-// rows, window 257 with tangents 300 us a training step against 314 with three times, 16384 rows, window 512
-// 316 against 319, 16 heads of 128 over 2, 24577 rows, window 1000 966 against 976; four CTAs a group 362,
-// 357 and 1054.
+// With a window below 2048 all walks are as long, and the fewest that fill the places once do (a fill of one):
+// 16 heads over 4, 8192 rows, windows of 128, 512, 1024 and 2048 86, 127, 176 and 268 us backward against 98 to
+// 143, 190 and 274 with a fill of three, with tangents 147, 246, 375 and 606 against 174, 270, 387 and 543; 16
+// heads of 128 over 2, 24576 rows, window 1024 657 against 641, with sinks 685 against 711; a training step with
+// four CTAs a group, 16384 rows, window 512 357 against 316.  Longer windows walk like none: windows of 2048,
+// 4096 and 8192 in 16384 rows 535, 907 and 1563 against 530, 843 and 1397, in four sequences with 16 heads
+// over 2 498, 618 and 612 against 446, 528 and 528 (504 without a window).
 int kv_share(int group, int64_t ctas, int per_sm, int fill) {
   int best = 1;
   for (int n = 1; n <= 8 && n <= group; ++n) {
@@ -2158,7 +2162,7 @@ cudaError_t launch_bwd(const AttnParams& a, cudaStream_t s) {
   });
   if (e != cudaSuccess) return e;
   TcParams2 p = tc_params(a);
-  p.share = kv_share(p.G, static_cast<int64_t>(p.tiles) * a.Hkv, C::CTAS, WIN ? 1 : 3);
+  p.share = kv_share(p.G, static_cast<int64_t>(p.tiles) * a.Hkv, C::CTAS, WIN && a.window < 2048 ? 1 : 3);
   p.Gs = p.G / p.share;
   e = launch_k(attn_tc_bwd_q_kernel<DUAL, HDP, WIN>, tile_grid(a.Hq, p.tiles), dim3(C::THREADS),
                C::SMEM_Q, s, qr[0], qr[1], qr[2], qr[3], ks[0], ks[1], ks[2], ks[3], p);
