@@ -509,6 +509,8 @@ def mf_attn_bwd(q, k, v, o, lse, d_o, dq, dk, dv, n_heads, n_kv_heads, head_dim,
 def _window_ints(window, n_sink):
     """window and n_sink within the C types: ctypes would cut the upper bits off, and 2^32 + 1 sinks
     be one.  The ends mean the same (every row; more sinks than there may be; less than none)."""
+    if -1 <= window < 2 ** 63 and -1 <= n_sink < 2 ** 31:
+        return window, n_sink
     return min(max(window, -1), 2 ** 63 - 1), min(max(n_sink, -1), 2 ** 31 - 1)
 
 
