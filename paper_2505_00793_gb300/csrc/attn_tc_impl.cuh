@@ -696,9 +696,8 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
       else find_max(std::false_type{});
       const float t2 = mx * p.c2;
       float f = 1.f;
-      bool again = DUAL && j == j1, heavy = mx_tile;
+      bool again = DUAL && j == j1;
       if (t2 > m2 + TAU) {
-        heavy |= m2 != -INFINITY;
         f = ex2(m2 - t2);
         m2 = t2;
         again = true;
@@ -709,43 +708,43 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
       if (__any_sync(0xffffffffu, again)) {
         float dc = 0.f;
         if (DUAL) {
-          // Over a row's first whole tile the plain mean.  In a mixed one, where the row may have few
-          // keys and this be its last, and where its maximum has moved, that with the weights P over all
-          // keys so far: rbar itself, if no more come or none that weigh.
+          // The mean with the weights P over all keys so far: rbar itself, if no more come or none that
+          // weigh.
           float wl = 0.f, ws = 0.f;
-          auto mean = [&](auto weighted) {
-            constexpr bool W = decltype(weighted)::value;
-#pragma unroll 1
+          const uint64_t nmb = pair(-base, -base);
+          auto mean = [&](auto masked) {
+            constexpr bool MASK = decltype(masked)::value;
+            uint64_t wl2 = 0, ws2 = 0;
+#pragma unroll
             for (int c0 = 0; c0 < TK; c0 += 16) {
               float x[16], y[16];
-              if (W) tmem_ld16_nowait(aS + c0, x);
+              tmem_ld16_nowait(aS + c0, x);
               tmem_ld16_nowait(aSd + c0, y);
               tmem_wait_ld();
-              if constexpr (W) {
-                const uint32_t w = mx_tile ? (c0 < 32 ? own[0] : own[TK / 32 - 1]) >> (c0 & 16) : 0xffffu;
+              const uint32_t w = MASK ? (c0 < 32 ? own[0] : own[TK / 32 - 1]) >> (c0 & 16) : 0u;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  x[i] = heavy ? ex2(fmaf(x[i], p.c2, -base)) : 1.f;
-                  x[i] = w >> i & 1 ? x[i] : 0.f;
-                  y[i] = w >> i & 1 ? x[i] * y[i] : 0.f;
+              for (int i = 0; i < 16; i += 2) {
+                const float2 e = halves(fma2(pair(x[i], x[i + 1]), c2p, nmb));
+                float p0 = ex2(e.x), p1 = ex2(e.y);
+                if (MASK) {
+                  p0 = w >> i & 1 ? p0 : 0.f;
+                  p1 = w >> (i + 1) & 1 ? p1 : 0.f;
+                  y[i] = w >> i & 1 ? y[i] : 0.f;
+                  y[i + 1] = w >> (i + 1) & 1 ? y[i + 1] : 0.f;
                 }
+                const uint64_t pp = pair(p0, p1);
+                wl2 = add2(wl2, pp);
+                ws2 = fma2(pp, pair(y[i], y[i + 1]), ws2);
               }
-#pragma unroll
-              for (int k = 8; k > 0; k >>= 1)
-#pragma unroll
-                for (int i = 0; i < k; ++i) {
-                  if (W) x[i] += x[i + k];
-                  y[i] += y[i + k];
-                }
-              if (W) wl += x[0];
-              ws += y[0];
             }
+            const float2 a = halves(wl2), b = halves(ws2);
+            wl = a.x + a.y;
+            ws = b.x + b.y;
           };
-          if (__any_sync(0xffffffffu, again && heavy)) mean(std::true_type{});
-          else mean(std::false_type{});
+          if (!mx_tile) mean(std::false_type{});
+          else mean(std::true_type{});
           if (again && m2 != -INFINITY) {
-            dc = heavy ? __fdividef(fmaf(cen, wl, -p.scale * ws) - rs, l + wl)
-                       : fmaf(-p.scale / TK, ws, cen);
+            dc = __fdividef(fmaf(cen, wl, -p.scale * ws) - rs, l + wl);
             rs = fmaf(dc, l, rs);
             cen -= dc;
           }
