@@ -300,14 +300,14 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).
 // The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T into S';
 // P [V | V'] -> [O | T], then (P (*) (S' - c)) V into T; o' = T / l - (rbar - c) o.  c is a mean of
-// the row's S', over its first tiles and over keys that outweigh those: what all of a row's S' have
+// the row's S' by P, over its first tiles and again where its maximum moves by TAU: what all of a row's S' have
 // in common (keys or their tangents with a common part) cancels in o', and rounded to bf16 as part
 // of P (*) S' it would leave 2^-9 of itself.  With keys of 10 of a unit vector in common o' was off by
-// 0.012 in relative L2, with 30 by 0.035; now 0.0022.  The mean costs nothing where scores spread like a
-// unit normal (16 heads with tangents, eight sequences of 1024: 79 us either way); where maxima move
-// on many tiles it costs a look more at each: scores of std 3 and 8 82 to 92 us and 89 to 118, o' off
-// by 0.0030 and 0.0045 where it was by 0.0032 and 0.0052.  The plain mean of the first tile alone took 82
-// and 90 us, but left rows of one heavy key further off than P (*) S' did.
+// 0.012 in relative L2, with 30 by 0.035; now 0.0022.  By P, since a sequence's first keys may outweigh
+// the rest: with the plain mean of the first whole tile such rows, whose other S' differed by 4 and 30, had o'
+// off by 0.010 and 0.095, dq' (through D') by 0.08 and 0.17; now 0.0025 and 0.016.  It costs 1 % of long walks
+// where scores spread like a unit normal (16 heads over 4, one sequence of 8192 338 us against 334) and
+// nothing elsewhere (eight of 1024, 16 heads: 82 us).
 // What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 344 to 350 us, 1.58 PF/s of
 // causal work; 358 with scores read 32 columns at a time, the tensor pipe busy 67 % of the cycles); at 64
 // the chain scores - maximum -
@@ -696,7 +696,10 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
       else find_max(std::false_type{});
       const float t2 = mx * p.c2;
       float f = 1.f;
-      bool again = DUAL && j == j1;
+      // with a window also where one key outweighs all before (16384 rows, window 1000, scores of std 1, 2, 3 and 8
+      // 234, 285, 299 and 305 us against 233, 281, 287 and 301; without one 8192 rows 82, 94, 105 and 111
+      // against 82, 84, 90 and 108)
+      bool again = DUAL && (j == j1 || (WIN && ex2(t2 - m2) > l));
       if (t2 > m2 + TAU) {
         f = ex2(m2 - t2);
         m2 = t2;
