@@ -22,7 +22,7 @@
 //   1024 tokens             o 0.0020, o' 0.0022, dv, dv' 0.0023, dq, dk, dq', dk' 0.0025
 //   2 tokens                dq, dk 0.0038, dq', dk' 0.0042 (8 tokens 0.0031): dP - D is a difference of
 //                           near values, and D carries o's rounding
-//   scores of std 3, 8      o' 0.0030, 0.0045, dq .. dk' up to 0.0035, 0.0075
+//   scores of std 3, 8      o' 0.0030, 0.0039 (with a window 0.0025), dq .. dk' up to 0.0038, 0.0058
 //   keys with 3, 10 of a unit vector in common    dq, dq' 0.0088, 0.029, all else as above: the roundings
 //                           of dS and D leave sum dS = 0 off by 2^-9 of its terms, times what the keys share
 //
@@ -300,14 +300,14 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // the rows, a thread each (two threads a row, which have to agree on its maximum, took longer).
 // The tangent shares the operands: Q [K | K']^T -> [S | Q K'^T], then Q' K^T into S';
 // P [V | V'] -> [O | T], then (P (*) (S' - c)) V into T; o' = T / l - (rbar - c) o.  c is a mean of
-// the row's S' by P, over its first tiles and again where its maximum moves by TAU: what all of a row's S' have
-// in common (keys or their tangents with a common part) cancels in o', and rounded to bf16 as part
-// of P (*) S' it would leave 2^-9 of itself.  With keys of 10 of a unit vector in common o' was off by
+// the row's S' by P, over its first tiles and again where its maximum moves by TAU or a key outweighs what came
+// before: what all of a row's S' have in common (keys or their tangents with a common part) cancels in o', and
+// rounded to bf16 as part of P (*) S' it would leave 2^-9 of itself.  With keys of 10 of a unit vector in common o' was off by
 // 0.012 in relative L2, with 30 by 0.035; now 0.0022.  By P, since a sequence's first keys may outweigh
 // the rest: with the plain mean of the first whole tile such rows, whose other S' differed by 4 and 30, had o'
-// off by 0.010 and 0.095, dq' (through D') by 0.08 and 0.17; now 0.0025 and 0.016.  It costs 1 % of long walks
-// where scores spread like a unit normal (16 heads over 4, one sequence of 8192 338 us against 334) and
-// nothing elsewhere (eight of 1024, 16 heads: 82 us).
+// off by 0.010 and 0.095, dq' (through D') by 0.08 and 0.17; now 0.0025 and 0.016.  Scores of std 1, 2, 3 and 8
+// take 342, 348, 384 and 446 us against 334, 336, 390 and 492 with that (16 heads over 4, one sequence of 8192;
+// eight of 1024, 16 heads: 82, 84, 96 and 109 against 82, 82, 94 and 121).
 // What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 344 to 350 us, 1.58 PF/s of
 // causal work; 358 with scores read 32 columns at a time, the tensor pipe busy 67 % of the cycles); at 64
 // the chain scores - maximum -
@@ -696,10 +696,11 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
       else find_max(std::false_type{});
       const float t2 = mx * p.c2;
       float f = 1.f;
-      // with a window also where one key outweighs all before (16384 rows, window 1000, scores of std 1, 2, 3 and 8
-      // 234, 285, 299 and 305 us against 233, 281, 287 and 301; without one 8192 rows 82, 94, 105 and 111
-      // against 82, 84, 90 and 108)
-      bool again = DUAL && (j == j1 || (WIN && ex2(t2 - m2) > l));
+      // also where one key outweighs all before, with a window, or eight times all before: scores of std 1, 2, 3
+      // and 8 in 16384 rows, window 1000 take 234, 285, 299 and 305 us against 233, 281, 287 and 301 without;
+      // 8192 rows, no window 342, 348, 384 and 446 against 338, 344, 376 and 432, and outweighed once 341, 356,
+      // 409 and 468
+      bool again = DUAL && (j == j1 || ex2(t2 - m2 - (WIN ? 0.f : 3.f)) > l);
       if (t2 > m2 + TAU) {
         f = ex2(m2 - t2);
         m2 = t2;
