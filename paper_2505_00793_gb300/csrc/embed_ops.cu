@@ -144,12 +144,6 @@ __device__ __forceinline__ int token_key(const EmbedParams& p, int row, int tota
   return row < total && id >= 0 && id < p.vocab ? id : p.vocab;
 }
 
-// The token behind the last of the tile that begins at a.  Tiles are gone through in steps of up to SORT_SUB
-// tokens, the last of which may lie behind 2^31 - 1: places of tokens are unsigned there.
-__device__ __forceinline__ unsigned tile_end(const EmbedParams& p, unsigned a, int tile) {
-  return min(static_cast<unsigned>(p.seq.rows), a + tile);
-}
-
 // Inclusive sum over a warp.
 __device__ __forceinline__ int warp_sum_scan(int v, int lane) {
 #pragma unroll
@@ -305,13 +299,15 @@ __global__ void __launch_bounds__(SORT_THREADS)
   cnt[t] = 0;
   for (int k = 1; k < m.passes; ++k) hist[(k * m.tiles + tile) * DIGITS + t] = 0;
   __syncthreads();
-  const unsigned a = static_cast<unsigned>(tile) * m.tile, end = tile_end(p, a, m.tile);
-  for (unsigned i0 = a; i0 < end; i0 += SORT_SUB) {
+  const int64_t a = static_cast<int64_t>(tile) * m.tile;
+  const int end = static_cast<int>(min(static_cast<int64_t>(p.seq.rows), a + m.tile));
+  // a tile holds tokens, and the token behind its last step may lie behind 2^31 - 1
+  for (int i0 = static_cast<int>(a);; i0 += SORT_SUB) {
     int d[SORT_ROUNDS];
 #pragma unroll
     for (int k = 0; k < SORT_ROUNDS; ++k) {
-      const unsigned i = i0 + k * SORT_THREADS + t;
-      d[k] = i < end ? token_key(p, static_cast<int>(i), total) & ((1 << m.bits) - 1) : -1;
+      const int i = i0 + k * SORT_THREADS + t;
+      d[k] = i < end ? token_key(p, i, total) & ((1 << m.bits) - 1) : -1;
     }
 #pragma unroll
     for (int k = 0; k < SORT_ROUNDS; ++k) {
@@ -319,6 +315,7 @@ __global__ void __launch_bounds__(SORT_THREADS)
       const unsigned peers = peers_of(d[k], m.bits) & __ballot_sync(ALL, d[k] >= 0);
       if (d[k] >= 0 && lane == __ffs(peers) - 1) atomicAdd(&cnt[d[k]], __popc(peers));
     }
+    if (end - i0 <= SORT_SUB) break;
   }
   __syncthreads();
   hist[tile * DIGITS + t] = cnt[t];
@@ -333,22 +330,22 @@ __global__ void __launch_bounds__(SORT_THREADS)
   const int shift = pass * m.bits, mask = (1 << m.bits) - 1;
   const int* h = hist + pass * m.tiles * DIGITS + t;
   int* next = pass + 1 < m.passes ? hist + (pass + 1) * m.tiles * DIGITS : nullptr;
-  const unsigned a = static_cast<unsigned>(tile) * m.tile, end = tile_end(p, a, m.tile);
+  const int64_t a = static_cast<int64_t>(tile) * m.tile;
+  const int end = static_cast<int>(min(static_cast<int64_t>(p.seq.rows), a + m.tile));
   const int rounds = min(m.tile / SORT_THREADS, SORT_ROUNDS);
   int tile_bits = 0;
   while ((m.tiles - 1) >> tile_bits) ++tile_bits;
   int2 x[SORT_ROUNDS];
   int rank[SORT_ROUNDS];
-  auto load = [&](unsigned s0) {
+  auto load = [&](int s0) {
 #pragma unroll
     for (int k = 0; k < SORT_ROUNDS; ++k) {
-      const unsigned i = s0 + (w * rounds + k) * 32 + lane;
+      const int i = s0 + (w * rounds + k) * 32 + lane;
       x[k] = make_int2(-1, 0);
-      if (k < rounds && i < end)
-        x[k] = pass == 0 ? make_int2(token_key(p, static_cast<int>(i), total), static_cast<int>(i)) : from[i];
+      if (k < rounds && i < end) x[k] = pass == 0 ? make_int2(token_key(p, i, total), i) : from[i];
     }
   };
-  load(a);
+  load(static_cast<int>(a));
   int before = 0, all = 0;
 #pragma unroll 16
   for (int k = 0; k < m.tiles; ++k) {
@@ -357,7 +354,7 @@ __global__ void __launch_bounds__(SORT_THREADS)
     before += k < tile ? c : 0;
   }
   int base = before + smaller_digits(all, sh);
-  for (unsigned s0 = a; s0 < end; s0 += rounds * SORT_THREADS) {
+  for (int s0 = static_cast<int>(a);; s0 += rounds * SORT_THREADS) {
     if (s0 > a) load(s0);
     const int mine = rank_tokens(x, rank, rounds, shift, m.bits, sh);
     sh.base[t] = base;
@@ -380,6 +377,7 @@ __global__ void __launch_bounds__(SORT_THREADS)
         if (in && lane == __ffs(peers) - 1) atomicAdd(&next[to_tile * DIGITS + d], __popc(peers));
       }
     }
+    if (end - s0 <= rounds * SORT_THREADS) break;
     __syncthreads();                  // base and cnt are written again
   }
 }
