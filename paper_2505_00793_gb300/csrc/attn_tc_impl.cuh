@@ -305,11 +305,11 @@ __device__ __forceinline__ void scrub(uint8_t* base, int rows, int atoms, uint32
 // rounded to bf16 as part of P (*) S' it would leave 2^-9 of itself.  With keys of 10 of a unit vector in common o' was off by
 // 0.012 in relative L2, with 30 by 0.035; now 0.0022.  By P, since a sequence's first keys may outweigh
 // the rest: with the plain mean of the first whole tile such rows, whose other S' differed by 4 and 30, had o'
-// off by 0.010 and 0.095, dq' (through D') by 0.08 and 0.17; now 0.0025 and 0.016.  Scores of std 1, 2, 3 and 8
-// take 342, 348, 384 and 446 us against 334, 336, 390 and 492 with that (16 heads over 4, one sequence of 8192;
-// eight of 1024, 16 heads: 82, 84, 96 and 109 against 82, 82, 94 and 121).
-// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 344 to 350 us, 1.58 PF/s of
-// causal work; 358 with scores read 32 columns at a time, the tensor pipe busy 67 % of the cycles); at 64
+// off by 0.010 and 0.095, dq' (through D') by 0.08 and 0.17; now 0.0024 and 0.016.  Scores of std 1, 2, 3 and 8
+// take 342, 348, 384 and 446 us against 335, 337, 389 and 492 with that (16 heads over 4, one sequence of 8192;
+// 16384 rows in four, window 1000: 229, 277, 289 and 293 against 231, 307, 319 and 336).
+// What bounds it: at 128 columns the products (8 heads over one, 16384 rows: 342 to 366 us, 1.50 to 1.60 PF/s
+// of causal work; the tensor pipe busy 67 % of the cycles with scores read 32 columns at a time); at 64
 // the chain scores - maximum -
 // exponentials - product of each CTA, which two or three CTAs an SM fill by turns (16 heads, 16384
 // rows: 0.94 PF/s; 16 heads with tangents, eight sequences of 1024: 79 us, pipe 36 %).  Taking the
@@ -393,7 +393,7 @@ __device__ __forceinline__ void stage_out(const uint8_t* buf, int nvalid, int D,
 // first scores 4000, results 2200) beside 1900 a tile, weigh more than without one.  Of the products
 // that the pairs need, at 1888 TF/s: 16 heads of 64 over 4, 32768 rows, window 1024 203 us forward (72: 669
 // TF/s); window 512, 16384 rows 292 us forward and backward (45); 16 heads of 128 over 2, 24577 rows,
-// window 1000 938 us (305).  Issue slots are half used, the tensor pipe 30 %: the chain of a tile
+// window 1000 935 us (305).  Issue slots are half used, the tensor pipe 30 %: the chain of a tile
 // bounds it, and four CTAs an SM fill what three left.  Tried, and no faster: products and exponentials of
 // no more sinks than there are, columns that no row of a warp attends to left out of masked tiles, two
 // buffers of scores, the next CTA's rows fetched into L2.
@@ -696,10 +696,10 @@ __global__ void __launch_bounds__(FwdCfg<DUAL, HDP, TKEYS, WIN>::THREADS, FwdCfg
       else find_max(std::false_type{});
       const float t2 = mx * p.c2;
       float f = 1.f;
-      // also where one key outweighs all before, with a window, or eight times all before: scores of std 1, 2, 3
-      // and 8 in 16384 rows, window 1000 take 234, 285, 299 and 305 us against 233, 281, 287 and 301 without;
-      // 8192 rows, no window 342, 348, 384 and 446 against 338, 344, 376 and 432, and outweighed once 341, 356,
-      // 409 and 468
+      // also where one key outweighs all before, with a window, or eight times all before.  Scores of std 1, 2, 3
+      // and 8 in 16384 rows, window 1000 took 234, 285, 299 and 305 us with that and 233, 281, 287 and 301
+      // without; 8192 rows, no window 342, 348, 384 and 446 against 338, 344, 376 and 432, and outweighed once
+      // 341, 356, 409 and 468.
       bool again = DUAL && (j == j1 || ex2(t2 - m2 - (WIN ? 0.f : 3.f)) > l);
       if (t2 > m2 + TAU) {
         f = ex2(m2 - t2);

@@ -8,10 +8,11 @@
 // nowhere, and reads every token's row once.  Tokens are sorted by id (radix sort, stable, so that
 // an id's tokens stay in their order), and the list of tokens and the list of table rows are merged
 // into one path of "add a token's row" and "write a table's row", cut into ranges of equal length:
-// however the ids are spread, every warp moves the same bytes.
+// however the ids are spread, every warp moves the same bytes.  A few tokens take one launch instead
+// (embed_plan), in which a block has the table rows that it owns and all of their tokens.
 //
 // Measured (of 6.75 TB/s, a plain copy): 8192 tokens, 32768 ids, two tables of 1024 columns, float32: lookup
-// 94 MB in 18 us (78 %), gradient 335 MB in 70 us (71 %), of which the sort takes 10, the sums 57 (87 %)
+// 94 MB in 18 us (78 %), gradient 335 MB in 72 us (69 %), of which the sort takes 10, the sums 57 (87 %)
 // and the rows that blocks share 4; 131071 tokens, 50001 ids, 768 columns of bf16 355 MB in 96 us (55 %):
 // 23, 65 and 8.  4096 tokens, 8192 ids, 512 columns take one launch, 21 MB in 12 us, latencies.  Zeros
 // written by blocks beside the sort, and sums of the ids that occur alone, took longer (87 us in the
